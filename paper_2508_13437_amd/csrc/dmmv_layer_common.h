@@ -1,0 +1,220 @@
+// Shared by the operators of a quantised linear layer (include/dmmv_layer.h): checks of block
+// matrices, the e4m3 block format on the device, loads and stores of eight columns a lane.
+#pragma once
+
+#include "dmmv_common.h"
+#include "../../include/dmmv_layer.h"
+
+namespace dmmv {
+
+// A block matrix as kernels take it.
+struct BlockView {
+    uint8_t* codes;
+    int64_t ld;
+    void* scales;         // NULL: all 1
+    int64_t srow, sblk;
+    int32_t e8m0;         // scales are exponent bytes, else float
+    int32_t shift;        // log2(rows per scale): 0 or 7
+};
+
+// host checks; `what` names the argument in the message
+dmmv_status layer_check_dtype(int32_t dtype);
+dmmv_status layer_check_sizes(int64_t rows, int64_t cols, const char* what);
+// a row-major array of elements of `width` bytes (empty ones may be NULL)
+dmmv_status layer_check_array(const void* p, int64_t rows, int64_t cols, int64_t ld, int width, const char* what);
+dmmv_status layer_check_block(const dmmv_block_matrix* q, bool output, const char* what);
+dmmv_status layer_check_workspace(const void* ws, size_t have, size_t need);
+BlockView layer_view(const dmmv_block_matrix* q);      // all zero for NULL
+
+static inline int layer_width(int32_t dtype) { return dtype == DMMV_BF16 ? 2 : 4; }
+
+// out[j] = sum over the parts of part[p][j], by ascending p inside each of 16 interleaved strands;
+// the first n0 columns go to out0, the others to out1 (either may be NULL)
+dmmv_status layer_sum_parts(const float* part, int64_t parts, int64_t n, float* out0, int64_t n0, float* out1,
+                            hipStream_t stream);
+
+#ifdef __HIPCC__
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef int intx8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8_t;
+// 16 and 8 bytes at any address of the element's own alignment: global loads need no more
+typedef uint32_t piece16 __attribute__((ext_vector_type(4)));
+typedef uint32_t piece8 __attribute__((ext_vector_type(2)));
+typedef piece16 piece16_any __attribute__((aligned(1)));
+typedef piece8 piece8_any __attribute__((aligned(1)));
+
+struct bf16_t { uint16_t u; };
+
+__device__ __forceinline__ float bf16_value(uint32_t low16) { return __uint_as_float(low16 << 16); }
+// nearest, ties to even; NaN stays NaN
+__device__ __forceinline__ uint32_t bf16_bits(float v) {
+    const __bf16 b = (__bf16)v;
+    return (uint32_t)__builtin_bit_cast(uint16_t, b);
+}
+
+// eight columns of a row from `col` on, zero past `cols`
+__device__ __forceinline__ void load8(const float* __restrict__ row, int64_t col, int64_t cols, float (&v)[8]) {
+    if (col + 8 <= cols) {
+        const piece16 a = *reinterpret_cast<const piece16_any*>(row + col), b = *reinterpret_cast<const piece16_any*>(row + col + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[i] = __uint_as_float(a[i]); v[i + 4] = __uint_as_float(b[i]); }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = col + i < cols ? row[col + i] : 0.0f;
+    }
+}
+__device__ __forceinline__ void load8(const bf16_t* __restrict__ row, int64_t col, int64_t cols, float (&v)[8]) {
+    if (col + 8 <= cols) {
+        const piece16 a = *reinterpret_cast<const piece16_any*>(row + col);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[2 * i] = bf16_value(a[i] & 0xFFFFu); v[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u); }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = col + i < cols ? bf16_value(row[col + i].u) : 0.0f;
+    }
+}
+__device__ __forceinline__ void store8(float* __restrict__ row, int64_t col, int64_t cols, const float (&v)[8]) {
+    if (col + 8 <= cols) {
+        piece16 a, b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { a[i] = __float_as_uint(v[i]); b[i] = __float_as_uint(v[i + 4]); }
+        *reinterpret_cast<piece16_any*>(row + col) = a;
+        *reinterpret_cast<piece16_any*>(row + col + 4) = b;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (col + i < cols) row[col + i] = v[i];
+    }
+}
+__device__ __forceinline__ void store8(bf16_t* __restrict__ row, int64_t col, int64_t cols, const float (&v)[8]) {
+    if (col + 8 <= cols) {
+        piece16 a;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = bf16_bits(v[2 * i]) | (bf16_bits(v[2 * i + 1]) << 16);
+        *reinterpret_cast<piece16_any*>(row + col) = a;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (col + i < cols) row[col + i].u = (uint16_t)bf16_bits(v[i]);
+    }
+}
+__device__ __forceinline__ piece8 load8_codes(const uint8_t* __restrict__ row, int64_t col, int64_t cols) {
+    if (col + 8 <= cols) return *reinterpret_cast<const piece8_any*>(row + col);
+    piece8 a = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (col + i < cols) a[i >> 2] |= (uint32_t)row[col + i] << (8 * (i & 3));
+    return a;
+}
+__device__ __forceinline__ void store8_codes(uint8_t* __restrict__ row, int64_t col, int64_t cols, piece8 a) {
+    if (col + 8 <= cols) {
+        *reinterpret_cast<piece8_any*>(row + col) = a;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (col + i < cols) row[col + i] = (uint8_t)(a[i >> 2] >> (8 * (i & 3)));
+    }
+}
+
+// ---- scales ---------------------------------------------------------------------------------
+__device__ __forceinline__ float e8m0_value(uint32_t b) {
+    return __uint_as_float(b == 255u ? 0x7FC00000u : b == 0u ? 0x00400000u : b << 23);
+}
+__device__ __forceinline__ float scale_at(const BlockView& q, int64_t row, int64_t block) {
+    if (!q.scales) return 1.0f;
+    const int64_t at = (row >> q.shift) * q.srow + block * q.sblk;
+    return q.e8m0 ? e8m0_value(static_cast<const uint8_t*>(q.scales)[at]) : static_cast<const float*>(q.scales)[at];
+}
+__device__ __forceinline__ void scale_put(const BlockView& q, int64_t scale_row, int64_t block, uint32_t b) {
+    const int64_t at = scale_row * q.srow + block * q.sblk;
+    if (q.e8m0) static_cast<uint8_t*>(q.scales)[at] = (uint8_t)b;
+    else static_cast<float*>(q.scales)[at] = e8m0_value(b);
+}
+
+// |x| as bits if finite, else 0 (the order of non-negative floats is that of their bits)
+__device__ __forceinline__ uint32_t finite_bits(float x) {
+    const uint32_t u = __float_as_uint(x) & 0x7FFFFFFFu;
+    return u < 0x7F800000u ? u : 0u;
+}
+// exponent byte of the smallest power of two >= a / 448: 448 = 1.75 * 2^8, so it is a's own exponent
+// less 8, or less 7 where a's fraction is over 0.75
+__device__ __forceinline__ uint32_t scale_byte(uint32_t a) {
+    if (a == 0u) return 127u;
+    const int e = (int)(a >> 23) - 8 + ((a & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return e < 1 ? 1u : (uint32_t)e;
+}
+// eight values to codes, scale 2^(b - 127) with 1 <= b <= 247; the conversion rounds to nearest even
+__device__ __forceinline__ piece8 encode8(const float (&v)[8], uint32_t b) {
+    const float inv = __uint_as_float((254u - b) << 23);
+    piece8 r;
+    uint32_t most = 0u;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h] * inv, v[4 * h + 1] * inv, 0, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h + 2] * inv, v[4 * h + 3] * inv, w, true);
+        r[h] = (uint32_t)w;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    if (most >= 0x7F800000u) {               // infinities and NaN: one code for all
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((__float_as_uint(v[i]) & 0x7FFFFFFFu) >= 0x7F800000u)
+                r[i >> 2] = (r[i >> 2] & ~(0xFFu << (8 * (i & 3)))) | (0x7Fu << (8 * (i & 3)));
+    }
+    return r;
+}
+__device__ __forceinline__ void decode8(piece8 c, float scale, float (&v)[8]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[h], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[h], true);
+        v[4 * h] = lo[0] * scale; v[4 * h + 1] = lo[1] * scale;
+        v[4 * h + 2] = hi[0] * scale; v[4 * h + 3] = hi[1] * scale;
+    }
+}
+
+// maximum over each row of 16 lanes (one block of 128 columns), in all its lanes; all 64 lanes active
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_u32(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
+}
+__device__ __forceinline__ uint32_t row16_max(uint32_t v) {
+    v = max(v, dpp_u32<DPP_QUAD_XOR1>(v));
+    v = max(v, dpp_u32<DPP_QUAD_XOR2>(v));
+    v = max(v, dpp_u32<DPP_ROW_HALF_MIRROR>(v));
+    return max(v, dpp_u32<DPP_ROW_MIRROR>(v));
+}
+__device__ __forceinline__ uint32_t max8_bits(const float (&v)[8]) {
+    uint32_t a = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a = max(a, finite_bits(v[i]));
+    return a;
+}
+// sum over the wavefront in a fixed order, the same value in every lane; all 64 lanes active
+__device__ __forceinline__ float wave_sum(float v) {
+    v += dpp_mov<DPP_QUAD_XOR1>(v);
+    v += dpp_mov<DPP_QUAD_XOR2>(v);
+    v += dpp_mov<DPP_ROW_HALF_MIRROR>(v);
+    v += dpp_mov<DPP_ROW_MIRROR>(v);
+    return (read_lane(v, 0) + read_lane(v, 16)) + (read_lane(v, 32) + read_lane(v, 48));
+}
+
+// A 32-bit number as the sum of three bf16 (8 + 8 + 8 significant bits, by truncation).  An infinity or NaN
+// stays whole in the first.
+__device__ __forceinline__ void split3(float x, uint32_t (&p)[3]) {
+    const uint32_t u = __float_as_uint(x);
+    if ((u & 0x7F800000u) == 0x7F800000u) {
+        p[0] = (u >> 16) | ((u & 0x7FFFFFu) ? 0x40u : 0u);
+        p[1] = p[2] = 0u;
+        return;
+    }
+    const float r1 = x - __uint_as_float(u & 0xFFFF0000u);
+    const uint32_t u1 = __float_as_uint(r1) & 0xFFFF0000u;
+    const float r2 = r1 - __uint_as_float(u1);
+    p[0] = u >> 16; p[1] = u1 >> 16; p[2] = __float_as_uint(r2) >> 16;
+}
+
+#endif  // __HIPCC__
+
+}  // namespace dmmv

@@ -1,0 +1,372 @@
+// Layer norm, forward and backward (include/dmmv_layer.h).
+//
+// Both passes are bound by memory: some ten operations for each element that is read.  A team of
+// threads (a wavefront, or a whole workgroup for long rows) holds its row in registers, so the row is
+// read once and the variance is the sum of squared deviations from the mean, not a difference of sums.
+// A lane has 8 consecutive columns of every chunk, 16 lanes a block of 128: the 8-bit results need no
+// exchange but the block's maximum.  Rows beyond the registers are walked three times instead.
+#include "dmmv_layer_common.h"
+
+namespace dmmv {
+
+// one array of a row that is there or not, and the 8-bit outputs
+template <class T>
+struct NormOut {
+    T* y;
+    int64_t ldy;
+    BlockView q, xq;
+    int32_t has_q, has_xq;
+};
+
+// sum over the TPR threads of a team, in every thread; `sh` [TPR / 64]
+template <int TPR>
+__device__ __forceinline__ float team_sum(float v, float* sh) {
+    v = wave_sum(v);
+    if constexpr (TPR > 64) {
+        const int w = threadIdx.x >> 6;
+        __syncthreads();                     // the last round's values have been read
+        if ((threadIdx.x & 63) == 0) sh[w] = v;
+        __syncthreads();
+        v = sh[0];
+#pragma unroll
+        for (int i = 1; i < TPR / 64; ++i) v += sh[i];
+    }
+    return v;
+}
+
+template <class T>
+__device__ __forceinline__ void put_q(const BlockView& q, int64_t row, int64_t col, int64_t cols, const float (&v)[8]) {
+    const uint32_t b = scale_byte(row16_max(max8_bits(v)));
+    if (col < cols) {
+        store8_codes(q.codes + row * q.ld, col, cols, encode8(v, b));
+        if ((threadIdx.x & 15) == 0) scale_put(q, row, col >> 7, b);
+    }
+}
+
+// v = (x - mean) rstd gamma + beta of 8 columns, zero past the row's end
+__device__ __forceinline__ void norm8(const float (&x)[8], int64_t col, int64_t cols, float mu, float rs,
+                                      const float* __restrict__ gamma, const float* __restrict__ beta, float (&v)[8]) {
+    float g[8], b[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { g[e] = 1.0f; b[e] = 0.0f; }
+    if (gamma) load8(gamma, col, cols, g);
+    if (beta) load8(beta, col, cols, b);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = col + e < cols ? dmmv_fma((x[e] - mu) * rs, g[e], b[e]) : 0.0f;
+}
+
+// TPR threads a row, CH chunks of 8 TPR columns in registers
+template <class T, int TPR, int CH>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm(int64_t rows, int64_t cols, const T* __restrict__ x, int64_t ldx,
+                                                                     const float* __restrict__ gamma, const float* __restrict__ beta,
+                                                                     float eps, NormOut<T> o, float* __restrict__ mean,
+                                                                     float* __restrict__ rstd) {
+    __shared__ float sh[TPR / 64];
+    constexpr int TEAMS = TPR < 256 ? 256 / TPR : 1;
+    const int team = threadIdx.x / TPR, t = threadIdx.x % TPR;
+    const int64_t row = blockIdx.x * (int64_t)TEAMS + team;
+    if (row >= rows) return;                 // whole wavefronts; with TPR > 64 there is one team and none leaves
+    const T* xr = x + row * ldx;
+    const float n = (float)cols;
+    float v[CH][8], s = 0.0f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) load8(xr, (c * TPR + t) * 8ll, cols, v[c]);
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s += v[c][e];
+    const float mu = team_sum<TPR>(s, sh) / n;
+    s = 0.0f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float d = (c * TPR + t) * 8ll + e < cols ? v[c][e] - mu : 0.0f;
+            s = dmmv_fma(d, d, s);
+        }
+    const float rs = 1.0f / __builtin_sqrtf(team_sum<TPR>(s, sh) / n + eps);
+    if (t == 0) {
+        if (mean) mean[row] = mu;
+        if (rstd) rstd[row] = rs;
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int64_t col = (c * TPR + t) * 8ll;
+        if (o.has_xq) put_q<T>(o.xq, row, col, cols, v[c]);
+        float w[8];
+        norm8(v[c], col, cols, mu, rs, gamma, beta, w);
+        if (o.y) store8(o.y + row * o.ldy, col, cols, w);
+        if (o.has_q) put_q<T>(o.q, row, col, cols, w);
+    }
+}
+
+// rows of any length: one workgroup, three walks over the row
+template <class T>
+__global__ __launch_bounds__(1024) void k_layernorm_wide(int64_t rows, int64_t cols, const T* __restrict__ x, int64_t ldx,
+                                                         const float* __restrict__ gamma, const float* __restrict__ beta, float eps,
+                                                         NormOut<T> o, float* __restrict__ mean, float* __restrict__ rstd) {
+    __shared__ float sh[16];
+    const int64_t row = blockIdx.x;
+    const T* xr = x + row * ldx;
+    const float n = (float)cols;
+    float s = 0.0f;
+    for (int64_t col = threadIdx.x * 8ll; col < cols; col += 8192) {
+        float v[8];
+        load8(xr, col, cols, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s += v[e];
+    }
+    const float mu = team_sum<1024>(s, sh) / n;
+    s = 0.0f;
+    for (int64_t col = threadIdx.x * 8ll; col < cols; col += 8192) {
+        float v[8];
+        load8(xr, col, cols, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float d = col + e < cols ? v[e] - mu : 0.0f;
+            s = dmmv_fma(d, d, s);
+        }
+    }
+    const float rs = 1.0f / __builtin_sqrtf(team_sum<1024>(s, sh) / n + eps);
+    if (threadIdx.x == 0) {
+        if (mean) mean[row] = mu;
+        if (rstd) rstd[row] = rs;
+    }
+    for (int64_t c0 = 0; c0 < cols; c0 += 8192) {            // every lane stays for the blocks' maxima
+        const int64_t col = c0 + threadIdx.x * 8ll;
+        float v[8], w[8];
+        load8(xr, col, cols, v);
+        if (o.has_xq) put_q<T>(o.xq, row, col, cols, v);
+        norm8(v, col, cols, mu, rs, gamma, beta, w);
+        if (o.y) store8(o.y + row * o.ldy, col, cols, w);
+        if (o.has_q) put_q<T>(o.q, row, col, cols, w);
+    }
+}
+
+// ---- backward ---------------------------------------------------------------------------------
+// the norm's input: a matrix, or its 8-bit checkpoint
+template <class T, bool Q8>
+struct NormIn {
+    const T* x;
+    int64_t ldx;
+    BlockView q;
+    __device__ __forceinline__ void get(int64_t row, int64_t col, int64_t cols, float (&v)[8]) const {
+        if constexpr (Q8) {
+            if (col < cols) {
+                decode8(load8_codes(q.codes + row * q.ld, col, cols), scale_at(q, row, col >> 7), v);
+                if (col + 8 > cols)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = col + e < cols ? v[e] : 0.0f;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+            }
+        } else {
+            load8(x + row * ldx, col, cols, v);
+        }
+    }
+};
+
+// sums of a row: s[row] = {sum a / n, sum a h / n}
+template <class T, bool Q8>
+__global__ __launch_bounds__(256) void k_layernorm_grad_sums(int64_t cols, const T* __restrict__ dy, int64_t lddy, NormIn<T, Q8> in,
+                                                             const float* __restrict__ gamma, const float* __restrict__ mean,
+                                                             const float* __restrict__ rstd, float2* __restrict__ sums) {
+    __shared__ float sh[4];
+    const int64_t row = blockIdx.x;
+    const float mu = mean[row], rs = rstd[row];
+    float s1 = 0.0f, s2 = 0.0f;
+    for (int64_t col = threadIdx.x * 8ll; col < cols; col += 2048) {
+        float d[8], v[8], g[8] = {1, 1, 1, 1, 1, 1, 1, 1};
+        load8(dy + row * lddy, col, cols, d);
+        in.get(row, col, cols, v);
+        if (gamma) load8(gamma, col, cols, g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float a = d[e] * g[e];
+            s1 += a;
+            s2 = dmmv_fma(a, (v[e] - mu) * rs, s2);
+        }
+    }
+    s1 = team_sum<256>(s1, sh);
+    s2 = team_sum<256>(s2, sh);
+    if (threadIdx.x == 0) sums[row] = make_float2(s1 / (float)cols, s2 / (float)cols);
+}
+
+// a strip of 2048 columns and every gridDim.y-th row: dx and this workgroup's share of dgamma, dbeta
+template <class T, bool Q8>
+__global__ __launch_bounds__(256) void k_layernorm_grad_apply(int64_t rows, int64_t cols, const T* __restrict__ dy, int64_t lddy,
+                                                              NormIn<T, Q8> in, const float* __restrict__ gamma,
+                                                              const float* __restrict__ mean, const float* __restrict__ rstd,
+                                                              const float2* __restrict__ sums, T* __restrict__ dx, int64_t lddx,
+                                                              float* __restrict__ part) {
+    const int64_t col = (blockIdx.x * 256ll + threadIdx.x) * 8;
+    if (col >= cols) return;
+    float g[8] = {1, 1, 1, 1, 1, 1, 1, 1}, dg[8] = {}, db[8] = {};
+    if (gamma) load8(gamma, col, cols, g);
+    for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
+        const float mu = mean[row], rs = rstd[row];
+        float d[8], v[8], w[8];
+        load8(dy + row * lddy, col, cols, d);
+        in.get(row, col, cols, v);
+        float2 s = make_float2(0.0f, 0.0f);
+        if (dx) s = sums[row];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float h = (v[e] - mu) * rs;
+            w[e] = rs * ((d[e] * g[e] - s.x) - h * s.y);
+            dg[e] = dmmv_fma(d[e], h, dg[e]);
+            db[e] += d[e];
+        }
+        if (dx) store8(dx + row * lddx, col, cols, w);
+    }
+    if (part) {
+        float* p = part + blockIdx.y * 2ll * cols;
+        store8(p, col, cols, dg);
+        store8(p + cols, col, cols, db);
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------------
+static int64_t norm_strips(int64_t rows, int64_t cols) {
+    int64_t s = 1024 / ceil_div(cols, 2048);
+    if (s < 1) s = 1;
+    return rows < s ? rows : s;
+}
+static size_t norm_workspace(int64_t rows, int64_t cols) {
+    if (rows <= 0 || cols <= 0) return 0;
+    const size_t sums = ((size_t)rows * 8 + 255) / 256 * 256;
+    return sums + (size_t)norm_strips(rows, cols) * 2 * cols * 4;
+}
+
+template <class T>
+static dmmv_status norm_forward(int64_t rows, int64_t cols, const T* x, int64_t ldx, const float* gamma, const float* beta,
+                                float eps, const NormOut<T>& o, float* mean, float* rstd, hipStream_t stream) {
+#define NORM_LAUNCH(TPR, CH)                                                                                         \
+    hipLaunchKernelGGL((k_layernorm<T, TPR, CH>), dim3((unsigned)ceil_div(rows, TPR < 256 ? 256 / TPR : 1)),         \
+                       dim3(TPR < 256 ? 256 : TPR), 0, stream, rows, cols, x, ldx, gamma, beta, eps, o, mean, rstd)
+    if (cols <= 512) NORM_LAUNCH(64, 1);
+    else if (cols <= 1024) NORM_LAUNCH(64, 2);
+    else if (cols <= 2048) NORM_LAUNCH(256, 1);
+    else if (cols <= 4096) NORM_LAUNCH(256, 2);
+    else if (cols <= 8192) NORM_LAUNCH(256, 4);
+    else if (cols <= 16384) NORM_LAUNCH(1024, 2);
+    else
+        hipLaunchKernelGGL((k_layernorm_wide<T>), dim3((unsigned)rows), dim3(1024), 0, stream, rows, cols, x, ldx, gamma, beta,
+                           eps, o, mean, rstd);
+#undef NORM_LAUNCH
+    DMMV_LAUNCH_CHECK();
+    return DMMV_OK;
+}
+
+template <class T, bool Q8>
+static dmmv_status norm_backward(int64_t rows, int64_t cols, const T* dy, int64_t lddy, const NormIn<T, Q8>& in, const float* gamma,
+                                 const float* mean, const float* rstd, T* dx, int64_t lddx, float* dgamma, float* dbeta,
+                                 char* ws, hipStream_t stream) {
+    float2* sums = reinterpret_cast<float2*>(ws);
+    float* part = reinterpret_cast<float*>(ws + ((size_t)rows * 8 + 255) / 256 * 256);
+    const int64_t strips = norm_strips(rows, cols);
+    if (dx) {
+        hipLaunchKernelGGL((k_layernorm_grad_sums<T, Q8>), dim3((unsigned)rows), dim3(256), 0, stream, cols, dy, lddy, in, gamma,
+                           mean, rstd, sums);
+        DMMV_LAUNCH_CHECK();
+    }
+    hipLaunchKernelGGL((k_layernorm_grad_apply<T, Q8>), dim3((unsigned)ceil_div(cols, 2048), (unsigned)strips), dim3(256), 0, stream,
+                       rows, cols, dy, lddy, in, gamma, mean, rstd, sums, dx, lddx, dgamma || dbeta ? part : nullptr);
+    DMMV_LAUNCH_CHECK();
+    if (dgamma || dbeta) DMMV_TRY(layer_sum_parts(part, strips, 2 * cols, dgamma, cols, dbeta, stream));
+    return DMMV_OK;
+}
+
+template <class T>
+static dmmv_status norm_backward_of(int64_t rows, int64_t cols, const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                                    const dmmv_block_matrix* xq, const float* gamma, const float* mean, const float* rstd,
+                                    void* dx, int64_t lddx, float* dgamma, float* dbeta, void* ws, hipStream_t s) {
+    if (xq) {
+        const NormIn<T, true> in{nullptr, 0, layer_view(xq)};
+        return norm_backward<T, true>(rows, cols, static_cast<const T*>(dy), lddy, in, gamma, mean, rstd, static_cast<T*>(dx), lddx,
+                                      dgamma, dbeta, static_cast<char*>(ws), s);
+    }
+    const NormIn<T, false> in{static_cast<const T*>(x), ldx, BlockView{}};
+    return norm_backward<T, false>(rows, cols, static_cast<const T*>(dy), lddy, in, gamma, mean, rstd, static_cast<T*>(dx), lddx,
+                                   dgamma, dbeta, static_cast<char*>(ws), s);
+}
+
+static dmmv_status check_vector(const float* p, bool needed, const char* what) {
+    if (needed && !p) return fail(DMMV_ERR_NULL, "%s is NULL", what);
+    if ((uintptr_t)p % 4) return fail(DMMV_ERR_SHAPE, "%s is not aligned to its elements", what);
+    return DMMV_OK;
+}
+
+static dmmv_status check_out_block(const dmmv_block_matrix* q, int64_t rows, int64_t cols, const char* what) {
+    DMMV_TRY(layer_check_block(q, true, what));
+    if (q->rows != rows || q->cols != cols) return fail(DMMV_ERR_SHAPE, "%s is not %lld x %lld", what, (long long)rows, (long long)cols);
+    if (q->scale_rows != 1) return fail(DMMV_ERR_UNSUPPORTED, "%s: a row's blocks have scales of their own (scale_rows 1)", what);
+    return DMMV_OK;
+}
+
+}  // namespace dmmv
+
+using namespace dmmv;
+
+extern "C" dmmv_status dmmv_layernorm(int32_t dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx, const float* gamma,
+                                      const float* beta, float eps, void* y, int64_t ldy, const dmmv_block_matrix* q,
+                                      const dmmv_block_matrix* xq, float* mean, float* rstd, void* hip_stream) {
+    DMMV_TRY(layer_check_dtype(dtype));
+    DMMV_TRY(layer_check_sizes(rows, cols, "x"));
+    if (!(eps >= 0.0f) || eps > 3.0e38f) return fail(DMMV_ERR_DOMAIN, "eps must be finite and not negative");
+    const int w = layer_width(dtype);
+    DMMV_TRY(layer_check_array(x, rows, cols, ldx, w, "x"));
+    if (y) DMMV_TRY(layer_check_array(y, rows, cols, ldy, w, "y"));
+    if (q) DMMV_TRY(check_out_block(q, rows, cols, "q"));
+    if (xq) DMMV_TRY(check_out_block(xq, rows, cols, "xq"));
+    DMMV_TRY(check_vector(gamma, false, "gamma"));
+    DMMV_TRY(check_vector(beta, false, "beta"));
+    DMMV_TRY(check_vector(mean, false, "mean"));
+    DMMV_TRY(check_vector(rstd, false, "rstd"));
+    if (rows == 0 || cols == 0) return DMMV_OK;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    if (dtype == DMMV_F32) {
+        const NormOut<float> o{static_cast<float*>(y), ldy, layer_view(q), layer_view(xq), q != nullptr, xq != nullptr};
+        return norm_forward(rows, cols, static_cast<const float*>(x), ldx, gamma, beta, eps, o, mean, rstd, s);
+    }
+    const NormOut<bf16_t> o{static_cast<bf16_t*>(y), ldy, layer_view(q), layer_view(xq), q != nullptr, xq != nullptr};
+    return norm_forward(rows, cols, static_cast<const bf16_t*>(x), ldx, gamma, beta, eps, o, mean, rstd, s);
+}
+
+extern "C" size_t dmmv_layernorm_workspace_bytes(int64_t rows, int64_t cols) {
+    if (layer_check_sizes(rows, cols, "x") != DMMV_OK) return 0;
+    return norm_workspace(rows, cols);
+}
+
+extern "C" dmmv_status dmmv_layernorm_backward(int32_t dtype, int64_t rows, int64_t cols, const void* dy, int64_t lddy, const void* x,
+                                               int64_t ldx, const dmmv_block_matrix* xq, const float* gamma, const float* mean,
+                                               const float* rstd, void* dx, int64_t lddx, float* dgamma, float* dbeta,
+                                               void* workspace, size_t workspace_bytes, void* hip_stream) {
+    DMMV_TRY(layer_check_dtype(dtype));
+    DMMV_TRY(layer_check_sizes(rows, cols, "x"));
+    const int w = layer_width(dtype);
+    const bool empty = rows == 0 || cols == 0;
+    if (x && xq) return fail(DMMV_ERR_NULL, "only one of x and xq can be given");
+    if (!x && !xq && !empty) return fail(DMMV_ERR_NULL, "x and xq are both NULL");
+    DMMV_TRY(layer_check_array(dy, rows, cols, lddy, w, "dy"));
+    if (x) DMMV_TRY(layer_check_array(x, rows, cols, ldx, w, "x"));
+    if (xq) {
+        DMMV_TRY(layer_check_block(xq, false, "xq"));
+        if (xq->rows != rows || xq->cols != cols)
+            return fail(DMMV_ERR_SHAPE, "xq is not %lld x %lld", (long long)rows, (long long)cols);
+    }
+    if (dx) DMMV_TRY(layer_check_array(dx, rows, cols, lddx, w, "dx"));
+    DMMV_TRY(check_vector(gamma, false, "gamma"));
+    DMMV_TRY(check_vector(mean, !empty, "mean"));
+    DMMV_TRY(check_vector(rstd, !empty, "rstd"));
+    DMMV_TRY(check_vector(dgamma, false, "dgamma"));
+    DMMV_TRY(check_vector(dbeta, false, "dbeta"));
+    DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, norm_workspace(rows, cols)));
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    if (cols == 0 || (!dx && !dgamma && !dbeta)) return DMMV_OK;
+    if (rows == 0) return layer_sum_parts(nullptr, 0, 2 * cols, dgamma, cols, dbeta, s);     // sums over no rows
+    if (dtype == DMMV_F32)
+        return norm_backward_of<float>(rows, cols, dy, lddy, x, ldx, xq, gamma, mean, rstd, dx, lddx, dgamma, dbeta, workspace, s);
+    return norm_backward_of<bf16_t>(rows, cols, dy, lddy, x, ldx, xq, gamma, mean, rstd, dx, lddx, dgamma, dbeta, workspace, s);
+}

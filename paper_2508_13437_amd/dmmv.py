@@ -18,7 +18,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdmmv.so")
 
-DMMV_F32, DMMV_F64 = 0, 1
+DMMV_F32, DMMV_F64, DMMV_BF16, DMMV_E8M0 = 0, 1, 2, 3
 DMMV_OK = 0
 STATUS_NAMES = {0: "DMMV_OK", -1: "DMMV_ERR_NULL", -2: "DMMV_ERR_SHAPE", -3: "DMMV_ERR_DTYPE",
                 -4: "DMMV_ERR_DOMAIN", -5: "DMMV_ERR_WORKSPACE", -6: "DMMV_ERR_HIP",
@@ -29,6 +29,9 @@ EXPORTS = ("dmmv_workspace_bytes", "dmmv_create", "dmmv_destroy", "dmmv_set_x",
            "dmmv_apply_move", "dmmv_get_state", "dmmv_solve", "dmmv_solve_static", "dmmv_alns", "dmmv_swap_move",
            "dmmv_l2_changes",
            "dmmv_time_eval", "dmmv_time_l2", "dmmv_loop_in_use", "dmmv_scoring_in_use",
+           "dmmv_block_quantize", "dmmv_block_dequantize", "dmmv_block_product_workspace_bytes",
+           "dmmv_block_product", "dmmv_block_backward_workspace_bytes", "dmmv_block_backward",
+           "dmmv_layernorm", "dmmv_layernorm_workspace_bytes", "dmmv_layernorm_backward",
            "dmmv_last_error",
            "dmmv_version")
 
@@ -106,6 +109,22 @@ def load() -> C.CDLL:
     lib.dmmv_time_eval.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_float)]
     lib.dmmv_time_l2.restype = C.c_int
     lib.dmmv_time_l2.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_float)]
+    p, i64, i32, f32 = C.c_void_p, C.c_int64, C.c_int32, C.c_float
+    for name, args in (
+            ("dmmv_block_quantize", [i32, p, i64, p, p]),
+            ("dmmv_block_dequantize", [p, i32, p, i64, p]),
+            ("dmmv_block_product", [p, p, p, i32, p, i64, p, C.c_size_t, p]),
+            ("dmmv_block_backward", [i32, i64, i64, i64, p, i64, p, p, p, i64, p, i64, p, p, C.c_size_t, p]),
+            ("dmmv_layernorm", [i32, i64, i64, p, i64, p, p, f32, p, i64, p, p, p, p, p]),
+            ("dmmv_layernorm_backward", [i32, i64, i64, p, i64, p, i64, p, p, p, p, p, i64, p, p, p, C.c_size_t, p])):
+        fn = getattr(lib, name)
+        fn.restype = C.c_int
+        fn.argtypes = args
+    for name, nargs in (("dmmv_block_product_workspace_bytes", 3), ("dmmv_block_backward_workspace_bytes", 3),
+                        ("dmmv_layernorm_workspace_bytes", 2)):
+        fn = getattr(lib, name)
+        fn.restype = C.c_size_t
+        fn.argtypes = [i64] * nargs
     lib.dmmv_last_error.restype = C.c_char_p
     lib.dmmv_version.restype = C.c_char_p
     _lib = lib
@@ -481,3 +500,221 @@ def from_instance(inst, device="cuda:0", **options) -> Handle:
     A = torch.from_numpy(np.ascontiguousarray(inst.A.T)).to(dev).t()    # column-major view
     scale = inst.scale if inst.kind == "batched" else None
     return Handle(D=inst.D, b=b, A=A, scale=scale, device=dev, **options)
+
+
+# ---- a quantised linear layer (include/dmmv_layer.h) --------------------------------------------
+# These calls have no handle: they are enqueued on PyTorch's current stream of the tensors' device,
+# and what they return is allocated there.  Matrices whose rows are not contiguous are copied first.
+class _BlockMatrix(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("codes", C.c_void_p), ("ld", C.c_int64),
+                ("scales", C.c_void_p), ("scale_row_stride", C.c_int64), ("scale_block_stride", C.c_int64),
+                ("scale_type", C.c_int32), ("scale_rows", C.c_int32)]
+
+
+class BlockMatrix:
+    """A matrix in 8 bits: e4m3 codes [rows][cols] (uint8 or float8_e4m3fn) and a scale for every 128
+    columns of a row (scale_rows = 1) or of 128 rows (scale_rows = 128).  scales [rows / scale_rows]
+    [cols / 128], rounded up, holds exponent bytes (uint8 or float8_e8m0fnu: 2^(byte - 127)) or float32,
+    with any strides: a scale per row is s[:, None].expand(-1, blocks).  None: all 1."""
+
+    __slots__ = ("codes", "scales", "scale_rows", "rows", "cols", "_c", "_p")
+
+    def __init__(self, codes: torch.Tensor, scales: Optional[torch.Tensor] = None, scale_rows: int = 1):
+        if codes.dim() != 2:
+            raise DmmvError(-2, "codes must be 2-D")
+        if codes.dtype != torch.uint8 and codes.dtype != torch.float8_e4m3fn:
+            raise DmmvError(-3, f"codes are {codes.dtype}, not uint8 or float8_e4m3fn")
+        if codes.device.type != "cuda":
+            raise DmmvError(-6, "tensors must live on the GPU")
+        if scale_rows not in (1, 128):
+            raise DmmvError(-2, "scale_rows must be 1 or 128")
+        codes = _rows(codes)
+        rows, cols = codes.shape
+        c = _BlockMatrix(rows, cols, codes.data_ptr(), codes.stride(0), None, 0, 0, DMMV_E8M0, scale_rows)
+        if scales is not None:
+            if scales.dtype == torch.float32:
+                c.scale_type = DMMV_F32
+            elif scales.dtype != torch.uint8 and scales.dtype != torch.float8_e8m0fnu:
+                raise DmmvError(-3, f"scales are {scales.dtype}, not uint8, float8_e8m0fnu or float32")
+            if tuple(scales.shape) != (-(-rows // scale_rows), -(-cols // 128)):
+                raise DmmvError(-2, f"scales must be {-(-rows // scale_rows)} x {-(-cols // 128)}")
+            if scales.device != codes.device:
+                raise DmmvError(-6, "codes and scales are on different devices")
+            c.scales = scales.data_ptr()
+            c.scale_row_stride, c.scale_block_stride = scales.stride()
+        self.codes, self.scales, self.scale_rows = codes, scales, scale_rows
+        self.rows, self.cols = rows, cols
+        self._c, self._p = c, C.addressof(c)
+
+    @property
+    def values8(self) -> torch.Tensor:
+        """The codes as float8_e4m3fn."""
+        return self.codes.view(torch.float8_e4m3fn)
+
+    @property
+    def device(self) -> torch.device:
+        return self.codes.device
+
+
+def _rows(t: torch.Tensor) -> torch.Tensor:
+    """t with contiguous rows that do not overlap."""
+    if t.numel() == 0 or ((t.stride(1) == 1 or t.shape[1] == 1) and (t.stride(0) >= t.shape[1] or t.shape[0] == 1)):
+        return t
+    return t.contiguous()
+
+
+def _matrix(t: torch.Tensor, what: str, rows: int = -1, cols: int = -1, dtype=None) -> torch.Tensor:
+    if t.dim() != 2:
+        raise DmmvError(-2, f"{what} must be 2-D")
+    if t.device.type != "cuda":
+        raise DmmvError(-6, "tensors must live on the GPU")
+    if dtype is not None and t.dtype != dtype:
+        raise DmmvError(-3, f"{what} is {t.dtype}, not {dtype}")
+    if (rows >= 0 and t.shape[0] != rows) or (cols >= 0 and t.shape[1] != cols):
+        raise DmmvError(-2, f"{what} is {t.shape[0]} x {t.shape[1]}, expected {rows} x {cols}")
+    return _rows(t)
+
+
+def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[torch.Tensor]:
+    if t is None:
+        return None
+    if t.dtype != torch.float32:
+        raise DmmvError(-3, f"{what} is {t.dtype}, not torch.float32")
+    if t.dim() != 1 or t.shape[0] != n:
+        raise DmmvError(-2, f"{what} must have {n} entries")
+    return t.contiguous()
+
+
+def _layer_dtype(dtype: torch.dtype) -> int:
+    if dtype == torch.bfloat16:
+        return DMMV_BF16
+    if dtype == torch.float32:
+        return DMMV_F32
+    raise DmmvError(-3, f"unsupported dtype {dtype}")
+
+
+def _addr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _enqueue(dev: torch.device, name: str, tensors, *args):
+    """One call on the device's current stream; the tensors must all live on that device."""
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise DmmvError(-6, "tensors are on different devices")
+    fn = getattr(load(), name)
+    stream = torch.cuda.current_stream(dev).cuda_stream
+    if torch.cuda.current_device() == dev.index:
+        _check(fn(*args, stream))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, stream))
+
+
+def _new_block(rows: int, cols: int, scale_rows: int, scale_dtype: torch.dtype, dev: torch.device) -> BlockMatrix:
+    codes = torch.empty((rows, cols), dtype=torch.uint8, device=dev)
+    scales = torch.empty((-(-rows // scale_rows), -(-cols // 128)), dtype=scale_dtype, device=dev)
+    return BlockMatrix(codes, scales, scale_rows)
+
+
+def dmmv_block_quantize(x: torch.Tensor, scale_rows: int = 1, scale_dtype: torch.dtype = torch.uint8) -> BlockMatrix:
+    """x (float32 or bfloat16) in 8 bits, each scale the smallest power of two that holds its block; as
+    exponent bytes (uint8) or float32."""
+    x = _matrix(x, "x")
+    q = _new_block(x.shape[0], x.shape[1], scale_rows, scale_dtype, x.device)
+    _enqueue(x.device, "dmmv_block_quantize", (), _layer_dtype(x.dtype), x.data_ptr(), x.stride(0), q._p)
+    return q
+
+
+def dmmv_block_dequantize(q: BlockMatrix, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """The values that q stands for."""
+    x = torch.empty((q.rows, q.cols), dtype=dtype, device=q.device)
+    _enqueue(q.device, "dmmv_block_dequantize", (), q._p, _layer_dtype(dtype), x.data_ptr(), x.stride(0))
+    return x
+
+
+def dmmv_block_product(x: BlockMatrix, w: BlockMatrix, bias: Optional[torch.Tensor] = None,
+                       dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """y = x w^T + bias, [x.rows][w.rows]."""
+    bias = _vector(bias, w.rows, "bias")
+    code = _layer_dtype(dtype)
+    dev = x.codes.device
+    y = torch.empty((x.rows, w.rows), dtype=dtype, device=dev)
+    nbytes = load().dmmv_block_product_workspace_bytes(x.rows, w.rows, x.cols)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    _enqueue(dev, "dmmv_block_product", (w.codes, bias), x._p, w._p, _addr(bias), code, y.data_ptr(), w.rows, _addr(ws), nbytes)
+    return y
+
+
+def dmmv_block_backward(dy: torch.Tensor, x: Optional[BlockMatrix], w: Optional[BlockMatrix], dx: bool = True,
+                        dw: bool = True, dbias: bool = True):
+    """Gradients of dmmv_block_product from those of its result: (dx [T][K] of dy's type, dw [O][K] and
+    dbias [O] in float32), None for those that are not asked for.  x is the checkpoint that the product
+    read; it may be None without dw, and w without dx."""
+    if (dw and x is None) or (dx and w is None):
+        raise DmmvError(-1, "dx needs w, dw needs x")
+    T, O = dy.shape if dy.dim() == 2 else (0, 0)
+    dy = _matrix(dy, "dy")
+    K = w.cols if w is not None else x.cols if x is not None else 0
+    code, dev = _layer_dtype(dy.dtype), dy.device
+    gx = torch.empty((T, K), dtype=dy.dtype, device=dev) if dx else None
+    gw = torch.empty((O, K), dtype=torch.float32, device=dev) if dw else None
+    gb = torch.empty((O,), dtype=torch.float32, device=dev) if dbias else None
+    nbytes = load().dmmv_block_backward_workspace_bytes(T, O, K)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    _enqueue(dev, "dmmv_block_backward", (x.codes if dw else None, w.codes if dx else None), code, T, O, K, dy.data_ptr(),
+             dy.stride(0), x._p if dw else None, w._p if dx else None, _addr(gx), K, _addr(gw), K, _addr(gb), _addr(ws), nbytes)
+    return gx, gw, gb
+
+
+@dataclass
+class LayerNormResult:
+    y: Optional[torch.Tensor]     # [T][F] of the input's type
+    q: Optional[BlockMatrix]      # y in 8 bits
+    xq: Optional[BlockMatrix]     # the input in 8 bits
+    mean: torch.Tensor            # [T] float32
+    rstd: torch.Tensor            # [T] float32
+
+
+def dmmv_layernorm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
+                   eps: float = 1e-5, y: bool = True, q: bool = False, xq: bool = False) -> LayerNormResult:
+    """Layer norm of the rows of x (float32 or bfloat16); gamma, beta float32.  y: the result in x's
+    type; q: the result in 8 bits, the operand of dmmv_block_product; xq: a checkpoint of x for
+    dmmv_layernorm_backward.  All from one pass over x."""
+    x = _matrix(x, "x")
+    T, F = x.shape
+    gamma, beta = _vector(gamma, F, "gamma"), _vector(beta, F, "beta")
+    dev = x.device
+    stats = torch.empty((2, T), dtype=torch.float32, device=dev)
+    out = torch.empty((T, F), dtype=x.dtype, device=dev) if y else None
+    oq = _new_block(T, F, 1, torch.uint8, dev) if q else None
+    ox = _new_block(T, F, 1, torch.uint8, dev) if xq else None
+    mean, rstd = stats[0], stats[1]
+    _enqueue(dev, "dmmv_layernorm", (gamma, beta), _layer_dtype(x.dtype), T, F, x.data_ptr(), x.stride(0), _addr(gamma),
+             _addr(beta), eps, _addr(out), F, oq._p if q else None, ox._p if xq else None, mean.data_ptr(), rstd.data_ptr())
+    return LayerNormResult(out, oq, ox, mean, rstd)
+
+
+def dmmv_layernorm_backward(dy: torch.Tensor, x, gamma: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
+                            dx: bool = True, dgamma: bool = True, dbeta: bool = True):
+    """Gradients (dx of dy's type, dgamma, dbeta in float32; None for those not asked for) of dmmv_layernorm.
+    x is its input, or the checkpoint of it (a BlockMatrix); mean and rstd are its own."""
+    dy = _matrix(dy, "dy")
+    T, F = dy.shape
+    code, dev = _layer_dtype(dy.dtype), dy.device
+    if isinstance(x, BlockMatrix):
+        if (x.rows, x.cols) != (T, F):
+            raise DmmvError(-2, f"x is {x.rows} x {x.cols}, expected {T} x {F}")
+        src, px, ldx, pq = x.codes, None, 0, x._p
+    else:
+        x = _matrix(x, "x", T, F, dy.dtype)
+        src, px, ldx, pq = x, x.data_ptr(), x.stride(0), None
+    gamma, mean, rstd = _vector(gamma, F, "gamma"), _vector(mean, T, "mean"), _vector(rstd, T, "rstd")
+    gx = torch.empty((T, F), dtype=dy.dtype, device=dev) if dx else None
+    gg = torch.empty((F,), dtype=torch.float32, device=dev) if dgamma else None
+    gb = torch.empty((F,), dtype=torch.float32, device=dev) if dbeta else None
+    nbytes = load().dmmv_layernorm_workspace_bytes(T, F)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    _enqueue(dev, "dmmv_layernorm_backward", (src, gamma, mean, rstd), code, T, F, dy.data_ptr(), dy.stride(0), px, ldx, pq,
+             _addr(gamma), mean.data_ptr(), rstd.data_ptr(), _addr(gx), F, _addr(gg), _addr(gb), _addr(ws), nbytes)
+    return gx, gg, gb
