@@ -5,26 +5,11 @@
 // (random codes; up to 2^-11 of sum |x w| for single results).  That is far below the rounding of a bf16 result
 // (2e-3), so bf16 results are summed by them; 32-bit results are summed by the 16-bit instructions, which keep the
 // 32-bit sum (8e-8) at half the rate: a code is exact in f16.
+#include <type_traits>
+
 #include "dmmv_layer_common.h"
 
 namespace dmmv {
-
-// 32 codes of a row from column `col` on, zero past `cols`
-__device__ __forceinline__ void codes32(const uint8_t* __restrict__ row, int64_t col, int64_t cols, bool ok, piece16 (&v)[2]) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int64_t c = col + 16 * h;
-        piece16 a = {0u, 0u, 0u, 0u};
-        if (ok && c + 16 <= cols) {
-            a = *reinterpret_cast<const piece16_any*>(row + c);
-        } else if (ok) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (c + i < cols) a[i >> 2] |= (uint32_t)row[c + i] << (8 * (i & 3));
-        }
-        v[h] = a;
-    }
-}
 
 typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
 typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
@@ -51,101 +36,237 @@ __device__ __forceinline__ floatx4 block_sum(const intx8& a, const intx8& b) {
     return p;
 }
 
-// 16 codes of which `left` (any number) belong to the row, the others zero
-__device__ __forceinline__ piece16 chunk_tail(const uint8_t* __restrict__ p, int left) {
+// 16 codes of a row of which `left` (any number) belong to the row, the others zero; `have` codes of the row lie before
+// them.  A piece that the row's end cuts is loaded so that it ends there, and shifted.
+__device__ __forceinline__ piece16 chunk_tail(const uint8_t* __restrict__ p, int left, int64_t have) {
     if (left >= 16) return *reinterpret_cast<const piece16_any*>(p);
     piece16 a = {0u, 0u, 0u, 0u};
+    if (left <= 0) return a;
+    if (have + left >= 16) {
+        const piece16 v = *reinterpret_cast<const piece16_any*>(p - (16 - left));
+        const uint64_t lo = v[0] | ((uint64_t)v[1] << 32), hi = v[2] | ((uint64_t)v[3] << 32);
+        const int s = 8 * (16 - left);               // 8 .. 120
+        const uint64_t l = s >= 64 ? hi >> (s - 64) : (lo >> s) | (hi << (64 - s)), h = s >= 64 ? 0 : hi >> s;
+        return piece16{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
+    }
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
+    for (int i = 0; i < 15; ++i)                     // rows shorter than 16
         if (i < left) a[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
     return a;
+}
+
+__device__ __forceinline__ intx8 words8(piece16 a, piece16 b) {
+    return intx8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+}
+
+// eight codes as bf16, times 2^(b - 127): exact
+__device__ __forceinline__ bf16x8_t scaled8(int lo, int hi, uint32_t b) {
+    const float s = __uint_as_float(b << 23);
+    const auto p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true);
+    const auto r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false), t = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true);
+    return bf16x8_t{p[0], p[1], q[0], q[1], r[0], r[1], t[0], t[1]};
 }
 
 __device__ __forceinline__ void put_y(float* y, float v) { *y = v; }
 __device__ __forceinline__ void put_y(bf16_t* y, float v) { y->u = (uint16_t)bf16_bits(v); }
 
-// Any sizes, strides and scales.  64 x 64 tile, 4 wavefronts of 32 x 32; the codes of one block of 128
-// go through the LDS, and the block's two scales are applied to its sum in 32 bits.
-template <class T>
-__global__ __launch_bounds__(256) void k_block_product(int64_t T_, int64_t O, int64_t K, BlockView x, BlockView w,
-                                                       const float* __restrict__ bias, T* __restrict__ y, int64_t ldy, int64_t tiles_o) {
-    constexpr int LS = 144;                                   // bytes of an LDS row: 128 and a skew of 16
-    __shared__ __align__(16) uint8_t As[64 * LS], Bs[64 * LS];
-    __shared__ float sa[64], sb[64];
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    const int64_t t0 = (blockIdx.x / tiles_o) * 64, o0 = (blockIdx.x % tiles_o) * 64;
-    const int m0 = (wv >> 1) * 32, n0 = (wv & 1) * 32;
-    floatx4 acc[2][2] = {};
-    const int r = tid >> 2, c = (tid & 3) * 32;
-    for (int64_t k0 = 0, kb = 0; k0 < K; k0 += 128, ++kb) {
-        piece16 a[2], b[2];
-        codes32(x.codes + (t0 + r) * x.ld, k0 + c, K, t0 + r < T_, a);
-        codes32(w.codes + (o0 + r) * w.ld, k0 + c, K, o0 + r < O, b);
-        float s = 0.0f;
-        if (tid < 64) s = t0 + tid < T_ ? scale_at(x, t0 + tid, kb) : 0.0f;
-        else if (tid < 128) s = o0 + tid - 64 < O ? scale_at(w, o0 + tid - 64, kb) : 0.0f;
-        __syncthreads();
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            *reinterpret_cast<piece16*>(As + r * LS + c + 16 * h) = a[h];
-            *reinterpret_cast<piece16*>(Bs + r * LS + c + 16 * h) = b[h];
-        }
-        if (tid < 64) sa[tid] = s;
-        else if (tid < 128) sb[tid - 64] = s;
-        __syncthreads();
-        intx8 fa[2], fb[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint8_t* pa = As + (m0 + 16 * i + (lane & 15)) * LS + (lane >> 4) * 32;
-            const uint8_t* pb = Bs + (n0 + 16 * i + (lane & 15)) * LS + (lane >> 4) * 32;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const piece16 qa = *reinterpret_cast<const piece16*>(pa + 16 * h), qb = *reinterpret_cast<const piece16*>(pb + 16 * h);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) { fa[i][4 * h + e] = (int)qa[e]; fb[i][4 * h + e] = (int)qb[e]; }
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const floatx4 p = block_sum<sizeof(T) == 4>(fa[i], fb[j]);
-                const float s_o = sb[n0 + 16 * j + (lane & 15)];
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    acc[i][j][e] = dmmv_fma(p[e], sa[m0 + 16 * i + (lane >> 4) * 4 + e] * s_o, acc[i][j][e]);
-            }
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int64_t o = o0 + n0 + 16 * j + (lane & 15);
-        if (o >= O) continue;
-        const float bo = bias ? bias[o] : 0.0f;
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t t = t0 + m0 + 16 * i + (lane >> 4) * 4 + e;
-                if (t < T_) put_y(y + t * ldy + o, acc[i][j][e] + bo);
-            }
-    }
+// The workgroup's tile.  Workgroups go to the 8 XCDs in turn, each with an L2 of its own: an XCD gets an eighth of the tiles in
+// a row, 4 tiles high and side by side, so that those of one moment share their operands' lines (4096 x 4096 x 11008: 171 us
+// against 188 with the tiles in rows; bands of 8: 185).
+__device__ __forceinline__ void tile_of_workgroup(int tiles_t, int tiles_o, int& tile_t, int& tile_o) {
+    const int n = tiles_t * tiles_o, per = n >> 3, b = (int)blockIdx.x;
+    const int id = b < per * 8 ? (b & 7) * per + (b >> 3) : b;
+    const int band = id / (4 * tiles_o), high = min(4, tiles_t - 4 * band), in = id - band * 4 * tiles_o;
+    // (a division runs on the vector unit: back to scalar registers)
+    tile_o = __builtin_amdgcn_readfirstlane(in / high);
+    tile_t = __builtin_amdgcn_readfirstlane(4 * band + in % high);
 }
 
-
-// ---- large products ------------------------------------------------------------------------------
-// Tile of 32 MI tokens x 32 NI outputs, 4 wavefronts (2 x 2), one block of 128 a step.  A step's codes go
-// through registers into one of two LDS stages while the other is multiplied.  The rows of w are the A
-// operand, so that a lane's four results are consecutive outputs of one token.
+// ---- any sizes, strides, scales ------------------------------------------------------------------
+// Tile of 64 tokens x 64 outputs, 4 wavefronts (2 x 2), one block of 128 a step.  A step's codes and scales go from
+// memory through registers, requested two steps ahead, into one of two LDS stages while the other is multiplied.  The
+// rows of w are the A operand, so that a lane's four results are consecutive outputs of one token.
 //   LDS row: 128 codes, the 16-byte chunk c of row r at c ^ (r & 7): neither the 8 lanes that write a row
 //   nor the 8 rows that are read together meet in a bank.
-// SCALED: power-of-two scales go into the instruction (8 bits) or the conversion to bf16 (32-bit results), four
-// blocks' exponents in one register; scales that are the same along a row are left to the end.
-// WTILE: the scales of w are the same for 128 rows, or for a whole row.
-// Otherwise a block's sum is multiplied by its two scales in 32 bits.
+// SCALED: power-of-two scales go into the instruction (8 bits) or the conversion to bf16 (32-bit results); scales that are
+// the same along a row are left to the end.  Otherwise a block's sum is multiplied by its two scales in 32 bits.
 struct ProductScales {
     int32_t x_blocks, w_blocks;         // SCALED: exponents per block, else constant along the row
 };
 
+// KS groups of 4 wavefronts share the blocks of a tile where the tiles alone do not fill the chip, joined in order.
+template <class T, int KS, bool SCALED>
+__global__ __launch_bounds__(256 * KS) void k_block_product(int64_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
+                                                       const float* __restrict__ bias, T* __restrict__ y, int64_t ldy, int32_t tiles_t, int32_t tiles_o) {
+    constexpr bool WIDE = sizeof(T) == 4;
+    constexpr int MI = 2, NI = 2, BM = 32 * MI, BN = 32 * NI;
+    __shared__ __align__(16) uint8_t codes_of[KS][2][128 * (BM + BN)];
+    __shared__ __align__(16) uint32_t scl_of[KS][2][BM + BN];
+    const int tid = threadIdx.x & 255, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+    const int group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    auto& codes = codes_of[group];
+    auto& scl = scl_of[group];
+    const int wt = (wv & 1) * (16 * MI), wo = (wv >> 1) * (16 * NI);
+    int tile_t, tile_o;
+    tile_of_workgroup(tiles_t, tiles_o, tile_t, tile_o);
+    const int64_t t0 = (int64_t)tile_t * BM, o0 = (int64_t)tile_o * BN;
+    const int nb = (int)((K + 127) >> 7);
+    const int b0 = (int)((int64_t)nb * group / KS), b1 = (int)((int64_t)nb * (group + 1) / KS), steps = (nb + KS - 1) / KS;
+    // this thread's chunks of a step: rows tid / 8 + 32 u of x, then of w; its scale: of row tid of both together
+    const int crow = tid >> 3, cchunk = tid & 7;
+    const uint8_t* xr[MI];
+    const uint8_t* wr[NI];
+#pragma unroll
+    for (int u = 0; u < MI; ++u) xr[u] = x.codes + min(t0 + crow + 32 * u, T_ - 1) * x.ld + cchunk * 16;
+#pragma unroll
+    for (int u = 0; u < NI; ++u) wr[u] = w.codes + min(o0 + crow + 32 * u, O - 1) * w.ld + cchunk * 16;
+    const int put = crow * 128 + ((cchunk ^ (crow & 7)) << 4);
+    const bool mine_x = tid < BM, mine = tid < BM + BN;
+    const BlockView& sq = mine_x ? x : w;
+    const int64_t srow = mine_x ? min(t0 + tid, T_ - 1) : min(o0 + tid - BM, O - 1);
+
+    struct Step {
+        piece16 c[MI + NI];
+        uint32_t s;
+    };
+    auto request = [&](Step& r, int kb) __attribute__((always_inline)) {
+        const int64_t at = kb * 128ll;
+        if (at + 128 <= K) {
+#pragma unroll
+            for (int u = 0; u < MI; ++u) r.c[u] = *reinterpret_cast<const piece16_any*>(xr[u] + at);
+#pragma unroll
+            for (int u = 0; u < NI; ++u) r.c[MI + u] = *reinterpret_cast<const piece16_any*>(wr[u] + at);
+        } else {
+            const int left = (int)(K - at) - cchunk * 16;
+#pragma unroll
+            for (int u = 0; u < MI; ++u) r.c[u] = chunk_tail(xr[u] + at, left, at + cchunk * 16);
+#pragma unroll
+            for (int u = 0; u < NI; ++u) r.c[MI + u] = chunk_tail(wr[u] + at, left, at + cchunk * 16);
+        }
+        // as it is stored: a conversion here would wait for the load
+        r.s = 127u;
+        if (mine && !(SCALED && !(mine_x ? how.x_blocks : how.w_blocks))) r.s = scale_bits(sq, srow, kb);
+    };
+    auto deposit = [&](const Step& r, int stage) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < MI + NI; ++u) *reinterpret_cast<piece16*>(&codes[stage][put + u * 4096]) = r.c[u];
+        if (mine) scl[stage][tid] = SCALED ? r.s : __float_as_uint(scale_of(sq, r.s));
+    };
+    floatx4 acc[NI][MI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < MI; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    const int c0 = (lg ^ (lr & 7)) << 4;
+    auto multiply = [&](int stage) __attribute__((always_inline)) {
+        const uint8_t* px = &codes[stage][(wt + lr) * 128];
+        const uint8_t* pw = &codes[stage][(BM + wo + lr) * 128];
+        intx8 fx[MI], fw[NI];
+#pragma unroll
+        for (int j = 0; j < MI; ++j)
+            fx[j] = words8(*reinterpret_cast<const piece16*>(px + j * 2048 + c0), *reinterpret_cast<const piece16*>(px + j * 2048 + (c0 ^ 64)));
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+            fw[i] = words8(*reinterpret_cast<const piece16*>(pw + i * 2048 + c0), *reinterpret_cast<const piece16*>(pw + i * 2048 + (c0 ^ 64)));
+        if constexpr (SCALED) {
+            uint32_t sx[MI], sw[NI];
+#pragma unroll
+            for (int j = 0; j < MI; ++j) sx[j] = scl[stage][wt + 16 * j + lr];
+#pragma unroll
+            for (int i = 0; i < NI; ++i) sw[i] = scl[stage][BM + wo + 16 * i + lr];
+            if constexpr (!WIDE) {
+#pragma unroll
+                for (int i = 0; i < NI; ++i)
+#pragma unroll
+                    for (int j = 0; j < MI; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[i], fx[j], acc[i][j], 0, 0, 0, (int)sw[i], 0, (int)sx[j]);
+            } else {
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    bf16x8_t bx[MI], bw[NI];
+#pragma unroll
+                    for (int j = 0; j < MI; ++j) bx[j] = scaled8(fx[j][2 * s], fx[j][2 * s + 1], sx[j]);
+#pragma unroll
+                    for (int i = 0; i < NI; ++i) bw[i] = scaled8(fw[i][2 * s], fw[i][2 * s + 1], sw[i]);
+#pragma unroll
+                    for (int i = 0; i < NI; ++i)
+#pragma unroll
+                        for (int j = 0; j < MI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[i], bx[j], acc[i][j], 0, 0, 0);
+                }
+            }
+        } else {
+            float sx[MI];
+#pragma unroll
+            for (int j = 0; j < MI; ++j) sx[j] = __uint_as_float(scl[stage][wt + 16 * j + lr]);
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const floatx4 sw = *reinterpret_cast<const floatx4*>(&scl[stage][BM + wo + 16 * i + lg * 4]);
+#pragma unroll
+                for (int j = 0; j < MI; ++j) {
+                    const floatx4 p = block_sum<WIDE>(fw[i], fx[j]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = dmmv_fma(p[e], sw[e] * sx[j], acc[i][j][e]);
+                }
+            }
+        }
+    };
+    Step r0 = {}, r1 = {};
+    if (b0 < b1) request(r0, b0);
+    if (b0 + 1 < b1) request(r1, b0 + 1);
+    deposit(r0, 0);
+    if (b0 + 2 < b1) request(r0, b0 + 2);
+    __syncthreads();
+    for (int k = 0; k < steps; k += 2) {             // every group has the same barriers, the last may have no block
+        const int kb = b0 + k;
+        deposit(r1, 1);                              // block kb + 1, if there is one
+        if (kb + 3 < b1) request(r1, kb + 3);
+        if (kb < b1) multiply(0);
+        __syncthreads();
+        if (k + 1 >= steps) break;
+        deposit(r0, 0);                              // block kb + 2
+        if (kb + 4 < b1) request(r0, kb + 4);
+        if (kb + 1 < b1) multiply(1);
+        __syncthreads();
+    }
+    if constexpr (KS > 1) {
+        floatx4* join = reinterpret_cast<floatx4*>(&codes_of[0][0][0]);      // [KS - 1][NI * MI][256]
+        if (group > 0)
+#pragma unroll
+            for (int i = 0; i < NI * MI; ++i) join[((group - 1) * NI * MI + i) * 256 + tid] = acc[i / MI][i % MI];
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int g = 1; g < KS; ++g)
+#pragma unroll
+            for (int i = 0; i < NI * MI; ++i) acc[i / MI][i % MI] += join[((g - 1) * NI * MI + i) * 256 + tid];
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        float bo[4], so[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t o = min(o0 + wo + 16 * i + lg * 4 + e, O - 1);
+            bo[e] = bias ? bias[o] : 0.0f;
+            so[e] = SCALED && !how.w_blocks ? scale_at(w, o, 0) : 1.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < MI; ++j) {
+            const int64_t t = t0 + wt + 16 * j + lr, o = o0 + wo + 16 * i + lg * 4;
+            if (t >= T_) continue;
+            const float st = SCALED && !how.x_blocks ? scale_at(x, t, 0) : 1.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (o + e < O) put_y(y + t * ldy + o + e, dmmv_fma(acc[i][j][e], so[e] * st, bo[e]));
+        }
+    }
+}
+
+// ---- large products ------------------------------------------------------------------------------
+// The same tiles, LDS rows and operands for bf16 results with SCALED scales, where rows are aligned to 16 bytes: the
+// codes go straight from memory into the LDS (NST stages of one block of 128), and the loop is written so that the matrix
+// unit has a product at all times: what else there is to do is placed in the products' shadows by hand.
+// WTILE: the scales of w are the same for 128 rows, or for a whole row.
 template <class T>
 __device__ __forceinline__ void put4(T* __restrict__ row, const float (&v)[4]);
 template <>
@@ -176,25 +297,29 @@ __device__ __forceinline__ void stage_exponents(const BlockView& q, int64_t row0
     }
 }
 
-constexpr int product_lds(int MI, int NI, int width, bool wtile) {
-    const int stages = 2 * 128 * 32 * (MI + NI) + 68 * (32 * MI + (wtile ? (32 * NI + 127) / 128 : 32 * NI)), out = 32 * MI * (32 * NI * width + 16);
+constexpr int product_lds(int MI, int NI, int width, bool wtile, int nst) {
+    const int stages = nst * 128 * 32 * (MI + NI) + 68 * (32 * MI + (wtile ? (32 * NI + 127) / 128 : 32 * NI)), out = 32 * MI * (32 * NI * width + 16);
     return stages > out ? stages : out;
 }
 
-// a pointer that is the same in every lane, in scalar registers
-__device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
-    const uint64_t u = (uint64_t)p;
-    return (const uint8_t*)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32)) << 32) |
-                            (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)u));
-}
-// 16 bytes a lane from memory (a uniform base and an offset of 32 bits each) to 1 KB of LDS at a uniform address, in the
-// order of the lanes; in flight until lds_requests_done().  The instruction writes no register.
-__device__ __forceinline__ void lds_request(const uint8_t* base, uint32_t off, uint32_t at) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(off), "s"(base));
-}
-__device__ __forceinline__ void lds_requests_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+typedef int intx4 __attribute__((ext_vector_type(4)));
 
-template <class T, int MI, int NI, bool SCALED, bool WTILE>
+// `bytes` bytes from p on as a buffer (p the same in every lane): reads past them give zero
+__device__ __forceinline__ intx4 buffer_of(const uint8_t* p, uint32_t bytes) {
+    const uint64_t u = (uint64_t)p;
+    return intx4{__builtin_amdgcn_readfirstlane((int)(uint32_t)u), __builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32) & 0xFFFF),
+                 __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000};
+}
+// 16 bytes a lane from a buffer (offsets: `off` a lane's, `soff` the wavefront's) to 1 KB of the LDS at the uniform address `at`,
+// in the order of the lanes; in flight until lds_requests_left().  The instruction writes no register.
+__device__ __forceinline__ void lds_request(intx4 buf, uint32_t off, uint32_t soff, uint32_t at) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(at), "v"(off), "s"(buf), "s"(soff));
+}
+// until at most N of the wavefront's requests are in flight
+template <int N>
+__device__ __forceinline__ void lds_requests_left() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+template <class T, int MI, int NI, bool SCALED, bool WTILE, int NST>
 __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
                                                              const float* __restrict__ bias, T* __restrict__ y, int64_t ldy,
                                                              int32_t tiles_t, int32_t tiles_o) {
@@ -203,20 +328,22 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
     const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wt = (wv & 1) * (16 * MI), wo = (wv >> 1) * (16 * NI);
-    // (a division runs on the vector unit: the tile's place goes back to scalar registers)
-    const int tile_t = __builtin_amdgcn_readfirstlane((int)blockIdx.x / tiles_o), tile_o = (int)blockIdx.x - tile_t * tiles_o;
+    int tile_t, tile_o;
+    tile_of_workgroup(tiles_t, tiles_o, tile_t, tile_o);
     const int64_t t0 = (int64_t)tile_t * BM, o0 = (int64_t)tile_o * BN;
     const int nb = (int)((K + 127) >> 7);
 
     // One request brings 8 rows of a step (1 KB) from memory to the LDS, 16 bytes a lane in the order of the lanes:
     // lane l has row l / 8 and the chunk that belongs at place l % 8 of it.  A wavefront brings 8 MI rows of x and
     // 8 NI of w.
-    const uint8_t* xb = uniform(x.codes + t0 * x.ld);
-    const uint8_t* wb = uniform(w.codes + o0 * w.ld);
+    const uint8_t* xb = x.codes + t0 * x.ld;
+    const uint8_t* wb = w.codes + o0 * w.ld;
     const uint32_t ldx = (uint32_t)x.ld, ldw = (uint32_t)w.ld;                    // below 2^23
     const uint32_t lastx = (uint32_t)min((int64_t)BM - 1, T_ - 1 - t0), lastw = (uint32_t)min((int64_t)BN - 1, O - 1 - o0);
+    const intx4 bufx = buffer_of(xb, lastx * ldx + (uint32_t)K), bufw = buffer_of(wb, lastw * ldw + (uint32_t)K);
     const int crow = lane >> 3, cchunk = (lane & 7) ^ crow;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+    const uint32_t offx = crow * ldx + cchunk * 16, offw = crow * ldw + cchunk * 16;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds + wv * (MI * 1024);
 
     floatx4 acc[NI][MI];
 #pragma unroll
@@ -227,7 +354,7 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
     // Exponents of SB blocks of every row of the tile, one byte each (WTILE: of every 128 rows of w), past the stages; a
     // lane has those of two steps in a register.
     constexpr int SB = 64, SROW = SB + 4, WROWS = WTILE ? ((BN + 127) / 128) : BN, NS = WTILE ? 1 : NI;
-    uint8_t* scl = lds + 2 * STAGE;
+    uint8_t* scl = lds + NST * STAGE;
     uint32_t sx[MI], sw[NS];
     if (SCALED) {                                    // what is not read from the tables is 1
         for (int i = tid; i < (BM + WROWS) * (SROW / 4); i += 256) reinterpret_cast<uint32_t*>(scl)[i] = 0x7F7F7F7Fu;
@@ -249,85 +376,96 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
 
     // request q of a step: 8 rows of x (q < MI) or of w
     static_assert(MI == NI && MI % 4 == 0, "quadrants of the wavefront's tile");
-    // (rows' offsets are made anew each time: three instructions instead of a register)
-#define BP_FRESH()            \
-    uint32_t r_ = crow;       \
-    asm volatile("" : "+v"(r_))
-#define BP_ROW(q) ((uint32_t)(wv * 8 * MI + 8 * ((q) % MI)) + r_)
-#define BP_OFF(q) ((q) < MI ? __umul24(min(BP_ROW(q), lastx), ldx) : __umul24(min(BP_ROW(q), lastw), ldw))
-#define BP_PLACE(q) (((q) < MI ? 0 : BM * 128) + (wv * MI + (q) % MI) * 1024)
-#define BP_BRING(kb, stage, q)                                                                                  \
-    lds_request(((q) < MI ? xb : wb) + (int64_t)(kb) * 128, BP_OFF(q) + cchunk * 16u, lds0 + (stage) * STAGE + BP_PLACE(q))
+    // (a block that is not there is past the buffer's end in the last row only; the caller asks for blocks that are there)
+    auto place = [&](int q) __attribute__((always_inline)) { return (q < MI ? 0 : BM * 128) + (q % MI) * 1024; };
+    auto bring = [&](int kb, int stage, int q) __attribute__((always_inline)) {
+        lds_request(q < MI ? bufx : bufw, q < MI ? offx : offw,
+                    (uint32_t)kb * 128u + (uint32_t)(8 * (wv * MI + q % MI)) * (q < MI ? ldx : ldw), lds0 + stage + place(q));
+    };
 
-    intx8 fx[MI], fw[NI];
-    const int c0 = (lg ^ (lr & 7)) << 4, c1 = c0 ^ 64;
-    const uint8_t* px0 = lds + (wt + lr) * 128;
-    const uint8_t* pw0 = lds + BM * 128 + (wo + lr) * 128;
-#define BP_FRAG(f, p, stage, i)                                                                                 \
-    {                                                                                                           \
-        const piece16 a_ = *reinterpret_cast<const piece16*>((p) + (stage) * STAGE + (i) * 2048 + c0);          \
-        const piece16 b_ = *reinterpret_cast<const piece16*>((p) + (stage) * STAGE + (i) * 2048 + c1);          \
-        f[i] = intx8{(int)a_[0], (int)a_[1], (int)a_[2], (int)a_[3], (int)b_[0], (int)b_[1], (int)b_[2], (int)b_[3]}; \
-    }
-#define BP_MUL(byte, i, j)                                                                                            \
-    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[i], fx[j], acc[i][j], 0, 0, byte, (int)sw[WTILE ? 0 : (i)], byte, (int)sx[j])
-    // One quadrant of the wavefront's tile in MI/2 groups: a fragment for a later quadrant, some requests, NI/2 products
-#define BP_QUAD(byte, ih, jh, FRAG, REQ0, NREQ, REQ_STAGE, REQ_KB)                                                    \
-    _Pragma("unroll") for (int g = 0; g < MI / 2; ++g) {                                                        \
-        FRAG;                                                                                                   \
-        BP_FRESH();                                                                                             \
-        _Pragma("unroll") for (int q = 0; q < (NREQ); ++q) BP_BRING(REQ_KB, REQ_STAGE, (REQ0) + g * (NREQ) + q); \
-        _Pragma("unroll") for (int i = 0; i < NI / 2; ++i) BP_MUL(byte, (ih) * (NI / 2) + i, (jh) * (MI / 2) + g); \
-        __builtin_amdgcn_sched_barrier(0);                                                                      \
-    }
-#define BP_FRAG_X(stage, h) BP_FRAG(fx, px0, stage, (h) * (MI / 2) + g)
-#define BP_FRAG_W(stage, h) BP_FRAG(fw, pw0, stage, (h) * (NI / 2) + g)
+    piece16 fx[MI][2], fw[NI][2];                    // a fragment's 32 codes, in two halves
+    const int c0 = (lg ^ (lr & 7)) << 4;
+    const uint8_t* px[2] = {lds + (wt + lr) * 128 + c0, lds + (wt + lr) * 128 + (c0 ^ 64)};
+    const uint8_t* pw[2] = {lds + BM * 128 + (wo + lr) * 128 + c0, lds + BM * 128 + (wo + lr) * 128 + (c0 ^ 64)};
+    auto mul = [&](auto byte, int i, int j) __attribute__((always_inline)) {
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(words8(fw[i][0], fw[i][1]), words8(fx[j][0], fx[j][1]), acc[i][j], 0, 0,
+                                                                     byte.value, (int)sw[WTILE ? 0 : i], byte.value, (int)sx[j]);
+    };
+    auto frag_x = [&](int stage, int j, int h) __attribute__((always_inline)) {
+        fx[j][h] = *reinterpret_cast<const piece16*>(px[h] + stage + j * 2048);
+    };
+    auto frag_w = [&](int stage, int i, int h) __attribute__((always_inline)) {
+        fw[i][h] = *reinterpret_cast<const piece16*>(pw[h] + stage + i * 2048);
+    };
+    // One quadrant of the wavefront's tile (halves ih of w, jh of x) with step parity P.  Between the products, a few
+    // instructions in the shadow of each and in this order: the fragments of half `fh` of x (FX) or w for the next
+    // quadrant, from the stage at fs, and with REQ the requests of half r of block kb into the stage at rs.
+    auto quad = [&](auto P, auto ih, auto jh, auto FX, int fs, auto fh, auto REQ, auto r, int kb, int rs) __attribute__((always_inline)) {
+#pragma unroll
+        for (int g = 0; g < MI / 2; ++g) {
+#pragma unroll
+            for (int i = 0; i < NI / 2; ++i) {
+                mul(P, ih.value * (NI / 2) + i, jh.value * (MI / 2) + g);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (k * (NI / 2) / 4 != i) continue;
+                    if (k < 2) {
+                        if (FX.value) frag_x(fs, fh.value * (MI / 2) + g, k);
+                        else frag_w(fs, fh.value * (NI / 2) + g, k);
+                    } else if (REQ.value) {
+                        bring(kb, rs, r.value * MI + 2 * g + k - 2);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
     // A step: four quadrants, each with one new half of fragments.  X0: the half of x that is there at the start;
     // the other half comes first, and at the end next step's w half 0 and x half 1 - X0 are there.  The barrier between
-    // the second and third quadrant: every wavefront has read all of this stage, and the next stage is whole; from there
-    // on this stage takes the step after next.
-#define BP_STEP(P, X0, kb)                                                                                      \
-    {                                                                                                           \
-        const int k2_ = min((kb) + 2, last);                                                                    \
-        BP_QUAD(P, 0, X0, BP_FRAG_X(P, 1 - (X0)), 0, 0, 0, 0);                                                  \
-        BP_QUAD(P, 0, 1 - (X0), BP_FRAG_W(P, 1), 0, 0, 0, 0);                                                   \
-        lds_requests_done();                                                                                    \
-        __syncthreads();                                                                                        \
-        BP_QUAD(P, 1, 1 - (X0), BP_FRAG_W(1 - (P), 0), 0, 2, P, k2_);                                           \
-        BP_QUAD(P, 1, X0, BP_FRAG_X(1 - (P), 1 - (X0)), MI, 2, P, k2_);                                         \
-    }
+    // the second and third quadrant: every wavefront has read all of this stage, and the next stage is whole (the NST - 2
+    // after it may still be on their way); from there on this stage takes block `to`.
+    constexpr std::integral_constant<int, 0> C0{};
+    constexpr std::integral_constant<int, 1> C1{};
+    auto step = [&](auto P, auto N, int cur, int nxt, int to) __attribute__((always_inline)) {        // P: parity of the step and X0, N = 1 - P
+        quad(P, C0, P, C1, cur, N, C0, C0, 0, 0);
+        quad(P, C0, N, C0, cur, C1, C0, C0, 0, 0);
+        lds_requests_left<(NST - 2) * 2 * MI>();
+        __syncthreads();
+        quad(P, C1, N, C0, nxt, C0, C1, C0, to, cur);
+        quad(P, C1, P, C1, nxt, N, C1, C1, to, cur);
+    };
 
     // blocks in pairs (the loop's body is one piece of straight code, or the compiler takes the products out of it)
     const int paired = (int)(K >> 8) * 2, last = paired - 1;
     if (paired > 0) {
-        {
-            BP_FRESH();
 #pragma unroll
-            for (int q = 0; q < 2 * MI; ++q) BP_BRING(0, 0, q);
+        for (int st = 0; st < NST; ++st)
 #pragma unroll
-            for (int q = 0; q < 2 * MI; ++q) BP_BRING(1, 1, q);
-        }
+            for (int q = 0; q < 2 * MI; ++q) bring(min(st, last), st * STAGE, q);
         if (SCALED) BP_SCALES_STAGE(0);
-        lds_requests_done();
+        lds_requests_left<(NST - 1) * 2 * MI>();
         __syncthreads();
 #pragma unroll
-        for (int g = 0; g < MI / 2; ++g) {
-            BP_FRAG_W(0, 0);
-            BP_FRAG_X(0, 0);
-        }
+        for (int g = 0; g < MI / 2; ++g)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                frag_w(0, g, h);
+                frag_x(0, g, h);
+            }
         for (int kb = 0;;) {
             const int end = min(kb + SB, paired);
             for (; kb < end; kb += 2) {
                 if (SCALED) BP_SCALES_TAKE(kb);
-                BP_STEP(0, 0, kb);
-                BP_STEP(1, 1, kb + 1);
+                const int at = NST == 2 ? 0 : (kb & (NST - 1)) * STAGE, after = NST == 2 ? 0 : ((kb + 2) & (NST - 1)) * STAGE;
+                step(C0, C1, at, at + STAGE, min(kb + NST, last));
+                step(C1, C0, at + STAGE, after, min(kb + NST + 1, last));
             }
             if (kb >= paired) break;
             __syncthreads();
             if (SCALED) BP_SCALES_STAGE(kb);
             __syncthreads();
         }
-        lds_requests_done();
+        lds_requests_left<0>();
     }
     // one whole block at most, and a last shorter one: zeros past the row's end
 #pragma unroll 1
@@ -335,14 +473,12 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
         const int left = (int)(K - kb * 128ll) - cchunk * 16;
         __syncthreads();
         if (SCALED && (kb == paired && (kb & (SB - 1)) == 0)) BP_SCALES_STAGE(kb);
-        {
-            BP_FRESH();
 #pragma unroll 1
-            for (int q = 0; q < MI; ++q) {
-                *reinterpret_cast<piece16*>(lds + BP_PLACE(q) + lane * 16) = chunk_tail(xb + kb * 128ll + BP_OFF(q) + cchunk * 16, left);
-                const int p = q + MI;
-                *reinterpret_cast<piece16*>(lds + BP_PLACE(p) + lane * 16) = chunk_tail(wb + kb * 128ll + BP_OFF(p) + cchunk * 16, left);
-            }
+        for (int q = 0; q < MI; ++q) {
+            const uint32_t row = 8 * (wv * MI + q) + crow;
+            uint8_t* to = lds + (wv * MI + q) * 1024 + lane * 16;
+            *reinterpret_cast<piece16*>(to) = chunk_tail(xb + kb * 128ll + min(row, lastx) * ldx + cchunk * 16, left, kb * 128ll + cchunk * 16);
+            *reinterpret_cast<piece16*>(to + BM * 128) = chunk_tail(wb + kb * 128ll + min(row, lastw) * ldw + cchunk * 16, left, kb * 128ll + cchunk * 16);
         }
         __syncthreads();
         if (SCALED) BP_SCALES_TAKE(kb & ~1);
@@ -353,16 +489,16 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
             for (int i = 0; i < NS; ++i) sw[i] >>= 8;
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int i = 0; i < NI; ++i)
 #pragma unroll
-            for (int g = 0; g < MI / 2; ++g) {
-                BP_FRAG_W(0, h);
-                BP_FRAG_X(0, h);
+            for (int h = 0; h < 2; ++h) {
+                frag_w(0, i, h);
+                frag_x(0, i, h);
             }
 #pragma unroll
         for (int i = 0; i < NI; ++i)
 #pragma unroll
-            for (int j = 0; j < MI; ++j) BP_MUL(0, i, j);
+            for (int j = 0; j < MI; ++j) mul(C0, i, j);
     }
     __syncthreads();
     // results through the LDS: rows of the tile, stored 16 bytes a lane
@@ -402,21 +538,170 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
     }
 }
 
+
+// ---- few tokens ------------------------------------------------------------------------------------
+// Up to 64 tokens: the weights are read once, straight into registers in the order of the operands (a lane 32 codes of
+// a row and block, 128 bytes of a row side by side), and nothing else counts.  A workgroup has 16 outputs and
+// 16 MT tokens, its WAVES wavefronts a share of the blocks each, joined in order through the LDS.  U blocks are
+// requested at a time.
+template <class T, int MT, int WAVES, bool SCALED>
+__global__ __launch_bounds__(64 * WAVES) void k_block_product_few(int32_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
+                                                                  const float* __restrict__ bias, T* __restrict__ y, int64_t ldy) {
+    constexpr bool WIDE = sizeof(T) == 4;
+    constexpr int U = MT >= 4 ? 2 : 4;
+    __shared__ floatx4 part[WAVES][MT][64];
+    const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t o0 = blockIdx.x * 16ll, t0 = blockIdx.y * (16ll * MT);
+    const int nb = (int)((K + 127) >> 7), full = (int)(K >> 7);
+    const int b0 = (int)((int64_t)nb * wv / WAVES), b1 = (int)((int64_t)nb * (wv + 1) / WAVES);
+    const int64_t orow = min(o0 + lr, O - 1);
+    const uint8_t* wr = w.codes + orow * w.ld + lg * 32;
+    const uint8_t* xr[MT];
+    int64_t trow[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        trow[m] = min(t0 + 16 * m + lr, (int64_t)T_ - 1);
+        xr[m] = x.codes + trow[m] * x.ld + lg * 32;
+    }
+    floatx4 acc[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) acc[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    // one block's codes and scales in registers
+    struct Block {
+        piece16 w[2], x[MT][2];
+        uint32_t ew, ex[MT];           // SCALED: exponents
+        uint32_t fw[4], fx[MT];        // else: scales of this lane's four outputs, of its tokens, as they are stored
+    };
+    auto exponent = [&](const BlockView& q, int64_t row, int b) __attribute__((always_inline)) {
+        return (uint32_t)static_cast<const uint8_t*>(q.scales)[(row >> q.shift) * q.srow + b * q.sblk];
+    };
+    auto scales = [&](Block& k, int b) __attribute__((always_inline)) {
+        if constexpr (SCALED) {
+            k.ew = 127u;
+            if (how.w_blocks) k.ew = exponent(w, orow, b);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                k.ex[m] = 127u;
+                if (how.x_blocks) k.ex[m] = exponent(x, trow[m], b);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) k.fw[e] = scale_bits(w, min(o0 + lg * 4 + e, O - 1), b);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) k.fx[m] = scale_bits(x, trow[m], b);
+        }
+    };
+    auto multiply = [&](const Block& k) __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const intx8 a = words8(k.w[0], k.w[1]), b = words8(k.x[m][0], k.x[m][1]);
+            if constexpr (SCALED && !WIDE) {
+                acc[m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[m], 0, 0, 0, (int)k.ew, 0, (int)k.ex[m]);
+            } else {
+                const floatx4 p = block_sum<WIDE>(a, b);
+                if constexpr (SCALED) {
+                    // 32-bit results, exponents: a row of w belongs to lane lr, its results to lanes of another order
+                    const float fx = e8m0_value(k.ex[m]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        acc[m][e] = dmmv_fma(p[e], e8m0_value((uint32_t)__shfl((int)k.ew, lg * 4 + e, 64)) * fx, acc[m][e]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[m][e] = dmmv_fma(p[e], scale_of(w, k.fw[e]) * scale_of(x, k.fx[m]), acc[m][e]);
+                }
+            }
+        }
+    };
+    int b = b0;
+    for (; b + U <= b1 && b + U <= full; b += U) {
+        Block k[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) k[u].w[h] = *reinterpret_cast<const piece16_any*>(wr + (int64_t)(b + u) * 128 + 16 * h);
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) k[u].x[m][h] = *reinterpret_cast<const piece16_any*>(xr[m] + (int64_t)(b + u) * 128 + 16 * h);
+            scales(k[u], b + u);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) multiply(k[u]);
+    }
+#pragma unroll 1
+    for (; b < b1; ++b) {
+        Block k;
+        const int left = (int)min(K - b * 128ll, (int64_t)128) - lg * 32;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) k.w[h] = chunk_tail(wr + (int64_t)b * 128 + 16 * h, left - 16 * h, b * 128ll + lg * 32 + 16 * h);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) k.x[m][h] = chunk_tail(xr[m] + (int64_t)b * 128 + 16 * h, left - 16 * h, b * 128ll + lg * 32 + 16 * h);
+        scales(k, b);
+        multiply(k);
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) part[wv][m][lane] = acc[m];
+    __syncthreads();
+    // wavefront m joins and stores tile m
+    for (int m = wv; m < MT; m += WAVES) {
+        floatx4 v = part[0][m][lane];
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) v += part[i][m][lane];
+        const int64_t t = t0 + 16 * m + lr;
+        if (t >= T_) continue;
+        const float st = SCALED && !how.x_blocks ? scale_at(x, t, 0) : 1.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t o = o0 + lg * 4 + e;
+            if (o >= O) continue;
+            const float so = SCALED && !how.w_blocks ? scale_at(w, o, 0) : 1.0f;
+            put_y(y + t * ldy + o, dmmv_fma(v[e], so * st, bias ? bias[o] : 0.0f));
+        }
+    }
+}
+
+template <class T, int MT, int WAVES>
+static dmmv_status launch_few_of(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const ProductScales& how, bool scaled, const float* bias,
+                                 T* y, int64_t ldy, hipStream_t s) {
+    const dim3 grid((unsigned)ceil_div(w->rows, 16), (unsigned)ceil_div(x->rows, 16 * MT));
+    if (scaled)
+        hipLaunchKernelGGL((k_block_product_few<T, MT, WAVES, true>), grid, dim3(64 * WAVES), 0, s, (int32_t)x->rows, w->rows, x->cols,
+                           layer_view(x), layer_view(w), how, bias, y, ldy);
+    else
+        hipLaunchKernelGGL((k_block_product_few<T, MT, WAVES, false>), grid, dim3(64 * WAVES), 0, s, (int32_t)x->rows, w->rows, x->cols,
+                           layer_view(x), layer_view(w), how, bias, y, ldy);
+    DMMV_LAUNCH_CHECK();
+    return DMMV_OK;
+}
+
+template <class T>
+static dmmv_status launch_few(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const ProductScales& how, bool scaled, const float* bias,
+                              T* y, int64_t ldy, hipStream_t s) {
+    const bool many = w->rows >= 8192;                 // 16 outputs x 4 wavefronts fill the chip
+    if (x->rows <= 16) return many ? launch_few_of<T, 1, 4>(x, w, how, scaled, bias, y, ldy, s) : launch_few_of<T, 1, 8>(x, w, how, scaled, bias, y, ldy, s);
+    if (x->rows <= 32) return many ? launch_few_of<T, 2, 4>(x, w, how, scaled, bias, y, ldy, s) : launch_few_of<T, 2, 8>(x, w, how, scaled, bias, y, ldy, s);
+    return many ? launch_few_of<T, 4, 4>(x, w, how, scaled, bias, y, ldy, s) : launch_few_of<T, 4, 8>(x, w, how, scaled, bias, y, ldy, s);
+}
+
 // scales that are the same along a row leave the sum
 static bool constant_rows(const dmmv_block_matrix* q) { return !q->scales || q->scale_block_stride == 0 || q->cols <= 128; }
 
 // rows that requests of 16 bytes can bring to the LDS, with offsets of 24 x 24 bits
 static bool aligned(const dmmv_block_matrix* q) { return q->ld < 1 << 23 && q->ld % 16 == 0 && (uintptr_t)q->codes % 16 == 0; }
 
-template <class T, int MI, int NI, bool SCALED, bool WTILE>
+template <class T, int MI, int NI, bool SCALED, bool WTILE, int NST>
 static dmmv_status launch_tiled(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, T* y, int64_t ldy, hipStream_t s) {
     const int64_t tiles_t = ceil_div(x->rows, 32 * MI), tiles_o = ceil_div(w->rows, 32 * NI);
-    if (tiles_t > INT32_MAX / tiles_o) return fail(DMMV_ERR_SHAPE, "y: more tiles than a launch takes");
-    const void* kern = (const void*)k_block_product_tiled<T, MI, NI, SCALED, WTILE>;
-    constexpr int bytes = product_lds(MI, NI, sizeof(T), WTILE);
+    if (tiles_t > INT32_MAX / 4 / tiles_o) return fail(DMMV_ERR_SHAPE, "y: more tiles than a launch takes");
+    const void* kern = (const void*)k_block_product_tiled<T, MI, NI, SCALED, WTILE, NST>;
+    constexpr int bytes = product_lds(MI, NI, sizeof(T), WTILE, NST);
     DMMV_TRY(ensure_dynamic_lds(kern, bytes));
     const ProductScales how = {!constant_rows(x), !constant_rows(w)};
-    hipLaunchKernelGGL((k_block_product_tiled<T, MI, NI, SCALED, WTILE>), dim3((unsigned)(tiles_t * tiles_o)), dim3(256), bytes, s, x->rows, w->rows,
+    hipLaunchKernelGGL((k_block_product_tiled<T, MI, NI, SCALED, WTILE, NST>), dim3((unsigned)(tiles_t * tiles_o)), dim3(256), bytes, s, x->rows, w->rows,
                        x->cols, layer_view(x), layer_view(w), how, bias, y, ldy, (int32_t)tiles_t, (int32_t)tiles_o);
     DMMV_LAUNCH_CHECK();
     return DMMV_OK;
@@ -424,17 +709,33 @@ static dmmv_status launch_tiled(const dmmv_block_matrix* x, const dmmv_block_mat
 
 template <class T>
 static dmmv_status product(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, T* y, int64_t ldy, hipStream_t s) {
+    const ProductScales how = {!constant_rows(x), !constant_rows(w)};
     const bool scaled = (constant_rows(x) || x->scale_type == DMMV_E8M0) && (constant_rows(w) || w->scale_type == DMMV_E8M0);
+    if (x->rows <= 64) return launch_few(x, w, how, scaled, bias, y, ldy, s);
     if constexpr (sizeof(T) == 2)
         if (scaled && aligned(x) && aligned(w)) {
             const bool wtile = constant_rows(w) || w->scale_rows == 128;
-            if (x->rows >= 1024 && wtile) return launch_tiled<T, 8, 8, true, true>(x, w, bias, y, ldy, s);
-            return launch_tiled<T, 4, 4, true, false>(x, w, bias, y, ldy, s);
+            int dev = 0, cus = 0;
+            DMMV_HIP_CHECK(hipGetDevice(&dev));
+            DMMV_HIP_CHECK(hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev));
+            const int64_t small = ceil_div(x->rows, 128) * ceil_div(w->rows, 128);
+            // a round of large tiles takes 2.25 times one of small ones (K = 4096: 46 us and 20.5)
+            const int64_t large = ceil_div(x->rows, 256) * ceil_div(w->rows, 256);
+            if (wtile && 9 * ceil_div(large, cus) < 4 * ceil_div(small, cus)) return launch_tiled<T, 8, 8, true, true, 2>(x, w, bias, y, ldy, s);
+            return launch_tiled<T, 4, 4, true, false, 4>(x, w, bias, y, ldy, s);
         }
     const int64_t tiles_t = ceil_div(x->rows, 64), tiles_o = ceil_div(w->rows, 64);
-    if (tiles_t > INT32_MAX / tiles_o) return fail(DMMV_ERR_SHAPE, "y: more tiles than a launch takes");
-    hipLaunchKernelGGL((k_block_product<T>), dim3((unsigned)(tiles_t * tiles_o)), dim3(256), 0, s, x->rows, w->rows, x->cols,
-                       layer_view(x), layer_view(w), bias, y, ldy, tiles_o);
+    if (tiles_t > INT32_MAX / 4 / tiles_o) return fail(DMMV_ERR_SHAPE, "y: more tiles than a launch takes");
+    const dim3 grid((unsigned)(tiles_t * tiles_o));
+    const bool share = tiles_t * tiles_o < 512 && x->cols > 128;
+#define BP_ANY(KS, SCALED)                                                                                                       \
+    hipLaunchKernelGGL((k_block_product<T, KS, SCALED>), grid, dim3(256 * KS), 0, s, x->rows, w->rows, x->cols, layer_view(x), layer_view(w), \
+                       how, bias, y, ldy, (int32_t)tiles_t, (int32_t)tiles_o)
+    if (share && scaled) BP_ANY(2, true);
+    else if (share) BP_ANY(2, false);
+    else if (scaled) BP_ANY(1, true);
+    else BP_ANY(1, false);
+#undef BP_ANY
     DMMV_LAUNCH_CHECK();
     return DMMV_OK;
 }

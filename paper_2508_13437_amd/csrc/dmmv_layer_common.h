@@ -121,11 +121,14 @@ __device__ __forceinline__ void store8_codes(uint8_t* __restrict__ row, int64_t 
 __device__ __forceinline__ float e8m0_value(uint32_t b) {
     return __uint_as_float(b == 255u ? 0x7FC00000u : b == 0u ? 0x00400000u : b << 23);
 }
-__device__ __forceinline__ float scale_at(const BlockView& q, int64_t row, int64_t block) {
-    if (!q.scales) return 1.0f;
+// a scale as it is stored, and its value; apart, because a conversion waits for the load
+__device__ __forceinline__ uint32_t scale_bits(const BlockView& q, int64_t row, int64_t block) {
+    if (!q.scales) return q.e8m0 ? 127u : 0x3F800000u;
     const int64_t at = (row >> q.shift) * q.srow + block * q.sblk;
-    return q.e8m0 ? e8m0_value(static_cast<const uint8_t*>(q.scales)[at]) : static_cast<const float*>(q.scales)[at];
+    return q.e8m0 ? static_cast<const uint8_t*>(q.scales)[at] : static_cast<const uint32_t*>(q.scales)[at];
 }
+__device__ __forceinline__ float scale_of(const BlockView& q, uint32_t bits) { return q.e8m0 ? e8m0_value(bits) : __uint_as_float(bits); }
+__device__ __forceinline__ float scale_at(const BlockView& q, int64_t row, int64_t block) { return scale_of(q, scale_bits(q, row, block)); }
 __device__ __forceinline__ void scale_put(const BlockView& q, int64_t scale_row, int64_t block, uint32_t b) {
     const int64_t at = scale_row * q.srow + block * q.sblk;
     if (q.e8m0) static_cast<uint8_t*>(q.scales)[at] = (uint8_t)b;

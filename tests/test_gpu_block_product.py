@@ -72,6 +72,26 @@ def test_product(gpu_device, T, O, K, kx, kw):
         assert torch.equal(got, dmmv.dmmv_block_product(x, w, bias, dtype=dtype))
 
 
+# the large tiles, many steps and more blocks than a table of exponents holds, with and without aligned rows; small and large
+# tiles of the general kernel
+LARGE = [(1300, 2100, 8512), (2304, 4600, 400), (1100, 2000, 8209), (70, 2500, 16640), (900, 1800, 1072)]
+
+
+@pytest.mark.parametrize("kx,kw", [("e8m0", "e8m0"), ("e8m0", "row"), ("f32", "f32")])
+@pytest.mark.parametrize("T,O,K", LARGE)
+def test_large_products_of_integers_are_exact(gpu_device, T, O, K, kx, kw):
+    from paper_2508_13437_amd import dmmv
+
+    for g in (1, 128) if kw == "e8m0" else (None,):
+        x = block(T, K, kx, T + O, gpu_device, integers=True)
+        w = block(O, K, kw, K + O, gpu_device, integers=True, g=g)
+        want = torch.from_numpy(vals(x)).to(gpu_device) @ torch.from_numpy(vals(w)).to(gpu_device).t()
+        bias = torch.arange(O, device=gpu_device, dtype=torch.float32) - 7.0
+        assert torch.equal(dmmv.dmmv_block_product(x, w, bias, dtype=torch.float32).double(), want + bias)
+        # integers beyond 2^13 times the smallest product are what the 8-bit instructions drop: none here
+        assert torch.equal(dmmv.dmmv_block_product(x, w, bias, dtype=torch.bfloat16), (want + bias).to(torch.bfloat16))
+
+
 @pytest.mark.parametrize("kx,kw", KINDS)
 @pytest.mark.parametrize("T,O,K", [s for s in SIZES if s[2] <= 4096])
 def test_product_of_integers_is_exact(gpu_device, T, O, K, kx, kw):
