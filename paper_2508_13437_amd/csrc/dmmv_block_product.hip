@@ -59,29 +59,6 @@ __device__ __forceinline__ intx8 words8(piece16 a, piece16 b) {
     return intx8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
 }
 
-// eight codes as bf16, times 2^(b - 127): exact
-__device__ __forceinline__ bf16x8_t scaled8(int lo, int hi, uint32_t b) {
-    const float s = __uint_as_float(b << 23);
-    const auto p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true);
-    const auto r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false), t = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true);
-    return bf16x8_t{p[0], p[1], q[0], q[1], r[0], r[1], t[0], t[1]};
-}
-
-__device__ __forceinline__ void put_y(float* y, float v) { *y = v; }
-__device__ __forceinline__ void put_y(bf16_t* y, float v) { y->u = (uint16_t)bf16_bits(v); }
-
-// The workgroup's tile.  Workgroups go to the 8 XCDs in turn, each with an L2 of its own: an XCD gets an eighth of the tiles in
-// a row, 4 tiles high and side by side, so that those of one moment share their operands' lines (4096 x 4096 x 11008: 171 us
-// against 188 with the tiles in rows; bands of 8: 185).
-__device__ __forceinline__ void tile_of_workgroup(int tiles_t, int tiles_o, int& tile_t, int& tile_o) {
-    const int n = tiles_t * tiles_o, per = n >> 3, b = (int)blockIdx.x;
-    const int id = b < per * 8 ? (b & 7) * per + (b >> 3) : b;
-    const int band = id / (4 * tiles_o), high = min(4, tiles_t - 4 * band), in = id - band * 4 * tiles_o;
-    // (a division runs on the vector unit: back to scalar registers)
-    tile_o = __builtin_amdgcn_readfirstlane(in / high);
-    tile_t = __builtin_amdgcn_readfirstlane(4 * band + in % high);
-}
-
 // ---- any sizes, strides, scales ------------------------------------------------------------------
 // Tile of 64 tokens x 64 outputs, 4 wavefronts (2 x 2), one block of 128 a step.  A step's codes and scales go from
 // memory through registers, requested two steps ahead, into one of two LDS stages while the other is multiplied.  The
@@ -267,17 +244,6 @@ __global__ __launch_bounds__(256 * KS) void k_block_product(int64_t T_, int64_t 
 // codes go straight from memory into the LDS (NST stages of one block of 128), and the loop is written so that the matrix
 // unit has a product at all times: what else there is to do is placed in the products' shadows by hand.
 // WTILE: the scales of w are the same for 128 rows, or for a whole row.
-template <class T>
-__device__ __forceinline__ void put4(T* __restrict__ row, const float (&v)[4]);
-template <>
-__device__ __forceinline__ void put4(float* __restrict__ row, const float (&v)[4]) {
-    *reinterpret_cast<floatx4*>(row) = floatx4{v[0], v[1], v[2], v[3]};
-}
-template <>
-__device__ __forceinline__ void put4(bf16_t* __restrict__ row, const float (&v)[4]) {
-    *reinterpret_cast<piece8*>(row) = piece8{bf16_bits(v[0]) | (bf16_bits(v[1]) << 16), bf16_bits(v[2]) | (bf16_bits(v[3]) << 16)};
-}
-
 // exponents of `blocks` blocks from kb on for `rows` rows (or groups of `per` rows) of a tile, to bytes of the LDS
 __device__ __forceinline__ void stage_exponents(const BlockView& q, int64_t row0, int64_t last, int per, int rows, int kb, int blocks,
                                                 uint8_t* to, int stride) {
@@ -301,23 +267,6 @@ constexpr int product_lds(int MI, int NI, int width, bool wtile, int nst) {
     const int stages = nst * 128 * 32 * (MI + NI) + 68 * (32 * MI + (wtile ? (32 * NI + 127) / 128 : 32 * NI)), out = 32 * MI * (32 * NI * width + 16);
     return stages > out ? stages : out;
 }
-
-typedef int intx4 __attribute__((ext_vector_type(4)));
-
-// `bytes` bytes from p on as a buffer (p the same in every lane): reads past them give zero
-__device__ __forceinline__ intx4 buffer_of(const uint8_t* p, uint32_t bytes) {
-    const uint64_t u = (uint64_t)p;
-    return intx4{__builtin_amdgcn_readfirstlane((int)(uint32_t)u), __builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32) & 0xFFFF),
-                 __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000};
-}
-// 16 bytes a lane from a buffer (offsets: `off` a lane's, `soff` the wavefront's) to 1 KB of the LDS at the uniform address `at`,
-// in the order of the lanes; in flight until lds_requests_left().  The instruction writes no register.
-__device__ __forceinline__ void lds_request(intx4 buf, uint32_t off, uint32_t soff, uint32_t at) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(at), "v"(off), "s"(buf), "s"(soff));
-}
-// until at most N of the wavefront's requests are in flight
-template <int N>
-__device__ __forceinline__ void lds_requests_left() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 template <class T, int MI, int NI, bool SCALED, bool WTILE, int NST>
 __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,

@@ -194,6 +194,20 @@ def test_backward_of_integers_is_exact(gpu_device, T, O, K, dtype):
     assert np.array_equal(f64(dw), f64(dy).T @ vals(x)) and np.array_equal(f64(db), f64(dy).sum(0))
 
 
+# the large tiles: whole and partial ones, contractions of whole pairs of steps, a step and a part more, less than a pair
+@pytest.mark.parametrize("T,O,K", [(512, 768, 1024), (1000, 1352, 784), (328, 264, 272), (1096, 1072, 2064), (2050, 520, 400), (260, 2312, 272)])
+def test_large_backward_of_integers_is_exact(gpu_device, T, O, K):
+    from paper_2508_13437_amd import dmmv
+
+    for kind, g in (("e8m0", 128), ("e8m0", 1), ("none", 1)):
+        x, w = block(T, K, kind, T + O, gpu_device, integers=True, g=1), block(O, K, kind, K + O, gpu_device, integers=True, g=g)
+        dy = gradients(T, O, torch.bfloat16, T, gpu_device, integers=True)
+        dx, dw, db = dmmv.dmmv_block_backward(dy, x, w)
+        X, W = (torch.from_numpy(vals(q)).to(gpu_device) for q in (x, w))
+        assert torch.equal(dx, (dy.double() @ W).to(torch.bfloat16))
+        assert torch.equal(dw.double(), dy.double().t() @ X) and torch.equal(db.double(), dy.double().sum(0))
+
+
 def test_gradient_against_differences(gpu_device):
     """sum(dy * product) moves by dx (dw) times the scale when one integer code moves by one: exactly."""
     from paper_2508_13437_amd import dmmv
