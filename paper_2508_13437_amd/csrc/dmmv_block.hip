@@ -128,15 +128,24 @@ __global__ __launch_bounds__(256) void k_block_dequantize(int64_t rows, int64_t 
 }
 
 // ---- sums of parts (the second stage of every reduction over rows) -------------------------------
-// A workgroup takes 64 columns; its 16 wavefronts read every 16th part each and are joined in order.
+// A workgroup takes 64 columns; its 16 wavefronts read every 16th part each, in 8 chains, and are joined in order.
 __global__ __launch_bounds__(1024) void k_layer_sum_parts(const float* __restrict__ part, int64_t parts, int64_t n,
                                                           float* __restrict__ out0, int64_t n0, float* __restrict__ out1) {
     __shared__ float sh[16][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int64_t j = blockIdx.x * 64ll + lane;
-    float s = 0.0f;
-    if (j < n)
-        for (int64_t p = w; p < parts; p += 16) s += part[p * n + j];
+    // eight parts' numbers are requested together, a chain of sums for each
+    float c[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (j < n) {
+        int64_t p = w;
+        for (; p + 112 < parts; p += 128)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) c[u] += part[(p + 16 * u) * n + j];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (p + 16 * u < parts) c[u] += part[(p + 16 * u) * n + j];
+    }
+    float s = ((c[0] + c[1]) + (c[2] + c[3])) + ((c[4] + c[5]) + (c[6] + c[7]));
     sh[w][lane] = s;
     __syncthreads();
     if (w != 0 || j >= n) return;

@@ -10,73 +10,253 @@
 
 namespace dmmv {
 
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+
+// 4 x 4 numbers of 16 bits a lane, transposed in its group of 16 lanes
+__device__ __forceinline__ piece8 read_transposed(const uint8_t* p) {
+    return __builtin_bit_cast(piece8, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)p));
+}
+
+// ---- eight numbers of a row as they are stored, and what a row's end cuts off -----------------------
+// A piece is loaded whole, from `moved` places further left where the row ends inside it, and put right when it is used:
+// the request does not wait.  Rows shorter than 8 are read one by one.
+template <class T> struct Raw8;
+template <> struct Raw8<float> {
+    piece16 v[2];
+    __device__ __forceinline__ void load(const float* p) {
+        v[0] = *reinterpret_cast<const piece16_any*>(p);
+        v[1] = *reinterpret_cast<const piece16_any*>(p + 4);
+    }
+    __device__ __forceinline__ void set(int i, float x) { v[i >> 2][i & 3] = __float_as_uint(x); }
+    __device__ __forceinline__ void right(int n) {   // by n < 8 numbers, zeros after them
+#pragma unroll
+        for (int s = 4; s >= 1; s >>= 1)
+            if (n & s) {
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = i + s < 8 ? v[(i + s) >> 2][(i + s) & 3] : 0u;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = w[i];
+            }
+    }
+    __device__ __forceinline__ float get(int i) const { return __uint_as_float(v[i >> 2][i & 3]); }
+};
+template <> struct Raw8<bf16_t> {
+    piece16 v;
+    __device__ __forceinline__ void load(const bf16_t* p) { v = *reinterpret_cast<const piece16_any*>(p); }
+    __device__ __forceinline__ void set(int i, bf16_t x) { v[i >> 1] |= (uint32_t)x.u << (16 * (i & 1)); }
+    __device__ __forceinline__ void right(int n) {
+        const uint64_t lo = v[0] | ((uint64_t)v[1] << 32), hi = v[2] | ((uint64_t)v[3] << 32);
+        const int s = 16 * n;
+        const uint64_t l = s >= 64 ? hi >> (s - 64) : s == 0 ? lo : (lo >> s) | (hi << (64 - s)), h = s >= 64 ? 0 : hi >> s;
+        v = piece16{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
+    }
+    __device__ __forceinline__ float get(int i) const { return i & 1 ? __uint_as_float(v[i >> 1] & 0xFFFF0000u) : bf16_value(v[i >> 1] & 0xFFFFu); }
+};
+template <> struct Raw8<uint8_t> {
+    piece8 v;
+    __device__ __forceinline__ void load(const uint8_t* p) { v = *reinterpret_cast<const piece8_any*>(p); }
+    __device__ __forceinline__ void set(int i, uint8_t x) { v[i >> 2] |= (uint32_t)x << (8 * (i & 3)); }
+    __device__ __forceinline__ void right(int n) {
+        const uint64_t w = (v[0] | ((uint64_t)v[1] << 32)) >> (8 * n);
+        v = piece8{(uint32_t)w, (uint32_t)(w >> 32)};
+    }
+};
+template <class T>
+__device__ __forceinline__ void raw_request(Raw8<T>& r, const T* __restrict__ row, int64_t col, int64_t cols) {
+    if (cols >= 8) {
+        r.load(row + min(col, cols - 8));
+    } else {
+        r = Raw8<T>{};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (col + i < cols) r.set(i, row[col + i]);
+    }
+}
+// the piece as it belongs: zeros past the row's end, all zero unless `ok`
+template <class T>
+__device__ __forceinline__ void raw_settle(Raw8<T>& r, int64_t col, int64_t cols, bool ok) {
+    const int64_t moved = cols >= 8 ? col - min(col, cols - 8) : 0;
+    if (!ok || moved >= 8) r = Raw8<T>{};
+    else if (moved > 0) r.right((int)moved);
+}
+
 // C[m][n] = sum_k A(m, k) B(k, n), A(m, k) = a[m][k] or (TRANS) a[k][m], B a block matrix [k][n].
-// PA, PB: parts that an operand is cut into.  64 x 64 tile, 4 wavefronts of 32 x 32, 32 of k a step.
-template <class TA, bool TRANS, int PA, int PB, class TC>
-__global__ __launch_bounds__(256) void k_block_grad(int64_t M, int64_t N, int64_t Kc, const TA* __restrict__ a, int64_t lda, BlockView b,
-                                                    TC* __restrict__ c, int64_t ldc, int64_t tiles_n) {
-    constexpr int LS = 40;                                    // 32 and a skew of 8
-    __shared__ __align__(16) uint16_t As[PA][64 * LS], Bs[PB][64 * LS];
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    const int64_t m0 = (blockIdx.x / tiles_n) * 64, n0 = (blockIdx.x % tiles_n) * 64;
-    const int wm = (wv >> 1) * 32, wn = (wv & 1) * 32;
-    floatx4 acc[2][2] = {};
-    for (int64_t k0 = 0; k0 < Kc; k0 += 32) {
-        float va[8] = {}, vb[8] = {};
-        const int am = TRANS ? (tid & 7) * 8 : tid >> 2, ak = TRANS ? tid >> 3 : (tid & 3) * 8;
-        if (TRANS) {
-            if (k0 + ak < Kc) load8(a + (k0 + ak) * lda, m0 + am, M, va);
-        } else {
-            if (m0 + am < M) load8(a + (m0 + am) * lda, k0 + ak, Kc, va);
+// PA, PB: bf16 parts that an operand is cut into.  Any sizes, strides and scales.
+// 64 x 64 tile, 4 wavefronts of 32 x 32, 64 of k a step, requested two steps ahead, two LDS stages; KS groups of 4 wavefronts
+// and `slices` workgroups share the contraction where the tiles alone do not fill the chip (the groups are joined
+// in order here, the slices by k_block_grad_join).
+//   LDS rows of 64 numbers, 128 bytes: [k][.] with the 16-byte chunk c of row k at c ^ 2 (k & 3), read transposed;
+//   [m][k] with chunk c of row m at c ^ (m & 7), read as it is.
+// The codes are the A operand of the instruction, so that a lane's results come in fours along a row of C.
+template <class TA, bool TRANS, int PA, int PB, int KS, class TC>
+__global__ __launch_bounds__(256 * KS) void k_block_grad(int64_t M, int64_t N, int64_t Kc, const TA* __restrict__ a, int64_t lda, BlockView b,
+                                                         TC* __restrict__ c, int64_t ldc, int32_t tiles_m, int32_t tiles_n, int32_t slices,
+                                                         float* __restrict__ part) {
+    constexpr int STAGE = (PA + PB) * 8192;
+    extern __shared__ __align__(16) uint8_t lds_all[];
+    const int tid = threadIdx.x & 255, lane = tid & 63;
+    const int group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    uint8_t* lds = lds_all + group * (2 * STAGE);
+    const int wm = (wv & 1) * 32, wn = (wv >> 1) * 32;
+    const int tiles = tiles_m * tiles_n, slice = __builtin_amdgcn_readfirstlane((int)blockIdx.x / tiles), tile = (int)blockIdx.x - slice * tiles;
+    const int tile_m = __builtin_amdgcn_readfirstlane(tile / tiles_n), tile_n = tile - tile_m * tiles_n;
+    const int64_t m0 = tile_m * 64ll, n0 = tile_n * 64ll;
+    // this group's share of the steps; all groups have the same barriers
+    const int64_t nb = (Kc + 63) >> 6;
+    const int64_t share = (nb + slices * KS - 1) / (slices * KS);
+    const int64_t first = min((slice * KS + group) * share, nb), end = min(first + share, nb);
+
+    const int row = tid >> 3, col = (tid & 7) * 8;   // rows row, row + 32 of a step, 8 columns
+    struct Step {
+        Raw8<TA> a[2];
+        Raw8<uint8_t> b[2];
+        uint32_t s[2];
+    };
+    auto request = [&](Step& r, int64_t kb) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int64_t k = min(kb * 64 + row + 32 * u, Kc - 1);
+            if (TRANS) raw_request(r.a[u], a + k * lda, m0 + col, M);
+            else raw_request(r.a[u], a + min(m0 + row + 32 * u, M - 1) * lda, kb * 64 + col, Kc);
+            raw_request(r.b[u], (const uint8_t*)b.codes + k * b.ld, n0 + col, N);
+            r.s[u] = scale_bits(b, k, min(n0 + col, N - 1) >> 7);
         }
-        const int bk = tid >> 3, bn = (tid & 7) * 8;
-        if (k0 + bk < Kc && n0 + bn < N)
-            decode8(load8_codes(b.codes + (k0 + bk) * b.ld, n0 + bn, N), scale_at(b, k0 + bk, (n0 + bn) >> 7), vb);
-        __syncthreads();
+    };
+    auto deposit = [&](Step& r, int64_t kb, int stage) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            uint32_t p[3];
-            if (PA == 3) split3(va[e], p);
-            else p[0] = bf16_bits(va[e]);
-            const int at = TRANS ? (am + e) * LS + ak : am * LS + ak + e;
+        for (int u = 0; u < 2; ++u) {
+            const int64_t k = kb * 64 + row + 32 * u;
+            if (TRANS) raw_settle(r.a[u], m0 + col, M, k < Kc);
+            else raw_settle(r.a[u], kb * 64 + col, Kc, true);
+            raw_settle(r.b[u], n0 + col, N, k < Kc);
+            const int rr = row + 32 * u;
+            uint8_t* pa = lds + stage * STAGE + rr * 128 + (((tid & 7) ^ (TRANS ? (rr & 3) << 1 : rr & 7)) << 4);
+            uint8_t* pb = lds + stage * STAGE + PA * 8192 + rr * 128 + (((tid & 7) ^ ((rr & 3) << 1)) << 4);
+            if constexpr (PA == 1) {
+                *reinterpret_cast<piece16*>(pa) = r.a[u].v;
+            } else {
+                piece16 w[3];
 #pragma unroll
-            for (int i = 0; i < PA; ++i) As[i][at] = (uint16_t)p[i];
-            if (PB == 3) split3(vb[e], p);
-            else p[0] = bf16_bits(vb[e]);
+                for (int e = 0; e < 8; e += 2) {
+                    uint32_t p[3], q[3];
+                    split3(r.a[u].get(e), p);
+                    split3(r.a[u].get(e + 1), q);
 #pragma unroll
-            for (int i = 0; i < PB; ++i) Bs[i][(bn + e) * LS + bk] = (uint16_t)p[i];
+                    for (int i = 0; i < 3; ++i) w[i][e >> 1] = p[i] | (q[i] << 16);
+                }
+#pragma unroll
+                for (int i = 0; i < 3; ++i) *reinterpret_cast<piece16*>(pa + i * 8192) = w[i];
+            }
+            const float s = k < Kc ? scale_of(b, r.s[u]) : 0.0f;
+            float v[8];
+            decode8(r.b[u].v, s, v);
+            piece16 w[3];
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                uint32_t p[3], q[3];
+                if constexpr (PB == 3) {
+                    split3(v[e], p);
+                    split3(v[e + 1], q);
+                } else {
+                    p[0] = bf16_bits(v[e]);          // exact
+                    q[0] = bf16_bits(v[e + 1]);
+                }
+#pragma unroll
+                for (int i = 0; i < PB; ++i) w[i][e >> 1] = p[i] | (q[i] << 16);
+            }
+#pragma unroll
+            for (int i = 0; i < PB; ++i) *reinterpret_cast<piece16*>(pb + i * 8192) = w[i];
         }
-        __syncthreads();
-        bf16x8_t fa[PA][2], fb[PB][2];
+    };
+    floatx16 acc;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-#pragma unroll
-            for (int p = 0; p < PA; ++p)
-                fa[p][i] = *reinterpret_cast<const bf16x8_t*>(&As[p][(wm + 16 * i + (lane & 15)) * LS + (lane >> 4) * 8]);
-#pragma unroll
-            for (int p = 0; p < PB; ++p)
-                fb[p][i] = *reinterpret_cast<const bf16x8_t*>(&Bs[p][(wn + 16 * i + (lane & 15)) * LS + (lane >> 4) * 8]);
-        }
-        constexpr int PM = PA > PB ? PA : PB;                 // parts i, j with i + j >= PM are below 24 bits
+    for (int v = 0; v < 16; ++v) acc[v] = 0.0f;
+    const int tk = (lane >> 5) * 8 + ((lane & 15) >> 2), tn = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+    auto transposed = [&](const uint8_t* base, int w0, int s) __attribute__((always_inline)) {
+        piece8 h[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
+            h[i] = read_transposed(base + (16 * s + tk + 4 * i) * 128 + ((((w0 + tn) >> 3) ^ ((tk & 3) << 1)) << 4) + (tn & 7) * 2);
+        return __builtin_bit_cast(bf16x8_t, piece16{h[0][0], h[0][1], h[1][0], h[1][1]});
+    };
+    auto multiply = [&](int stage) __attribute__((always_inline)) {
+        const uint8_t* pa = lds + stage * STAGE;
+        const uint8_t* pb = pa + PA * 8192;
+        const int mr = wm + (lane & 31);
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+        for (int s = 0; s < 4; ++s) {
+            bf16x8_t fm[PA], fn[PB];
 #pragma unroll
-                for (int p = PA - 1; p >= 0; --p)
-#pragma unroll
-                    for (int r = PB - 1; r >= 0; --r)
-                        if (p + r < PM) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[p][i], fb[r][j], acc[i][j], 0, 0, 0);
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t m = m0 + wm + 16 * i + (lane >> 4) * 4 + e, n = n0 + wn + 16 * j + (lane & 15);
-                if (m < M && n < N) put_y(c + m * ldc + n, acc[i][j][e]);
+            for (int p = 0; p < PA; ++p) {
+                if constexpr (TRANS) fm[p] = transposed(pa + p * 8192, wm, s);
+                else fm[p] = *reinterpret_cast<const bf16x8_t*>(pa + p * 8192 + mr * 128 + (((2 * s + (lane >> 5)) ^ (mr & 7)) << 4));
             }
+#pragma unroll
+            for (int p = 0; p < PB; ++p) fn[p] = transposed(pb + p * 8192, wn, s);
+            constexpr int PM = PA > PB ? PA : PB;     // parts p, r with p + r >= PM are below 24 bits
+#pragma unroll
+            for (int p = PA - 1; p >= 0; --p)
+#pragma unroll
+                for (int r = PB - 1; r >= 0; --r)
+                    if (p + r < PM) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fn[r], fm[p], acc, 0, 0, 0);
+        }
+    };
+    Step r0 = {}, r1 = {};
+    if (first < end) request(r0, first);
+    if (first + 1 < end) request(r1, first + 1);
+    if (first < end) deposit(r0, first, 0);
+    if (first + 2 < end) request(r0, first + 2);
+    __syncthreads();
+    for (int64_t k = 0; k < share; k += 2) {
+        const int64_t kb = first + k;
+        if (kb + 1 < end) deposit(r1, kb + 1, 1);
+        if (kb + 3 < end) request(r1, kb + 3);
+        if (kb < end) multiply(0);
+        __syncthreads();
+        if (k + 1 >= share) break;
+        if (kb + 2 < end) deposit(r0, kb + 2, 0);
+        if (kb + 4 < end) request(r0, kb + 4);
+        if (kb + 1 < end) multiply(1);
+        __syncthreads();
+    }
+    if constexpr (KS > 1) {
+        floatx4* join = reinterpret_cast<floatx4*>(lds_all);     // [KS - 1][4][256]
+        if (group > 0)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                join[((group - 1) * 4 + g) * 256 + tid] = floatx4{acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]};
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int q = 1; q < KS; ++q)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[v] += join[((q - 1) * 4 + (v >> 2)) * 256 + tid][v & 3];
+    }
+    const int64_t m = m0 + wm + (lane & 31);
+    if (m >= M) return;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const int64_t n = n0 + wn + 8 * g + (lane >> 5) * 4;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (n + e >= N) continue;
+            if (slices > 1) part[((int64_t)slice * M + m) * N + n + e] = acc[4 * g + e];
+            else put_y(c + m * ldc + n + e, acc[4 * g + e]);
+        }
+    }
+}
+
+// c = the sum of the slices, by ascending slice
+template <class TC>
+__global__ __launch_bounds__(256) void k_block_grad_join(int64_t M, int64_t N, int32_t slices, const float* __restrict__ part,
+                                                         TC* __restrict__ c, int64_t ldc) {
+    const int64_t i = blockIdx.x * 256ll + threadIdx.x;
+    if (i >= M * N) return;
+    float s = part[i];
+    for (int p = 1; p < slices; ++p) s += part[p * M * N + i];
+    put_y(c + (i / N) * ldc + i % N, s);
 }
 
 // ---- large gradients ---------------------------------------------------------------------------------
@@ -90,15 +270,7 @@ __global__ __launch_bounds__(256) void k_block_grad(int64_t M, int64_t N, int64_
 //   The 4 x 32 lanes of a transposed read are 4 rows of 32 bytes; the places above put 8 such pieces on all 64 banks.
 // The codes are the A operand, so that a lane's results come in fours along a row of the output.
 // The loop is that of the large product: a quadrant of 16 products at a time, all else in their shadows.
-typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef short shortx4 __attribute__((ext_vector_type(4)));
-
 constexpr int GT_STAGE = 65536, GT_LDS = 256 * (256 * 2 + 16) > 2 * GT_STAGE ? 256 * (256 * 2 + 16) : 2 * GT_STAGE;
-
-// 4 x 4 results of 16 bits a lane, transposed in its group of 16 lanes
-__device__ __forceinline__ piece8 read_transposed(const uint8_t* p) {
-    return __builtin_bit_cast(piece8, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)p));
-}
 
 template <bool TRANS, class TC>
 __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, int64_t Kc, const bf16_t* __restrict__ a, int64_t lda,
@@ -368,24 +540,56 @@ static int64_t bias_strips(int64_t T, int64_t O) {
     const int64_t most = ceil_div(T, 4);
     return most < s ? most : s;
 }
-static size_t backward_workspace(int64_t T, int64_t O, int64_t) {
+// Slices of the contraction of a product of 64 x 64 tiles: where the tiles are fewer than the compute units (256), enough for
+// all, with four steps of 64 for each of a workgroup's two groups.
+static int32_t grad_slices(int64_t M, int64_t N, int64_t Kc) {
+    const int64_t tiles = ceil_div(M, 64) * ceil_div(N, 64), most = Kc / 512;
+    if (tiles <= 0 || tiles >= 256) return 1;
+    int64_t s = 256 / tiles;
+    if (s > most) s = most;
+    return (int32_t)(s < 1 ? 1 : s);
+}
+static size_t grad_part_bytes(int64_t M, int64_t N, int64_t Kc) {
+    const int32_t s = grad_slices(M, N, Kc);
+    return s > 1 ? ((size_t)s * M * N * 4 + 255) / 256 * 256 : 0;
+}
+// one part, used by dx, dw and dbias one after the other
+static size_t backward_workspace(int64_t T, int64_t O, int64_t K) {
     if (T <= 0 || O <= 0) return 0;
-    return ((size_t)bias_strips(T, O) * O * 4 + 255) / 256 * 256;
+    size_t n = ((size_t)bias_strips(T, O) * O * 4 + 255) / 256 * 256;
+    const size_t gx = grad_part_bytes(T, K, O), gw = grad_part_bytes(O, K, T);
+    if (gx > n) n = gx;
+    return gw > n ? gw : n;
+}
+
+template <class TA, bool TRANS, int PA, int PB, class TC>
+static dmmv_status grad_any(int64_t M, int64_t N, int64_t Kc, const TA* a, int64_t lda, const dmmv_block_matrix* b, TC* c, int64_t ldc,
+                            float* part, hipStream_t s) {
+    constexpr int KS = PA + PB <= 4 ? 2 : 1, bytes = KS * 2 * (PA + PB) * 8192;
+    const int64_t tiles_m = ceil_div(M, 64), tiles_n = ceil_div(N, 64);
+    const int32_t slices = grad_slices(M, N, Kc);
+    if (tiles_m > INT32_MAX / 4 / tiles_n) return fail(DMMV_ERR_SHAPE, "gradient: more tiles than a launch takes");
+    const void* kern = (const void*)k_block_grad<TA, TRANS, PA, PB, KS, TC>;
+    DMMV_TRY(ensure_dynamic_lds(kern, bytes));
+    hipLaunchKernelGGL((k_block_grad<TA, TRANS, PA, PB, KS, TC>), dim3((unsigned)(tiles_m * tiles_n * slices)), dim3(256 * KS), bytes, s, M, N, Kc,
+                       a, lda, layer_view(b), c, ldc, (int32_t)tiles_m, (int32_t)tiles_n, slices, part);
+    DMMV_LAUNCH_CHECK();
+    if (slices > 1) {
+        hipLaunchKernelGGL((k_block_grad_join<TC>), dim3((unsigned)ceil_div(M * N, 256)), dim3(256), 0, s, M, N, slices, part, c, ldc);
+        DMMV_LAUNCH_CHECK();
+    }
+    return DMMV_OK;
 }
 
 template <class TA, bool TRANS, class TC>
-static dmmv_status grad(int64_t M, int64_t N, int64_t Kc, const TA* a, int64_t lda, const dmmv_block_matrix* b, TC* c, int64_t ldc,
+static dmmv_status grad(int64_t M, int64_t N, int64_t Kc, const TA* a, int64_t lda, const dmmv_block_matrix* b, TC* c, int64_t ldc, float* part,
                         hipStream_t s) {
     if (M == 0 || N == 0) return DMMV_OK;
-    const int64_t tiles_m = ceil_div(M, 64), tiles_n = ceil_div(N, 64);
-    if (tiles_m > INT32_MAX / tiles_n) return fail(DMMV_ERR_SHAPE, "gradient: more tiles than a launch takes");
-    constexpr int PA = sizeof(TA) == 4 ? 3 : 1;
-    const dim3 grid((unsigned)(tiles_m * tiles_n));
     const bool exact = !b->scales || b->scale_type == DMMV_E8M0;
     if constexpr (sizeof(TA) == 2) {
         const int64_t big = ceil_div(M, 256) * ceil_div(N, 256);
-        if (exact && M >= 256 && N >= 256 && (TRANS ? M : Kc) % 8 == 0 && N % 16 == 0 && lda % 8 == 0 && lda < 1 << 22 && (uintptr_t)a % 16 == 0 && b->ld % 16 == 0 &&
-            (uintptr_t)b->codes % 16 == 0 && big <= INT32_MAX / 4) {
+        if (exact && M >= 256 && N >= 256 && (TRANS ? M : Kc) % 8 == 0 && N % 16 == 0 && lda % 8 == 0 && lda < 1 << 22 && (uintptr_t)a % 16 == 0 &&
+            b->ld % 16 == 0 && (uintptr_t)b->codes % 16 == 0 && big <= INT32_MAX / 4) {
             const void* kern = (const void*)k_block_grad_tiled<TRANS, TC>;
             DMMV_TRY(ensure_dynamic_lds(kern, GT_LDS));
             hipLaunchKernelGGL((k_block_grad_tiled<TRANS, TC>), dim3((unsigned)big), dim3(256), GT_LDS, s, M, N, Kc, a, lda, layer_view(b), c,
@@ -394,19 +598,16 @@ static dmmv_status grad(int64_t M, int64_t N, int64_t Kc, const TA* a, int64_t l
             return DMMV_OK;
         }
     }
-    if (exact)
-        hipLaunchKernelGGL((k_block_grad<TA, TRANS, PA, 1, TC>), grid, dim3(256), 0, s, M, N, Kc, a, lda, layer_view(b), c, ldc, tiles_n);
-    else
-        hipLaunchKernelGGL((k_block_grad<TA, TRANS, PA, 3, TC>), grid, dim3(256), 0, s, M, N, Kc, a, lda, layer_view(b), c, ldc, tiles_n);
-    DMMV_LAUNCH_CHECK();
-    return DMMV_OK;
+    constexpr int PA = sizeof(TA) == 4 ? 3 : 1;
+    return exact ? grad_any<TA, TRANS, PA, 1, TC>(M, N, Kc, a, lda, b, c, ldc, part, s)
+                 : grad_any<TA, TRANS, PA, 3, TC>(M, N, Kc, a, lda, b, c, ldc, part, s);
 }
 
 template <class T>
 static dmmv_status backward(int64_t Tn, int64_t O, int64_t K, const T* dy, int64_t lddy, const dmmv_block_matrix* x,
                             const dmmv_block_matrix* w, T* dx, int64_t lddx, float* dw, int64_t lddw, float* dbias, void* ws, hipStream_t s) {
-    if (dx) DMMV_TRY((grad<T, false, T>(Tn, K, O, dy, lddy, w, dx, lddx, s)));
-    if (dw) DMMV_TRY((grad<T, true, float>(O, K, Tn, dy, lddy, x, dw, lddw, s)));
+    if (dx) DMMV_TRY((grad<T, false, T>(Tn, K, O, dy, lddy, w, dx, lddx, static_cast<float*>(ws), s)));
+    if (dw) DMMV_TRY((grad<T, true, float>(O, K, Tn, dy, lddy, x, dw, lddw, static_cast<float*>(ws), s)));
     if (dbias && O > 0) {
         float* part = static_cast<float*>(ws);
         const int64_t strips = Tn > 0 ? bias_strips(Tn, O) : 0;

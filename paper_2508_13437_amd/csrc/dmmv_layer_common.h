@@ -28,7 +28,7 @@ BlockView layer_view(const dmmv_block_matrix* q);      // all zero for NULL
 
 static inline int layer_width(int32_t dtype) { return dtype == DMMV_BF16 ? 2 : 4; }
 
-// out[j] = sum over the parts of part[p][j], by ascending p inside each of 16 interleaved strands;
+// out[j] = sum over the parts of part[p][j], in an order that the number of parts fixes;
 // the first n0 columns go to out0, the others to out1 (either may be NULL)
 dmmv_status layer_sum_parts(const float* part, int64_t parts, int64_t n, float* out0, int64_t n0, float* out1,
                             hipStream_t stream);

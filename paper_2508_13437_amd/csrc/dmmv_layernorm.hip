@@ -167,6 +167,104 @@ struct NormIn {
     }
 };
 
+// Rows of up to 8192 columns: a team of TPR threads holds a row (its a and h) in registers between the two sums and dx, and keeps
+// its columns' share of dgamma and dbeta over all the rows it takes; the THREADS / TPR teams of a workgroup join theirs at the
+// end, in order, in the LDS.  Everything is read once.
+template <class T, bool Q8, int TPR, int CH, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_layernorm_grad(int64_t rows, int64_t cols, const T* __restrict__ dy, int64_t lddy, NormIn<T, Q8> in,
+                                                            const float* __restrict__ gamma, const float* __restrict__ mean,
+                                                            const float* __restrict__ rstd, T* __restrict__ dx, int64_t lddx,
+                                                            float* __restrict__ part) {
+    constexpr int TEAMS = THREADS / TPR, WAVES = TPR / 64;
+    __shared__ float2 sh[2][TEAMS][WAVES];
+    __shared__ float join[TPR * 8];
+    const int team = threadIdx.x / TPR, t = threadIdx.x % TPR;
+    const float n = (float)cols;
+    float g[CH][8], dg[CH][8], db[CH][8];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { g[c][e] = 1.0f; dg[c][e] = db[c][e] = 0.0f; }
+    if (gamma)
+#pragma unroll
+        for (int c = 0; c < CH; ++c) load8(gamma, (c * TPR + t) * 8ll, cols, g[c]);
+    int parity = 0;
+    for (int64_t r0 = blockIdx.x * (int64_t)TEAMS; r0 < rows; r0 += gridDim.x * (int64_t)TEAMS, parity ^= 1) {
+        const bool there = r0 + team < rows;
+        const int64_t row = there ? r0 + team : rows - 1;
+        const float mu = mean[row], rs = rstd[row];
+        float a[CH][8], h[CH][8];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            load8(dy + row * lddy, (c * TPR + t) * 8ll, cols, a[c]);
+            in.get(row, (c * TPR + t) * 8ll, cols, h[c]);
+        }
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = a[c][e];
+                h[c][e] = (h[c][e] - mu) * rs;
+                if (there && (c * TPR + t) * 8ll + e < cols) {
+                    dg[c][e] = dmmv_fma(d, h[c][e], dg[c][e]);
+                    db[c][e] += d;
+                    a[c][e] = d * g[c][e];
+                    s1 += a[c][e];
+                    s2 = dmmv_fma(a[c][e], h[c][e], s2);
+                }
+            }
+        if (!dx) continue;
+        s1 = wave_sum(s1);
+        s2 = wave_sum(s2);
+        if constexpr (WAVES > 1) {
+            // (two sets in turn: one barrier a row)
+            if ((t & 63) == 0) sh[parity][team][t >> 6] = make_float2(s1, s2);
+            __syncthreads();
+            s1 = s2 = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) { s1 += sh[parity][team][w].x; s2 += sh[parity][team][w].y; }
+        }
+        s1 /= n;
+        s2 /= n;
+        if (!there) continue;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            float w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = rs * ((a[c][e] - s1) - h[c][e] * s2);
+            const int64_t col = (c * TPR + t) * 8ll;
+            if (col < cols) store8(dx + row * lddx, col, cols, w);
+        }
+    }
+    if (!part) return;
+    float* p = part + blockIdx.x * 2ll * cols;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float* v = k ? db[c] : dg[c];
+            for (int w = 1; w < TEAMS; ++w) {
+                __syncthreads();
+                if (team == w)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) join[e * TPR + t] = v[e];
+                __syncthreads();
+                if (team == 0)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] += join[e * TPR + t];
+            }
+            const int64_t col = (c * TPR + t) * 8ll;
+            if (team == 0 && col < cols) {
+                float o[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = v[e];
+                store8(p + k * cols, col, cols, o);
+            }
+        }
+}
+
+// ---- longer rows: the sums first, then strips of columns ------------------------------------------
 // sums of a row: s[row] = {sum a / n, sum a h / n}
 template <class T, bool Q8>
 __global__ __launch_bounds__(256) void k_layernorm_grad_sums(int64_t cols, const T* __restrict__ dy, int64_t lddy, NormIn<T, Q8> in,
@@ -228,14 +326,24 @@ __global__ __launch_bounds__(256) void k_layernorm_grad_apply(int64_t rows, int6
 }
 
 // ---- host ---------------------------------------------------------------------------------------
+// Parts of the sums over rows.  Rows in registers: a workgroup of 1024 threads a compute unit; while those would have fewer than
+// two rounds of rows, workgroups of 256, 512 at most (513 x 1003: see the table of cases).
+constexpr int64_t NORM_REGS = 8192;
+static int norm_team(int64_t cols) { return cols <= 1024 ? 64 : 256; }
+static bool norm_small(int64_t rows, int64_t cols) { return rows < 512 * (1024 / norm_team(cols)); }
 static int64_t norm_strips(int64_t rows, int64_t cols) {
+    if (cols <= NORM_REGS) {
+        const int64_t teams = (norm_small(rows, cols) ? 256 : cols > 4096 ? 512 : 1024) / norm_team(cols), most = norm_small(rows, cols) ? 512 : 256;
+        const int64_t n = ceil_div(rows, teams);
+        return n < most ? n : most;
+    }
     int64_t s = 1024 / ceil_div(cols, 2048);
     if (s < 1) s = 1;
     return rows < s ? rows : s;
 }
 static size_t norm_workspace(int64_t rows, int64_t cols) {
     if (rows <= 0 || cols <= 0) return 0;
-    const size_t sums = ((size_t)rows * 8 + 255) / 256 * 256;
+    const size_t sums = cols <= NORM_REGS ? 0 : ((size_t)rows * 8 + 255) / 256 * 256;
     return sums + (size_t)norm_strips(rows, cols) * 2 * cols * 4;
 }
 
@@ -263,6 +371,30 @@ template <class T, bool Q8>
 static dmmv_status norm_backward(int64_t rows, int64_t cols, const T* dy, int64_t lddy, const NormIn<T, Q8>& in, const float* gamma,
                                  const float* mean, const float* rstd, T* dx, int64_t lddx, float* dgamma, float* dbeta,
                                  char* ws, hipStream_t stream) {
+    if (cols <= NORM_REGS) {
+        float* parts = reinterpret_cast<float*>(ws);
+        float* to = dgamma || dbeta ? parts : nullptr;
+        const int64_t n = norm_strips(rows, cols);
+#define NORM_GRAD(TPR, CH, THREADS)                                                                                              \
+    hipLaunchKernelGGL((k_layernorm_grad<T, Q8, TPR, CH, THREADS>), dim3((unsigned)n), dim3(THREADS), 0, stream, rows, cols, dy, lddy, in, \
+                       gamma, mean, rstd, dx, lddx, to)
+        if (norm_small(rows, cols)) {
+            if (cols <= 512) NORM_GRAD(64, 1, 256);
+            else if (cols <= 1024) NORM_GRAD(64, 2, 256);
+            else if (cols <= 2048) NORM_GRAD(256, 1, 256);
+            else if (cols <= 4096) NORM_GRAD(256, 2, 256);
+            else NORM_GRAD(256, 4, 256);
+        } else {
+            if (cols <= 512) NORM_GRAD(64, 1, 1024);
+            else if (cols <= 1024) NORM_GRAD(64, 2, 1024);
+            else if (cols <= 2048) NORM_GRAD(256, 1, 1024);
+            else if (cols <= 4096) NORM_GRAD(256, 2, 1024);
+            else NORM_GRAD(256, 4, 512);
+        }
+#undef NORM_GRAD
+        DMMV_LAUNCH_CHECK();
+        return to ? layer_sum_parts(parts, n, 2 * cols, dgamma, cols, dbeta, stream) : DMMV_OK;
+    }
     float2* sums = reinterpret_cast<float2*>(ws);
     float* part = reinterpret_cast<float*>(ws + ((size_t)rows * 8 + 255) / 256 * 256);
     const int64_t strips = norm_strips(rows, cols);

@@ -8,6 +8,7 @@ not been built (``python -m paper_2508_13437_amd.build``).
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional, Sequence
@@ -524,27 +525,29 @@ class BlockMatrix:
             raise DmmvError(-2, "codes must be 2-D")
         if codes.dtype != torch.uint8 and codes.dtype != torch.float8_e4m3fn:
             raise DmmvError(-3, f"codes are {codes.dtype}, not uint8 or float8_e4m3fn")
-        if codes.device.type != "cuda":
+        if not codes.is_cuda:
             raise DmmvError(-6, "tensors must live on the GPU")
         if scale_rows not in (1, 128):
             raise DmmvError(-2, "scale_rows must be 1 or 128")
         codes = _rows(codes)
         rows, cols = codes.shape
-        c = _BlockMatrix(rows, cols, codes.data_ptr(), codes.stride(0), None, 0, 0, DMMV_E8M0, scale_rows)
-        if scales is not None:
-            if scales.dtype == torch.float32:
-                c.scale_type = DMMV_F32
-            elif scales.dtype != torch.uint8 and scales.dtype != torch.float8_e8m0fnu:
-                raise DmmvError(-3, f"scales are {scales.dtype}, not uint8, float8_e8m0fnu or float32")
-            if tuple(scales.shape) != (-(-rows // scale_rows), -(-cols // 128)):
-                raise DmmvError(-2, f"scales must be {-(-rows // scale_rows)} x {-(-cols // 128)}")
-            if scales.device != codes.device:
-                raise DmmvError(-6, "codes and scales are on different devices")
-            c.scales = scales.data_ptr()
-            c.scale_row_stride, c.scale_block_stride = scales.stride()
+        if scales is None:
+            self._fill(codes, None, scale_rows, rows, cols, codes.stride(0), None, 0, 0, DMMV_E8M0)
+            return
+        kind = _SCALE_TYPES.get(scales.dtype)
+        if kind is None:
+            raise DmmvError(-3, f"scales are {scales.dtype}, not uint8, float8_e8m0fnu or float32")
+        if tuple(scales.shape) != (-(-rows // scale_rows), -(-cols // 128)):
+            raise DmmvError(-2, f"scales must be {-(-rows // scale_rows)} x {-(-cols // 128)}")
+        if scales.device != codes.device:
+            raise DmmvError(-6, "codes and scales are on different devices")
+        self._fill(codes, scales, scale_rows, rows, cols, codes.stride(0), scales.data_ptr(), *scales.stride(), kind)
+
+    def _fill(self, codes, scales, scale_rows, rows, cols, ld, scales_ptr, row_stride, block_stride, kind):
         self.codes, self.scales, self.scale_rows = codes, scales, scale_rows
         self.rows, self.cols = rows, cols
-        self._c, self._p = c, C.addressof(c)
+        self._c = c = _BlockMatrix(rows, cols, codes.data_ptr(), ld, scales_ptr, row_stride, block_stride, kind, scale_rows)
+        self._p = C.addressof(c)
 
     @property
     def values8(self) -> torch.Tensor:
@@ -556,93 +559,114 @@ class BlockMatrix:
         return self.codes.device
 
 
+_SCALE_TYPES = {torch.float32: DMMV_F32, torch.uint8: DMMV_E8M0, torch.float8_e8m0fnu: DMMV_E8M0}
+_LAYER_TYPES = {torch.bfloat16: DMMV_BF16, torch.float32: DMMV_F32}
+# (the calls are short beside the cost of Python: what is checked here is checked in few steps, what is right first)
+
+
 def _rows(t: torch.Tensor) -> torch.Tensor:
     """t with contiguous rows that do not overlap."""
-    if t.numel() == 0 or ((t.stride(1) == 1 or t.shape[1] == 1) and (t.stride(0) >= t.shape[1] or t.shape[0] == 1)):
+    if t.is_contiguous() or ((t.stride(1) == 1 or t.shape[1] == 1) and (t.stride(0) >= t.shape[1] or t.shape[0] == 1)):
         return t
     return t.contiguous()
 
 
-def _matrix(t: torch.Tensor, what: str, rows: int = -1, cols: int = -1, dtype=None) -> torch.Tensor:
+def _matrix(t: torch.Tensor, what: str) -> torch.Tensor:
     if t.dim() != 2:
         raise DmmvError(-2, f"{what} must be 2-D")
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise DmmvError(-6, "tensors must live on the GPU")
-    if dtype is not None and t.dtype != dtype:
-        raise DmmvError(-3, f"{what} is {t.dtype}, not {dtype}")
-    if (rows >= 0 and t.shape[0] != rows) or (cols >= 0 and t.shape[1] != cols):
-        raise DmmvError(-2, f"{what} is {t.shape[0]} x {t.shape[1]}, expected {rows} x {cols}")
     return _rows(t)
 
 
-def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[torch.Tensor]:
+def _vector(t: Optional[torch.Tensor], n: int, dev: int, what: str) -> Optional[int]:
+    """Address of a float32 vector of n entries on the device (the caller keeps t, a copy is kept by the allocator until the
+    stream has passed it)."""
     if t is None:
         return None
     if t.dtype != torch.float32:
         raise DmmvError(-3, f"{what} is {t.dtype}, not torch.float32")
     if t.dim() != 1 or t.shape[0] != n:
         raise DmmvError(-2, f"{what} must have {n} entries")
-    return t.contiguous()
+    _same(t, dev)
+    return t.data_ptr() if t.is_contiguous() else t.contiguous().data_ptr()
+
+
+def _same(t: torch.Tensor, dev: int):
+    if t.get_device() != dev:
+        raise DmmvError(-6, "tensors are on different devices")
 
 
 def _layer_dtype(dtype: torch.dtype) -> int:
-    if dtype == torch.bfloat16:
-        return DMMV_BF16
-    if dtype == torch.float32:
-        return DMMV_F32
-    raise DmmvError(-3, f"unsupported dtype {dtype}")
+    kind = _LAYER_TYPES.get(dtype)
+    if kind is None:
+        raise DmmvError(-3, f"unsupported dtype {dtype}")
+    return kind
 
 
 def _addr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-def _enqueue(dev: torch.device, name: str, tensors, *args):
-    """One call on the device's current stream; the tensors must all live on that device."""
-    for t in tensors:
-        if t is not None and t.device != dev:
-            raise DmmvError(-6, "tensors are on different devices")
-    fn = getattr(load(), name)
+def _enqueue(dev: int, fn, *args):
+    """One call on the current stream of device `dev`."""
     stream = torch.cuda.current_stream(dev).cuda_stream
-    if torch.cuda.current_device() == dev.index:
-        _check(fn(*args, stream))
+    if torch.cuda.current_device() == dev:
+        status = fn(*args, stream)
     else:
         with torch.cuda.device(dev):
-            _check(fn(*args, stream))
+            status = fn(*args, stream)
+    if status:
+        _check(status)
+
+
+@functools.lru_cache(maxsize=1024)
+def _workspace(name: str, *sizes: int) -> int:
+    return getattr(load(), name)(*sizes)
 
 
 def _new_block(rows: int, cols: int, scale_rows: int, scale_dtype: torch.dtype, dev: torch.device) -> BlockMatrix:
+    blocks = -(-cols // 128)
     codes = torch.empty((rows, cols), dtype=torch.uint8, device=dev)
-    scales = torch.empty((-(-rows // scale_rows), -(-cols // 128)), dtype=scale_dtype, device=dev)
-    return BlockMatrix(codes, scales, scale_rows)
+    scales = torch.empty((-(-rows // scale_rows), blocks), dtype=scale_dtype, device=dev)
+    q = BlockMatrix.__new__(BlockMatrix)
+    q._fill(codes, scales, scale_rows, rows, cols, cols, scales.data_ptr(), blocks, 1, _SCALE_TYPES[scale_dtype])
+    return q
 
 
 def dmmv_block_quantize(x: torch.Tensor, scale_rows: int = 1, scale_dtype: torch.dtype = torch.uint8) -> BlockMatrix:
     """x (float32 or bfloat16) in 8 bits, each scale the smallest power of two that holds its block; as
     exponent bytes (uint8) or float32."""
     x = _matrix(x, "x")
-    q = _new_block(x.shape[0], x.shape[1], scale_rows, scale_dtype, x.device)
-    _enqueue(x.device, "dmmv_block_quantize", (), _layer_dtype(x.dtype), x.data_ptr(), x.stride(0), q._p)
+    kind = _layer_dtype(x.dtype)
+    if scale_rows not in (1, 128) or scale_dtype not in _SCALE_TYPES:
+        raise DmmvError(-2, "scale_rows must be 1 or 128, scale_dtype uint8 or float32")
+    rows, cols = x.shape
+    q = _new_block(rows, cols, scale_rows, scale_dtype, x.device)
+    _enqueue(x.get_device(), load().dmmv_block_quantize, kind, x.data_ptr(), x.stride(0), q._p)
     return q
 
 
 def dmmv_block_dequantize(q: BlockMatrix, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """The values that q stands for."""
-    x = torch.empty((q.rows, q.cols), dtype=dtype, device=q.device)
-    _enqueue(q.device, "dmmv_block_dequantize", (), q._p, _layer_dtype(dtype), x.data_ptr(), x.stride(0))
+    kind = _layer_dtype(dtype)
+    x = torch.empty((q.rows, q.cols), dtype=dtype, device=q.codes.device)
+    _enqueue(x.get_device(), load().dmmv_block_dequantize, q._p, kind, x.data_ptr(), q.cols)
     return x
 
 
 def dmmv_block_product(x: BlockMatrix, w: BlockMatrix, bias: Optional[torch.Tensor] = None,
                        dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """y = x w^T + bias, [x.rows][w.rows]."""
-    bias = _vector(bias, w.rows, "bias")
-    code = _layer_dtype(dtype)
-    dev = x.codes.device
-    y = torch.empty((x.rows, w.rows), dtype=dtype, device=dev)
-    nbytes = load().dmmv_block_product_workspace_bytes(x.rows, w.rows, x.cols)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-    _enqueue(dev, "dmmv_block_product", (w.codes, bias), x._p, w._p, _addr(bias), code, y.data_ptr(), w.rows, _addr(ws), nbytes)
+    kind = _layer_dtype(dtype)
+    dev = x.codes.get_device()
+    _same(w.codes, dev)
+    T, O = x.rows, w.rows
+    b = _vector(bias, O, dev, "bias")
+    y = torch.empty((T, O), dtype=dtype, device=x.codes.device)
+    nbytes = _workspace("dmmv_block_product_workspace_bytes", T, O, x.cols)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=y.device) if nbytes else None
+    _enqueue(dev, load().dmmv_block_product, x._p, w._p, b, kind, y.data_ptr(), O, _addr(ws), nbytes)
     return y
 
 
@@ -653,17 +677,22 @@ def dmmv_block_backward(dy: torch.Tensor, x: Optional[BlockMatrix], w: Optional[
     read; it may be None without dw, and w without dx."""
     if (dw and x is None) or (dx and w is None):
         raise DmmvError(-1, "dx needs w, dw needs x")
-    T, O = dy.shape if dy.dim() == 2 else (0, 0)
     dy = _matrix(dy, "dy")
+    kind = _layer_dtype(dy.dtype)
+    T, O = dy.shape
     K = w.cols if w is not None else x.cols if x is not None else 0
-    code, dev = _layer_dtype(dy.dtype), dy.device
-    gx = torch.empty((T, K), dtype=dy.dtype, device=dev) if dx else None
-    gw = torch.empty((O, K), dtype=torch.float32, device=dev) if dw else None
-    gb = torch.empty((O,), dtype=torch.float32, device=dev) if dbias else None
-    nbytes = load().dmmv_block_backward_workspace_bytes(T, O, K)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-    _enqueue(dev, "dmmv_block_backward", (x.codes if dw else None, w.codes if dx else None), code, T, O, K, dy.data_ptr(),
-             dy.stride(0), x._p if dw else None, w._p if dx else None, _addr(gx), K, _addr(gw), K, _addr(gb), _addr(ws), nbytes)
+    dev, on = dy.get_device(), dy.device
+    if dw:
+        _same(x.codes, dev)
+    if dx:
+        _same(w.codes, dev)
+    gx = torch.empty((T, K), dtype=dy.dtype, device=on) if dx else None
+    gw = torch.empty((O, K), dtype=torch.float32, device=on) if dw else None
+    gb = torch.empty((O,), dtype=torch.float32, device=on) if dbias else None
+    nbytes = _workspace("dmmv_block_backward_workspace_bytes", T, O, K)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=on) if nbytes else None
+    _enqueue(dev, load().dmmv_block_backward, kind, T, O, K, dy.data_ptr(), dy.stride(0), x._p if dw else None,
+             w._p if dx else None, _addr(gx), K, _addr(gw), K, _addr(gb), _addr(ws), nbytes)
     return gx, gw, gb
 
 
@@ -682,16 +711,17 @@ def dmmv_layernorm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: 
     type; q: the result in 8 bits, the operand of dmmv_block_product; xq: a checkpoint of x for
     dmmv_layernorm_backward.  All from one pass over x."""
     x = _matrix(x, "x")
+    kind = _layer_dtype(x.dtype)
     T, F = x.shape
-    gamma, beta = _vector(gamma, F, "gamma"), _vector(beta, F, "beta")
-    dev = x.device
-    stats = torch.empty((2, T), dtype=torch.float32, device=dev)
-    out = torch.empty((T, F), dtype=x.dtype, device=dev) if y else None
-    oq = _new_block(T, F, 1, torch.uint8, dev) if q else None
-    ox = _new_block(T, F, 1, torch.uint8, dev) if xq else None
-    mean, rstd = stats[0], stats[1]
-    _enqueue(dev, "dmmv_layernorm", (gamma, beta), _layer_dtype(x.dtype), T, F, x.data_ptr(), x.stride(0), _addr(gamma),
-             _addr(beta), eps, _addr(out), F, oq._p if q else None, ox._p if xq else None, mean.data_ptr(), rstd.data_ptr())
+    dev, on = x.get_device(), x.device
+    g, b = _vector(gamma, F, dev, "gamma"), _vector(beta, F, dev, "beta")
+    mean = torch.empty((T,), dtype=torch.float32, device=on)
+    rstd = torch.empty((T,), dtype=torch.float32, device=on)
+    out = torch.empty((T, F), dtype=x.dtype, device=on) if y else None
+    oq = _new_block(T, F, 1, torch.uint8, on) if q else None
+    ox = _new_block(T, F, 1, torch.uint8, on) if xq else None
+    _enqueue(dev, load().dmmv_layernorm, kind, T, F, x.data_ptr(), x.stride(0), g, b, eps, _addr(out), F, oq._p if q else None,
+             ox._p if xq else None, mean.data_ptr(), rstd.data_ptr())
     return LayerNormResult(out, oq, ox, mean, rstd)
 
 
@@ -700,21 +730,28 @@ def dmmv_layernorm_backward(dy: torch.Tensor, x, gamma: Optional[torch.Tensor], 
     """Gradients (dx of dy's type, dgamma, dbeta in float32; None for those not asked for) of dmmv_layernorm.
     x is its input, or the checkpoint of it (a BlockMatrix); mean and rstd are its own."""
     dy = _matrix(dy, "dy")
+    kind = _layer_dtype(dy.dtype)
     T, F = dy.shape
-    code, dev = _layer_dtype(dy.dtype), dy.device
+    dev, on = dy.get_device(), dy.device
     if isinstance(x, BlockMatrix):
-        if (x.rows, x.cols) != (T, F):
+        if x.rows != T or x.cols != F:
             raise DmmvError(-2, f"x is {x.rows} x {x.cols}, expected {T} x {F}")
-        src, px, ldx, pq = x.codes, None, 0, x._p
+        _same(x.codes, dev)
+        px, ldx, pq = None, 0, x._p
     else:
-        x = _matrix(x, "x", T, F, dy.dtype)
-        src, px, ldx, pq = x, x.data_ptr(), x.stride(0), None
-    gamma, mean, rstd = _vector(gamma, F, "gamma"), _vector(mean, T, "mean"), _vector(rstd, T, "rstd")
-    gx = torch.empty((T, F), dtype=dy.dtype, device=dev) if dx else None
-    gg = torch.empty((F,), dtype=torch.float32, device=dev) if dgamma else None
-    gb = torch.empty((F,), dtype=torch.float32, device=dev) if dbeta else None
-    nbytes = load().dmmv_layernorm_workspace_bytes(T, F)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-    _enqueue(dev, "dmmv_layernorm_backward", (src, gamma, mean, rstd), code, T, F, dy.data_ptr(), dy.stride(0), px, ldx, pq,
-             _addr(gamma), mean.data_ptr(), rstd.data_ptr(), _addr(gx), F, _addr(gg), _addr(gb), _addr(ws), nbytes)
+        x = _matrix(x, "x")
+        if x.dtype != dy.dtype:
+            raise DmmvError(-3, f"x is {x.dtype}, not {dy.dtype}")
+        if x.shape != dy.shape:
+            raise DmmvError(-2, f"x is {x.shape[0]} x {x.shape[1]}, expected {T} x {F}")
+        _same(x, dev)
+        px, ldx, pq = x.data_ptr(), x.stride(0), None
+    g, mu, rs = _vector(gamma, F, dev, "gamma"), _vector(mean, T, dev, "mean"), _vector(rstd, T, dev, "rstd")
+    gx = torch.empty((T, F), dtype=dy.dtype, device=on) if dx else None
+    gg = torch.empty((F,), dtype=torch.float32, device=on) if dgamma else None
+    gb = torch.empty((F,), dtype=torch.float32, device=on) if dbeta else None
+    nbytes = _workspace("dmmv_layernorm_workspace_bytes", T, F)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=on) if nbytes else None
+    _enqueue(dev, load().dmmv_layernorm_backward, kind, T, F, dy.data_ptr(), dy.stride(0), px, ldx, pq, g, mu, rs, _addr(gx), F,
+             _addr(gg), _addr(gb), _addr(ws), nbytes)
     return gx, gg, gb
