@@ -260,7 +260,7 @@ __global__ __launch_bounds__(256) void k_block_grad_join(int64_t M, int64_t N, i
 }
 
 // ---- large gradients ---------------------------------------------------------------------------------
-// bf16 gradients and power-of-two scales, rows of whole chunks of 16 bytes, aligned: tile of 256 x 256, 4 wavefronts (2 x 2, one a SIMD,
+// Rows of whole chunks of 16 bytes, aligned, power-of-two scales: tile of 256 x 256, 4 wavefronts (2 x 2, one a SIMD,
 // 128 x 128 each), 64 of the contraction a step, two LDS stages.
 //   The rows of dy go straight from memory into the LDS.  dx: [m][k], the 16-byte chunk c of row m at c ^ (m & 7), read as it
 //   is; dw: [k][m], chunk c of row k at c ^ 4 (k & 3), read transposed.
@@ -269,12 +269,14 @@ __global__ __launch_bounds__(256) void k_block_grad_join(int64_t M, int64_t N, i
 //   fragment has 8 rows.)
 //   The 4 x 32 lanes of a transposed read are 4 rows of 32 bytes; the places above put 8 such pieces on all 64 banks.
 // The codes are the A operand, so that a lane's results come in fours along a row of the output.
+// dy may come as several bf16 parts that sum to it (`planes`, `plane` numbers apart): the contraction then runs over all.
 // The loop is that of the large product: a quadrant of 16 products at a time, all else in their shadows.
 constexpr int GT_STAGE = 65536, GT_LDS = 256 * (256 * 2 + 16) > 2 * GT_STAGE ? 256 * (256 * 2 + 16) : 2 * GT_STAGE;
 
 template <bool TRANS, class TC>
 __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, int64_t Kc, const bf16_t* __restrict__ a, int64_t lda,
-                                                          BlockView b, TC* __restrict__ c, int64_t ldc, int32_t tiles_m, int32_t tiles_n) {
+                                                          int32_t planes, int64_t plane, BlockView b, int64_t brows, TC* __restrict__ c, int64_t ldc,
+                                                          int32_t tiles_m, int32_t tiles_n) {
     extern __shared__ __align__(16) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -286,7 +288,7 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
     // requests of dy: 1 KB each, 8 a wavefront and step.  dx: 8 rows of 64; dw: 2 rows of 256
     const uint32_t lda2 = (uint32_t)lda * 2;
     const uint8_t* ab = reinterpret_cast<const uint8_t*>(TRANS ? a + m0 : a + m0 * lda);
-    const int64_t arows = TRANS ? Kc : min(M - m0, (int64_t)256), acols = TRANS ? M - m0 : Kc;
+    const int64_t arows = TRANS ? Kc : min(M - m0, (int64_t)256), acols = TRANS ? (M - m0 + 7) & ~7ll : Kc;   // (rows of whole chunks)
     uint32_t offa[2];                                // TRANS: of even and odd requests
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
@@ -299,15 +301,19 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
         }
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
-    auto bring = [&](int kb, int stage, int q) __attribute__((always_inline)) {      // q: 0 .. 7
-        const int at = wv * 8 + q;
+    const int steps = (int)(Kc >> 7) * 2;            // of one part, in pairs
+    // step f of all parts: step f % steps of part f / steps (three at most)
+    auto part_of = [&](int f) __attribute__((always_inline)) { return (f >= steps ? 1 : 0) + (f >= 2 * steps ? 1 : 0); };
+    auto bring = [&](int f, int stage, int q) __attribute__((always_inline)) {       // q: 0 .. 7
+        const int at = wv * 8 + q, p = part_of(f), kb = f - p * steps;
+        const uint8_t* ap = ab + p * plane * 2;
         if constexpr (TRANS) {
             // a buffer of the step's 64 rows: offsets stay small however many rows there are
             const int64_t row0 = (int64_t)kb * 64;
-            const intx4 buf = buffer_of(ab + row0 * lda2, (uint32_t)((min(arows - row0, (int64_t)64) - 1) * lda2 + min(acols, (int64_t)256) * 2));
+            const intx4 buf = buffer_of(ap + row0 * lda2, (uint32_t)((min(arows - row0, (int64_t)64) - 1) * lda2 + min(acols, (int64_t)256) * 2));
             lds_request(buf, offa[q & 1], (uint32_t)(2 * at) * lda2, lds0 + stage + at * 1024);
         } else {
-            const intx4 buf = buffer_of(ab, (uint32_t)(arows - 1) * lda2 + (uint32_t)acols * 2);
+            const intx4 buf = buffer_of(ap, (uint32_t)(arows - 1) * lda2 + (uint32_t)acols * 2);
             lds_request(buf, offa[0], (uint32_t)kb * 128 + (uint32_t)(8 * at) * lda2, lds0 + stage + at * 1024);
         }
     };
@@ -316,15 +322,15 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
     const int64_t bcol = n0 + bchunk * 16;
     const int64_t fb = min(bcol, N - 1) >> 7;
     const uint8_t* bb = b.codes + n0;
-    const int nlast = (int)min(N - n0, (int64_t)256);
+    const int nlast = ((int)min(N - n0, (int64_t)256) + 15) & ~15;
     // without scales a byte is read all the same (a branch around the load would wait for it) and not used
     const uint8_t* sp = b.scales ? static_cast<const uint8_t*>(b.scales) : b.codes;
     const int64_t srow = b.scales ? b.srow : 0, sblk = b.scales ? b.sblk : 0;
     piece16 rb[4];
     uint32_t rs[4];
     auto request = [&](int kb, int u) __attribute__((always_inline)) {
-        const int64_t row = min((int64_t)kb * 64 + brow + 16 * u, Kc - 1);
-        // (a chunk past the row's end gives columns that are not stored: the row's last is taken)
+        const int64_t row = min((int64_t)kb * 64 + brow + 16 * u, brows - 1);
+        // (rows past the last meet zeros of dy; a chunk past the row's end gives columns that are not stored: the row's last is taken)
         rb[u] = *reinterpret_cast<const piece16*>(bb + row * b.ld + min(bchunk * 16, nlast - 16));
         rs[u] = sp[(row >> b.shift) * srow + fb * sblk];
     };
@@ -388,7 +394,7 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
                 if (NEXT.value) {
                     if ((slot & 3) == 1) bring(to, rs_, r.value * 4 + (slot >> 2));
                     if ((slot & 7) == 2) deposit(rs_, r.value * 2 + (slot >> 3));
-                    if ((slot & 7) == 6) request(then, r.value * 2 + (slot >> 3));
+                    if ((slot & 7) == 6) request(then - part_of(then) * steps, r.value * 2 + (slot >> 3));
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -405,7 +411,7 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
         quad(C1, P, C1, nxt, Q, C1, C1, to, cur, then);
     };
 
-    const int paired = (int)(Kc >> 7) * 2, last = paired - 1, nb = (int)((Kc + 63) >> 6);
+    const int paired = steps * planes, last = paired - 1, nb = (int)((Kc + 63) >> 6);
     if (paired > 0) {
 #pragma unroll
         for (int q = 0; q < 8; ++q) bring(0, 0, q);
@@ -416,7 +422,7 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 if (k > 0) deposit((k - 1) * GT_STAGE, u);
-                request(min(k, last), u);
+                request(min(k, last) - part_of(min(k, last)) * steps, u);
             }
         lds_requests_left<0>();
         __syncthreads();
@@ -435,9 +441,9 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
         }
         lds_requests_left<0>();
     }
-    // what is left of the contraction, at most one whole block and a shorter one
+    // what is left of the contraction of one part, at most one whole block and a shorter one (several are padded to whole pairs)
 #pragma unroll 1
-    for (int kb = paired; kb < nb; ++kb) {
+    for (int kb = steps; kb < nb; ++kb) {
         const int left = (int)(Kc - kb * 64ll);
         __syncthreads();
 #pragma unroll 1
@@ -510,6 +516,51 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
     }
 }
 
+// dy as PARTS bf16 parts that sum to it (32 bits, or bf16 times scales of 32 bits; two keep 16 bits, for results in bf16), or as
+// it is, [Tp][Op] each with zeros in the margin.  A scale that is the same along a row of the block matrix belongs to
+// a place of the contraction: BY 1, a column of dy (dx); BY 2, a row (dw).
+template <class T, int PARTS, int BY>
+__global__ __launch_bounds__(256) void k_block_lay_gradient(int64_t rows, int64_t cols, const T* __restrict__ dy, int64_t ld, BlockView b,
+                                                            uint16_t* __restrict__ out, int64_t Tp, int64_t Op) {
+    const int64_t i = blockIdx.x * 256ll + threadIdx.x, chunks = Op >> 3, row = i / chunks, col = (i - row * chunks) * 8;
+    if (row >= Tp) return;
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (row < rows && col < cols) load8(dy + row * ld, col, cols, v);
+    if constexpr (BY != 0) {
+        const float s = BY == 2 && row < rows ? scale_at(b, row, 0) : 1.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (BY == 1) v[e] = row < rows && col + e < cols ? v[e] * scale_at(b, col + e, 0) : 0.0f;
+            else v[e] *= s;
+        }
+    }
+    piece16 w[3];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        uint32_t p[3], q[3];
+        if constexpr (PARTS == 1) {
+            p[0] = bf16_bits(v[e]);                  // exact
+            q[0] = bf16_bits(v[e + 1]);
+        } else {
+            split3(v[e], p);
+            split3(v[e + 1], q);
+        }
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) w[k][e >> 1] = p[k] | (q[k] << 16);
+    }
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) *reinterpret_cast<piece16*>(out + (PARTS - 1 - k) * Tp * Op + row * Op + col) = w[k];      // smallest first
+}
+
+// codes with rows of whole aligned chunks of 16 bytes
+__global__ __launch_bounds__(256) void k_block_lay_codes(int64_t rows, int64_t cols, const uint8_t* __restrict__ codes, int64_t ld,
+                                                         uint8_t* __restrict__ out, int64_t Kp) {
+    const int64_t i = blockIdx.x * 256ll + threadIdx.x, chunks = Kp >> 4, row = i / chunks, col = (i - row * chunks) * 16;
+    if (row >= rows) return;
+    const piece8 a = load8_codes(codes + row * ld, col, cols), b = load8_codes(codes + row * ld, col + 8, cols);
+    *reinterpret_cast<piece16*>(out + row * Kp + col) = piece16{a[0], a[1], b[0], b[1]};
+}
+
 // a strip of 512 columns and every gridDim.y-th group of 4 rows
 template <class T>
 __global__ __launch_bounds__(256) void k_block_column_sums(int64_t rows, int64_t cols, const T* __restrict__ dy, int64_t lddy,
@@ -553,13 +604,31 @@ static size_t grad_part_bytes(int64_t M, int64_t N, int64_t Kc) {
     const int32_t s = grad_slices(M, N, Kc);
     return s > 1 ? ((size_t)s * M * N * 4 + 255) / 256 * 256 : 0;
 }
-// one part, used by dx, dw and dbias one after the other
+// Large tiles or small ones?  us by the rates measured (small: 240 TFLOP/s with one part, 110 with three products for one;
+// large: 1.25 us a step of 64, laying out 4 TB/s and two launches).
+static bool large_tiles(int64_t M, int64_t N, int64_t Kc, int parts, double lay_bytes) {
+    const double small = 2.0 * M * N * Kc / (parts == 1 ? 240e6 : 110e6);
+    const int64_t rounds = ceil_div(ceil_div(M, 256) * ceil_div(N, 256), 256);
+    const double large = 1.25 * rounds * parts * ceil_div(Kc, 64) + lay_bytes / 4e6 + (lay_bytes > 0 ? 10 : 0);
+    return large < small;
+}
+static int64_t up(int64_t n, int64_t to) { return ceil_div(n, to) * to; }
+// dy laid out (three parts at most), then the codes of w or x
+static size_t lay_bytes(int64_t T, int64_t O, int64_t K) {
+    const double lay = 2.0 * T * O;
+    const bool dx = large_tiles(T, K, O, 1, lay), dw = large_tiles(O, K, T, 1, lay), dx3 = large_tiles(T, K, O, 3, lay), dw3 = large_tiles(O, K, T, 3, lay);
+    if (!dx && !dw && !dx3 && !dw3) return 0;
+    const int64_t rows = T > O ? T : O;
+    return (size_t)((dx3 || dw3 ? 3 : 1) * up(T, 128) * up(O, 128) * 2) + (size_t)(rows * up(K, 16));
+}
+// one after the other: dx, dw and dbias use the same bytes
 static size_t backward_workspace(int64_t T, int64_t O, int64_t K) {
     if (T <= 0 || O <= 0) return 0;
     size_t n = ((size_t)bias_strips(T, O) * O * 4 + 255) / 256 * 256;
-    const size_t gx = grad_part_bytes(T, K, O), gw = grad_part_bytes(O, K, T);
+    const size_t gx = grad_part_bytes(T, K, O), gw = grad_part_bytes(O, K, T), lay = K > 0 ? (lay_bytes(T, O, K) + 255) / 256 * 256 : 0;
     if (gx > n) n = gx;
-    return gw > n ? gw : n;
+    if (gw > n) n = gw;
+    return lay > n ? lay : n;
 }
 
 template <class TA, bool TRANS, int PA, int PB, class TC>
@@ -581,33 +650,79 @@ static dmmv_status grad_any(int64_t M, int64_t N, int64_t Kc, const TA* a, int64
     return DMMV_OK;
 }
 
+template <bool TRANS, class TC>
+static dmmv_status grad_tiled(int64_t M, int64_t N, int64_t Kc, const bf16_t* a, int64_t lda, int planes, int64_t plane, const BlockView& b,
+                              int64_t brows, TC* c, int64_t ldc, hipStream_t s) {
+    const int64_t tiles_m = ceil_div(M, 256), tiles_n = ceil_div(N, 256);
+    if (tiles_m > INT32_MAX / 4 / tiles_n) return fail(DMMV_ERR_SHAPE, "gradient: more tiles than a launch takes");
+    DMMV_TRY(ensure_dynamic_lds((const void*)k_block_grad_tiled<TRANS, TC>, GT_LDS));
+    hipLaunchKernelGGL((k_block_grad_tiled<TRANS, TC>), dim3((unsigned)(tiles_m * tiles_n)), dim3(256), GT_LDS, s, M, N, Kc, a, lda, planes, plane, b,
+                       brows, c, ldc, (int32_t)tiles_m, (int32_t)tiles_n);
+    DMMV_LAUNCH_CHECK();
+    return DMMV_OK;
+}
+
+template <class TA, int PARTS, int BY>
+static dmmv_status lay_gradient(int64_t T, int64_t O, const TA* dy, int64_t ld, const BlockView& b, uint16_t* out, hipStream_t s) {
+    const int64_t Tp = up(T, 128), Op = up(O, 128);
+    hipLaunchKernelGGL((k_block_lay_gradient<TA, PARTS, BY>), dim3((unsigned)ceil_div(Tp * (Op / 8), 256)), dim3(256), 0, s, T, O, dy, ld, b, out, Tp, Op);
+    DMMV_LAUNCH_CHECK();
+    return DMMV_OK;
+}
+
+// TRANS: c = dw [O][K] from x [T][K]; else dx [T][K] from w [O][K].  ws: the call's workspace; laid: dy lies there in PA parts
+// without scales.
 template <class TA, bool TRANS, class TC>
-static dmmv_status grad(int64_t M, int64_t N, int64_t Kc, const TA* a, int64_t lda, const dmmv_block_matrix* b, TC* c, int64_t ldc, float* part,
-                        hipStream_t s) {
-    if (M == 0 || N == 0) return DMMV_OK;
-    const bool exact = !b->scales || b->scale_type == DMMV_E8M0;
-    if constexpr (sizeof(TA) == 2) {
-        const int64_t big = ceil_div(M, 256) * ceil_div(N, 256);
-        if (exact && M >= 256 && N >= 256 && (TRANS ? M : Kc) % 8 == 0 && N % 16 == 0 && lda % 8 == 0 && lda < 1 << 22 && (uintptr_t)a % 16 == 0 &&
-            b->ld % 16 == 0 && (uintptr_t)b->codes % 16 == 0 && big <= INT32_MAX / 4) {
-            const void* kern = (const void*)k_block_grad_tiled<TRANS, TC>;
-            DMMV_TRY(ensure_dynamic_lds(kern, GT_LDS));
-            hipLaunchKernelGGL((k_block_grad_tiled<TRANS, TC>), dim3((unsigned)big), dim3(256), GT_LDS, s, M, N, Kc, a, lda, layer_view(b), c,
-                               ldc, (int32_t)ceil_div(M, 256), (int32_t)ceil_div(N, 256));
-            DMMV_LAUNCH_CHECK();
-            return DMMV_OK;
-        }
-    }
+static dmmv_status grad(int64_t T, int64_t O, int64_t K, const TA* dy, int64_t ld, const dmmv_block_matrix* b, TC* c, int64_t ldc, char* ws,
+                        bool* laid, hipStream_t s) {
+    const int64_t M = TRANS ? O : T, Kc = TRANS ? T : O;
+    if (M == 0 || K == 0) return DMMV_OK;
     constexpr int PA = sizeof(TA) == 4 ? 3 : 1;
-    return exact ? grad_any<TA, TRANS, PA, 1, TC>(M, N, Kc, a, lda, b, c, ldc, part, s)
-                 : grad_any<TA, TRANS, PA, 3, TC>(M, N, Kc, a, lda, b, c, ldc, part, s);
+    const bool exact = !b->scales || b->scale_type == DMMV_E8M0;
+    const bool codes_aligned = K % 16 == 0 && b->ld % 16 == 0 && (uintptr_t)b->codes % 16 == 0;
+    const bool dy_aligned = O % 8 == 0 && ld % 8 == 0 && ld < 1 << 22 && (uintptr_t)dy % 16 == 0;
+    if constexpr (PA == 1)
+        if (exact && codes_aligned && dy_aligned && large_tiles(M, K, Kc, 1, 0.0))
+            return grad_tiled<TRANS, TC>(M, K, Kc, dy, ld, 1, 0, layer_view(b), Kc, c, ldc, s);
+    const bool rowwise = !exact && (b->scale_block_stride == 0 || K <= 128);
+    const int parts = PA == 3 ? 3 : exact ? 1 : sizeof(TC) == 2 ? 2 : 3;
+    const int64_t Tp = up(T, 128), Op = up(O, 128);
+    if ((exact || rowwise) && Op < 1 << 22 && Tp * Op / 8 / 256 < INT32_MAX && Kc > 0 &&
+        large_tiles(M, K, Kc, parts, 2.0 * T * O) && large_tiles(M, K, Kc, parts == 1 ? 1 : 3, 2.0 * T * O)) {
+        uint16_t* lay = reinterpret_cast<uint16_t*>(ws);
+        BlockView v = layer_view(b);
+        constexpr int BY = TRANS ? 2 : 1;
+        if (exact) {
+            if (!*laid) DMMV_TRY((lay_gradient<TA, PA, 0>(T, O, dy, ld, v, lay, s)));
+            *laid = true;
+        } else {
+            *laid = false;
+            if (parts == 2) DMMV_TRY((lay_gradient<TA, 2, BY>(T, O, dy, ld, v, lay, s)));
+            else DMMV_TRY((lay_gradient<TA, 3, BY>(T, O, dy, ld, v, lay, s)));
+            v.scales = nullptr;                      // they are in dy now
+        }
+        if (!codes_aligned) {
+            const int64_t Kp = up(K, 16);
+            uint8_t* to = reinterpret_cast<uint8_t*>(lay + (size_t)parts * Tp * Op);
+            hipLaunchKernelGGL(k_block_lay_codes, dim3((unsigned)ceil_div(Kc * (Kp / 16), 256)), dim3(256), 0, s, Kc, K, v.codes, v.ld, to, Kp);
+            DMMV_LAUNCH_CHECK();
+            v.codes = to;
+            v.ld = Kp;
+        }
+        return grad_tiled<TRANS, TC>(M, K, TRANS ? Tp : Op, reinterpret_cast<const bf16_t*>(lay), Op, parts, Tp * Op, v, Kc, c, ldc, s);
+    }
+    *laid = false;                                   // the slices go there
+    float* part = reinterpret_cast<float*>(ws);
+    return exact ? grad_any<TA, TRANS, PA, 1, TC>(M, K, Kc, dy, ld, b, c, ldc, part, s)
+                 : grad_any<TA, TRANS, PA, 3, TC>(M, K, Kc, dy, ld, b, c, ldc, part, s);
 }
 
 template <class T>
 static dmmv_status backward(int64_t Tn, int64_t O, int64_t K, const T* dy, int64_t lddy, const dmmv_block_matrix* x,
                             const dmmv_block_matrix* w, T* dx, int64_t lddx, float* dw, int64_t lddw, float* dbias, void* ws, hipStream_t s) {
-    if (dx) DMMV_TRY((grad<T, false, T>(Tn, K, O, dy, lddy, w, dx, lddx, static_cast<float*>(ws), s)));
-    if (dw) DMMV_TRY((grad<T, true, float>(O, K, Tn, dy, lddy, x, dw, lddw, static_cast<float*>(ws), s)));
+    bool laid = false;
+    if (dx) DMMV_TRY((grad<T, false, T>(Tn, O, K, dy, lddy, w, dx, lddx, static_cast<char*>(ws), &laid, s)));
+    if (dw) DMMV_TRY((grad<T, true, float>(Tn, O, K, dy, lddy, x, dw, lddw, static_cast<char*>(ws), &laid, s)));
     if (dbias && O > 0) {
         float* part = static_cast<float*>(ws);
         const int64_t strips = Tn > 0 ? bias_strips(Tn, O) : 0;

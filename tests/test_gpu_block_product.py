@@ -208,6 +208,31 @@ def test_large_backward_of_integers_is_exact(gpu_device, T, O, K):
         assert torch.equal(dw.double(), dy.double().t() @ X) and torch.equal(db.double(), dy.double().sum(0))
 
 
+@pytest.mark.parametrize("T,O,K", [(2048, 4096, 2064), (2050, 4101, 2051), (4099, 2049, 1999)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_large_gradients_laid_out_first(gpu_device, T, O, K, dtype):
+    """32-bit gradients, scales per row and rows that are not aligned, at sizes that the large tiles take."""
+    from paper_2508_13437_amd import dmmv
+
+    for kx, kw in (("e8m0", "e8m0"), ("row", "row"), ("e8m0", "row")):
+        x, w = block(T, K, kx, T + O, gpu_device, integers=True, g=1), block(O, K, kw, K + O, gpu_device, integers=True, g=128 if kw == "e8m0" else None)
+        dy = gradients(T, O, dtype, T, gpu_device, integers=True, pad=1 if dtype == torch.bfloat16 else 0)
+        dx, dw, db = dmmv.dmmv_block_backward(dy, x, w)
+        X, W = (torch.from_numpy(vals(q)).to(gpu_device) for q in (x, w))
+        assert torch.equal(dx, (dy.double() @ W).to(dtype))
+        assert torch.equal(dw.double(), dy.double().t() @ X) and torch.equal(db.double(), dy.double().sum(0))
+    # numbers that need all their bits
+    x, w = block(T, K, "e8m0", 5, gpu_device, g=1), block(O, K, "row", 6, gpu_device)
+    dy = gradients(T, O, dtype, 7, gpu_device)
+    dx, dw, _ = dmmv.dmmv_block_backward(dy, x, w)
+    X, W = (torch.from_numpy(vals(q)).to(gpu_device) for q in (x, w))
+    for g, want, size, n, dt in ((dx, dy.double() @ W, dy.double().abs() @ W.abs(), O, dtype), (dw, dy.double().t() @ X, dy.double().t().abs() @ X.abs(), T, torch.float32)):
+        # (a bf16 result may come from products of 16 bits)
+        e = ((n + 12) * 2 * U + (2.0 ** -15 if dt == torch.bfloat16 else 0.0)) * size
+        assert bool(((g.double() - want).abs() <= e + half_ulp(dt) * 1.01 * (want.abs() + e)).all())
+        assert float((g.double() - want).norm()) <= (2e-6 + 1.01 * half_ulp(dt)) * float(want.norm())
+
+
 def test_gradient_against_differences(gpu_device):
     """sum(dy * product) moves by dx (dw) times the scale when one integer code moves by one: exactly."""
     from paper_2508_13437_amd import dmmv
