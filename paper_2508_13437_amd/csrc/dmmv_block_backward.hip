@@ -104,9 +104,8 @@ __global__ __launch_bounds__(256 * KS) void k_block_grad(int64_t M, int64_t N, i
     const int tile_m = __builtin_amdgcn_readfirstlane(tile / tiles_n), tile_n = tile - tile_m * tiles_n;
     const int64_t m0 = tile_m * 64ll, n0 = tile_n * 64ll;
     // this group's share of the steps; all groups have the same barriers
-    const int64_t nb = (Kc + 63) >> 6;
-    const int64_t share = (nb + slices * KS - 1) / (slices * KS);
-    const int64_t first = min((slice * KS + group) * share, nb), end = min(first + share, nb);
+    const int nb = (int)((Kc + 63) >> 6), share = (nb + slices * KS - 1) / (slices * KS);
+    const int first = min((slice * KS + group) * share, nb), end = min(first + share, nb);
 
     const int row = tid >> 3, col = (tid & 7) * 8;   // rows row, row + 32 of a step, 8 columns
     struct Step {
@@ -114,60 +113,81 @@ __global__ __launch_bounds__(256 * KS) void k_block_grad(int64_t M, int64_t N, i
         Raw8<uint8_t> b[2];
         uint32_t s[2];
     };
-    auto request = [&](Step& r, int64_t kb) __attribute__((always_inline)) {
+    // Whole steps of rows of 8 numbers and more, and what is addressed number by number: the last step, short rows.
+    const bool short_rows = (TRANS ? M : Kc) < 8 || N < 8;
+    const int full = short_rows ? 0 : (int)(Kc >> 6), lastw = max(full - 1, 0);
+    const int a_cut = TRANS ? (int)((m0 + col) - min(m0 + col, M - 8)) : 0, b_cut = (int)((n0 + col) - min(n0 + col, N - 8));    // as raw_settle's `moved`
+    const int64_t blk = (min(n0 + col, N - 1) >> 7) * b.sblk;
+    const TA* ap[2];
+    const uint8_t* bp[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        ap[u] = TRANS ? a + (row + 32 * u) * lda + (m0 + col - a_cut) : a + min(m0 + row + 32 * u, M - 1) * lda + col;
+        bp[u] = b.codes + (row + 32 * u) * b.ld + (n0 + col - b_cut);
+    }
+    const int64_t a_step = TRANS ? 64 * lda : 64, b_step = 64 * b.ld;
+    auto scale_place = [&](int k) __attribute__((always_inline)) { return (int64_t)(k >> b.shift) * b.srow + blk; };
+    auto request = [&](Step& r, int kb) __attribute__((always_inline)) {      // a whole step
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int64_t k = min(kb * 64 + row + 32 * u, Kc - 1);
-            if (TRANS) raw_request(r.a[u], a + k * lda, m0 + col, M);
-            else raw_request(r.a[u], a + min(m0 + row + 32 * u, M - 1) * lda, kb * 64 + col, Kc);
-            raw_request(r.b[u], (const uint8_t*)b.codes + k * b.ld, n0 + col, N);
-            r.s[u] = scale_bits(b, k, min(n0 + col, N - 1) >> 7);
+            r.a[u].load(ap[u] + kb * a_step);
+            r.b[u].load(bp[u] + kb * b_step);
+            r.s[u] = *scale_word(b, scale_place(kb * 64 + row + 32 * u));
         }
     };
-    auto deposit = [&](Step& r, int64_t kb, int stage) __attribute__((always_inline)) {
+    auto request_slow = [&](Step& r, int kb) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int64_t k = kb * 64 + row + 32 * u;
-            if (TRANS) raw_settle(r.a[u], m0 + col, M, k < Kc);
-            else raw_settle(r.a[u], kb * 64 + col, Kc, true);
-            raw_settle(r.b[u], n0 + col, N, k < Kc);
+            const int64_t k = min(kb * 64ll + row + 32 * u, Kc - 1);
+            if (TRANS) raw_request(r.a[u], a + k * lda, m0 + col, M);
+            else raw_request(r.a[u], a + min(m0 + row + 32 * u, M - 1) * lda, kb * 64ll + col, Kc);
+            raw_request(r.b[u], (const uint8_t*)b.codes + k * b.ld, n0 + col, N);
+            r.s[u] = *scale_word(b, scale_place((int)k));
+        }
+    };
+    auto deposit = [&](Step& r, int kb, int stage, bool slow) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int64_t k = kb * 64ll + row + 32 * u;
+            if (!slow) {
+                if (TRANS && a_cut > 0) {
+                    if (a_cut >= 8) r.a[u] = Raw8<TA>{};
+                    else r.a[u].right(a_cut);
+                }
+                if (b_cut > 0) {
+                    if (b_cut >= 8) r.b[u] = Raw8<uint8_t>{};
+                    else r.b[u].right(b_cut);
+                }
+            } else {
+                if (TRANS) raw_settle(r.a[u], m0 + col, M, k < Kc);
+                else raw_settle(r.a[u], kb * 64ll + col, Kc, true);
+                raw_settle(r.b[u], n0 + col, N, k < Kc);
+            }
+            const uint32_t sbits = word_bits(b, scale_place((int)min(k, Kc - 1)), r.s[u]);
             const int rr = row + 32 * u;
             uint8_t* pa = lds + stage * STAGE + rr * 128 + (((tid & 7) ^ (TRANS ? (rr & 3) << 1 : rr & 7)) << 4);
             uint8_t* pb = lds + stage * STAGE + PA * 8192 + rr * 128 + (((tid & 7) ^ ((rr & 3) << 1)) << 4);
             if constexpr (PA == 1) {
                 *reinterpret_cast<piece16*>(pa) = r.a[u].v;
             } else {
+                float v[8];
                 piece16 w[3];
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    uint32_t p[3], q[3];
-                    split3(r.a[u].get(e), p);
-                    split3(r.a[u].get(e + 1), q);
-#pragma unroll
-                    for (int i = 0; i < 3; ++i) w[i][e >> 1] = p[i] | (q[i] << 16);
-                }
+                for (int e = 0; e < 8; ++e) v[e] = r.a[u].get(e);
+                split8<3>(v, w);
 #pragma unroll
                 for (int i = 0; i < 3; ++i) *reinterpret_cast<piece16*>(pa + i * 8192) = w[i];
             }
-            const float s = k < Kc ? scale_of(b, r.s[u]) : 0.0f;
-            float v[8];
-            decode8(r.b[u].v, s, v);
-            piece16 w[3];
+            if constexpr (PB == 1) {                 // exponents: exact
+                *reinterpret_cast<bf16x8_t*>(pb) = scaled8((int)r.b[u].v[0], (int)r.b[u].v[1], b.e8m0 ? (k < Kc ? sbits : 127u) : 127u);
+            } else {
+                float v[8];
+                piece16 w[3];
+                decode8(r.b[u].v, k < Kc ? scale_of(b, sbits) : 0.0f, v);
+                split8<3>(v, w);
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                uint32_t p[3], q[3];
-                if constexpr (PB == 3) {
-                    split3(v[e], p);
-                    split3(v[e + 1], q);
-                } else {
-                    p[0] = bf16_bits(v[e]);          // exact
-                    q[0] = bf16_bits(v[e + 1]);
-                }
-#pragma unroll
-                for (int i = 0; i < PB; ++i) w[i][e >> 1] = p[i] | (q[i] << 16);
+                for (int i = 0; i < 3; ++i) *reinterpret_cast<piece16*>(pb + i * 8192) = w[i];
             }
-#pragma unroll
-            for (int i = 0; i < PB; ++i) *reinterpret_cast<piece16*>(pb + i * 8192) = w[i];
         }
     };
     floatx16 acc;
@@ -203,22 +223,38 @@ __global__ __launch_bounds__(256 * KS) void k_block_grad(int64_t M, int64_t N, i
                     if (p + r < PM) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fn[r], fm[p], acc, 0, 0, 0);
         }
     };
-    Step r0 = {}, r1 = {};
-    if (first < end) request(r0, first);
-    if (first + 1 < end) request(r1, first + 1);
-    if (first < end) deposit(r0, first, 0);
-    if (first + 2 < end) request(r0, first + 2);
-    __syncthreads();
-    for (int64_t k = 0; k < share; k += 2) {
-        const int64_t kb = first + k;
-        if (kb + 1 < end) deposit(r1, kb + 1, 1);
-        if (kb + 3 < end) request(r1, kb + 3);
-        if (kb < end) multiply(0);
+    // Requests are made without a condition, or a use would wait for all of them; those past the end ask for the last whole
+    // step again.  Every group has the same barriers.
+    Step r0, r1;
+    const int e1 = min(end, full);
+    if (full > 0) {
+        request(r0, min(first, lastw));
+        request(r1, min(first + 1, lastw));
+        deposit(r0, min(first, lastw), 0, false);
+        request(r0, min(first + 2, lastw));
         __syncthreads();
-        if (k + 1 >= share) break;
-        if (kb + 2 < end) deposit(r0, kb + 2, 0);
-        if (kb + 4 < end) request(r0, kb + 4);
-        if (kb + 1 < end) multiply(1);
+        for (int k = 0; k < share; k += 2) {
+            const int kb = first + k;
+            deposit(r1, min(kb + 1, lastw), 1, false);
+            request(r1, min(kb + 3, lastw));
+            if (kb < e1) multiply(0);
+            __syncthreads();
+            deposit(r0, min(kb + 2, lastw), 0, false);
+            request(r0, min(kb + 4, lastw));
+            if (kb + 1 < e1) multiply(1);
+            __syncthreads();
+        }
+    }
+    const int slow = short_rows ? share : full < nb ? 1 : 0;
+#pragma unroll 1
+    for (int i = 0; i < slow; ++i) {
+        const int kb = short_rows ? first + i : full;
+        if (kb < end && kb >= first) {
+            request_slow(r0, kb);
+            deposit(r0, kb, 0, true);
+        }
+        __syncthreads();
+        if (kb < end && kb >= first) multiply(0);
         __syncthreads();
     }
     if constexpr (KS > 1) {
@@ -535,18 +571,11 @@ __global__ __launch_bounds__(256) void k_block_lay_gradient(int64_t rows, int64_
         }
     }
     piece16 w[3];
+    if constexpr (PARTS == 1) {
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-        uint32_t p[3], q[3];
-        if constexpr (PARTS == 1) {
-            p[0] = bf16_bits(v[e]);                  // exact
-            q[0] = bf16_bits(v[e + 1]);
-        } else {
-            split3(v[e], p);
-            split3(v[e + 1], q);
-        }
-#pragma unroll
-        for (int k = 0; k < PARTS; ++k) w[k][e >> 1] = p[k] | (q[k] << 16);
+        for (int e = 0; e < 8; e += 2) w[0][e >> 1] = bf16_bits(v[e]) | (bf16_bits(v[e + 1]) << 16);      // exact
+    } else {
+        split8<PARTS>(v, w);
     }
 #pragma unroll
     for (int k = 0; k < PARTS; ++k) *reinterpret_cast<piece16*>(out + (PARTS - 1 - k) * Tp * Op + row * Op + col) = w[k];      // smallest first

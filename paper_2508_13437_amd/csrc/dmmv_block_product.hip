@@ -99,35 +99,30 @@ __global__ __launch_bounds__(256 * KS) void k_block_product(int64_t T_, int64_t 
     for (int u = 0; u < NI; ++u) wr[u] = w.codes + min(o0 + crow + 32 * u, O - 1) * w.ld + cchunk * 16;
     const int put = crow * 128 + ((cchunk ^ (crow & 7)) << 4);
     const bool mine_x = tid < BM, mine = tid < BM + BN;
-    const BlockView& sq = mine_x ? x : w;
-    const int64_t srow = mine_x ? min(t0 + tid, T_ - 1) : min(o0 + tid - BM, O - 1);
+    BlockView sq;                                    // (by value: a reference to one of two arguments is read from memory)
+    sq.codes = mine_x ? x.codes : w.codes;
+    sq.scales = mine_x ? x.scales : w.scales;
+    sq.e8m0 = mine_x ? x.e8m0 : w.e8m0;
+    if (SCALED && !(mine_x ? how.x_blocks : how.w_blocks)) sq.scales = nullptr, sq.e8m0 = 1;
+    const int64_t sblk = mine_x ? x.sblk : w.sblk;
+    const int64_t sat = mine_x ? (min(t0 + tid, T_ - 1) >> x.shift) * x.srow : (min(o0 + max(tid - BM, 0), O - 1) >> w.shift) * w.srow;
 
     struct Step {
         piece16 c[MI + NI];
         uint32_t s;
     };
-    auto request = [&](Step& r, int kb) __attribute__((always_inline)) {
-        const int64_t at = kb * 128ll;
-        if (at + 128 <= K) {
+    auto request = [&](Step& r, int kb) __attribute__((always_inline)) {      // a whole block
 #pragma unroll
-            for (int u = 0; u < MI; ++u) r.c[u] = *reinterpret_cast<const piece16_any*>(xr[u] + at);
+        for (int u = 0; u < MI; ++u) r.c[u] = *reinterpret_cast<const piece16_any*>(xr[u] + kb * 128ll);
 #pragma unroll
-            for (int u = 0; u < NI; ++u) r.c[MI + u] = *reinterpret_cast<const piece16_any*>(wr[u] + at);
-        } else {
-            const int left = (int)(K - at) - cchunk * 16;
-#pragma unroll
-            for (int u = 0; u < MI; ++u) r.c[u] = chunk_tail(xr[u] + at, left, at + cchunk * 16);
-#pragma unroll
-            for (int u = 0; u < NI; ++u) r.c[MI + u] = chunk_tail(wr[u] + at, left, at + cchunk * 16);
-        }
-        // as it is stored: a conversion here would wait for the load
-        r.s = 127u;
-        if (mine && !(SCALED && !(mine_x ? how.x_blocks : how.w_blocks))) r.s = scale_bits(sq, srow, kb);
+        for (int u = 0; u < NI; ++u) r.c[MI + u] = *reinterpret_cast<const piece16_any*>(wr[u] + kb * 128ll);
+        r.s = *scale_word(sq, sat + kb * sblk);
     };
-    auto deposit = [&](const Step& r, int stage) __attribute__((always_inline)) {
+    auto deposit = [&](const Step& r, int kb, int stage) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < MI + NI; ++u) *reinterpret_cast<piece16*>(&codes[stage][put + u * 4096]) = r.c[u];
-        if (mine) scl[stage][tid] = SCALED ? r.s : __float_as_uint(scale_of(sq, r.s));
+        const uint32_t bits = word_bits(sq, sat + kb * sblk, r.s);
+        if (mine) scl[stage][tid] = !SCALED && sq.e8m0 ? __float_as_uint(e8m0_value(bits)) : bits;
     };
     floatx4 acc[NI][MI];
 #pragma unroll
@@ -188,22 +183,39 @@ __global__ __launch_bounds__(256 * KS) void k_block_product(int64_t T_, int64_t 
             }
         }
     };
-    Step r0 = {}, r1 = {};
-    if (b0 < b1) request(r0, b0);
-    if (b0 + 1 < b1) request(r1, b0 + 1);
-    deposit(r0, 0);
-    if (b0 + 2 < b1) request(r0, b0 + 2);
-    __syncthreads();
-    for (int k = 0; k < steps; k += 2) {             // every group has the same barriers, the last may have no block
-        const int kb = b0 + k;
-        deposit(r1, 1);                              // block kb + 1, if there is one
-        if (kb + 3 < b1) request(r1, kb + 3);
-        if (kb < b1) multiply(0);
+    // The whole blocks.  Requests are made without a condition, or a use would wait for all of them; those past the end ask for
+    // the last block again.  Every group has the same barriers.
+    const int full = (int)(K >> 7), e1 = min(b1, full), most = max(full - 1, 0);
+    Step r0, r1;
+    if (full > 0) {
+        request(r0, min(b0, most));
+        request(r1, min(b0 + 1, most));
+        deposit(r0, min(b0, most), 0);
+        request(r0, min(b0 + 2, most));
         __syncthreads();
-        if (k + 1 >= steps) break;
-        deposit(r0, 0);                              // block kb + 2
-        if (kb + 4 < b1) request(r0, kb + 4);
-        if (kb + 1 < b1) multiply(1);
+        for (int k = 0; k < steps; k += 2) {
+            const int kb = b0 + k;
+            deposit(r1, min(kb + 1, most), 1);
+            request(r1, min(kb + 3, most));
+            if (kb < e1) multiply(0);
+            __syncthreads();
+            deposit(r0, min(kb + 2, most), 0);
+            request(r0, min(kb + 4, most));
+            if (kb + 1 < e1) multiply(1);
+            __syncthreads();
+        }
+    }
+    if (full < nb) {                                 // the last block, zeros past the row's end: the last group's
+        const int64_t at = full * 128ll;
+        const int left = (int)(K - at) - cchunk * 16;
+#pragma unroll
+        for (int u = 0; u < MI; ++u) r0.c[u] = chunk_tail(xr[u] + at, left, at + cchunk * 16);
+#pragma unroll
+        for (int u = 0; u < NI; ++u) r0.c[MI + u] = chunk_tail(wr[u] + at, left, at + cchunk * 16);
+        r0.s = *scale_word(sq, sat + full * sblk);
+        deposit(r0, full, 0);
+        __syncthreads();
+        if (b1 == nb && b0 < b1) multiply(0);
         __syncthreads();
     }
     if constexpr (KS > 1) {

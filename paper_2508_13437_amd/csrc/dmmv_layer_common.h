@@ -129,6 +129,16 @@ __device__ __forceinline__ uint32_t scale_bits(const BlockView& q, int64_t row, 
 }
 __device__ __forceinline__ float scale_of(const BlockView& q, uint32_t bits) { return q.e8m0 ? e8m0_value(bits) : __uint_as_float(bits); }
 __device__ __forceinline__ float scale_at(const BlockView& q, int64_t row, int64_t block) { return scale_of(q, scale_bits(q, row, block)); }
+// The same for loops that may not wait between a request and its use: the aligned word that holds the scale, always loaded (without
+// scales some word of the codes), and what it means.  A branch around a load makes the compiler wait for all loads.
+__device__ __forceinline__ const uint32_t* scale_word(const BlockView& q, int64_t at) {
+    const uintptr_t p = q.scales ? reinterpret_cast<uintptr_t>(q.scales) + (q.e8m0 ? at : 4 * at) : reinterpret_cast<uintptr_t>(q.codes);
+    return reinterpret_cast<const uint32_t*>(p & ~(uintptr_t)3);
+}
+__device__ __forceinline__ uint32_t word_bits(const BlockView& q, int64_t at, uint32_t word) {
+    if (!q.scales) return q.e8m0 ? 127u : 0x3F800000u;
+    return q.e8m0 ? (word >> (8 * ((reinterpret_cast<uintptr_t>(q.scales) + at) & 3))) & 0xFFu : word;
+}
 __device__ __forceinline__ void scale_put(const BlockView& q, int64_t scale_row, int64_t block, uint32_t b) {
     const int64_t at = scale_row * q.srow + block * q.sblk;
     if (q.e8m0) static_cast<uint8_t*>(q.scales)[at] = (uint8_t)b;
@@ -207,15 +217,44 @@ __device__ __forceinline__ float wave_sum(float v) {
 // stays whole in the first.
 __device__ __forceinline__ void split3(float x, uint32_t (&p)[3]) {
     const uint32_t u = __float_as_uint(x);
-    if ((u & 0x7F800000u) == 0x7F800000u) {
-        p[0] = (u >> 16) | ((u & 0x7FFFFFu) ? 0x40u : 0u);
-        p[1] = p[2] = 0u;
-        return;
-    }
     const float r1 = x - __uint_as_float(u & 0xFFFF0000u);
     const uint32_t u1 = __float_as_uint(r1) & 0xFFFF0000u;
     const float r2 = r1 - __uint_as_float(u1);
     p[0] = u >> 16; p[1] = u1 >> 16; p[2] = __float_as_uint(r2) >> 16;
+    if ((u & 0x7F800000u) == 0x7F800000u) {
+        p[0] |= (u & 0x7FFFFFu) ? 0x40u : 0u;
+        p[1] = p[2] = 0u;
+    }
+}
+// eight of them, as the words of three rows of eight bf16
+template <int PARTS>
+__device__ __forceinline__ void split8(const float (&v)[8], piece16 (&w)[3]) {
+    uint32_t most = 0u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+    if (most < 0x7F800000u) {                        // all finite: no selection between the parts
+        float r[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = v[e];
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) {
+#pragma unroll
+            for (int e = 0; e < 8; e += 2)           // the upper halves of two words
+                w[k][e >> 1] = __builtin_amdgcn_perm(__float_as_uint(r[e + 1]), __float_as_uint(r[e]), 0x07060302u);
+            if (k + 1 < PARTS)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) r[e] -= __uint_as_float(__float_as_uint(r[e]) & 0xFFFF0000u);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            uint32_t p[3], q[3];
+            split3(v[e], p);
+            split3(v[e + 1], q);
+#pragma unroll
+            for (int k = 0; k < PARTS; ++k) w[k][e >> 1] = p[k] | (q[k] << 16);
+        }
+    }
 }
 
 // ---- shared by the tiled products ------------------------------------------------------------
