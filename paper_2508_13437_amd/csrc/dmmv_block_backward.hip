@@ -299,7 +299,7 @@ __global__ __launch_bounds__(256) void k_block_grad_join(int64_t M, int64_t N, i
 // Rows of whole chunks of 16 bytes, aligned, power-of-two scales: tile of 256 x 256, 4 wavefronts (2 x 2, one a SIMD,
 // 128 x 128 each), 64 of the contraction a step, two LDS stages.
 //   The rows of dy go straight from memory into the LDS.  dx: [m][k], the 16-byte chunk c of row m at c ^ (m & 7), read as it
-//   is; dw: [k][m], chunk c of row k at c ^ 4 (k & 3), read transposed.
+//   is; dw: [half][k][128 m], chunk c of row k at c ^ 4 (k & 3), read transposed.
 //   The codes go through registers: a thread has 16 of a row, converted to bf16 with the row's one scale (exact), [k][n] with
 //   chunk c of row k at c ^ 4 (k & 3), read transposed.  (Scales along the contraction are the reason for converting here: a
 //   fragment has 8 rows.)
@@ -321,36 +321,31 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
     tile_of_workgroup(tiles_m, tiles_n, tile_m, tile_n);
     const int64_t m0 = (int64_t)tile_m * 256, n0 = (int64_t)tile_n * 256;
 
-    // requests of dy: 1 KB each, 8 a wavefront and step.  dx: 8 rows of 64; dw: 2 rows of 256
+    // requests of dy: 1 KB each, 8 a wavefront and step.  dx: 8 rows of 64; dw: 4 rows of one half of the wavefronts' columns
     const uint32_t lda2 = (uint32_t)lda * 2;
     const uint8_t* ab = reinterpret_cast<const uint8_t*>(TRANS ? a + m0 : a + m0 * lda);
     const int64_t arows = TRANS ? Kc : min(M - m0, (int64_t)256), acols = TRANS ? (M - m0 + 7) & ~7ll : Kc;   // (rows of whole chunks)
-    uint32_t offa[2];                                // TRANS: of even and odd requests
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-        if (TRANS) {
-            const int row = lane >> 5;
-            offa[p] = row * lda2 + (((lane & 31) ^ (((2 * p + row) & 3) << 2)) << 4);
-        } else {
-            const int row = lane >> 3;
-            offa[p] = row * lda2 + (((lane & 7) ^ row) << 4);
-        }
-    }
+    // dw: a lane's place (16 to a row) holds this chunk of the half's 16: 8 of each 128 columns
+    const int tchunk = (lane & 15) ^ ((lane >> 4) << 2), tcol = ((tchunk >> 3) * 16 + (tchunk & 7)) * 8;
+    const uint32_t offa = TRANS ? (lane >> 4) * lda2 + tcol * 2 : (lane >> 3) * lda2 + (((lane & 7) ^ (lane >> 3)) << 4);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
     const int steps = (int)(Kc >> 7) * 2;            // of one part, in pairs
     // step f of all parts: step f % steps of part f / steps (three at most)
     auto part_of = [&](int f) __attribute__((always_inline)) { return (f >= steps ? 1 : 0) + (f >= 2 * steps ? 1 : 0); };
-    auto bring = [&](int f, int stage, int q) __attribute__((always_inline)) {       // q: 0 .. 7
-        const int at = wv * 8 + q, p = part_of(f), kb = f - p * steps;
+    // request i (of 4) of this wavefront for half h of the wavefronts' rows (columns) of the tile, 64 each
+    auto bring = [&](int f, int stage, auto h, int i) __attribute__((always_inline)) {
+        const int p = part_of(f), kb = f - p * steps;
         const uint8_t* ap = ab + p * plane * 2;
         if constexpr (TRANS) {
             // a buffer of the step's 64 rows: offsets stay small however many rows there are
+            const int at = wv * 4 + i;
             const int64_t row0 = (int64_t)kb * 64;
             const intx4 buf = buffer_of(ap + row0 * lda2, (uint32_t)((min(arows - row0, (int64_t)64) - 1) * lda2 + min(acols, (int64_t)256) * 2));
-            lds_request(buf, offa[q & 1], (uint32_t)(2 * at) * lda2, lds0 + stage + at * 1024);
+            lds_request(buf, offa, (uint32_t)(4 * at) * lda2 + h.value * 128, lds0 + stage + h.value * 16384 + at * 1024);
         } else {
+            const int at = (wv >> 1) * 16 + h.value * 8 + (wv & 1) * 4 + i;
             const intx4 buf = buffer_of(ap, (uint32_t)(arows - 1) * lda2 + (uint32_t)acols * 2);
-            lds_request(buf, offa[0], (uint32_t)kb * 128 + (uint32_t)(8 * at) * lda2, lds0 + stage + at * 1024);
+            lds_request(buf, offa, (uint32_t)kb * 128 + (uint32_t)(8 * at) * lda2, lds0 + stage + at * 1024);
         }
     };
     // codes: thread has chunk tid % 16 of rows tid / 16 + 16 u
@@ -399,7 +394,8 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
     const int mrow = wm + (lane & 31);
     auto frag_m = [&](int stage, int j, int s, int h) __attribute__((always_inline)) {
         if constexpr (TRANS) {
-            fm[j][s][h] = transposed(stage, wm, j, s, h);
+            const int chunk = (wm >> 7) * 8 + (j & 1) * 4 + (tn >> 3);
+            fm[j][s][h] = read_transposed(lds + stage + (j >> 1) * 16384 + (tk + 4 * h + 16 * s) * 256 + ((chunk ^ ((tk & 3) << 2)) << 4) + (tn & 7) * 2);
         } else if (h == 0) {
             const piece16 v = *reinterpret_cast<const piece16*>(lds + stage + (mrow + 32 * j) * 128 + (((2 * s + (lane >> 5)) ^ (mrow & 7)) << 4));
             fm[j][s][0] = piece8{v[0], v[1]};
@@ -410,10 +406,12 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
         const piece16 n = {fn[i][s][0][0], fn[i][s][0][1], fn[i][s][1][0], fn[i][s][1][1]}, m = {fm[j][s][0][0], fm[j][s][0][1], fm[j][s][1][0], fm[j][s][1][1]};
         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, n), __builtin_bit_cast(bf16x8_t, m), acc[i][j], 0, 0, 0);
     };
+    const int paired = steps * planes, last = paired - 1, nb = (int)((Kc + 63) >> 6);
     // Products of half ih of the codes' tiles with half jh of dy's.  FM: the fragments for the next quadrant are of dy
-    // (half fh, from the stage at fs), else of the codes.  NEXT: block `to` of dy (requests 4 r ..) and of the codes
-    // (chunks 2 r ..; registers hold them already) go to the stage at rs, and the codes of block `to` + 1 are requested.
-    auto quad = [&](auto ih, auto jh, auto FM, int fs, auto fh, auto NEXT, auto r, int to, int rs_, int then) __attribute__((always_inline)) {
+    // (half fh, from the stage at fs), else of the codes.  Requests 2 r .. for half rh of dy's block `to` go to the stage at rs.
+    // NEXT: the codes of a block (chunks 2 r ..; registers hold them already) go to the stage at rs, and those of block `then` are
+    // requested.
+    auto quad = [&](auto ih, auto jh, auto FM, int fs, auto fh, auto NEXT, auto r, auto rh, int to, int rs_, int then) __attribute__((always_inline)) {
 #pragma unroll
         for (int s = 0; s < 4; ++s)
 #pragma unroll
@@ -427,8 +425,8 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
                     if (FM.value) frag_m(fs, fh.value * 2 + (f & 1), f >> 1, h);
                     else frag_n(fs, fh.value * 2 + (f & 1), f >> 1, h);
                 }
+                if ((slot & 7) == 1) bring(to, rs_, rh, r.value * 2 + (slot >> 3));
                 if (NEXT.value) {
-                    if ((slot & 3) == 1) bring(to, rs_, r.value * 4 + (slot >> 2));
                     if ((slot & 7) == 2) deposit(rs_, r.value * 2 + (slot >> 3));
                     if ((slot & 7) == 6) request(then - part_of(then) * steps, r.value * 2 + (slot >> 3));
                 }
@@ -437,22 +435,27 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
     };
     constexpr std::integral_constant<int, 0> C0{};
     constexpr std::integral_constant<int, 1> C1{};
-    auto step = [&](auto P, auto Q, int to, int then) __attribute__((always_inline)) {      // P: parity, Q = 1 - P
+    // As in the large product: of block j's rows (columns) of dy those that are read first, half j & 1, are requested a half step
+    // before the others, with a barrier in the middle and at the end of a step.
+    auto step = [&](auto P, auto Q, int to, int then) __attribute__((always_inline)) {      // P: parity, Q = 1 - P; to: this step + 2
         constexpr int cur = P.value * GT_STAGE, nxt = Q.value * GT_STAGE;
-        quad(C0, P, C1, cur, Q, C0, C0, 0, 0, 0);
-        quad(C0, Q, C0, cur, C1, C0, C0, 0, 0, 0);
-        lds_requests_left<0>();
+        quad(C0, P, C1, cur, Q, C0, C0, P, min(to - 1, last), nxt, 0);
+        quad(C0, Q, C0, cur, C1, C0, C1, P, min(to - 1, last), nxt, 0);
+        lds_requests_left<4>();
         __syncthreads();
-        quad(C1, Q, C0, nxt, C0, C1, C0, to, cur, then);
-        quad(C1, P, C1, nxt, Q, C1, C1, to, cur, then);
+        quad(C1, Q, C0, nxt, C0, C1, C0, P, min(to, last), cur, then);
+        quad(C1, P, C1, nxt, Q, C1, C1, P, min(to, last), cur, then);
+        lds_requests_left<8>();                      // (12 have followed: 4 of dy, the codes and their scales)
+        __syncthreads();
     };
 
-    const int paired = steps * planes, last = paired - 1, nb = (int)((Kc + 63) >> 6);
     if (paired > 0) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) bring(0, 0, q);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) bring(1, GT_STAGE, q);
+        for (int i = 0; i < 4; ++i) {
+            bring(0, 0, C0, i);
+            bring(0, 0, C1, i);
+            bring(1, GT_STAGE, C1, i);               // its other half follows in the first step
+        }
 #pragma unroll
         for (int k = 0; k < 3; ++k)
 #pragma unroll
@@ -472,8 +475,8 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
                     frag_m(0, t, s, h);
                 }
         for (int kb = 0; kb < paired; kb += 2) {
-            step(C0, C1, min(kb + 2, last), min(kb + 3, last));
-            step(C1, C0, min(kb + 3, last), min(kb + 4, last));
+            step(C0, C1, kb + 2, min(kb + 3, last));
+            step(C1, C0, kb + 3, min(kb + 4, last));
         }
         lds_requests_left<0>();
     }
@@ -485,10 +488,10 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
 #pragma unroll 1
         for (int q = 0; q < 8; ++q) {
             const int at = wv * 8 + q;
-            const int row = TRANS ? 2 * at + (lane >> 5) : 8 * at + (lane >> 3);
+            const int row = TRANS ? 4 * (at & 15) + (lane >> 4) : 8 * at + (lane >> 3);
             piece16 v = {0u, 0u, 0u, 0u};
             if constexpr (TRANS) {
-                const int col = ((lane & 31) ^ ((row & 3) << 2)) * 8;
+                const int col = tcol + (at >> 4) * 64;
                 if (row < left && m0 + col < M) v = *reinterpret_cast<const piece16*>(ab + ((int64_t)kb * 64 + row) * lda2 + col * 2);
             } else {
                 const int col = ((lane & 7) ^ (row & 7)) * 8;

@@ -304,7 +304,7 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
     const intx4 bufx = buffer_of(xb, lastx * ldx + (uint32_t)K), bufw = buffer_of(wb, lastw * ldw + (uint32_t)K);
     const int crow = lane >> 3, cchunk = (lane & 7) ^ crow;
     const uint32_t offx = crow * ldx + cchunk * 16, offw = crow * ldw + cchunk * 16;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds + wv * (MI * 1024);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
 
     floatx4 acc[NI][MI];
 #pragma unroll
@@ -317,10 +317,11 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
     constexpr int SB = 64, SROW = SB + 4, WROWS = WTILE ? ((BN + 127) / 128) : BN, NS = WTILE ? 1 : NI;
     uint8_t* scl = lds + NST * STAGE;
     uint32_t sx[MI], sw[NS];
-    if (SCALED) {                                    // what is not read from the tables is 1
+    auto scales_one = [&]() __attribute__((always_inline)) {         // what is not read from the tables is 1
+        if (!SCALED || (how.x_blocks && how.w_blocks)) return;
         for (int i = tid; i < (BM + WROWS) * (SROW / 4); i += 256) reinterpret_cast<uint32_t*>(scl)[i] = 0x7F7F7F7Fu;
         __syncthreads();
-    }
+    };
 #define BP_SCALES_STAGE(kb)                                                                                     \
     {                                                                                                           \
         if (how.x_blocks) stage_exponents(x, t0, T_, 1, BM, kb, min(nb - (kb), SB), scl, SROW);                 \
@@ -335,13 +336,12 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
             sw[i] = *reinterpret_cast<const uint16_t*>(p_ + (BM + (WTILE ? wo >> 7 : wo + 16 * i + lr)) * SROW); \
     }
 
-    // request q of a step: 8 rows of x (q < MI) or of w
+    // Request i (of MI / 2) of this wavefront for half `h` of the wavefronts' rows of x (W 0) or w (W 1): 8 rows
     static_assert(MI == NI && MI % 4 == 0, "quadrants of the wavefront's tile");
-    // (a block that is not there is past the buffer's end in the last row only; the caller asks for blocks that are there)
-    auto place = [&](int q) __attribute__((always_inline)) { return (q < MI ? 0 : BM * 128) + (q % MI) * 1024; };
-    auto bring = [&](int kb, int stage, int q) __attribute__((always_inline)) {
-        lds_request(q < MI ? bufx : bufw, q < MI ? offx : offw,
-                    (uint32_t)kb * 128u + (uint32_t)(8 * (wv * MI + q % MI)) * (q < MI ? ldx : ldw), lds0 + stage + place(q));
+    auto bring = [&](int kb, int stage, auto W, auto h, int i) __attribute__((always_inline)) {
+        const int row = (wv >> 1) * (16 * MI) + h.value * (8 * MI) + ((wv & 1) * (MI / 2) + i) * 8;
+        lds_request(W.value ? bufw : bufx, W.value ? offw : offx, (uint32_t)kb * 128u + (uint32_t)row * (W.value ? ldw : ldx),
+                    lds0 + stage + (W.value ? BM * 128 : 0) + row * 128);
     };
 
     piece16 fx[MI][2], fw[NI][2];                    // a fragment's 32 codes, in two halves
@@ -358,10 +358,12 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
     auto frag_w = [&](int stage, int i, int h) __attribute__((always_inline)) {
         fw[i][h] = *reinterpret_cast<const piece16*>(pw[h] + stage + i * 2048);
     };
+    // blocks in pairs (the loop's body is one piece of straight code, or the compiler takes the products out of it)
+    const int paired = (int)(K >> 8) * 2, last = paired - 1;
     // One quadrant of the wavefront's tile (halves ih of w, jh of x) with step parity P.  Between the products, a few
     // instructions in the shadow of each and in this order: the fragments of half `fh` of x (FX) or w for the next
-    // quadrant, from the stage at fs, and with REQ the requests of half r of block kb into the stage at rs.
-    auto quad = [&](auto P, auto ih, auto jh, auto FX, int fs, auto fh, auto REQ, auto r, int kb, int rs) __attribute__((always_inline)) {
+    // quadrant, from the stage at fs, and the requests for half rh of w (RW) or x of block kb into the stage at rs.
+    auto quad = [&](auto P, auto ih, auto jh, auto FX, int fs, auto fh, auto RW, auto rh, int kb, int rs) __attribute__((always_inline)) {
 #pragma unroll
         for (int g = 0; g < MI / 2; ++g) {
 #pragma unroll
@@ -373,38 +375,54 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
                     if (k < 2) {
                         if (FX.value) frag_x(fs, fh.value * (MI / 2) + g, k);
                         else frag_w(fs, fh.value * (NI / 2) + g, k);
-                    } else if (REQ.value) {
-                        bring(kb, rs, r.value * MI + 2 * g + k - 2);
+                    } else if (k == 2) {
+                        bring(kb, rs, RW, rh, g);
                     }
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
     };
-    // A step: four quadrants, each with one new half of fragments.  X0: the half of x that is there at the start;
-    // the other half comes first, and at the end next step's w half 0 and x half 1 - X0 are there.  The barrier between
-    // the second and third quadrant: every wavefront has read all of this stage, and the next stage is whole (the NST - 2
-    // after it may still be on their way); from there on this stage takes block `to`.
+    // A step: four quadrants, each with one new half of fragments and a quarter of a block's requests (all of them at once
+    // would keep the address unit, and with it the wavefront, for half of the step).  X0: the half of x that is there at the
+    // start; the other half comes first, and at the end next step's w half 0 and x half 1 - X0 are there.
+    // Block j's first requests are for what is read first, w half 0 and x half j & 1: made in the second half of step j - NST, when its
+    // stage has been read, and whole at the middle of step j - 1; the others a half step later.  So there is a barrier
+    // in the middle and at the end of a step, and at either the wavefront's last LEFT requests may still be on their way.
     constexpr std::integral_constant<int, 0> C0{};
     constexpr std::integral_constant<int, 1> C1{};
-    auto step = [&](auto P, auto N, int cur, int nxt, int to) __attribute__((always_inline)) {        // P: parity of the step and X0, N = 1 - P
-        quad(P, C0, P, C1, cur, N, C0, C0, 0, 0);
-        quad(P, C0, N, C0, cur, C1, C0, C0, 0, 0);
-        lds_requests_left<(NST - 2) * 2 * MI>();
+    constexpr int LEFT = (2 * NST - 3) * MI;
+    auto step = [&](auto P, auto N, int cur, int nxt, int prv, int to) __attribute__((always_inline)) {        // P: parity of the step and X0, N = 1 - P
+        quad(P, C0, P, C1, cur, N, C0, P, min(to - 1, last), prv);
+        quad(P, C0, N, C0, cur, C1, C1, C1, min(to - 1, last), prv);
+        lds_requests_left<LEFT>();
         __syncthreads();
-        quad(P, C1, N, C0, nxt, C0, C1, C0, to, cur);
-        quad(P, C1, P, C1, nxt, N, C1, C1, to, cur);
+        quad(P, C1, N, C0, nxt, C0, C1, C0, min(to, last), cur);
+        quad(P, C1, P, C1, nxt, N, C0, P, min(to, last), cur);
+        lds_requests_left<LEFT>();
+        __syncthreads();
     };
 
-    // blocks in pairs (the loop's body is one piece of straight code, or the compiler takes the products out of it)
-    const int paired = (int)(K >> 8) * 2, last = paired - 1;
     if (paired > 0) {
 #pragma unroll
-        for (int st = 0; st < NST; ++st)
+        for (int st = 0; st < NST; ++st) {           // all of NST - 1 blocks, the first half of one
+            const int kb = min(st, last);
+            auto half = [&](auto wh, auto xh) __attribute__((always_inline)) {
 #pragma unroll
-            for (int q = 0; q < 2 * MI; ++q) bring(min(st, last), st * STAGE, q);
+                for (int i = 0; i < MI / 2; ++i) bring(kb, st * STAGE, C1, wh, i);
+#pragma unroll
+                for (int i = 0; i < MI / 2; ++i) bring(kb, st * STAGE, C0, xh, i);
+            };
+            if (st & 1) half(C0, C1);
+            else half(C0, C0);
+            if (st < NST - 1) {
+                if (st & 1) half(C1, C0);
+                else half(C1, C1);
+            }
+        }
+        scales_one();
         if (SCALED) BP_SCALES_STAGE(0);
-        lds_requests_left<(NST - 1) * 2 * MI>();
+        lds_requests_left<LEFT>();
         __syncthreads();
 #pragma unroll
         for (int g = 0; g < MI / 2; ++g)
@@ -418,8 +436,9 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
             for (; kb < end; kb += 2) {
                 if (SCALED) BP_SCALES_TAKE(kb);
                 const int at = NST == 2 ? 0 : (kb & (NST - 1)) * STAGE, after = NST == 2 ? 0 : ((kb + 2) & (NST - 1)) * STAGE;
-                step(C0, C1, at, at + STAGE, min(kb + NST, last));
-                step(C1, C0, at + STAGE, after, min(kb + NST + 1, last));
+                const int before = NST == 2 ? STAGE : ((kb - 1) & (NST - 1)) * STAGE;
+                step(C0, C1, at, at + STAGE, before, kb + NST);
+                step(C1, C0, at + STAGE, after, at, kb + NST + 1);
             }
             if (kb >= paired) break;
             __syncthreads();
@@ -433,6 +452,7 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
     for (int kb = paired; kb < nb; ++kb) {
         const int left = (int)(K - kb * 128ll) - cchunk * 16;
         __syncthreads();
+        if (paired == 0 && kb == 0) scales_one();
         if (SCALED && (kb == paired && (kb & (SB - 1)) == 0)) BP_SCALES_STAGE(kb);
 #pragma unroll 1
         for (int q = 0; q < MI; ++q) {
