@@ -325,6 +325,10 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
     const uint32_t lda2 = (uint32_t)lda * 2;
     const uint8_t* ab = reinterpret_cast<const uint8_t*>(TRANS ? a + m0 : a + m0 * lda);
     const int64_t arows = TRANS ? Kc : min(M - m0, (int64_t)256), acols = TRANS ? (M - m0 + 7) & ~7ll : Kc;   // (rows of whole chunks)
+    const intx4 first = buffer_of(ab, 0);            // (in scalar registers)
+    const uint64_t abase = ((uint64_t)(uint32_t)first[1] << 32) | (uint32_t)first[0];
+    const uint32_t abytes = (uint32_t)__builtin_amdgcn_readfirstlane(
+        (int)(TRANS ? 63u * lda2 + (uint32_t)min(acols, (int64_t)256) * 2 : (uint32_t)(arows - 1) * lda2 + (uint32_t)acols * 2));
     // dw: a lane's place (16 to a row) holds this chunk of the half's 16: 8 of each 128 columns
     const int tchunk = (lane & 15) ^ ((lane >> 4) << 2), tcol = ((tchunk >> 3) * 16 + (tchunk & 7)) * 8;
     const uint32_t offa = TRANS ? (lane >> 4) * lda2 + tcol * 2 : (lane >> 3) * lda2 + (((lane & 7) ^ (lane >> 3)) << 4);
@@ -335,35 +339,39 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
     // request i (of 4) of this wavefront for half h of the wavefronts' rows (columns) of the tile, 64 each
     auto bring = [&](int f, int stage, auto h, int i) __attribute__((always_inline)) {
         const int p = part_of(f), kb = f - p * steps;
-        const uint8_t* ap = ab + p * plane * 2;
+        // (the buffer begins with the part, dw: with the step's 64 rows, so that offsets stay small; all whole)
+        const uint64_t at64 = abase + (uint64_t)p * (uint64_t)(plane * 2) + (TRANS ? (uint64_t)(uint32_t)kb * (uint64_t)(64u * lda2) : 0ull);
+        const intx4 buf = {(int)(uint32_t)at64, (int)(uint32_t)(at64 >> 32) & 0xFFFF, (int)abytes, 0x00020000};
         if constexpr (TRANS) {
-            // a buffer of the step's 64 rows: offsets stay small however many rows there are
             const int at = wv * 4 + i;
-            const int64_t row0 = (int64_t)kb * 64;
-            const intx4 buf = buffer_of(ap + row0 * lda2, (uint32_t)((min(arows - row0, (int64_t)64) - 1) * lda2 + min(acols, (int64_t)256) * 2));
             lds_request(buf, offa, (uint32_t)(4 * at) * lda2 + h.value * 128, lds0 + stage + h.value * 16384 + at * 1024);
         } else {
             const int at = (wv >> 1) * 16 + h.value * 8 + (wv & 1) * 4 + i;
-            const intx4 buf = buffer_of(ap, (uint32_t)(arows - 1) * lda2 + (uint32_t)acols * 2);
             lds_request(buf, offa, (uint32_t)kb * 128 + (uint32_t)(8 * at) * lda2, lds0 + stage + at * 1024);
         }
     };
     // codes: thread has chunk tid % 16 of rows tid / 16 + 16 u
     const int brow = tid >> 4, bchunk = tid & 15;
     const int64_t bcol = n0 + bchunk * 16;
-    const int64_t fb = min(bcol, N - 1) >> 7;
-    const uint8_t* bb = b.codes + n0;
+    const uint32_t fb = (uint32_t)(min(bcol, N - 1) >> 7);
     const int nlast = ((int)min(N - n0, (int64_t)256) + 15) & ~15;
+    // (a chunk past the row's end gives columns that are not stored: the row's last is taken)
+    const uint32_t bld = (uint32_t)b.ld, boff = (uint32_t)min(bchunk * 16, nlast - 16);
+    const intx4 bfirst = buffer_of(b.codes + n0, 0);
+    typedef const __attribute__((address_space(1))) uint8_t* global_bytes;         // (of an address put together: not a flat access)
+    const global_bytes bb = (global_bytes)(((uint64_t)(uint32_t)bfirst[1] << 32) | (uint32_t)bfirst[0]);
     // without scales a byte is read all the same (a branch around the load would wait for it) and not used
-    const uint8_t* sp = b.scales ? static_cast<const uint8_t*>(b.scales) : b.codes;
-    const int64_t srow = b.scales ? b.srow : 0, sblk = b.scales ? b.sblk : 0;
+    const global_bytes sp = (global_bytes)(b.scales ? static_cast<const uint8_t*>(b.scales) : b.codes);
+    const uint32_t srow = b.scales ? (uint32_t)b.srow : 0u, soff = b.scales ? fb * (uint32_t)b.sblk : 0u, each = b.shift ? 0u : srow;
+    const int blast = (int)brows - 1;
     piece16 rb[4];
     uint32_t rs[4];
-    auto request = [&](int kb, int u) __attribute__((always_inline)) {
-        const int64_t row = min((int64_t)kb * 64 + brow + 16 * u, brows - 1);
-        // (rows past the last meet zeros of dy; a chunk past the row's end gives columns that are not stored: the row's last is taken)
-        rb[u] = *reinterpret_cast<const piece16*>(bb + row * b.ld + min(bchunk * 16, nlast - 16));
-        rs[u] = sp[(row >> b.shift) * srow + fb * sblk];
+    auto request = [&](int step_of, int u) __attribute__((always_inline)) {
+        // (rows past the last meet zeros of dy: the last one is read, of the last step that has any)
+        const int kb = min(step_of, blast >> 6);
+        const uint32_t r = (uint32_t)min(brow + 16 * u, blast - kb * 64);
+        rb[u] = *(const __attribute__((address_space(1))) piece16*)(bb + (uint64_t)(uint32_t)kb * (uint64_t)(64u * bld) + (__umul24(r, bld) + boff));
+        rs[u] = (sp + (uint64_t)(((uint32_t)kb * 64u) >> b.shift) * srow)[__umul24(r, each) + soff];
     };
     const int bput = 32768 + brow * 512 + (((bchunk * 2) ^ ((brow & 3) << 2)) << 4);
     auto deposit = [&](int stage, int u) __attribute__((always_inline)) {
@@ -711,15 +719,17 @@ static dmmv_status grad(int64_t T, int64_t O, int64_t K, const TA* dy, int64_t l
     if (M == 0 || K == 0) return DMMV_OK;
     constexpr int PA = sizeof(TA) == 4 ? 3 : 1;
     const bool exact = !b->scales || b->scale_type == DMMV_E8M0;
-    const bool codes_aligned = K % 16 == 0 && b->ld % 16 == 0 && (uintptr_t)b->codes % 16 == 0;
+    const bool codes_aligned = K % 16 == 0 && b->ld % 16 == 0 && (uintptr_t)b->codes % 16 == 0 && b->ld < 1 << 23;
+    // (offsets of 24 x 24 bits, of 32 bits along a row)
+    const bool near = !b->scales || (b->scale_row_stride < 1 << 23 && b->scale_block_stride < 1 << 23 && ceil_div(K, 128) * b->scale_block_stride < 1 << 30);
     const bool dy_aligned = O % 8 == 0 && ld % 8 == 0 && ld < 1 << 22 && (uintptr_t)dy % 16 == 0;
     if constexpr (PA == 1)
-        if (exact && codes_aligned && dy_aligned && large_tiles(M, K, Kc, 1, 0.0))
+        if (exact && near && codes_aligned && dy_aligned && large_tiles(M, K, Kc, 1, 0.0))
             return grad_tiled<TRANS, TC>(M, K, Kc, dy, ld, 1, 0, layer_view(b), Kc, c, ldc, s);
     const bool rowwise = !exact && (b->scale_block_stride == 0 || K <= 128);
     const int parts = PA == 3 ? 3 : exact ? 1 : sizeof(TC) == 2 ? 2 : 3;
     const int64_t Tp = up(T, 128), Op = up(O, 128);
-    if ((exact || rowwise) && Op < 1 << 22 && Tp * Op / 8 / 256 < INT32_MAX && Kc > 0 &&
+    if ((exact ? near : rowwise) && K < 1 << 22 && Op < 1 << 22 && Tp * Op / 8 / 256 < INT32_MAX && Kc > 0 &&
         large_tiles(M, K, Kc, parts, 2.0 * T * O) && large_tiles(M, K, Kc, parts == 1 ? 1 : 3, 2.0 * T * O)) {
         uint16_t* lay = reinterpret_cast<uint16_t*>(ws);
         BlockView v = layer_view(b);
