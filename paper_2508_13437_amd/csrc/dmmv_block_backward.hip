@@ -18,70 +18,6 @@ __device__ __forceinline__ piece8 read_transposed(const uint8_t* p) {
     return __builtin_bit_cast(piece8, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)p));
 }
 
-// ---- eight numbers of a row as they are stored, and what a row's end cuts off -----------------------
-// A piece is loaded whole, from `moved` places further left where the row ends inside it, and put right when it is used:
-// the request does not wait.  Rows shorter than 8 are read one by one.
-template <class T> struct Raw8;
-template <> struct Raw8<float> {
-    piece16 v[2];
-    __device__ __forceinline__ void load(const float* p) {
-        v[0] = *reinterpret_cast<const piece16_any*>(p);
-        v[1] = *reinterpret_cast<const piece16_any*>(p + 4);
-    }
-    __device__ __forceinline__ void set(int i, float x) { v[i >> 2][i & 3] = __float_as_uint(x); }
-    __device__ __forceinline__ void right(int n) {   // by n < 8 numbers, zeros after them
-#pragma unroll
-        for (int s = 4; s >= 1; s >>= 1)
-            if (n & s) {
-                uint32_t w[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) w[i] = i + s < 8 ? v[(i + s) >> 2][(i + s) & 3] : 0u;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = w[i];
-            }
-    }
-    __device__ __forceinline__ float get(int i) const { return __uint_as_float(v[i >> 2][i & 3]); }
-};
-template <> struct Raw8<bf16_t> {
-    piece16 v;
-    __device__ __forceinline__ void load(const bf16_t* p) { v = *reinterpret_cast<const piece16_any*>(p); }
-    __device__ __forceinline__ void set(int i, bf16_t x) { v[i >> 1] |= (uint32_t)x.u << (16 * (i & 1)); }
-    __device__ __forceinline__ void right(int n) {
-        const uint64_t lo = v[0] | ((uint64_t)v[1] << 32), hi = v[2] | ((uint64_t)v[3] << 32);
-        const int s = 16 * n;
-        const uint64_t l = s >= 64 ? hi >> (s - 64) : s == 0 ? lo : (lo >> s) | (hi << (64 - s)), h = s >= 64 ? 0 : hi >> s;
-        v = piece16{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
-    }
-    __device__ __forceinline__ float get(int i) const { return i & 1 ? __uint_as_float(v[i >> 1] & 0xFFFF0000u) : bf16_value(v[i >> 1] & 0xFFFFu); }
-};
-template <> struct Raw8<uint8_t> {
-    piece8 v;
-    __device__ __forceinline__ void load(const uint8_t* p) { v = *reinterpret_cast<const piece8_any*>(p); }
-    __device__ __forceinline__ void set(int i, uint8_t x) { v[i >> 2] |= (uint32_t)x << (8 * (i & 3)); }
-    __device__ __forceinline__ void right(int n) {
-        const uint64_t w = (v[0] | ((uint64_t)v[1] << 32)) >> (8 * n);
-        v = piece8{(uint32_t)w, (uint32_t)(w >> 32)};
-    }
-};
-template <class T>
-__device__ __forceinline__ void raw_request(Raw8<T>& r, const T* __restrict__ row, int64_t col, int64_t cols) {
-    if (cols >= 8) {
-        r.load(row + min(col, cols - 8));
-    } else {
-        r = Raw8<T>{};
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (col + i < cols) r.set(i, row[col + i]);
-    }
-}
-// the piece as it belongs: zeros past the row's end, all zero unless `ok`
-template <class T>
-__device__ __forceinline__ void raw_settle(Raw8<T>& r, int64_t col, int64_t cols, bool ok) {
-    const int64_t moved = cols >= 8 ? col - min(col, cols - 8) : 0;
-    if (!ok || moved >= 8) r = Raw8<T>{};
-    else if (moved > 0) r.right((int)moved);
-}
-
 // C[m][n] = sum_k A(m, k) B(k, n), A(m, k) = a[m][k] or (TRANS) a[k][m], B a block matrix [k][n].
 // PA, PB: bf16 parts that an operand is cut into.  Any sizes, strides and scales.
 // 64 x 64 tile, 4 wavefronts of 32 x 32, 64 of k a step, requested two steps ahead, two LDS stages; KS groups of 4 wavefronts
@@ -298,12 +234,13 @@ __global__ __launch_bounds__(256) void k_block_grad_join(int64_t M, int64_t N, i
 // ---- large gradients ---------------------------------------------------------------------------------
 // Rows of whole chunks of 16 bytes, aligned, power-of-two scales: tile of 256 x 256, 4 wavefronts (2 x 2, one a SIMD,
 // 128 x 128 each), 64 of the contraction a step, two LDS stages.
-//   The rows of dy go straight from memory into the LDS.  dx: [m][k], the 16-byte chunk c of row m at c ^ (m & 7), read as it
-//   is; dw: [half][k][128 m], chunk c of row k at c ^ 4 (k & 3), read transposed.
+//   The rows of dy go straight from memory into the LDS.  dx: [m][k], the 16-byte chunk c of row m at c ^ (m & 7) ^ (m / 16 & 1),
+//   read as it is; dw: [half][k][128 m], chunk c of row k at c ^ 4 (k & 3), read transposed.
 //   The codes go through registers: a thread has 16 of a row, converted to bf16 with the row's one scale (exact), [k][n] with
 //   chunk c of row k at c ^ 4 (k & 3), read transposed.  (Scales along the contraction are the reason for converting here: a
 //   fragment has 8 rows.)
-//   The 4 x 32 lanes of a transposed read are 4 rows of 32 bytes; the places above put 8 such pieces on all 64 banks.
+//   The 4 x 32 lanes of a transposed read are 4 rows of 32 bytes; the places above put 8 such pieces on all 64 banks,
+//   and 16 rows of dx that are read together too.
 // The codes are the A operand, so that a lane's results come in fours along a row of the output.
 // dy may come as several bf16 parts that sum to it (`planes`, `plane` numbers apart): the contraction then runs over all.
 // The loop is that of the large product: a quadrant of 16 products at a time, all else in their shadows.
@@ -331,7 +268,9 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
         (int)(TRANS ? 63u * lda2 + (uint32_t)min(acols, (int64_t)256) * 2 : (uint32_t)(arows - 1) * lda2 + (uint32_t)acols * 2));
     // dw: a lane's place (16 to a row) holds this chunk of the half's 16: 8 of each 128 columns
     const int tchunk = (lane & 15) ^ ((lane >> 4) << 2), tcol = ((tchunk >> 3) * 16 + (tchunk & 7)) * 8;
-    const uint32_t offa = TRANS ? (lane >> 4) * lda2 + tcol * 2 : (lane >> 3) * lda2 + (((lane & 7) ^ (lane >> 3)) << 4);
+    // (dx: the place of a chunk also goes by bit 4 of the row, which is the request's)
+    const uint32_t offa[2] = {TRANS ? (lane >> 4) * lda2 + tcol * 2 : (lane >> 3) * lda2 + (((lane & 7) ^ (lane >> 3)) << 4),
+                              (lane >> 3) * lda2 + (((lane & 7) ^ (lane >> 3) ^ 1) << 4)};
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
     const int steps = (int)(Kc >> 7) * 2;            // of one part, in pairs
     // step f of all parts: step f % steps of part f / steps (three at most)
@@ -344,10 +283,10 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
         const intx4 buf = {(int)(uint32_t)at64, (int)(uint32_t)(at64 >> 32) & 0xFFFF, (int)abytes, 0x00020000};
         if constexpr (TRANS) {
             const int at = wv * 4 + i;
-            lds_request(buf, offa, (uint32_t)(4 * at) * lda2 + h.value * 128, lds0 + stage + h.value * 16384 + at * 1024);
+            lds_request(buf, offa[0], (uint32_t)(4 * at) * lda2 + h.value * 128, lds0 + stage + h.value * 16384 + at * 1024);
         } else {
             const int at = (wv >> 1) * 16 + h.value * 8 + (wv & 1) * 4 + i;
-            lds_request(buf, offa, (uint32_t)kb * 128 + (uint32_t)(8 * at) * lda2, lds0 + stage + at * 1024);
+            lds_request(buf, offa[(i >> 1) & 1], (uint32_t)kb * 128 + (uint32_t)(8 * at) * lda2, lds0 + stage + at * 1024);
         }
     };
     // codes: thread has chunk tid % 16 of rows tid / 16 + 16 u
@@ -405,7 +344,7 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
             const int chunk = (wm >> 7) * 8 + (j & 1) * 4 + (tn >> 3);
             fm[j][s][h] = read_transposed(lds + stage + (j >> 1) * 16384 + (tk + 4 * h + 16 * s) * 256 + ((chunk ^ ((tk & 3) << 2)) << 4) + (tn & 7) * 2);
         } else if (h == 0) {
-            const piece16 v = *reinterpret_cast<const piece16*>(lds + stage + (mrow + 32 * j) * 128 + (((2 * s + (lane >> 5)) ^ (mrow & 7)) << 4));
+            const piece16 v = *reinterpret_cast<const piece16*>(lds + stage + (mrow + 32 * j) * 128 + (((2 * s + (lane >> 5)) ^ (mrow & 7) ^ ((mrow >> 4) & 1)) << 4));
             fm[j][s][0] = piece8{v[0], v[1]};
             fm[j][s][1] = piece8{v[2], v[3]};
         }
@@ -502,7 +441,7 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
                 const int col = tcol + (at >> 4) * 64;
                 if (row < left && m0 + col < M) v = *reinterpret_cast<const piece16*>(ab + ((int64_t)kb * 64 + row) * lda2 + col * 2);
             } else {
-                const int col = ((lane & 7) ^ (row & 7)) * 8;
+                const int col = ((lane & 7) ^ (row & 7) ^ ((row >> 4) & 1)) * 8;
                 if (m0 + row < M && col < left) v = *reinterpret_cast<const piece16*>(ab + (int64_t)row * lda2 + ((int64_t)kb * 64 + col) * 2);
             }
             *reinterpret_cast<piece16*>(lds + at * 1024 + lane * 16) = v;

@@ -257,6 +257,70 @@ __device__ __forceinline__ void split8(const float (&v)[8], piece16 (&w)[3]) {
     }
 }
 
+// ---- eight numbers of a row as they are stored, and what a row's end cuts off -----------------------
+// A piece is loaded whole, from `moved` places further left where the row ends inside it, and put right when it is used:
+// the request does not wait.  Rows shorter than 8 are read one by one.
+template <class T> struct Raw8;
+template <> struct Raw8<float> {
+    piece16 v[2];
+    __device__ __forceinline__ void load(const float* p) {
+        v[0] = *reinterpret_cast<const piece16_any*>(p);
+        v[1] = *reinterpret_cast<const piece16_any*>(p + 4);
+    }
+    __device__ __forceinline__ void set(int i, float x) { v[i >> 2][i & 3] = __float_as_uint(x); }
+    __device__ __forceinline__ void right(int n) {   // by n < 8 numbers, zeros after them
+#pragma unroll
+        for (int s = 4; s >= 1; s >>= 1)
+            if (n & s) {
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = i + s < 8 ? v[(i + s) >> 2][(i + s) & 3] : 0u;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = w[i];
+            }
+    }
+    __device__ __forceinline__ float get(int i) const { return __uint_as_float(v[i >> 2][i & 3]); }
+};
+template <> struct Raw8<bf16_t> {
+    piece16 v;
+    __device__ __forceinline__ void load(const bf16_t* p) { v = *reinterpret_cast<const piece16_any*>(p); }
+    __device__ __forceinline__ void set(int i, bf16_t x) { v[i >> 1] |= (uint32_t)x.u << (16 * (i & 1)); }
+    __device__ __forceinline__ void right(int n) {
+        const uint64_t lo = v[0] | ((uint64_t)v[1] << 32), hi = v[2] | ((uint64_t)v[3] << 32);
+        const int s = 16 * n;
+        const uint64_t l = s >= 64 ? hi >> (s - 64) : s == 0 ? lo : (lo >> s) | (hi << (64 - s)), h = s >= 64 ? 0 : hi >> s;
+        v = piece16{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
+    }
+    __device__ __forceinline__ float get(int i) const { return i & 1 ? __uint_as_float(v[i >> 1] & 0xFFFF0000u) : bf16_value(v[i >> 1] & 0xFFFFu); }
+};
+template <> struct Raw8<uint8_t> {
+    piece8 v;
+    __device__ __forceinline__ void load(const uint8_t* p) { v = *reinterpret_cast<const piece8_any*>(p); }
+    __device__ __forceinline__ void set(int i, uint8_t x) { v[i >> 2] |= (uint32_t)x << (8 * (i & 3)); }
+    __device__ __forceinline__ void right(int n) {
+        const uint64_t w = (v[0] | ((uint64_t)v[1] << 32)) >> (8 * n);
+        v = piece8{(uint32_t)w, (uint32_t)(w >> 32)};
+    }
+};
+template <class T>
+__device__ __forceinline__ void raw_request(Raw8<T>& r, const T* __restrict__ row, int64_t col, int64_t cols) {
+    if (cols >= 8) {
+        r.load(row + min(col, cols - 8));
+    } else {
+        r = Raw8<T>{};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (col + i < cols) r.set(i, row[col + i]);
+    }
+}
+// the piece as it belongs: zeros past the row's end, all zero unless `ok`
+template <class T>
+__device__ __forceinline__ void raw_settle(Raw8<T>& r, int64_t col, int64_t cols, bool ok) {
+    const int64_t moved = cols >= 8 ? col - min(col, cols - 8) : 0;
+    if (!ok || moved >= 8) r = Raw8<T>{};
+    else if (moved > 0) r.right((int)moved);
+}
+
 // ---- shared by the tiled products ------------------------------------------------------------
 // The workgroup's tile.  Workgroups go to the 8 XCDs in turn, each with an L2 of its own: an XCD gets an eighth of the tiles in
 // a row, 4 tiles high and side by side, so that those of one moment share their operands' lines (4096 x 4096 x 11008: 171 us

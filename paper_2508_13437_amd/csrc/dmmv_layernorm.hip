@@ -167,52 +167,92 @@ struct NormIn {
     }
 };
 
+// eight numbers of the input as they are stored
+template <class T, bool Q8>
+struct RawIn {
+    Raw8<T> x;
+    __device__ __forceinline__ void request(const NormIn<T, Q8>& in, int64_t row, int64_t col, int64_t cols) {
+        raw_request(x, in.x + row * in.ldx, col, cols);
+    }
+    __device__ __forceinline__ void get(const NormIn<T, Q8>&, int64_t, int64_t col, int64_t cols, float (&v)[8]) {
+        raw_settle(x, col, cols, col < cols);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = x.get(e);
+    }
+};
+template <class T>
+struct RawIn<T, true> {
+    Raw8<uint8_t> x;
+    uint32_t s;
+    __device__ __forceinline__ void request(const NormIn<T, true>& in, int64_t row, int64_t col, int64_t cols) {
+        raw_request(x, (const uint8_t*)in.q.codes + row * in.q.ld, col, cols);
+        s = *scale_word(in.q, (row >> in.q.shift) * in.q.srow + (col >> 7) * in.q.sblk);
+    }
+    __device__ __forceinline__ void get(const NormIn<T, true>& in, int64_t row, int64_t col, int64_t cols, float (&v)[8]) {
+        raw_settle(x, col, cols, col < cols);
+        const uint32_t bits = word_bits(in.q, (row >> in.q.shift) * in.q.srow + (col >> 7) * in.q.sblk, s);
+        decode8(x.v, scale_of(in.q, bits), v);
+        if (col + 8 > cols)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = col + e < cols ? v[e] : 0.0f;
+    }
+};
+
 // Rows of up to 8192 columns: a team of TPR threads holds a row (its a and h) in registers between the two sums and dx, and keeps
 // its columns' share of dgamma and dbeta over all the rows it takes; the THREADS / TPR teams of a workgroup join theirs at the
 // end, in order, in the LDS.  Everything is read once.
-template <class T, bool Q8, int TPR, int CH, int THREADS>
+template <class T, bool Q8, int TPR, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_layernorm_grad(int64_t rows, int64_t cols, const T* __restrict__ dy, int64_t lddy, NormIn<T, Q8> in,
                                                             const float* __restrict__ gamma, const float* __restrict__ mean,
                                                             const float* __restrict__ rstd, T* __restrict__ dx, int64_t lddx,
                                                             float* __restrict__ part) {
     constexpr int TEAMS = THREADS / TPR, WAVES = TPR / 64;
+    // (8 columns a thread: with 16 the registers of 1024 threads do not hold the next row as well)
     __shared__ float2 sh[2][TEAMS][WAVES];
     __shared__ float join[TPR * 8];
     const int team = threadIdx.x / TPR, t = threadIdx.x % TPR;
     const float n = (float)cols;
-    float g[CH][8], dg[CH][8], db[CH][8];
+    const int64_t col = t * 8ll;
+    float g[8], dg[8], db[8];
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { g[c][e] = 1.0f; dg[c][e] = db[c][e] = 0.0f; }
-    if (gamma)
-#pragma unroll
-        for (int c = 0; c < CH; ++c) load8(gamma, (c * TPR + t) * 8ll, cols, g[c]);
+    for (int e = 0; e < 8; ++e) { g[e] = 1.0f; dg[e] = db[e] = 0.0f; }
+    if (gamma) load8(gamma, col, cols, g);
+    // the row after this one is requested before this one's sums are waited for
+    Raw8<T> nd;
+    RawIn<T, Q8> nx;
+    float nmu, nrs;
+    auto request = [&](int64_t r0) __attribute__((always_inline)) {
+        const int64_t row = min(r0 + team, rows - 1);
+        nmu = mean[row];
+        nrs = rstd[row];
+        if (col >= cols) return;                     // (whole wavefronts but one)
+        raw_request(nd, dy + row * lddy, col, cols);
+        nx.request(in, row, col, cols);
+    };
+    request(blockIdx.x * (int64_t)TEAMS);
     int parity = 0;
     for (int64_t r0 = blockIdx.x * (int64_t)TEAMS; r0 < rows; r0 += gridDim.x * (int64_t)TEAMS, parity ^= 1) {
         const bool there = r0 + team < rows;
         const int64_t row = there ? r0 + team : rows - 1;
-        const float mu = mean[row], rs = rstd[row];
-        float a[CH][8], h[CH][8];
+        const float mu = nmu, rs = nrs;
+        float a[8], h[8];
+        raw_settle(nd, col, cols, col < cols);
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            load8(dy + row * lddy, (c * TPR + t) * 8ll, cols, a[c]);
-            in.get(row, (c * TPR + t) * 8ll, cols, h[c]);
-        }
+        for (int e = 0; e < 8; ++e) a[e] = nd.get(e);
+        nx.get(in, row, col, cols, h);
+        request(r0 + gridDim.x * (int64_t)TEAMS);    // (past the last: the last again)
+        // (past the row's end dy is zero, and so is what follows from it)
         float s1 = 0.0f, s2 = 0.0f;
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
+        if (there)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float d = a[c][e];
-                h[c][e] = (h[c][e] - mu) * rs;
-                if (there && (c * TPR + t) * 8ll + e < cols) {
-                    dg[c][e] = dmmv_fma(d, h[c][e], dg[c][e]);
-                    db[c][e] += d;
-                    a[c][e] = d * g[c][e];
-                    s1 += a[c][e];
-                    s2 = dmmv_fma(a[c][e], h[c][e], s2);
-                }
+                const float d = a[e];
+                h[e] = (h[e] - mu) * rs;
+                dg[e] = dmmv_fma(d, h[e], dg[e]);
+                db[e] += d;
+                a[e] = d * g[e];
+                s1 += a[e];
+                s2 = dmmv_fma(a[e], h[e], s2);
             }
         if (!dx) continue;
         s1 = wave_sum(s1);
@@ -228,40 +268,33 @@ __global__ __launch_bounds__(THREADS) void k_layernorm_grad(int64_t rows, int64_
         s1 /= n;
         s2 /= n;
         if (!there) continue;
+        float w[8];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            float w[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = rs * ((a[c][e] - s1) - h[c][e] * s2);
-            const int64_t col = (c * TPR + t) * 8ll;
-            if (col < cols) store8(dx + row * lddx, col, cols, w);
-        }
+        for (int e = 0; e < 8; ++e) w[e] = rs * ((a[e] - s1) - h[e] * s2);
+        if (col < cols) store8(dx + row * lddx, col, cols, w);
     }
     if (!part) return;
     float* p = part + blockIdx.x * 2ll * cols;
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+    for (int b = 0; b < 2; ++b) {
+        float* v = b ? db : dg;
+        for (int w = 1; w < TEAMS; ++w) {
+            __syncthreads();
+            if (team == w)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            float* v = k ? db[c] : dg[c];
-            for (int w = 1; w < TEAMS; ++w) {
-                __syncthreads();
-                if (team == w)
+                for (int e = 0; e < 8; ++e) join[e * TPR + t] = v[e];
+            __syncthreads();
+            if (team == 0)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) join[e * TPR + t] = v[e];
-                __syncthreads();
-                if (team == 0)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] += join[e * TPR + t];
-            }
-            const int64_t col = (c * TPR + t) * 8ll;
-            if (team == 0 && col < cols) {
-                float o[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = v[e];
-                store8(p + k * cols, col, cols, o);
-            }
+                for (int e = 0; e < 8; ++e) v[e] += join[e * TPR + t];
         }
+        if (team == 0 && col < cols) {
+            float o[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = v[e];
+            store8(p + b * cols, col, cols, o);
+        }
+    }
 }
 
 // ---- longer rows: the sums first, then strips of columns ------------------------------------------
@@ -327,14 +360,14 @@ __global__ __launch_bounds__(256) void k_layernorm_grad_apply(int64_t rows, int6
 
 // ---- host ---------------------------------------------------------------------------------------
 // Parts of the sums over rows.  Rows in registers: a workgroup of 1024 threads a compute unit; while those would have fewer than
-// two rounds of rows, workgroups of 256, 512 at most (513 x 1003: see the table of cases).
+// two rounds of rows, workgroups of 256 (or of a row, where it needs more), 512 at most.
 constexpr int64_t NORM_REGS = 8192;
-static int norm_team(int64_t cols) { return cols <= 1024 ? 64 : 256; }
+static int norm_team(int64_t cols) { return cols <= 512 ? 64 : cols <= 1024 ? 128 : cols <= 2048 ? 256 : cols <= 4096 ? 512 : 1024; }
 static bool norm_small(int64_t rows, int64_t cols) { return rows < 512 * (1024 / norm_team(cols)); }
 static int64_t norm_strips(int64_t rows, int64_t cols) {
     if (cols <= NORM_REGS) {
-        const int64_t teams = (norm_small(rows, cols) ? 256 : cols > 4096 ? 512 : 1024) / norm_team(cols), most = norm_small(rows, cols) ? 512 : 256;
-        const int64_t n = ceil_div(rows, teams);
+        const int team = norm_team(cols), threads = norm_small(rows, cols) ? (team < 256 ? 256 : team) : 1024;
+        const int64_t n = ceil_div(rows, threads / team), most = norm_small(rows, cols) ? 512 : 256;
         return n < most ? n : most;
     }
     int64_t s = 1024 / ceil_div(cols, 2048);
@@ -375,22 +408,15 @@ static dmmv_status norm_backward(int64_t rows, int64_t cols, const T* dy, int64_
         float* parts = reinterpret_cast<float*>(ws);
         float* to = dgamma || dbeta ? parts : nullptr;
         const int64_t n = norm_strips(rows, cols);
-#define NORM_GRAD(TPR, CH, THREADS)                                                                                              \
-    hipLaunchKernelGGL((k_layernorm_grad<T, Q8, TPR, CH, THREADS>), dim3((unsigned)n), dim3(THREADS), 0, stream, rows, cols, dy, lddy, in, \
-                       gamma, mean, rstd, dx, lddx, to)
-        if (norm_small(rows, cols)) {
-            if (cols <= 512) NORM_GRAD(64, 1, 256);
-            else if (cols <= 1024) NORM_GRAD(64, 2, 256);
-            else if (cols <= 2048) NORM_GRAD(256, 1, 256);
-            else if (cols <= 4096) NORM_GRAD(256, 2, 256);
-            else NORM_GRAD(256, 4, 256);
-        } else {
-            if (cols <= 512) NORM_GRAD(64, 1, 1024);
-            else if (cols <= 1024) NORM_GRAD(64, 2, 1024);
-            else if (cols <= 2048) NORM_GRAD(256, 1, 1024);
-            else if (cols <= 4096) NORM_GRAD(256, 2, 1024);
-            else NORM_GRAD(256, 4, 512);
-        }
+#define NORM_GRAD(TPR, THREADS)                                                                                                  \
+    hipLaunchKernelGGL((k_layernorm_grad<T, Q8, TPR, THREADS>), dim3((unsigned)n), dim3(THREADS), 0, stream, rows, cols, dy, lddy, in, gamma, \
+                       mean, rstd, dx, lddx, to)
+        const bool small = norm_small(rows, cols);
+        if (cols <= 512) { if (small) NORM_GRAD(64, 256); else NORM_GRAD(64, 1024); }
+        else if (cols <= 1024) { if (small) NORM_GRAD(128, 256); else NORM_GRAD(128, 1024); }
+        else if (cols <= 2048) { if (small) NORM_GRAD(256, 256); else NORM_GRAD(256, 1024); }
+        else if (cols <= 4096) { if (small) NORM_GRAD(512, 512); else NORM_GRAD(512, 1024); }
+        else NORM_GRAD(1024, 1024);
 #undef NORM_GRAD
         DMMV_LAUNCH_CHECK();
         return to ? layer_sum_parts(parts, n, 2 * cols, dgamma, cols, dbeta, stream) : DMMV_OK;
