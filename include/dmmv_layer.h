@@ -67,8 +67,8 @@ dmmv_status dmmv_block_dequantize(const dmmv_block_matrix* q, int32_t dtype, voi
 /* y[t][o] = sum_k x(t, k) w(o, k) + bias[o], x [T][K], w [O][K], y [T][ldy] of dtype DMMV_F32 or
  * DMMV_BF16, bias float [O] or NULL.  A 32-bit result is summed in 32 bits; a bf16 result by the 8-bit
  * matrix instructions, whose sums carry an error of about 5e-5 of the result's norm before the rounding
- * to bf16 (1.7e-3).  The workspace (size from the HOST function, 0 is possible,
- * 256-byte aligned) holds partial sums where few outputs share a long contraction. */
+ * to bf16 (1.7e-3).  The workspace (size from the HOST function, 0 is possible, 256-byte aligned) holds the operands of a
+ * large product once more where their rows are no multiples of 16 codes. */
 size_t dmmv_block_product_workspace_bytes(int64_t T, int64_t O, int64_t K);
 dmmv_status dmmv_block_product(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, int32_t dtype,
                                void* y, int64_t ldy, void* workspace, size_t workspace_bytes, void* hip_stream);
@@ -78,7 +78,9 @@ dmmv_status dmmv_block_product(const dmmv_block_matrix* x, const dmmv_block_matr
  *   dw[o][k] = sum_t dy[t][o] x(t, k)       [O][lddw] float        (x may be NULL if dw is)
  *   dbias[o] = sum_t dy[t][o]               [O] float
  * Each of the three may be NULL.  They are the gradients with respect to the values that the 8-bit
- * matrices stand for.  T, O, K are the sizes; every product is exact or rounded to 24 bits. */
+ * matrices stand for.  T, O, K are the sizes.  Every product is exact or rounded to 24 bits; bf16 dx and scales that are the same
+ * along a row of w: to 16.  The workspace (256-byte aligned) holds partial sums, and dy as up to three bf16 parts and
+ * codes with aligned rows where a large gradient is made from those. */
 size_t dmmv_block_backward_workspace_bytes(int64_t T, int64_t O, int64_t K);
 dmmv_status dmmv_block_backward(int32_t dtype, int64_t T, int64_t O, int64_t K, const void* dy, int64_t lddy,
                                 const dmmv_block_matrix* x, const dmmv_block_matrix* w, void* dx, int64_t lddx, float* dw,

@@ -163,6 +163,23 @@ dmmv_status layer_sum_parts(const float* part, int64_t parts, int64_t n, float* 
     return DMMV_OK;
 }
 
+// codes with rows of whole aligned chunks of 16 bytes
+__global__ __launch_bounds__(256) void k_block_lay_codes(int64_t rows, int64_t cols, const uint8_t* __restrict__ codes, int64_t ld,
+                                                         uint8_t* __restrict__ out, int64_t Kp) {
+    const int64_t i = blockIdx.x * 256ll + threadIdx.x, chunks = Kp >> 4, row = i / chunks, col = (i - row * chunks) * 16;
+    if (row >= rows) return;
+    const piece8 a = load8_codes(codes + row * ld, col, cols), b = load8_codes(codes + row * ld, col + 8, cols);
+    *reinterpret_cast<piece16*>(out + row * Kp + col) = piece16{a[0], a[1], b[0], b[1]};
+}
+
+dmmv_status layer_lay_codes(const dmmv_block_matrix* q, uint8_t* out, int64_t ld, hipStream_t stream) {
+    const int64_t grid = ceil_div(q->rows * (ld / 16), 256);
+    if (grid > INT32_MAX) return fail(DMMV_ERR_SHAPE, "more codes than a launch takes");
+    hipLaunchKernelGGL(k_block_lay_codes, dim3((unsigned)grid), dim3(256), 0, stream, q->rows, q->cols, static_cast<const uint8_t*>(q->codes), q->ld, out, ld);
+    DMMV_LAUNCH_CHECK();
+    return DMMV_OK;
+}
+
 template <class T>
 static dmmv_status quantize(const T* x, int64_t ldx, const dmmv_block_matrix* q, hipStream_t stream) {
     const int64_t nb = ceil_div(q->cols, 128);

@@ -531,15 +531,6 @@ __global__ __launch_bounds__(256) void k_block_lay_gradient(int64_t rows, int64_
     for (int k = 0; k < PARTS; ++k) *reinterpret_cast<piece16*>(out + (PARTS - 1 - k) * Tp * Op + row * Op + col) = w[k];      // smallest first
 }
 
-// codes with rows of whole aligned chunks of 16 bytes
-__global__ __launch_bounds__(256) void k_block_lay_codes(int64_t rows, int64_t cols, const uint8_t* __restrict__ codes, int64_t ld,
-                                                         uint8_t* __restrict__ out, int64_t Kp) {
-    const int64_t i = blockIdx.x * 256ll + threadIdx.x, chunks = Kp >> 4, row = i / chunks, col = (i - row * chunks) * 16;
-    if (row >= rows) return;
-    const piece8 a = load8_codes(codes + row * ld, col, cols), b = load8_codes(codes + row * ld, col + 8, cols);
-    *reinterpret_cast<piece16*>(out + row * Kp + col) = piece16{a[0], a[1], b[0], b[1]};
-}
-
 // a strip of 512 columns and every gridDim.y-th group of 4 rows
 template <class T>
 __global__ __launch_bounds__(256) void k_block_column_sums(int64_t rows, int64_t cols, const T* __restrict__ dy, int64_t lddy,
@@ -583,12 +574,14 @@ static size_t grad_part_bytes(int64_t M, int64_t N, int64_t Kc) {
     const int32_t s = grad_slices(M, N, Kc);
     return s > 1 ? ((size_t)s * M * N * 4 + 255) / 256 * 256 : 0;
 }
-// Large tiles or small ones?  us by the rates measured (small: 240 TFLOP/s with one part, 110 with three products for one;
-// large: 1.25 us a step of 64, laying out 4 TB/s and two launches).
+// Large tiles or small ones?  us by the rates measured: small tiles 260 TFLOP/s with one part and 145 with three products for
+// one; large 1.4 us a step of 64 and round of 256 tiles, laying out 4 TB/s and two launches.  (All three gradients, small and
+// large, us: 2048 x 2048 x 1024 bf16 69 and 90; 2048^3 in 32 bits 245 and 289; dx of 2048 x 4096 x 1024 with a scale
+// per row 133 and 61; 4096^3 in 32 bits 2380 and 715.)
 static bool large_tiles(int64_t M, int64_t N, int64_t Kc, int parts, double lay_bytes) {
-    const double small = 2.0 * M * N * Kc / (parts == 1 ? 240e6 : 110e6);
+    const double small = 2.0 * M * N * Kc / (parts == 1 ? 260e6 : 145e6);
     const int64_t rounds = ceil_div(ceil_div(M, 256) * ceil_div(N, 256), 256);
-    const double large = 1.25 * rounds * parts * ceil_div(Kc, 64) + lay_bytes / 4e6 + (lay_bytes > 0 ? 10 : 0);
+    const double large = 1.4 * rounds * parts * ceil_div(Kc, 64) + lay_bytes / 4e6 + (lay_bytes > 0 ? 10 : 0);
     return large < small;
 }
 static int64_t up(int64_t n, int64_t to) { return ceil_div(n, to) * to; }
@@ -685,8 +678,7 @@ static dmmv_status grad(int64_t T, int64_t O, int64_t K, const TA* dy, int64_t l
         if (!codes_aligned) {
             const int64_t Kp = up(K, 16);
             uint8_t* to = reinterpret_cast<uint8_t*>(lay + (size_t)parts * Tp * Op);
-            hipLaunchKernelGGL(k_block_lay_codes, dim3((unsigned)ceil_div(Kc * (Kp / 16), 256)), dim3(256), 0, s, Kc, K, v.codes, v.ld, to, Kp);
-            DMMV_LAUNCH_CHECK();
+            DMMV_TRY(layer_lay_codes(b, to, Kp, s));
             v.codes = to;
             v.ld = Kp;
         }

@@ -71,24 +71,20 @@ struct ProductScales {
     int32_t x_blocks, w_blocks;         // SCALED: exponents per block, else constant along the row
 };
 
-// KS groups of 4 wavefronts share the blocks of a tile where the tiles alone do not fill the chip, joined in order.
-template <class T, int KS, bool SCALED>
-__global__ __launch_bounds__(256 * KS) void k_block_product(int64_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
+template <class T, bool SCALED>
+__global__ __launch_bounds__(256) void k_block_product(int64_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
                                                        const float* __restrict__ bias, T* __restrict__ y, int64_t ldy, int32_t tiles_t, int32_t tiles_o) {
     constexpr bool WIDE = sizeof(T) == 4;
     constexpr int MI = 2, NI = 2, BM = 32 * MI, BN = 32 * NI;
-    __shared__ __align__(16) uint8_t codes_of[KS][2][128 * (BM + BN)];
-    __shared__ __align__(16) uint32_t scl_of[KS][2][BM + BN];
-    const int tid = threadIdx.x & 255, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
-    const int group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    auto& codes = codes_of[group];
-    auto& scl = scl_of[group];
+    __shared__ __align__(16) uint8_t codes[2][128 * (BM + BN)];
+    __shared__ __align__(16) uint32_t scl[2][BM + BN];
+    const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wt = (wv & 1) * (16 * MI), wo = (wv >> 1) * (16 * NI);
     int tile_t, tile_o;
     tile_of_workgroup(tiles_t, tiles_o, tile_t, tile_o);
     const int64_t t0 = (int64_t)tile_t * BM, o0 = (int64_t)tile_o * BN;
     const int nb = (int)((K + 127) >> 7);
-    const int b0 = (int)((int64_t)nb * group / KS), b1 = (int)((int64_t)nb * (group + 1) / KS), steps = (nb + KS - 1) / KS;
     // this thread's chunks of a step: rows tid / 8 + 32 u of x, then of w; its scale: of row tid of both together
     const int crow = tid >> 3, cchunk = tid & 7;
     const uint8_t* xr[MI];
@@ -184,28 +180,27 @@ __global__ __launch_bounds__(256 * KS) void k_block_product(int64_t T_, int64_t 
         }
     };
     // The whole blocks.  Requests are made without a condition, or a use would wait for all of them; those past the end ask for
-    // the last block again.  Every group has the same barriers.
-    const int full = (int)(K >> 7), e1 = min(b1, full), most = max(full - 1, 0);
+    // the last block again.
+    const int full = (int)(K >> 7), most = full - 1;
     Step r0, r1;
     if (full > 0) {
-        request(r0, min(b0, most));
-        request(r1, min(b0 + 1, most));
-        deposit(r0, min(b0, most), 0);
-        request(r0, min(b0 + 2, most));
+        request(r0, 0);
+        request(r1, min(1, most));
+        deposit(r0, 0, 0);
+        request(r0, min(2, most));
         __syncthreads();
-        for (int k = 0; k < steps; k += 2) {
-            const int kb = b0 + k;
+        for (int kb = 0; kb < full; kb += 2) {
             deposit(r1, min(kb + 1, most), 1);
             request(r1, min(kb + 3, most));
-            if (kb < e1) multiply(0);
+            multiply(0);
             __syncthreads();
             deposit(r0, min(kb + 2, most), 0);
             request(r0, min(kb + 4, most));
-            if (kb + 1 < e1) multiply(1);
+            if (kb + 1 < full) multiply(1);
             __syncthreads();
         }
     }
-    if (full < nb) {                                 // the last block, zeros past the row's end: the last group's
+    if (full < nb) {                                 // the last block, zeros past the row's end
         const int64_t at = full * 128ll;
         const int left = (int)(K - at) - cchunk * 16;
 #pragma unroll
@@ -215,20 +210,7 @@ __global__ __launch_bounds__(256 * KS) void k_block_product(int64_t T_, int64_t 
         r0.s = *scale_word(sq, sat + full * sblk);
         deposit(r0, full, 0);
         __syncthreads();
-        if (b1 == nb && b0 < b1) multiply(0);
-        __syncthreads();
-    }
-    if constexpr (KS > 1) {
-        floatx4* join = reinterpret_cast<floatx4*>(&codes_of[0][0][0]);      // [KS - 1][NI * MI][256]
-        if (group > 0)
-#pragma unroll
-            for (int i = 0; i < NI * MI; ++i) join[((group - 1) * NI * MI + i) * 256 + tid] = acc[i / MI][i % MI];
-        __syncthreads();
-        if (group > 0) return;
-#pragma unroll
-        for (int g = 1; g < KS; ++g)
-#pragma unroll
-            for (int i = 0; i < NI * MI; ++i) acc[i / MI][i % MI] += join[((g - 1) * NI * MI + i) * 256 + tid];
+        multiply(0);
     }
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
@@ -523,13 +505,13 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
 // ---- few tokens ------------------------------------------------------------------------------------
 // Up to 64 tokens: the weights are read once, straight into registers in the order of the operands (a lane 32 codes of
 // a row and block, 128 bytes of a row side by side), and nothing else counts.  A workgroup has 16 outputs and
-// 16 MT tokens, its WAVES wavefronts a share of the blocks each, joined in order through the LDS.  U blocks are
+// 16 MT tokens, its four wavefronts a share of the blocks each, joined in order through the LDS.  U blocks are
 // requested at a time.
-template <class T, int MT, int WAVES, bool SCALED>
-__global__ __launch_bounds__(64 * WAVES) void k_block_product_few(int32_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
+template <class T, int MT, bool SCALED>
+__global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
                                                                   const float* __restrict__ bias, T* __restrict__ y, int64_t ldy) {
     constexpr bool WIDE = sizeof(T) == 4;
-    constexpr int U = MT >= 4 ? 2 : 4;
+    constexpr int U = MT >= 4 ? 2 : 4, WAVES = 4;
     __shared__ floatx4 part[WAVES][MT][64];
     const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -645,16 +627,16 @@ __global__ __launch_bounds__(64 * WAVES) void k_block_product_few(int32_t T_, in
     }
 }
 
-template <class T, int MT, int WAVES>
+template <class T, int MT>
 static dmmv_status launch_few_of(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const ProductScales& how, bool scaled, const float* bias,
                                  T* y, int64_t ldy, hipStream_t s) {
     const dim3 grid((unsigned)ceil_div(w->rows, 16), (unsigned)ceil_div(x->rows, 16 * MT));
     if (scaled)
-        hipLaunchKernelGGL((k_block_product_few<T, MT, WAVES, true>), grid, dim3(64 * WAVES), 0, s, (int32_t)x->rows, w->rows, x->cols,
-                           layer_view(x), layer_view(w), how, bias, y, ldy);
+        hipLaunchKernelGGL((k_block_product_few<T, MT, true>), grid, dim3(256), 0, s, (int32_t)x->rows, w->rows, x->cols, layer_view(x), layer_view(w),
+                           how, bias, y, ldy);
     else
-        hipLaunchKernelGGL((k_block_product_few<T, MT, WAVES, false>), grid, dim3(64 * WAVES), 0, s, (int32_t)x->rows, w->rows, x->cols,
-                           layer_view(x), layer_view(w), how, bias, y, ldy);
+        hipLaunchKernelGGL((k_block_product_few<T, MT, false>), grid, dim3(256), 0, s, (int32_t)x->rows, w->rows, x->cols, layer_view(x), layer_view(w),
+                           how, bias, y, ldy);
     DMMV_LAUNCH_CHECK();
     return DMMV_OK;
 }
@@ -662,10 +644,9 @@ static dmmv_status launch_few_of(const dmmv_block_matrix* x, const dmmv_block_ma
 template <class T>
 static dmmv_status launch_few(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const ProductScales& how, bool scaled, const float* bias,
                               T* y, int64_t ldy, hipStream_t s) {
-    const bool many = w->rows >= 8192;                 // 16 outputs x 4 wavefronts fill the chip
-    if (x->rows <= 16) return many ? launch_few_of<T, 1, 4>(x, w, how, scaled, bias, y, ldy, s) : launch_few_of<T, 1, 8>(x, w, how, scaled, bias, y, ldy, s);
-    if (x->rows <= 32) return many ? launch_few_of<T, 2, 4>(x, w, how, scaled, bias, y, ldy, s) : launch_few_of<T, 2, 8>(x, w, how, scaled, bias, y, ldy, s);
-    return many ? launch_few_of<T, 4, 4>(x, w, how, scaled, bias, y, ldy, s) : launch_few_of<T, 4, 8>(x, w, how, scaled, bias, y, ldy, s);
+    if (x->rows <= 16) return launch_few_of<T, 1>(x, w, how, scaled, bias, y, ldy, s);
+    if (x->rows <= 32) return launch_few_of<T, 2>(x, w, how, scaled, bias, y, ldy, s);
+    return launch_few_of<T, 4>(x, w, how, scaled, bias, y, ldy, s);
 }
 
 // scales that are the same along a row leave the sum
@@ -688,40 +669,57 @@ static dmmv_status launch_tiled(const dmmv_block_matrix* x, const dmmv_block_mat
     return DMMV_OK;
 }
 
+// bf16 results by the large tiles: 256 x 256, or 128 x 128 with more stages
+static dmmv_status product_tiled(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, bf16_t* y, int64_t ldy, hipStream_t s) {
+    const bool wtile = constant_rows(w) || w->scale_rows == 128;
+    int dev = 0, cus = 0;
+    DMMV_HIP_CHECK(hipGetDevice(&dev));
+    DMMV_HIP_CHECK(hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev));
+    const int64_t small = ceil_div(x->rows, 128) * ceil_div(w->rows, 128), large = ceil_div(x->rows, 256) * ceil_div(w->rows, 256);
+    // a round of large tiles takes 2.25 times one of small ones (K = 4096: 46 us and 20.5; 1024 x 4096 x 11008 54 and 62 us,
+    // 2048 x 4096 x 4096 51 and 44)
+    if (wtile && 9 * ceil_div(large, cus) < 4 * ceil_div(small, cus)) return launch_tiled<bf16_t, 8, 8, true, true, 2>(x, w, bias, y, ldy, s);
+    return launch_tiled<bf16_t, 4, 4, true, false, 4>(x, w, bias, y, ldy, s);
+}
+
+// Rows that are no multiple of 16 codes are laid out for the large tiles where the general kernel (0.4 to 0.55 PFLOP/s) would
+// take over some 30 us: 4096 x 4095 x 11008 225 us against 660, and the other way about 500 x 2731 x 1777 two launches
+// for 20 us.  Bytes, 0 = not.
+static size_t product_workspace(int64_t T, int64_t O, int64_t K) {
+    if (K % 16 == 0 || T <= 64 || ceil_div(K, 128) * 128 >= 1 << 23 || 2.0 * (double)T * (double)O * (double)K < 12e9) return 0;
+    return (size_t)(T + O) * (size_t)(ceil_div(K, 128) * 128);
+}
+
 template <class T>
-static dmmv_status product(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, T* y, int64_t ldy, hipStream_t s) {
+static dmmv_status product(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, T* y, int64_t ldy, void* ws, hipStream_t s) {
     const ProductScales how = {!constant_rows(x), !constant_rows(w)};
     const bool scaled = (constant_rows(x) || x->scale_type == DMMV_E8M0) && (constant_rows(w) || w->scale_type == DMMV_E8M0);
-    if (x->rows <= 64) return launch_few(x, w, how, scaled, bias, y, ldy, s);
-    if constexpr (sizeof(T) == 2)
-        if (scaled && aligned(x) && aligned(w)) {
-            const bool wtile = constant_rows(w) || w->scale_rows == 128;
-            int dev = 0, cus = 0;
-            DMMV_HIP_CHECK(hipGetDevice(&dev));
-            DMMV_HIP_CHECK(hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev));
-            const int64_t small = ceil_div(x->rows, 128) * ceil_div(w->rows, 128);
-            // a round of large tiles takes 2.25 times one of small ones (K = 4096: 46 us and 20.5)
-            const int64_t large = ceil_div(x->rows, 256) * ceil_div(w->rows, 256);
-            if (wtile && 9 * ceil_div(large, cus) < 4 * ceil_div(small, cus)) return launch_tiled<T, 8, 8, true, true, 2>(x, w, bias, y, ldy, s);
-            return launch_tiled<T, 4, 4, true, false, 4>(x, w, bias, y, ldy, s);
-        }
+    // Few tokens (4096 x 4096, then 4096 x 11008, us): 16 tokens 9.2 by registers and 16.3 by tiles, 32: 10.6 and 16.3, 64: 16.4 and
+    // 16.3, 40.5 and 16.9; where the large tiles do not apply, 64 (32 bits): 17.4 and 19.3, 128: 32.5 and 20.
+    const bool tiles = sizeof(T) == 2 && scaled && aligned(x) && aligned(w);
+    if (x->rows <= (tiles ? 32 : 64)) return launch_few(x, w, how, scaled, bias, y, ldy, s);
+    if (tiles) return product_tiled(x, w, bias, reinterpret_cast<bf16_t*>(y), ldy, s);
+    if (sizeof(T) == 2 && scaled && product_workspace(x->rows, w->rows, x->cols) > 0) {
+        dmmv_block_matrix lx = *x, lw = *w;
+        lx.ld = lw.ld = ceil_div(x->cols, 128) * 128;
+        lx.codes = ws;
+        lw.codes = static_cast<uint8_t*>(ws) + x->rows * lx.ld;
+        DMMV_TRY(layer_lay_codes(x, static_cast<uint8_t*>(lx.codes), lx.ld, s));
+        DMMV_TRY(layer_lay_codes(w, static_cast<uint8_t*>(lw.codes), lw.ld, s));
+        return product_tiled(&lx, &lw, bias, reinterpret_cast<bf16_t*>(y), ldy, s);
+    }
     const int64_t tiles_t = ceil_div(x->rows, 64), tiles_o = ceil_div(w->rows, 64);
     if (tiles_t > INT32_MAX / 4 / tiles_o) return fail(DMMV_ERR_SHAPE, "y: more tiles than a launch takes");
     const dim3 grid((unsigned)(tiles_t * tiles_o));
-    const bool share = tiles_t * tiles_o < 512 && x->cols > 128;
-#define BP_ANY(KS, SCALED)                                                                                                       \
-    hipLaunchKernelGGL((k_block_product<T, KS, SCALED>), grid, dim3(256 * KS), 0, s, x->rows, w->rows, x->cols, layer_view(x), layer_view(w), \
-                       how, bias, y, ldy, (int32_t)tiles_t, (int32_t)tiles_o)
-    if (share && scaled) BP_ANY(2, true);
-    else if (share) BP_ANY(2, false);
-    else if (scaled) BP_ANY(1, true);
-    else BP_ANY(1, false);
-#undef BP_ANY
+    if (scaled)
+        hipLaunchKernelGGL((k_block_product<T, true>), grid, dim3(256), 0, s, x->rows, w->rows, x->cols, layer_view(x), layer_view(w), how, bias, y,
+                           ldy, (int32_t)tiles_t, (int32_t)tiles_o);
+    else
+        hipLaunchKernelGGL((k_block_product<T, false>), grid, dim3(256), 0, s, x->rows, w->rows, x->cols, layer_view(x), layer_view(w), how, bias, y,
+                           ldy, (int32_t)tiles_t, (int32_t)tiles_o);
     DMMV_LAUNCH_CHECK();
     return DMMV_OK;
 }
-
-static size_t product_workspace(int64_t, int64_t, int64_t) { return 0; }
 
 }  // namespace dmmv
 
@@ -743,5 +741,6 @@ extern "C" dmmv_status dmmv_block_product(const dmmv_block_matrix* x, const dmmv
     DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, product_workspace(x->rows, w->rows, x->cols)));
     if (x->rows == 0 || w->rows == 0) return DMMV_OK;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    return dtype == DMMV_F32 ? product(x, w, bias, static_cast<float*>(y), ldy, s) : product(x, w, bias, static_cast<bf16_t*>(y), ldy, s);
+    return dtype == DMMV_F32 ? product(x, w, bias, static_cast<float*>(y), ldy, workspace, s)
+                             : product(x, w, bias, static_cast<bf16_t*>(y), ldy, workspace, s);
 }

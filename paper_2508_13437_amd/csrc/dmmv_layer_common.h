@@ -33,6 +33,9 @@ static inline int layer_width(int32_t dtype) { return dtype == DMMV_BF16 ? 2 : 4
 dmmv_status layer_sum_parts(const float* part, int64_t parts, int64_t n, float* out0, int64_t n0, float* out1,
                             hipStream_t stream);
 
+// a copy of the codes with rows of ld bytes (a multiple of 16), zeros after the columns
+dmmv_status layer_lay_codes(const dmmv_block_matrix* q, uint8_t* out, int64_t ld, hipStream_t stream);
+
 #ifdef __HIPCC__
 
 typedef float floatx4 __attribute__((ext_vector_type(4)));

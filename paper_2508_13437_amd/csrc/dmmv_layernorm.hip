@@ -211,7 +211,7 @@ __global__ __launch_bounds__(THREADS) void k_layernorm_grad(int64_t rows, int64_
     __shared__ float2 sh[2][TEAMS][WAVES];
     __shared__ float join[TPR * 8];
     const int team = threadIdx.x / TPR, t = threadIdx.x % TPR;
-    const float n = (float)cols;
+    const float inv_n = 1.0f / (float)cols;
     const int64_t col = t * 8ll;
     float g[8], dg[8], db[8];
 #pragma unroll
@@ -265,8 +265,8 @@ __global__ __launch_bounds__(THREADS) void k_layernorm_grad(int64_t rows, int64_
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) { s1 += sh[parity][team][w].x; s2 += sh[parity][team][w].y; }
         }
-        s1 /= n;
-        s2 /= n;
+        s1 *= inv_n;
+        s2 *= inv_n;
         if (!there) continue;
         float w[8];
 #pragma unroll
