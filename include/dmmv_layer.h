@@ -91,7 +91,7 @@ dmmv_status dmmv_block_backward(int32_t dtype, int64_t T, int64_t O, int64_t K, 
  *   v = (x - mean) * rstd * gamma + beta            (gamma, beta float [cols], NULL = 1, 0)
  * Outputs, each may be NULL: y [rows][ldy] = v in dtype; q = v in 8 bits, quantised like
  * dmmv_block_quantize from the 32-bit v; xq = x in 8 bits (scale_rows 1 for both); mean, rstd float
- * [rows].  eps >= 0 and finite. */
+ * [rows] (NaN where cols = 0).  eps >= 0 and finite. */
 dmmv_status dmmv_layernorm(int32_t dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx, const float* gamma,
                            const float* beta, float eps, void* y, int64_t ldy, const dmmv_block_matrix* q,
                            const dmmv_block_matrix* xq, float* mean, float* rstd, void* hip_stream);

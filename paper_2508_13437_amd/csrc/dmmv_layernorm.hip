@@ -482,7 +482,7 @@ extern "C" dmmv_status dmmv_layernorm(int32_t dtype, int64_t rows, int64_t cols,
     DMMV_TRY(check_vector(beta, false, "beta"));
     DMMV_TRY(check_vector(mean, false, "mean"));
     DMMV_TRY(check_vector(rstd, false, "rstd"));
-    if (rows == 0 || cols == 0) return DMMV_OK;
+    if (rows == 0) return DMMV_OK;             // (rows without columns: mean and rstd are 0 / 0)
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     if (dtype == DMMV_F32) {
         const NormOut<float> o{static_cast<float*>(y), ldy, layer_view(q), layer_view(xq), q != nullptr, xq != nullptr};

@@ -579,9 +579,9 @@ def _matrix(t: torch.Tensor, what: str) -> torch.Tensor:
     return _rows(t)
 
 
-def _vector(t: Optional[torch.Tensor], n: int, dev: int, what: str) -> Optional[int]:
-    """Address of a float32 vector of n entries on the device (the caller keeps t, a copy is kept by the allocator until the
-    stream has passed it)."""
+def _vector(t: Optional[torch.Tensor], n: int, dev: int, what: str) -> Optional[torch.Tensor]:
+    """t, a float32 vector of n entries on the device, or a contiguous copy that the caller keeps until its call is enqueued (or
+    the call's own results would be allocated in its place)."""
     if t is None:
         return None
     if t.dtype != torch.float32:
@@ -589,7 +589,7 @@ def _vector(t: Optional[torch.Tensor], n: int, dev: int, what: str) -> Optional[
     if t.dim() != 1 or t.shape[0] != n:
         raise DmmvError(-2, f"{what} must have {n} entries")
     _same(t, dev)
-    return t.data_ptr() if t.is_contiguous() else t.contiguous().data_ptr()
+    return t if t.is_contiguous() else t.contiguous()
 
 
 def _same(t: torch.Tensor, dev: int):
@@ -627,8 +627,8 @@ def _workspace(name: str, *sizes: int) -> int:
 
 def _new_block(rows: int, cols: int, scale_rows: int, scale_dtype: torch.dtype, dev: torch.device) -> BlockMatrix:
     blocks = -(-cols // 128)
-    codes = torch.empty((rows, cols), dtype=torch.uint8, device=dev)
-    scales = torch.empty((-(-rows // scale_rows), blocks), dtype=scale_dtype, device=dev)
+    codes = torch.empty(rows, cols, dtype=torch.uint8, device=dev)
+    scales = torch.empty(-(-rows // scale_rows), blocks, dtype=scale_dtype, device=dev)
     q = BlockMatrix.__new__(BlockMatrix)
     q._fill(codes, scales, scale_rows, rows, cols, cols, scales.data_ptr(), blocks, 1, _SCALE_TYPES[scale_dtype])
     return q
@@ -650,7 +650,7 @@ def dmmv_block_quantize(x: torch.Tensor, scale_rows: int = 1, scale_dtype: torch
 def dmmv_block_dequantize(q: BlockMatrix, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """The values that q stands for."""
     kind = _layer_dtype(dtype)
-    x = torch.empty((q.rows, q.cols), dtype=dtype, device=q.codes.device)
+    x = torch.empty(q.rows, q.cols, dtype=dtype, device=q.codes.device)
     _enqueue(x.get_device(), load().dmmv_block_dequantize, q._p, kind, x.data_ptr(), q.cols)
     return x
 
@@ -663,10 +663,10 @@ def dmmv_block_product(x: BlockMatrix, w: BlockMatrix, bias: Optional[torch.Tens
     _same(w.codes, dev)
     T, O = x.rows, w.rows
     b = _vector(bias, O, dev, "bias")
-    y = torch.empty((T, O), dtype=dtype, device=x.codes.device)
+    y = torch.empty(T, O, dtype=dtype, device=x.codes.device)
     nbytes = _workspace("dmmv_block_product_workspace_bytes", T, O, x.cols)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=y.device) if nbytes else None
-    _enqueue(dev, load().dmmv_block_product, x._p, w._p, b, kind, y.data_ptr(), O, _addr(ws), nbytes)
+    _enqueue(dev, load().dmmv_block_product, x._p, w._p, _addr(b), kind, y.data_ptr(), O, _addr(ws), nbytes)
     return y
 
 
@@ -686,9 +686,9 @@ def dmmv_block_backward(dy: torch.Tensor, x: Optional[BlockMatrix], w: Optional[
         _same(x.codes, dev)
     if dx:
         _same(w.codes, dev)
-    gx = torch.empty((T, K), dtype=dy.dtype, device=on) if dx else None
-    gw = torch.empty((O, K), dtype=torch.float32, device=on) if dw else None
-    gb = torch.empty((O,), dtype=torch.float32, device=on) if dbias else None
+    gx = torch.empty(T, K, dtype=dy.dtype, device=on) if dx else None
+    gw = torch.empty(O, K, dtype=torch.float32, device=on) if dw else None
+    gb = torch.empty(O, dtype=torch.float32, device=on) if dbias else None
     nbytes = _workspace("dmmv_block_backward_workspace_bytes", T, O, K)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=on) if nbytes else None
     _enqueue(dev, load().dmmv_block_backward, kind, T, O, K, dy.data_ptr(), dy.stride(0), x._p if dw else None,
@@ -715,13 +715,13 @@ def dmmv_layernorm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: 
     T, F = x.shape
     dev, on = x.get_device(), x.device
     g, b = _vector(gamma, F, dev, "gamma"), _vector(beta, F, dev, "beta")
-    mean = torch.empty((T,), dtype=torch.float32, device=on)
-    rstd = torch.empty((T,), dtype=torch.float32, device=on)
-    out = torch.empty((T, F), dtype=x.dtype, device=on) if y else None
+    mean = torch.empty(T, dtype=torch.float32, device=on)
+    rstd = torch.empty(T, dtype=torch.float32, device=on)
+    out = torch.empty(T, F, dtype=x.dtype, device=on) if y else None
     oq = _new_block(T, F, 1, torch.uint8, on) if q else None
     ox = _new_block(T, F, 1, torch.uint8, on) if xq else None
-    _enqueue(dev, load().dmmv_layernorm, kind, T, F, x.data_ptr(), x.stride(0), g, b, eps, _addr(out), F, oq._p if q else None,
-             ox._p if xq else None, mean.data_ptr(), rstd.data_ptr())
+    _enqueue(dev, load().dmmv_layernorm, kind, T, F, x.data_ptr(), x.stride(0), _addr(g), _addr(b), eps, _addr(out), F,
+             oq._p if q else None, ox._p if xq else None, mean.data_ptr(), rstd.data_ptr())
     return LayerNormResult(out, oq, ox, mean, rstd)
 
 
@@ -747,11 +747,11 @@ def dmmv_layernorm_backward(dy: torch.Tensor, x, gamma: Optional[torch.Tensor], 
         _same(x, dev)
         px, ldx, pq = x.data_ptr(), x.stride(0), None
     g, mu, rs = _vector(gamma, F, dev, "gamma"), _vector(mean, T, dev, "mean"), _vector(rstd, T, dev, "rstd")
-    gx = torch.empty((T, F), dtype=dy.dtype, device=on) if dx else None
-    gg = torch.empty((F,), dtype=torch.float32, device=on) if dgamma else None
-    gb = torch.empty((F,), dtype=torch.float32, device=on) if dbeta else None
+    gx = torch.empty(T, F, dtype=dy.dtype, device=on) if dx else None
+    gg = torch.empty(F, dtype=torch.float32, device=on) if dgamma else None
+    gb = torch.empty(F, dtype=torch.float32, device=on) if dbeta else None
     nbytes = _workspace("dmmv_layernorm_workspace_bytes", T, F)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=on) if nbytes else None
-    _enqueue(dev, load().dmmv_layernorm_backward, kind, T, F, dy.data_ptr(), dy.stride(0), px, ldx, pq, g, mu, rs, _addr(gx), F,
-             _addr(gg), _addr(gb), _addr(ws), nbytes)
+    _enqueue(dev, load().dmmv_layernorm_backward, kind, T, F, dy.data_ptr(), dy.stride(0), px, ldx, pq, _addr(g), mu.data_ptr(),
+             rs.data_ptr(), _addr(gx), F, _addr(gg), _addr(gb), _addr(ws), nbytes)
     return gx, gg, gb

@@ -157,6 +157,32 @@ def test_gradient_against_differences(gpu_device):
         assert abs(db[j] - D[:, j].sum()) <= 2e-6 * np.abs(db).max()
 
 
+def test_vectors_with_gaps(gpu_device):
+    """Copies of strided vectors outlive the allocation of the results, which have their size here."""
+    from paper_2508_13437_amd import dmmv
+
+    n = 640
+    x = make(n, n, torch.float32, 12, gpu_device)
+    gamma, beta = vectors(n, 13, gpu_device)
+    apart = [torch.stack([v, torch.zeros_like(v)], 1)[:, 0] for v in (gamma, beta)]
+    r, s = dmmv.dmmv_layernorm(x, gamma, beta, xq=True), dmmv.dmmv_layernorm(x, *apart, xq=True)
+    for a, b in ((r.y, s.y), (r.mean, s.mean), (r.rstd, s.rstd), (r.xq.codes, s.xq.codes)):
+        assert torch.equal(a, b)
+    stats = [torch.stack([v, torch.zeros_like(v)], 1)[:, 0] for v in (r.mean, r.rstd)]
+    for a, b in zip(dmmv.dmmv_layernorm_backward(x, x, gamma, r.mean, r.rstd), dmmv.dmmv_layernorm_backward(x, x, apart[0], *stats)):
+        assert torch.equal(a, b)
+    row = dmmv.dmmv_block_quantize(x[:1])
+    assert torch.equal(dmmv.dmmv_block_product(row, r.xq, beta, torch.float32),
+                       dmmv.dmmv_block_product(row, r.xq, apart[1], torch.float32))
+
+
+def test_rows_without_columns(gpu_device):
+    from paper_2508_13437_amd import dmmv
+
+    r = dmmv.dmmv_layernorm(torch.empty(300, 0, device=gpu_device), q=True, xq=True)
+    assert r.y.shape == (300, 0) and torch.isnan(r.mean).all() and torch.isnan(r.rstd).all()
+
+
 def test_no_rows_and_another_stream(gpu_device):
     from paper_2508_13437_amd import dmmv
 
