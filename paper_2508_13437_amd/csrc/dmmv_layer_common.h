@@ -134,13 +134,15 @@ __device__ __forceinline__ float scale_of(const BlockView& q, uint32_t bits) { r
 __device__ __forceinline__ float scale_at(const BlockView& q, int64_t row, int64_t block) { return scale_of(q, scale_bits(q, row, block)); }
 // The same for loops that may not wait between a request and its use: the aligned word that holds the scale, always loaded (without
 // scales some word of the codes), and what it means.  A branch around a load makes the compiler wait for all loads.
-__device__ __forceinline__ const uint32_t* scale_word(const BlockView& q, int64_t at) {
+__device__ __forceinline__ const __attribute__((address_space(1))) uint32_t* scale_word(const BlockView& q, int64_t at) {
     const uintptr_t p = q.scales ? reinterpret_cast<uintptr_t>(q.scales) + (q.e8m0 ? at : 4 * at) : reinterpret_cast<uintptr_t>(q.codes);
-    return reinterpret_cast<const uint32_t*>(p & ~(uintptr_t)3);
+    // (a pointer made of a number is not known to be one to global memory: its load would be counted with those of the LDS)
+    return (const __attribute__((address_space(1))) uint32_t*)(p & ~(uintptr_t)3);
 }
 __device__ __forceinline__ uint32_t word_bits(const BlockView& q, int64_t at, uint32_t word) {
-    if (!q.scales) return q.e8m0 ? 127u : 0x3F800000u;
-    return q.e8m0 ? (word >> (8 * ((reinterpret_cast<uintptr_t>(q.scales) + at) & 3))) & 0xFFu : word;
+    const uint32_t byte = (word >> (8 * ((reinterpret_cast<uintptr_t>(q.scales) + at) & 3))) & 0xFFu;      // (no branch)
+    const uint32_t there = q.e8m0 ? byte : word, one = q.e8m0 ? 127u : 0x3F800000u;
+    return q.scales ? there : one;
 }
 __device__ __forceinline__ void scale_put(const BlockView& q, int64_t scale_row, int64_t block, uint32_t b) {
     const int64_t at = scale_row * q.srow + block * q.sblk;
