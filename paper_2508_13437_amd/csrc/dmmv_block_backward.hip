@@ -19,7 +19,8 @@ __device__ __forceinline__ piece8 read_transposed(const uint8_t* p) {
 }
 
 // C[m][n] = sum_k A(m, k) B(k, n), A(m, k) = a[m][k] or (TRANS) a[k][m], B a block matrix [k][n].
-// PA, PB: bf16 parts that an operand is cut into.  Any sizes, strides and scales.
+// PA, PB: bf16 parts that an operand is cut into.  Any sizes, strides and scales.  LAID (TA bf16, PA > 1): `a` is laid out as PA parts
+// `plane` numbers apart, the smallest first, with zeros up to a multiple of 128 rows and columns.
 // 64 x 64 tile, 4 wavefronts of 32 x 32, 64 of k a step, requested two steps ahead, two LDS stages; KS groups of 4 wavefronts
 // and `slices` workgroups share the contraction where the tiles alone do not fill the chip (the groups are joined
 // in order here, the slices by k_block_grad_join).
@@ -29,8 +30,10 @@ __device__ __forceinline__ piece8 read_transposed(const uint8_t* p) {
 template <class TA, bool TRANS, int PA, int PB, int KS, class TC>
 __global__ __launch_bounds__(256 * KS) void k_block_grad(int64_t M, int64_t N, int64_t Kc, const TA* __restrict__ a, int64_t lda, BlockView b,
                                                          TC* __restrict__ c, int64_t ldc, int32_t tiles_m, int32_t tiles_n, int32_t slices,
-                                                         float* __restrict__ part) {
+                                                         float* __restrict__ part, int64_t plane) {
     constexpr int STAGE = (PA + PB) * 8192;
+    constexpr bool LAID = sizeof(TA) == 2 && PA > 1;
+    constexpr int RA = LAID ? PA : 1;
     extern __shared__ __align__(16) uint8_t lds_all[];
     const int tid = threadIdx.x & 255, lane = tid & 63;
     const int group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -45,38 +48,49 @@ __global__ __launch_bounds__(256 * KS) void k_block_grad(int64_t M, int64_t N, i
 
     const int row = tid >> 3, col = (tid & 7) * 8;   // rows row, row + 32 of a step, 8 columns
     struct Step {
-        Raw8<TA> a[2];
+        Raw8<TA> a[2][RA];
         Raw8<uint8_t> b[2];
         uint32_t s[2];
     };
     // Whole steps of rows of 8 numbers and more, and what is addressed number by number: the last step, short rows.
-    const bool short_rows = (TRANS ? M : Kc) < 8 || N < 8;
-    const int full = short_rows ? 0 : (int)(Kc >> 6), lastw = max(full - 1, 0);
-    const int a_cut = TRANS ? (int)((m0 + col) - min(m0 + col, M - 8)) : 0, b_cut = (int)((n0 + col) - min(n0 + col, N - 8));    // as raw_settle's `moved`
+    const bool short_rows = (!LAID && (TRANS ? M : Kc) < 8) || N < 8;
+    const int full = short_rows ? 0 : LAID ? nb : (int)(Kc >> 6), lastw = max(full - 1, 0);
+    const int a_cut = TRANS && !LAID ? (int)((m0 + col) - min(m0 + col, M - 8)) : 0, b_cut = (int)((n0 + col) - min(n0 + col, N - 8));    // as raw_settle's `moved`
     const int64_t blk = (min(n0 + col, N - 1) >> 7) * b.sblk;
     const TA* ap[2];
     const uint8_t* bp[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        ap[u] = TRANS ? a + (row + 32 * u) * lda + (m0 + col - a_cut) : a + min(m0 + row + 32 * u, M - 1) * lda + col;
-        bp[u] = b.codes + (row + 32 * u) * b.ld + (n0 + col - b_cut);
+        ap[u] = TRANS ? a + (row + 32 * u) * lda + (m0 + col - a_cut) : a + (LAID ? m0 + row + 32 * u : min(m0 + row + 32 * u, M - 1)) * lda + col;
+        bp[u] = b.codes + (LAID ? 0 : (row + 32 * u) * b.ld) + (n0 + col - b_cut);
     }
     const int64_t a_step = TRANS ? 64 * lda : 64, b_step = 64 * b.ld;
     auto scale_place = [&](int k) __attribute__((always_inline)) { return (int64_t)(k >> b.shift) * b.srow + blk; };
+    auto request_a = [&](Step& r, int u, int kb) __attribute__((always_inline)) {
+#pragma unroll
+        for (int p = 0; p < RA; ++p) r.a[u][p].load(ap[u] + kb * a_step + p * plane);
+    };
     auto request = [&](Step& r, int kb) __attribute__((always_inline)) {      // a whole step
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            r.a[u].load(ap[u] + kb * a_step);
-            r.b[u].load(bp[u] + kb * b_step);
-            r.s[u] = *scale_word(b, scale_place(kb * 64 + row + 32 * u));
+            request_a(r, u, kb);
+            if constexpr (LAID) {                    // rows past the last meet zeros of `a`: the last again
+                const int k = min(kb * 64 + row + 32 * u, (int)Kc - 1);
+                r.b[u].load(bp[u] + k * b.ld);
+                r.s[u] = *scale_word(b, scale_place(k));
+            } else {
+                r.b[u].load(bp[u] + kb * b_step);
+                r.s[u] = *scale_word(b, scale_place(kb * 64 + row + 32 * u));
+            }
         }
     };
     auto request_slow = [&](Step& r, int kb) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int64_t k = min(kb * 64ll + row + 32 * u, Kc - 1);
-            if (TRANS) raw_request(r.a[u], a + k * lda, m0 + col, M);
-            else raw_request(r.a[u], a + min(m0 + row + 32 * u, M - 1) * lda, kb * 64ll + col, Kc);
+            if (LAID) request_a(r, u, kb);
+            else if (TRANS) raw_request(r.a[u][0], a + k * lda, m0 + col, M);
+            else raw_request(r.a[u][0], a + min(m0 + row + 32 * u, M - 1) * lda, kb * 64ll + col, Kc);
             raw_request(r.b[u], (const uint8_t*)b.codes + k * b.ld, n0 + col, N);
             r.s[u] = *scale_word(b, scale_place((int)k));
         }
@@ -87,16 +101,18 @@ __global__ __launch_bounds__(256 * KS) void k_block_grad(int64_t M, int64_t N, i
             const int64_t k = kb * 64ll + row + 32 * u;
             if (!slow) {
                 if (TRANS && a_cut > 0) {
-                    if (a_cut >= 8) r.a[u] = Raw8<TA>{};
-                    else r.a[u].right(a_cut);
+                    if (a_cut >= 8) r.a[u][0] = Raw8<TA>{};
+                    else r.a[u][0].right(a_cut);
                 }
                 if (b_cut > 0) {
                     if (b_cut >= 8) r.b[u] = Raw8<uint8_t>{};
                     else r.b[u].right(b_cut);
                 }
             } else {
-                if (TRANS) raw_settle(r.a[u], m0 + col, M, k < Kc);
-                else raw_settle(r.a[u], kb * 64ll + col, Kc, true);
+                if (!LAID) {
+                    if (TRANS) raw_settle(r.a[u][0], m0 + col, M, k < Kc);
+                    else raw_settle(r.a[u][0], kb * 64ll + col, Kc, true);
+                }
                 raw_settle(r.b[u], n0 + col, N, k < Kc);
             }
             const uint32_t sbits = word_bits(b, scale_place((int)min(k, Kc - 1)), r.s[u]);
@@ -104,18 +120,21 @@ __global__ __launch_bounds__(256 * KS) void k_block_grad(int64_t M, int64_t N, i
             uint8_t* pa = lds + stage * STAGE + rr * 128 + (((tid & 7) ^ (TRANS ? (rr & 3) << 1 : rr & 7)) << 4);
             uint8_t* pb = lds + stage * STAGE + PA * 8192 + rr * 128 + (((tid & 7) ^ ((rr & 3) << 1)) << 4);
             if constexpr (PA == 1) {
-                *reinterpret_cast<piece16*>(pa) = r.a[u].v;
+                *reinterpret_cast<piece16*>(pa) = r.a[u][0].v;
+            } else if constexpr (LAID) {
+#pragma unroll
+                for (int i = 0; i < PA; ++i) *reinterpret_cast<piece16*>(pa + i * 8192) = r.a[u][PA - 1 - i].v;
             } else {
                 float v[8];
                 piece16 w[3];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = r.a[u].get(e);
+                for (int e = 0; e < 8; ++e) v[e] = r.a[u][0].get(e);
                 split8<3>(v, w);
 #pragma unroll
                 for (int i = 0; i < 3; ++i) *reinterpret_cast<piece16*>(pa + i * 8192) = w[i];
             }
             if constexpr (PB == 1) {                 // exponents: exact
-                *reinterpret_cast<bf16x8_t*>(pb) = scaled8((int)r.b[u].v[0], (int)r.b[u].v[1], b.e8m0 ? (k < Kc ? sbits : 127u) : 127u);
+                *reinterpret_cast<bf16x8_t*>(pb) = scaled8((int)r.b[u].v[0], (int)r.b[u].v[1], b.e8m0 ? (LAID || k < Kc ? sbits : 127u) : 127u);
             } else {
                 float v[8];
                 piece16 w[3];
@@ -508,8 +527,8 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
 template <class T, int PARTS, int BY>
 __global__ __launch_bounds__(256) void k_block_lay_gradient(int64_t rows, int64_t cols, const T* __restrict__ dy, int64_t ld, BlockView b,
                                                             uint16_t* __restrict__ out, int64_t Tp, int64_t Op) {
-    const int64_t i = blockIdx.x * 256ll + threadIdx.x, chunks = Op >> 3, row = i / chunks, col = (i - row * chunks) * 8;
-    if (row >= Tp) return;
+    const int64_t row = blockIdx.x * 4ll + (threadIdx.x >> 6), col = (blockIdx.y * 64ll + (threadIdx.x & 63)) * 8;
+    if (col >= Op) return;
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (row < rows && col < cols) load8(dy + row * ld, col, cols, v);
     if constexpr (BY != 0) {
@@ -612,6 +631,15 @@ static bool large_tiles(int64_t M, int64_t N, int64_t Kc, int parts, double lay_
     return large < small;
 }
 static int64_t up(int64_t n, int64_t to) { return ceil_div(n, to) * to; }
+// Small tiles of 32-bit gradients: dy laid out in parts first (once for dx and dw), or cut by every workgroup?  With a scale per row
+// always, as the scales go into dy and three products are left of six (2707 x 975 x 671, dx: 47 us against 83).  Exponents:
+// where the kernel's last step is a part of one (777 x 1365 x 1003: 55 us against 62; 1400 x 1403 x 1100 79 and 89; but 64^3 23
+// and 20), or the product is large (1500 x 1024 x 1024 63 and 62, 1024^3 43 and 41).
+static size_t lay_small_bytes(int64_t T, int64_t O) { return T >= 64 && O >= 64 ? (size_t)(3 * up(T, 128) * up(O, 128) * 2) : 0; }
+static bool lay_small(int64_t T, int64_t O, int64_t K, bool exact) {
+    const double work = (double)T * (double)O * (double)K;
+    return lay_small_bytes(T, O) > 0 && (!exact || (work >= 5e7 && (T % 64 || O % 64)) || work >= 1.6e9);
+}
 // dy laid out (three parts at most), then the codes of w or x
 static size_t lay_bytes(int64_t T, int64_t O, int64_t K) {
     const double lay = 2.0 * T * O;
@@ -624,24 +652,33 @@ static size_t lay_bytes(int64_t T, int64_t O, int64_t K) {
 static size_t backward_workspace(int64_t T, int64_t O, int64_t K) {
     if (T <= 0 || O <= 0) return 0;
     size_t n = ((size_t)bias_strips(T, O) * O * 4 + 255) / 256 * 256;
-    const size_t gx = grad_part_bytes(T, K, O), gw = grad_part_bytes(O, K, T), lay = K > 0 ? (lay_bytes(T, O, K) + 255) / 256 * 256 : 0;
+    const size_t small = lay_small_bytes(T, O), gx = small + grad_part_bytes(T, K, O), gw = small + grad_part_bytes(O, K, T), lay = K > 0 ? (lay_bytes(T, O, K) + 255) / 256 * 256 : 0;
     if (gx > n) n = gx;
     if (gw > n) n = gw;
     return lay > n ? lay : n;
 }
 
 template <class TA, bool TRANS, int PA, int PB, class TC>
-static dmmv_status grad_any(int64_t M, int64_t N, int64_t Kc, const TA* a, int64_t lda, const dmmv_block_matrix* b, TC* c, int64_t ldc,
-                            float* part, hipStream_t s) {
-    constexpr int KS = PA + PB <= 4 ? 2 : 1, bytes = KS * 2 * (PA + PB) * 8192;
+static dmmv_status grad_any(int64_t M, int64_t N, int64_t Kc, const TA* a, int64_t lda, const BlockView& b, TC* c, int64_t ldc,
+                            float* part, hipStream_t s, int64_t plane = 0) {
     const int64_t tiles_m = ceil_div(M, 64), tiles_n = ceil_div(N, 64);
     const int32_t slices = grad_slices(M, N, Kc);
     if (tiles_m > INT32_MAX / 4 / tiles_n) return fail(DMMV_ERR_SHAPE, "gradient: more tiles than a launch takes");
-    const void* kern = (const void*)k_block_grad<TA, TRANS, PA, PB, KS, TC>;
-    DMMV_TRY(ensure_dynamic_lds(kern, bytes));
-    hipLaunchKernelGGL((k_block_grad<TA, TRANS, PA, PB, KS, TC>), dim3((unsigned)(tiles_m * tiles_n * slices)), dim3(256 * KS), bytes, s, M, N, Kc,
-                       a, lda, layer_view(b), c, ldc, (int32_t)tiles_m, (int32_t)tiles_n, slices, part);
-    DMMV_LAUNCH_CHECK();
+    auto launch = [&](auto groups) {
+        constexpr int KS = decltype(groups)::value, bytes = KS * 2 * (PA + PB) * 8192;
+        DMMV_TRY(ensure_dynamic_lds((const void*)k_block_grad<TA, TRANS, PA, PB, KS, TC>, bytes));
+        hipLaunchKernelGGL((k_block_grad<TA, TRANS, PA, PB, KS, TC>), dim3((unsigned)(tiles_m * tiles_n * slices)), dim3(256 * KS), bytes, s, M, N,
+                           Kc, a, lda, b, c, ldc, (int32_t)tiles_m, (int32_t)tiles_n, slices, part, plane);
+        DMMV_LAUNCH_CHECK();
+        return DMMV_OK;
+    };
+    // Two groups a workgroup (one workgroup a compute unit) where the tiles are no more than the compute units, else two
+    // workgroups of one group (three parts, 396 tiles of 13 steps: 24.6 us against 35.5).
+    if (PA + PB <= 4 && tiles_m * tiles_n <= 256) {
+        if constexpr (PA + PB <= 4) DMMV_TRY(launch(std::integral_constant<int, 2>{}));
+    } else {
+        DMMV_TRY(launch(std::integral_constant<int, 1>{}));
+    }
     if (slices > 1) {
         hipLaunchKernelGGL((k_block_grad_join<TC>), dim3((unsigned)ceil_div(M * N, 256)), dim3(256), 0, s, M, N, slices, part, c, ldc);
         DMMV_LAUNCH_CHECK();
@@ -664,7 +701,7 @@ static dmmv_status grad_tiled(int64_t M, int64_t N, int64_t Kc, const bf16_t* a,
 template <class TA, int PARTS, int BY>
 static dmmv_status lay_gradient(int64_t T, int64_t O, const TA* dy, int64_t ld, const BlockView& b, uint16_t* out, hipStream_t s) {
     const int64_t Tp = up(T, 128), Op = up(O, 128);
-    hipLaunchKernelGGL((k_block_lay_gradient<TA, PARTS, BY>), dim3((unsigned)ceil_div(Tp * (Op / 8), 256)), dim3(256), 0, s, T, O, dy, ld, b, out, Tp, Op);
+    hipLaunchKernelGGL((k_block_lay_gradient<TA, PARTS, BY>), dim3((unsigned)(Tp / 4), (unsigned)ceil_div(Op, 512)), dim3(256), 0, s, T, O, dy, ld, b, out, Tp, Op);
     DMMV_LAUNCH_CHECK();
     return DMMV_OK;
 }
@@ -688,20 +725,22 @@ static dmmv_status grad(int64_t T, int64_t O, int64_t K, const TA* dy, int64_t l
     const bool rowwise = !exact && (b->scale_block_stride == 0 || K <= 128);
     const int parts = PA == 3 ? 3 : exact ? 1 : sizeof(TC) == 2 ? 2 : 3;
     const int64_t Tp = up(T, 128), Op = up(O, 128);
-    if ((exact ? near : rowwise) && K < 1 << 22 && Op < 1 << 22 && Tp * Op / 8 / 256 < INT32_MAX && Kc > 0 &&
-        large_tiles(M, K, Kc, parts, 2.0 * T * O) && large_tiles(M, K, Kc, parts == 1 ? 1 : 3, 2.0 * T * O)) {
-        uint16_t* lay = reinterpret_cast<uint16_t*>(ws);
-        BlockView v = layer_view(b);
+    uint16_t* lay = reinterpret_cast<uint16_t*>(ws);
+    BlockView v = layer_view(b);
+    // dy in parts, at the workspace's start; scales that are the same along a row go into it
+    auto lay_out = [&]() {
         constexpr int BY = TRANS ? 2 : 1;
-        if (exact) {
-            if (!*laid) DMMV_TRY((lay_gradient<TA, PA, 0>(T, O, dy, ld, v, lay, s)));
-            *laid = true;
-        } else {
-            *laid = false;
-            if (parts == 2) DMMV_TRY((lay_gradient<TA, 2, BY>(T, O, dy, ld, v, lay, s)));
-            else DMMV_TRY((lay_gradient<TA, 3, BY>(T, O, dy, ld, v, lay, s)));
-            v.scales = nullptr;                      // they are in dy now
-        }
+        if (exact && *laid) return DMMV_OK;
+        *laid = exact;
+        if (exact) return lay_gradient<TA, PA, 0>(T, O, dy, ld, v, lay, s);
+        BlockView by = v;
+        v.scales = nullptr;
+        if (parts == 2) return lay_gradient<TA, 2, BY>(T, O, dy, ld, by, lay, s);
+        return lay_gradient<TA, 3, BY>(T, O, dy, ld, by, lay, s);
+    };
+    const bool fits = K < 1 << 22 && Op < 1 << 22 && Tp / 4 < INT32_MAX && Kc > 0;
+    if ((exact ? near : rowwise) && fits && large_tiles(M, K, Kc, parts, 2.0 * T * O) && large_tiles(M, K, Kc, parts == 1 ? 1 : 3, 2.0 * T * O)) {
+        DMMV_TRY(lay_out());
         if (!codes_aligned) {
             const int64_t Kp = up(K, 16);
             uint8_t* to = reinterpret_cast<uint8_t*>(lay + (size_t)parts * Tp * Op);
@@ -711,10 +750,16 @@ static dmmv_status grad(int64_t T, int64_t O, int64_t K, const TA* dy, int64_t l
         }
         return grad_tiled<TRANS, TC>(M, K, TRANS ? Tp : Op, reinterpret_cast<const bf16_t*>(lay), Op, parts, Tp * Op, v, Kc, c, ldc, s);
     }
+    if constexpr (PA == 3)
+        if ((exact || rowwise) && fits && lay_small(T, O, K, exact)) {
+            DMMV_TRY(lay_out());
+            return grad_any<bf16_t, TRANS, 3, 1, TC>(M, K, Kc, reinterpret_cast<const bf16_t*>(lay), Op, v, c, ldc,
+                                                     reinterpret_cast<float*>(ws + lay_small_bytes(T, O)), s, Tp * Op);
+        }
     *laid = false;                                   // the slices go there
     float* part = reinterpret_cast<float*>(ws);
-    return exact ? grad_any<TA, TRANS, PA, 1, TC>(M, K, Kc, dy, ld, b, c, ldc, part, s)
-                 : grad_any<TA, TRANS, PA, 3, TC>(M, K, Kc, dy, ld, b, c, ldc, part, s);
+    return exact ? grad_any<TA, TRANS, PA, 1, TC>(M, K, Kc, dy, ld, v, c, ldc, part, s)
+                 : grad_any<TA, TRANS, PA, 3, TC>(M, K, Kc, dy, ld, v, c, ldc, part, s);
 }
 
 template <class T>

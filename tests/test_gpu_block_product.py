@@ -233,6 +233,41 @@ def test_large_gradients_laid_out_first(gpu_device, T, O, K, dtype):
         assert float((g.double() - want).norm()) <= (2e-6 + 1.01 * half_ulp(dt)) * float(want.norm())
 
 
+# small tiles of 32-bit gradients cut into parts beforehand: short rows, a part of a step, shares of the contraction, more tiles than
+# compute units, whole steps
+@pytest.mark.parametrize("T,O,K", [(64, 64, 3), (100, 70, 130), (65, 2050, 400), (2051, 66, 390), (777, 1365, 1003), (1601, 1024, 1000)])
+def test_small_gradients_laid_out_first(gpu_device, T, O, K):
+    from paper_2508_13437_amd import dmmv
+
+    for kx, kw in (("e8m0", "e8m0"), ("row", "row"), ("none", "row"), ("row", "e8m0")):
+        for integers in (True, False):
+            x = block(T, K, kx, T + O, gpu_device, integers=integers, g=1)
+            w = block(O, K, kw, K + O, gpu_device, integers=integers, g=128 if kw == "e8m0" else None)
+            dy = gradients(T, O, torch.float32, T + K, gpu_device, integers=integers, pad=1)
+            dx, dw, db = dmmv.dmmv_block_backward(dy, x, w)
+            X, W = (torch.from_numpy(vals(q)).to(gpu_device) for q in (x, w))
+            D = dy.double()
+            for g, want, size, n in ((dx, D @ W, D.abs() @ W.abs(), O), (dw, D.t() @ X, D.t().abs() @ X.abs(), T), (db, D.sum(0), D.abs().sum(0), T)):
+                if integers:
+                    assert torch.equal(g.double(), want)
+                else:
+                    assert bool(((g.double() - want).abs() <= (n + 12) * 2 * U * size + U * 1.01 * want.abs()).all())
+    # what is not finite stays in its rows and columns
+    x, w = block(T, K, "e8m0", 5, gpu_device, g=1), block(O, K, "row", 6, gpu_device)
+    w.codes.view(torch.uint8)[O - 1, 1] = 0x7F
+    x.codes.view(torch.uint8)[T - 1, 2] = 0x7F
+    dy = gradients(T, O, torch.float32, 7, gpu_device)
+    dy[3, 5] = float("inf")
+    dx, dw, db = dmmv.dmmv_block_backward(dy, x, w)
+    bad = torch.zeros(T, K, dtype=torch.bool, device=gpu_device)
+    bad[:, 1] = bad[3, :] = True
+    assert torch.equal(~torch.isfinite(dx), bad)
+    bad = torch.zeros(O, K, dtype=torch.bool, device=gpu_device)
+    bad[:, 2] = bad[5, :] = True
+    assert torch.equal(~torch.isfinite(dw), bad)
+    assert torch.isinf(db[5]) and torch.isfinite(db).sum() == O - 1
+
+
 def test_gradient_against_differences(gpu_device):
     """sum(dy * product) moves by dx (dw) times the scale when one integer code moves by one: exactly."""
     from paper_2508_13437_amd import dmmv
