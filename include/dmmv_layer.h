@@ -27,8 +27,8 @@
  * all work enqueued on the given hipStream_t (NULL = the default stream) without waiting, statuses
  * and dmmv_last_error().  Matrices are row-major with a row stride >= the columns, any alignment
  * their element type allows; 16-byte aligned rows are the fast ones.  Inputs and outputs do not
- * overlap.  Empty matrices are allowed.  Sums are held in 32 bits, in an order that the sizes alone
- * fix: equal calls give equal bits.  NaN and infinities of the inputs stay visible in what depends on them.
+ * overlap.  Empty matrices are allowed.  Sums are held in 32 bits, in an order that sizes, types and
+ * alignments fix: equal calls give equal bits.  NaN and infinities of the inputs stay visible in what depends on them.
  */
 #ifndef DMMV_LAYER_H
 #define DMMV_LAYER_H

@@ -117,6 +117,7 @@ __global__ __launch_bounds__(256) void k_block_quantize_tiles(int64_t rows, int6
     if (threadIdx.x == 0) scale_put(q, br, blk, b);
 }
 
+// 8 columns a lane, values are exact in 32 bits and rounded once.  11008 x 4096: to bf16 22.5 us (6.0 TB/s), to 32 bits 34 (6.6).
 template <class T>
 __global__ __launch_bounds__(256) void k_block_dequantize(int64_t rows, int64_t cols, int64_t chunks, BlockView q,
                                                           T* __restrict__ x, int64_t ldx) {

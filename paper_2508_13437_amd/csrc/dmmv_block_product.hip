@@ -67,6 +67,9 @@ __device__ __forceinline__ intx8 words8(piece16 a, piece16 b) {
 //   nor the 8 rows that are read together meet in a bank.
 // SCALED: power-of-two scales go into the instruction (8 bits) or the conversion to bf16 (32-bit results); scales that are
 // the same along a row are left to the end.  Otherwise a block's sum is multiplied by its two scales in 32 bits.
+// Bound by the vector unit (conversions to 16 bits, sums of blocks) and by the waits of four wavefronts in step: 4096 x 11008 x 4096 in
+// 32 bits 514 us, 0.72 PFLOP/s, with 32-bit scales per block 602; 500 x 1777 x 2731 in 32 bits 20 us.  Tiles of 64 x 64 keep the chip
+// full at such sizes (224 tiles); larger ones would leave most of it idle.
 struct ProductScales {
     int32_t x_blocks, w_blocks;         // SCALED: exponents per block, else constant along the row
 };
@@ -238,6 +241,9 @@ __global__ __launch_bounds__(256) void k_block_product(int64_t T_, int64_t O, in
 // codes go straight from memory into the LDS (NST stages of one block of 128), and the loop is written so that the matrix
 // unit has a product at all times: what else there is to do is placed in the products' shadows by hand.
 // WTILE: the scales of w are the same for 128 rows, or for a whole row.
+// 256 x 256 tiles, 128 x 128 a wavefront: 64 products a step from 16 + 16 fragments, which the LDS can deliver beside the requests;
+// smaller tiles are bound by it.  4096 x 11008 x 4096: 157 us, 2.35 PFLOP/s, the matrix unit busy for 53 % of the
+// cycles; 688 tiles are 2.7 rounds of the chip (256 tiles of K = 11008: 131 us, 2.8 PFLOP/s), the clock falls under this load.
 // exponents of `blocks` blocks from kb on for `rows` rows (or groups of `per` rows) of a tile, to bytes of the LDS
 __device__ __forceinline__ void stage_exponents(const BlockView& q, int64_t row0, int64_t last, int per, int rows, int kb, int blocks,
                                                 uint8_t* to, int stride) {
@@ -506,7 +512,8 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
 // Up to 64 tokens: the weights are read once, straight into registers in the order of the operands (a lane 32 codes of
 // a row and block, 128 bytes of a row side by side), and nothing else counts.  A workgroup has 16 outputs and
 // 16 MT tokens, its four wavefronts a share of the blocks each, joined in order through the LDS.  U blocks are
-// requested at a time.
+// requested at a time.  One token of 4096 by 11008 outputs: 10.5 us, 4.3 TB/s; 24 tokens of 4096 by 4096: 9.9 us, two thirds of it start,
+// join and end (eight wavefronts a workgroup were no faster).
 template <class T, int MT, bool SCALED>
 __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
                                                                   const float* __restrict__ bias, T* __restrict__ y, int64_t ldy) {
@@ -682,9 +689,9 @@ static dmmv_status product_tiled(const dmmv_block_matrix* x, const dmmv_block_ma
     return launch_tiled<bf16_t, 4, 4, true, false, 4>(x, w, bias, y, ldy, s);
 }
 
-// Rows that are no multiple of 16 codes are laid out for the large tiles where the general kernel (0.4 to 0.55 PFLOP/s) would
-// take over some 30 us: 4096 x 4095 x 11008 225 us against 660, and the other way about 500 x 2731 x 1777 two launches
-// for 20 us.  Bytes, 0 = not.
+// Rows that are no multiple of 16 codes are laid out for the large tiles where the general kernel would
+// take over some 30 us: 4096 outputs of 4095 for 11008 tokens 225 us against 660, and the other way about 500 x 1777 x 2731 two launches
+// more for 20 us.  Bytes, 0 = not.
 static size_t product_workspace(int64_t T, int64_t O, int64_t K) {
     if (K % 16 == 0 || T <= 64 || ceil_div(K, 128) * 128 >= 1 << 23 || 2.0 * (double)T * (double)O * (double)K < 12e9) return 0;
     return (size_t)(T + O) * (size_t)(ceil_div(K, 128) * 128);
