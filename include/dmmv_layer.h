@@ -68,7 +68,7 @@ dmmv_status dmmv_block_dequantize(const dmmv_block_matrix* q, int32_t dtype, voi
  * DMMV_BF16, bias float [O] or NULL.  A 32-bit result is summed in 32 bits; a bf16 result by the 8-bit
  * matrix instructions, whose sums carry an error of about 5e-5 of the result's norm before the rounding
  * to bf16 (1.7e-3).  The workspace (size from the HOST function, 0 is possible, 256-byte aligned) holds the operands of a
- * large product once more where their rows are no multiples of 16 codes. */
+ * large product once more where their rows are no multiples of 16 codes, and partial sums where few tiles share a long contraction. */
 size_t dmmv_block_product_workspace_bytes(int64_t T, int64_t O, int64_t K);
 dmmv_status dmmv_block_product(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, int32_t dtype,
                                void* y, int64_t ldy, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -241,6 +241,7 @@ __global__ __launch_bounds__(256) void k_block_product(int64_t T_, int64_t O, in
 // codes go straight from memory into the LDS (NST stages of one block of 128), and the loop is written so that the matrix
 // unit has a product at all times: what else there is to do is placed in the products' shadows by hand.
 // WTILE: the scales of w are the same for 128 rows, or for a whole row.
+// T float: workgroup row y of the grid takes its share of the contraction, and y [share][T_][O] is joined by k_block_product_join.
 // 256 x 256 tiles, 128 x 128 a wavefront: 64 products a step from 16 + 16 fragments, which the LDS can deliver beside the requests;
 // smaller tiles are bound by it.  4096 x 11008 x 4096: 157 us, 2.35 PFLOP/s, the matrix unit busy for 53 % of the
 // cycles; 688 tiles are 2.7 rounds of the chip (256 tiles of K = 11008: 131 us, 2.8 PFLOP/s), the clock falls under this load.
@@ -280,6 +281,15 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
     int tile_t, tile_o;
     tile_of_workgroup(tiles_t, tiles_o, tile_t, tile_o);
     const int64_t t0 = (int64_t)tile_t * BM, o0 = (int64_t)tile_o * BN;
+    if constexpr (sizeof(T) == 4) {                  // everything of this share but the place of its results begins at block `from`
+        const int64_t share = ((K + 127) / 128 + gridDim.y - 1) / gridDim.y, from = share * blockIdx.y;
+        x.codes += from * 128;
+        w.codes += from * 128;
+        if (how.x_blocks) x.scales = static_cast<uint8_t*>(x.scales) + from * x.sblk;
+        if (how.w_blocks) w.scales = static_cast<uint8_t*>(w.scales) + from * w.sblk;
+        K = min(K - from * 128, share * 128);
+        y += (int64_t)blockIdx.y * T_ * O;
+    }
     const int nb = (int)((K + 127) >> 7);
 
     // One request brings 8 rows of a step (1 KB) from memory to the LDS, 16 bytes a lane in the order of the lanes:
@@ -662,22 +672,71 @@ static bool constant_rows(const dmmv_block_matrix* q) { return !q->scales || q->
 // rows that requests of 16 bytes can bring to the LDS, with offsets of 24 x 24 bits
 static bool aligned(const dmmv_block_matrix* q) { return q->ld < 1 << 23 && q->ld % 16 == 0 && (uintptr_t)q->codes % 16 == 0; }
 
+// y = bias and the sum of the shares, by ascending share; 8 outputs a lane
+__global__ __launch_bounds__(256) void k_block_product_join(int64_t T_, int64_t O, int32_t shares, const float* __restrict__ part,
+                                                            const float* __restrict__ bias, bf16_t* __restrict__ y, int64_t ldy) {
+    const int64_t t = blockIdx.x * 4ll + (threadIdx.x >> 6), o = (blockIdx.y * 64ll + (threadIdx.x & 63)) * 8;
+    if (t >= T_ || o >= O) return;
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, p[8];
+#pragma unroll 4
+    for (int i = 0; i < shares; ++i) {
+        load8(part + (i * T_ + t) * O, o, O, p);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += p[e];
+    }
+    if (bias) {
+        load8(bias, o, O, p);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += p[e];
+    }
+    store8(y + t * ldy, o, O, v);
+}
+
 template <class T, int MI, int NI, bool SCALED, bool WTILE, int NST>
-static dmmv_status launch_tiled(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, T* y, int64_t ldy, hipStream_t s) {
+static dmmv_status launch_tiled(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, T* y, int64_t ldy, hipStream_t s,
+                                int32_t shares = 1) {
     const int64_t tiles_t = ceil_div(x->rows, 32 * MI), tiles_o = ceil_div(w->rows, 32 * NI);
     if (tiles_t > INT32_MAX / 4 / tiles_o) return fail(DMMV_ERR_SHAPE, "y: more tiles than a launch takes");
     const void* kern = (const void*)k_block_product_tiled<T, MI, NI, SCALED, WTILE, NST>;
     constexpr int bytes = product_lds(MI, NI, sizeof(T), WTILE, NST);
     DMMV_TRY(ensure_dynamic_lds(kern, bytes));
     const ProductScales how = {!constant_rows(x), !constant_rows(w)};
-    hipLaunchKernelGGL((k_block_product_tiled<T, MI, NI, SCALED, WTILE, NST>), dim3((unsigned)(tiles_t * tiles_o)), dim3(256), bytes, s, x->rows, w->rows,
+    hipLaunchKernelGGL((k_block_product_tiled<T, MI, NI, SCALED, WTILE, NST>), dim3((unsigned)(tiles_t * tiles_o), (unsigned)shares), dim3(256), bytes, s, x->rows, w->rows,
                        x->cols, layer_view(x), layer_view(w), how, bias, y, ldy, (int32_t)tiles_t, (int32_t)tiles_o);
     DMMV_LAUNCH_CHECK();
     return DMMV_OK;
 }
 
-// bf16 results by the large tiles: 256 x 256, or 128 x 128 with more stages
-static dmmv_status product_tiled(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, bf16_t* y, int64_t ldy, hipStream_t s) {
+// Shares of the contraction where tiles of 128 x 128 are fewer than the compute units, by the time that a step of
+// a tile takes (0.4 us), the second launch and the parts, written and read once.  33 x 4096 x 11008: 21 us with eight shares, 34 with
+// one (the weights alone are 9 us); 33 x 1024 x 4096 12.3 and 15.8, 128 x 4096 x 11008 25 and 36.
+static int32_t product_shares(int64_t T, int64_t O, int64_t K) {
+    const int64_t tiles = ceil_div(T, 128) * ceil_div(O, 128), nb = ceil_div(K, 128);
+    if (tiles <= 0 || tiles > 128) return 1;
+    int32_t best = 1;
+    double least = 0.4 * nb;
+    for (int64_t n = 2; n * tiles <= 256 && 2 * n <= nb; ++n) {
+        const double us = 0.4 * ceil_div(nb, n) + 5.0 + 8.0 * n * T * O / 4e6;
+        if (us < least && (n - 1) * ceil_div(nb, n) < nb) least = us, best = (int32_t)n;         // (every share has a block)
+    }
+    return best;
+}
+static size_t product_part_bytes(int64_t T, int64_t O, int64_t K) {
+    const int32_t n = product_shares(T, O, K);
+    return n > 1 ? (size_t)n * T * O * 4 : 0;
+}
+
+// bf16 results by the large tiles: 256 x 256, or 128 x 128 with more stages; part: room for the shares, or NULL
+static dmmv_status product_tiled(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, bf16_t* y, int64_t ldy, float* part,
+                                 hipStream_t s) {
+    const int32_t shares = part ? product_shares(x->rows, w->rows, x->cols) : 1;
+    if (shares > 1) {
+        DMMV_TRY((launch_tiled<float, 4, 4, true, false, 4>(x, w, nullptr, part, w->rows, s, shares)));
+        hipLaunchKernelGGL(k_block_product_join, dim3((unsigned)ceil_div(x->rows, 4), (unsigned)ceil_div(w->rows, 512)), dim3(256), 0, s, x->rows,
+                           w->rows, shares, part, bias, y, ldy);
+        DMMV_LAUNCH_CHECK();
+        return DMMV_OK;
+    }
     const bool wtile = constant_rows(w) || w->scale_rows == 128;
     int dev = 0, cus = 0;
     DMMV_HIP_CHECK(hipGetDevice(&dev));
@@ -692,28 +751,37 @@ static dmmv_status product_tiled(const dmmv_block_matrix* x, const dmmv_block_ma
 // Rows that are no multiple of 16 codes are laid out for the large tiles where the general kernel would
 // take over some 30 us: 4096 outputs of 4095 for 11008 tokens 225 us against 660, and the other way about 500 x 1777 x 2731 two launches
 // more for 20 us.  Bytes, 0 = not.
-static size_t product_workspace(int64_t T, int64_t O, int64_t K) {
+static size_t product_lay_bytes(int64_t T, int64_t O, int64_t K) {
     if (K % 16 == 0 || T <= 64 || ceil_div(K, 128) * 128 >= 1 << 23 || 2.0 * (double)T * (double)O * (double)K < 12e9) return 0;
     return (size_t)(T + O) * (size_t)(ceil_div(K, 128) * 128);
+}
+static bool product_shared(int64_t T, int64_t K, size_t lay) { return lay > 0 || (K % 16 == 0 && T > 32); }
+static size_t product_workspace(int64_t T, int64_t O, int64_t K) {
+    const size_t lay = (product_lay_bytes(T, O, K) + 255) / 256 * 256;
+    return lay + (product_shared(T, K, lay) ? product_part_bytes(T, O, K) : 0);
 }
 
 template <class T>
 static dmmv_status product(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, T* y, int64_t ldy, void* ws, hipStream_t s) {
     const ProductScales how = {!constant_rows(x), !constant_rows(w)};
     const bool scaled = (constant_rows(x) || x->scale_type == DMMV_E8M0) && (constant_rows(w) || w->scale_type == DMMV_E8M0);
-    // Few tokens (4096 x 4096, then 4096 x 11008, us): 16 tokens 9.2 by registers and 16.3 by tiles, 32: 10.6 and 16.3, 64: 16.4 and
-    // 16.3, 40.5 and 16.9; where the large tiles do not apply, 64 (32 bits): 17.4 and 19.3, 128: 32.5 and 20.
+    // Few tokens, us by registers and by tiles (T x O x K): 32 x 4096 x 4096 9.9 and 12.7, 24 x 8192 x 4096 15.3 and 16.1, 32 x 8192 x 4096
+    // 17.5 and 16.1, 24 x 11008 x 4096 21 and 16.5, 24 x 8192 x 8192 27.5 and 26; 64 x 4096 x 4096 16.4 and 13.8; where the large tiles
+    // do not apply, 64 (32 bits): 17.4 and 19.3, 128: 32.5 and 20.
     const bool tiles = sizeof(T) == 2 && scaled && aligned(x) && aligned(w);
-    if (x->rows <= (tiles ? 32 : 64)) return launch_few(x, w, how, scaled, bias, y, ldy, s);
-    if (tiles) return product_tiled(x, w, bias, reinterpret_cast<bf16_t*>(y), ldy, s);
-    if (sizeof(T) == 2 && scaled && product_workspace(x->rows, w->rows, x->cols) > 0) {
+    const bool wide = x->rows > 16 && w->rows >= 8192 && (double)x->rows * (double)w->rows * (double)x->cols >= 9e8;
+    if (x->rows <= (!tiles ? 64 : wide ? 16 : 32)) return launch_few(x, w, how, scaled, bias, y, ldy, s);
+    const size_t lay = product_lay_bytes(x->rows, w->rows, x->cols);
+    float* part = product_shared(x->rows, x->cols, lay) ? reinterpret_cast<float*>(static_cast<char*>(ws) + (lay + 255) / 256 * 256) : nullptr;
+    if (tiles) return product_tiled(x, w, bias, reinterpret_cast<bf16_t*>(y), ldy, part, s);
+    if (sizeof(T) == 2 && scaled && lay > 0) {
         dmmv_block_matrix lx = *x, lw = *w;
         lx.ld = lw.ld = ceil_div(x->cols, 128) * 128;
         lx.codes = ws;
         lw.codes = static_cast<uint8_t*>(ws) + x->rows * lx.ld;
         DMMV_TRY(layer_lay_codes(x, static_cast<uint8_t*>(lx.codes), lx.ld, s));
         DMMV_TRY(layer_lay_codes(w, static_cast<uint8_t*>(lw.codes), lw.ld, s));
-        return product_tiled(&lx, &lw, bias, reinterpret_cast<bf16_t*>(y), ldy, s);
+        return product_tiled(&lx, &lw, bias, reinterpret_cast<bf16_t*>(y), ldy, part, s);
     }
     const int64_t tiles_t = ceil_div(x->rows, 64), tiles_o = ceil_div(w->rows, 64);
     if (tiles_t > INT32_MAX / 4 / tiles_o) return fail(DMMV_ERR_SHAPE, "y: more tiles than a launch takes");

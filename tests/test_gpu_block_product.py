@@ -92,6 +92,36 @@ def test_large_products_of_integers_are_exact(gpu_device, T, O, K, kx, kw):
         assert torch.equal(dmmv.dmmv_block_product(x, w, bias, dtype=torch.bfloat16), (want + bias).to(torch.bfloat16))
 
 
+# few tiles and a long contraction, which workgroups share: a last share that is shorter, a last block that is not whole, more blocks
+# in a share than a table of exponents holds, rows laid out first; few tokens by tiles
+@pytest.mark.parametrize("kx,kw", [k for k in KINDS if "f32" not in k])
+@pytest.mark.parametrize("T,O,K", [(33, 100, 4112), (65, 1025, 3856), (200, 513, 8208), (40, 128, 80000), (120, 3000, 17001), (24, 11008, 3600)])
+def test_shared_contractions(gpu_device, T, O, K, kx, kw):
+    from paper_2508_13437_amd import dmmv
+
+    for g in (1, 128) if kw == "e8m0" else (None,):
+        x, w = block(T, K, kx, T + O, gpu_device), block(O, K, kw, K + O, gpu_device, g=g)
+        X, W = (torch.from_numpy(vals(q)).to(gpu_device) for q in (x, w))
+        bias = torch.randn(O, device=gpu_device)
+        for b in (bias, None):
+            got = dmmv.dmmv_block_product(x, w, b)
+            want, size = X @ W.t(), X.abs() @ W.abs().t()
+            if b is not None:
+                want, size = want + b.double(), size + b.double().abs()
+            e = (K + 8) * 2 * U * size + 2.0 ** -10 * size                       # as in test_product
+            assert bool(((got.double() - want).abs() <= e + half_ulp(torch.bfloat16) * 1.01 * (want.abs() + e)).all())
+            assert float((got.double() - want).norm()) <= (2e-6 + 1.01 * half_ulp(torch.bfloat16)) * float(want.norm()) + 1e-6 * float(size.norm()) / K ** 0.5
+            assert torch.equal(got, dmmv.dmmv_block_product(x, w, b))
+        if K > 40000:                                                            # (scales and codes that a sum in 32 bits holds exactly)
+            continue
+        x, w = block(T, K, kx, T + O, gpu_device, integers=True), block(O, K, kw, K + O, gpu_device, integers=True, g=g)
+        want = torch.from_numpy(vals(x)).to(gpu_device) @ torch.from_numpy(vals(w)).to(gpu_device).t()
+        assert torch.equal(dmmv.dmmv_block_product(x, w), want.to(torch.bfloat16))
+        x.codes.view(torch.uint8)[T - 1, K - 1] = 0x7F
+        got = dmmv.dmmv_block_product(x, w)
+        assert torch.isnan(got[T - 1]).all() and torch.equal(got[:T - 1], want[:T - 1].to(torch.bfloat16))
+
+
 @pytest.mark.parametrize("kx,kw", KINDS)
 @pytest.mark.parametrize("T,O,K", [s for s in SIZES if s[2] <= 4096])
 def test_product_of_integers_is_exact(gpu_device, T, O, K, kx, kw):
