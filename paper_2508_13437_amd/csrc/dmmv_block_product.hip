@@ -66,7 +66,8 @@ __device__ __forceinline__ intx8 words8(piece16 a, piece16 b) {
 //   LDS row: 128 codes, the 16-byte chunk c of row r at c ^ (r & 7): neither the 8 lanes that write a row
 //   nor the 8 rows that are read together meet in a bank.
 // SCALED: power-of-two scales go into the instruction (8 bits) or the conversion to bf16 (32-bit results); scales that are
-// the same along a row are left to the end.  Otherwise a block's sum is multiplied by its two scales in 32 bits.
+// the same along a row are left to the end.  Otherwise a block's sum is multiplied by its two scales in 32 bits, by one
+// after the other: their product may leave the range where the sum is 0.
 // Bound by the vector unit (conversions to 16 bits, sums of blocks) and by the waits of four wavefronts in step: 4096 x 11008 x 4096 in
 // 32 bits 514 us, 0.72 PFLOP/s, with 32-bit scales per block 602; 500 x 1777 x 2731 in 32 bits 20 us.  Tiles of 64 x 64 keep the chip
 // full at such sizes (224 tiles); larger ones would leave most of it idle.
@@ -177,7 +178,7 @@ __global__ __launch_bounds__(256) void k_block_product(int64_t T_, int64_t O, in
                 for (int j = 0; j < MI; ++j) {
                     const floatx4 p = block_sum<WIDE>(fw[i], fx[j]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[i][j][e] = dmmv_fma(p[e], sw[e] * sx[j], acc[i][j][e]);
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = dmmv_fma(p[e] * sw[e], sx[j], acc[i][j][e]);
                 }
             }
         }
@@ -231,7 +232,7 @@ __global__ __launch_bounds__(256) void k_block_product(int64_t T_, int64_t O, in
             const float st = SCALED && !how.x_blocks ? scale_at(x, t, 0) : 1.0f;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (o + e < O) put_y(y + t * ldy + o + e, dmmv_fma(acc[i][j][e], so[e] * st, bo[e]));
+                if (o + e < O) put_y(y + t * ldy + o + e, dmmv_fma(acc[i][j][e] * so[e], st, bo[e]));
         }
     }
 }
@@ -496,7 +497,7 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
             const float st = SCALED && !how.x_blocks ? scale_at(x, min(t0 + wt + 16 * j + lr, T_ - 1), 0) : 1.0f;
             float v[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = dmmv_fma(acc[i][j][e], so[e] * st, bo[e]);
+            for (int e = 0; e < 4; ++e) v[e] = dmmv_fma(acc[i][j][e] * so[e], st, bo[e]);
             put4(reinterpret_cast<T*>(lds + (wt + 16 * j + lr) * LDO) + wo + 16 * i + lg * 4, v);
         }
     }
@@ -586,10 +587,10 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
                     const float fx = e8m0_value(k.ex[m]);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        acc[m][e] = dmmv_fma(p[e], e8m0_value((uint32_t)__shfl((int)k.ew, lg * 4 + e, 64)) * fx, acc[m][e]);
+                        acc[m][e] = dmmv_fma(p[e] * e8m0_value((uint32_t)__shfl((int)k.ew, lg * 4 + e, 64)), fx, acc[m][e]);
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[m][e] = dmmv_fma(p[e], scale_of(w, k.fw[e]) * scale_of(x, k.fx[m]), acc[m][e]);
+                    for (int e = 0; e < 4; ++e) acc[m][e] = dmmv_fma(p[e] * scale_of(w, k.fw[e]), scale_of(x, k.fx[m]), acc[m][e]);
                 }
             }
         }
@@ -639,7 +640,7 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
             const int64_t o = o0 + lg * 4 + e;
             if (o >= O) continue;
             const float so = SCALED && !how.w_blocks ? scale_at(w, o, 0) : 1.0f;
-            put_y(y + t * ldy + o, dmmv_fma(v[e], so * st, bias ? bias[o] : 0.0f));
+            put_y(y + t * ldy + o, dmmv_fma(v[e] * so, st, bias ? bias[o] : 0.0f));
         }
     }
 }

@@ -148,6 +148,28 @@ def test_product_of_what_is_not_finite(gpu_device):
         assert np.array_equal(np.isnan(got), nan) and np.array_equal(got[~nan], want[~nan])
 
 
+@pytest.mark.parametrize("K", [256, 200])
+@pytest.mark.parametrize("T", [3, 40, 150])
+def test_zeros_times_large_scales(gpu_device, T, K):
+    """The scales' product is beyond the range, the rows and columns of zeros are not."""
+    from paper_2508_13437_amd import dmmv
+
+    g = torch.Generator().manual_seed(K)
+    codes = lambda rows: torch.randint(0x30, 0x40, (rows, K), generator=g, dtype=torch.uint8).to(gpu_device)
+    bias = torch.randn(80, generator=g).to(gpu_device)
+    byte, number = torch.full((1, 2), 227, dtype=torch.uint8, device=gpu_device), torch.full((1, 2), 2.0 ** 100, device=gpu_device)
+    x, w = codes(T), codes(80)
+    x[1], w[7] = 0, 0
+    for s in (byte, number):
+        for rows in (s.expand(-1, 2), s[:, :1].expand(-1, 2)):
+            a, b = dmmv.BlockMatrix(x, rows.expand(T, -1)), dmmv.BlockMatrix(w, rows.expand(80, -1).contiguous())
+            for p, q in ((a, b), (dmmv.BlockMatrix(x, rows.expand(T, -1).contiguous()), b)):
+                for dtype in (torch.float32, torch.bfloat16):
+                    y = dmmv.dmmv_block_product(p, q, bias, dtype)
+                    assert torch.equal(y[1], bias.to(dtype)) and torch.equal(y[:, 7], bias[7].to(dtype).expand(T))
+                    assert not torch.isfinite(y[0, :7]).any()
+
+
 def test_empty_products(gpu_device):
     from paper_2508_13437_amd import dmmv
 
