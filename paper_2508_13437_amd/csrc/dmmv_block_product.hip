@@ -244,7 +244,7 @@ __global__ __launch_bounds__(256) void k_block_product(int64_t T_, int64_t O, in
 // WTILE: the scales of w are the same for 128 rows, or for a whole row.
 // T float: workgroup row y of the grid takes its share of the contraction, and y [share][T_][O] is joined by k_block_product_join.
 // 256 x 256 tiles, 128 x 128 a wavefront: 64 products a step from 16 + 16 fragments, which the LDS can deliver beside the requests;
-// smaller tiles are bound by it.  4096 x 11008 x 4096: 157 us, 2.35 PFLOP/s, the matrix unit busy for 53 % of the
+// smaller tiles are bound by it.  4096 x 11008 x 4096: 157 to 166 us (2.2 to 2.35 PFLOP/s), the matrix unit busy for 53 % of the
 // cycles; 688 tiles are 2.7 rounds of the chip (256 tiles of K = 11008: 131 us, 2.8 PFLOP/s), the clock falls under this load.
 // exponents of `blocks` blocks from kb on for `rows` rows (or groups of `per` rows) of a tile, to bytes of the LDS
 __device__ __forceinline__ void stage_exponents(const BlockView& q, int64_t row0, int64_t last, int per, int rows, int kb, int blocks,
