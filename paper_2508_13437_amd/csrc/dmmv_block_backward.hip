@@ -743,7 +743,7 @@ static dmmv_status grad(int64_t T, int64_t O, int64_t K, const TA* dy, int64_t l
         if (parts == 2) return lay_gradient<TA, 2, BY>(T, O, dy, ld, by, lay, s);
         return lay_gradient<TA, 3, BY>(T, O, dy, ld, by, lay, s);
     };
-    const bool fits = K < 1 << 22 && Op < 1 << 22 && Tp / 4 < INT32_MAX && Kc > 0;
+    const bool fits = K < 1 << 22 && Op < 1 << 22 && Tp <= 1 << 25 && Kc > 0;
     if ((exact ? near : rowwise) && fits && large_tiles(M, K, Kc, parts, 2.0 * T * O) && large_tiles(M, K, Kc, parts == 1 ? 1 : 3, 2.0 * T * O)) {
         DMMV_TRY(lay_out());
         if (!codes_aligned) {
