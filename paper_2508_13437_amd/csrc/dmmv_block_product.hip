@@ -66,22 +66,27 @@ __device__ __forceinline__ intx8 words8(piece16 a, piece16 b) {
 //   LDS row: 128 codes, the 16-byte chunk c of row r at c ^ (r & 7): neither the 8 lanes that write a row
 //   nor the 8 rows that are read together meet in a bank.
 // SCALED: power-of-two scales go into the instruction (8 bits) or the conversion to bf16 (32-bit results); scales that are
-// the same along a row are left to the end.  Otherwise a block's sum is multiplied by its two scales in 32 bits, by one
-// after the other: their product may leave the range where the sum is 0.
+// the same along a row are left to the end.  Otherwise a block's sum is multiplied by the product of its two scales in 32 bits.  That is
+// right while all scales are moderate; where a tile has met others, its sums are made once more by add_scaled (a branch in the loop would cost
+// every product a fifth).
 // Bound by the vector unit (conversions to 16 bits, sums of blocks) and by the waits of four wavefronts in step: 4096 x 11008 x 4096 in
-// 32 bits 514 us, 0.72 PFLOP/s, with 32-bit scales per block 602; 500 x 1777 x 2731 in 32 bits 20 us.  Tiles of 64 x 64 keep the chip
+// 32 bits 490 to 514 us, 0.72 PFLOP/s, with 32-bit scales per block 570; 500 x 1777 x 2731 in 32 bits 20 us.  Tiles of 64 x 64 keep the chip
 // full at such sizes (224 tiles); larger ones would leave most of it idle.
 struct ProductScales {
     int32_t x_blocks, w_blocks;         // SCALED: exponents per block, else constant along the row
 };
 
-template <class T, bool SCALED>
-__global__ __launch_bounds__(256) void k_block_product(int64_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
+// WAVES: wavefronts a SIMD that the registers leave room for at least.  32-bit results with 32-bit scales have more than three allow: where a compute
+// unit gets one tile they stay (500 x 1777 x 2731 20.6 us, 21.5 with three), else not (4096 x 11008 x 4096 570 us, 650 without).
+template <class T, bool SCALED, int WAVES>
+__global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
                                                        const float* __restrict__ bias, T* __restrict__ y, int64_t ldy, int32_t tiles_t, int32_t tiles_o) {
     constexpr bool WIDE = sizeof(T) == 4;
     constexpr int MI = 2, NI = 2, BM = 32 * MI, BN = 32 * NI;
     __shared__ __align__(16) uint8_t codes[2][128 * (BM + BN)];
     __shared__ __align__(16) uint32_t scl[2][BM + BN];
+    __shared__ int again;                            // !SCALED: some scale is not moderate
+    if (!SCALED && threadIdx.x == 0) again = 0;      // (a barrier follows before it is set)
     const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wt = (wv & 1) * (16 * MI), wo = (wv >> 1) * (16 * NI);
@@ -118,20 +123,18 @@ __global__ __launch_bounds__(256) void k_block_product(int64_t T_, int64_t O, in
         for (int u = 0; u < NI; ++u) r.c[MI + u] = *reinterpret_cast<const piece16_any*>(wr[u] + kb * 128ll);
         r.s = *scale_word(sq, sat + kb * sblk);
     };
+    ScaleRange met;                                  // this thread's scales
     auto deposit = [&](const Step& r, int kb, int stage) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < MI + NI; ++u) *reinterpret_cast<piece16*>(&codes[stage][put + u * 4096]) = r.c[u];
         const uint32_t bits = word_bits(sq, sat + kb * sblk, r.s);
-        if (mine) scl[stage][tid] = !SCALED && sq.e8m0 ? __float_as_uint(e8m0_value(bits)) : bits;
+        const uint32_t s = !SCALED && sq.e8m0 ? __float_as_uint(e8m0_value(bits)) : bits;
+        if (mine) scl[stage][tid] = s;
+        if (!SCALED) met.take(__uint_as_float(s));
     };
     floatx4 acc[NI][MI];
-#pragma unroll
-    for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int j = 0; j < MI; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-
     const int c0 = (lg ^ (lr & 7)) << 4;
-    auto multiply = [&](int stage) __attribute__((always_inline)) {
+    auto multiply = [&](auto CAREFUL, int stage) __attribute__((always_inline)) {
         const uint8_t* px = &codes[stage][(wt + lr) * 128];
         const uint8_t* pw = &codes[stage][(BM + wo + lr) * 128];
         intx8 fx[MI], fw[NI];
@@ -178,7 +181,8 @@ __global__ __launch_bounds__(256) void k_block_product(int64_t T_, int64_t O, in
                 for (int j = 0; j < MI; ++j) {
                     const floatx4 p = block_sum<WIDE>(fw[i], fx[j]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[i][j][e] = dmmv_fma(p[e] * sw[e], sx[j], acc[i][j][e]);
+                    for (int e = 0; e < 4; ++e)
+                        acc[i][j][e] = CAREFUL.value ? add_scaled(p[e], sw[e], sx[j], acc[i][j][e]) : dmmv_fma(p[e], sw[e] * sx[j], acc[i][j][e]);
                 }
             }
         }
@@ -186,7 +190,26 @@ __global__ __launch_bounds__(256) void k_block_product(int64_t T_, int64_t O, in
     // The whole blocks.  Requests are made without a condition, or a use would wait for all of them; those past the end ask for
     // the last block again.
     const int full = (int)(K >> 7), most = full - 1;
+    auto clear = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+            for (int j = 0; j < MI; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    };
     Step r0, r1;
+    auto one = [&](auto CAREFUL, int kb) __attribute__((always_inline)) {     // any block, zeros past the row's end
+        const int64_t at = kb * 128ll;
+        const int left = (int)(K - at) - cchunk * 16;
+#pragma unroll
+        for (int u = 0; u < MI; ++u) r0.c[u] = chunk_tail(xr[u] + at, left, at + cchunk * 16);
+#pragma unroll
+        for (int u = 0; u < NI; ++u) r0.c[MI + u] = chunk_tail(wr[u] + at, left, at + cchunk * 16);
+        r0.s = *scale_word(sq, sat + kb * sblk);
+        deposit(r0, kb, 0);
+        __syncthreads();
+        multiply(CAREFUL, 0);
+    };
+    clear();
     if (full > 0) {
         request(r0, 0);
         request(r1, min(1, most));
@@ -196,25 +219,26 @@ __global__ __launch_bounds__(256) void k_block_product(int64_t T_, int64_t O, in
         for (int kb = 0; kb < full; kb += 2) {
             deposit(r1, min(kb + 1, most), 1);
             request(r1, min(kb + 3, most));
-            multiply(0);
+            multiply(std::false_type{}, 0);
             __syncthreads();
             deposit(r0, min(kb + 2, most), 0);
             request(r0, min(kb + 4, most));
-            if (kb + 1 < full) multiply(1);
+            if (kb + 1 < full) multiply(std::false_type{}, 1);
             __syncthreads();
         }
     }
-    if (full < nb) {                                 // the last block, zeros past the row's end
-        const int64_t at = full * 128ll;
-        const int left = (int)(K - at) - cchunk * 16;
-#pragma unroll
-        for (int u = 0; u < MI; ++u) r0.c[u] = chunk_tail(xr[u] + at, left, at + cchunk * 16);
-#pragma unroll
-        for (int u = 0; u < NI; ++u) r0.c[MI + u] = chunk_tail(wr[u] + at, left, at + cchunk * 16);
-        r0.s = *scale_word(sq, sat + full * sblk);
-        deposit(r0, full, 0);
+    if (full < nb) one(std::false_type{}, full);
+    if constexpr (!SCALED) {
+        if (!met.moderate()) again = 1;
         __syncthreads();
-        multiply(0);
+        if (again) {
+            clear();
+#pragma unroll 1
+            for (int kb = 0; kb < nb; ++kb) {
+                one(std::true_type{}, kb);
+                __syncthreads();
+            }
+        }
     }
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
@@ -546,8 +570,6 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
         xr[m] = x.codes + trow[m] * x.ld + lg * 32;
     }
     floatx4 acc[MT];
-#pragma unroll
-    for (int m = 0; m < MT; ++m) acc[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 
     // one block's codes and scales in registers
     struct Block {
@@ -574,7 +596,14 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
             for (int m = 0; m < MT; ++m) k.fx[m] = scale_bits(x, trow[m], b);
         }
     };
-    auto multiply = [&](const Block& k) __attribute__((always_inline)) {
+    ScaleRange met;                                  // as in the general kernel: this lane's scales
+    auto multiply = [&](auto CAREFUL, const Block& k) __attribute__((always_inline)) {
+        if constexpr (!SCALED) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) met.take(scale_of(w, k.fw[e]));
+#pragma unroll
+            for (int m = 0; m < MT; ++m) met.take(scale_of(x, k.fx[m]));
+        }
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             const intx8 a = words8(k.w[0], k.w[1]), b = words8(k.x[m][0], k.x[m][1]);
@@ -590,11 +619,28 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
                         acc[m][e] = dmmv_fma(p[e] * e8m0_value((uint32_t)__shfl((int)k.ew, lg * 4 + e, 64)), fx, acc[m][e]);
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[m][e] = dmmv_fma(p[e] * scale_of(w, k.fw[e]), scale_of(x, k.fx[m]), acc[m][e]);
+                    for (int e = 0; e < 4; ++e) {
+                        const float sw = scale_of(w, k.fw[e]), sx = scale_of(x, k.fx[m]);
+                        acc[m][e] = CAREFUL.value ? add_scaled(p[e], sw, sx, acc[m][e]) : dmmv_fma(p[e], sw * sx, acc[m][e]);
+                    }
                 }
             }
         }
     };
+    auto one = [&](auto CAREFUL, int b) __attribute__((always_inline)) {
+        Block k;
+        const int left = (int)min(K - b * 128ll, (int64_t)128) - lg * 32;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) k.w[h] = chunk_tail(wr + (int64_t)b * 128 + 16 * h, left - 16 * h, b * 128ll + lg * 32 + 16 * h);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) k.x[m][h] = chunk_tail(xr[m] + (int64_t)b * 128 + 16 * h, left - 16 * h, b * 128ll + lg * 32 + 16 * h);
+        scales(k, b);
+        multiply(CAREFUL, k);
+    };
+#pragma unroll
+    for (int m = 0; m < MT; ++m) acc[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
     int b = b0;
     for (; b + U <= b1 && b + U <= full; b += U) {
         Block k[U];
@@ -609,21 +655,17 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
             scales(k[u], b + u);
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) multiply(k[u]);
+        for (int u = 0; u < U; ++u) multiply(std::false_type{}, k[u]);
     }
 #pragma unroll 1
-    for (; b < b1; ++b) {
-        Block k;
-        const int left = (int)min(K - b * 128ll, (int64_t)128) - lg * 32;
+    for (; b < b1; ++b) one(std::false_type{}, b);
+    if constexpr (!SCALED)
+        if (!__all(met.moderate())) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) k.w[h] = chunk_tail(wr + (int64_t)b * 128 + 16 * h, left - 16 * h, b * 128ll + lg * 32 + 16 * h);
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) k.x[m][h] = chunk_tail(xr[m] + (int64_t)b * 128 + 16 * h, left - 16 * h, b * 128ll + lg * 32 + 16 * h);
-        scales(k, b);
-        multiply(k);
-    }
+            for (int m = 0; m < MT; ++m) acc[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+            for (b = b0; b < b1; ++b) one(std::true_type{}, b);
+        }
 #pragma unroll
     for (int m = 0; m < MT; ++m) part[wv][m][lane] = acc[m];
     __syncthreads();
@@ -787,12 +829,13 @@ static dmmv_status product(const dmmv_block_matrix* x, const dmmv_block_matrix* 
     const int64_t tiles_t = ceil_div(x->rows, 64), tiles_o = ceil_div(w->rows, 64);
     if (tiles_t > INT32_MAX / 4 / tiles_o) return fail(DMMV_ERR_SHAPE, "y: more tiles than a launch takes");
     const dim3 grid((unsigned)(tiles_t * tiles_o));
-    if (scaled)
-        hipLaunchKernelGGL((k_block_product<T, true>), grid, dim3(256), 0, s, x->rows, w->rows, x->cols, layer_view(x), layer_view(w), how, bias, y,
-                           ldy, (int32_t)tiles_t, (int32_t)tiles_o);
-    else
-        hipLaunchKernelGGL((k_block_product<T, false>), grid, dim3(256), 0, s, x->rows, w->rows, x->cols, layer_view(x), layer_view(w), how, bias, y,
-                           ldy, (int32_t)tiles_t, (int32_t)tiles_o);
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, x->rows, w->rows, x->cols, layer_view(x), layer_view(w), how, bias, y, ldy, (int32_t)tiles_t,
+                           (int32_t)tiles_o);
+    };
+    if (scaled) launch(k_block_product<T, true, 1>);
+    else if (sizeof(T) == 4 && tiles_t * tiles_o <= 256) launch(k_block_product<T, false, sizeof(T) == 4 ? 1 : 3>);
+    else launch(k_block_product<T, false, 3>);
     DMMV_LAUNCH_CHECK();
     return DMMV_OK;
 }

@@ -144,6 +144,24 @@ __device__ __forceinline__ uint32_t word_bits(const BlockView& q, int64_t at, ui
     const uint32_t there = q.e8m0 ? byte : word, one = q.e8m0 ? 127u : 0x3F800000u;
     return q.scales ? there : one;
 }
+// acc + p a b for a sum p of products of codes and the scales a, b of its operands.  The scales are multiplied first where their product is
+// a normal number, as p (2^-18 to 2^49, or 0) then leaves the range only where the result does.  Otherwise p meets the larger one first: beyond
+// the range both are over 1, below it p times the larger keeps its bits.
+__device__ __forceinline__ float add_scaled(float p, float a, float b, float acc) {
+    const float c = a * b;
+    if (__builtin_amdgcn_classf(c, 0x108) || a == 0.0f || b == 0.0f) return dmmv_fma(p, c, acc);
+    return fabsf(a) > fabsf(b) ? dmmv_fma(p * a, b, acc) : dmmv_fma(p * b, a, acc);
+}
+// The scales met so far need no such care: all are 2^-62 to 2^63 or 0, so that products of two are normal numbers or 0
+struct ScaleRange {
+    uint32_t lo = ~0u, hi = 0u;                      // magnitudes as bits, doubled; lo less 1, so that 0 does not count
+    __device__ __forceinline__ void take(float s) {
+        const uint32_t u = __float_as_uint(s) << 1;
+        hi = max(hi, u);
+        lo = min(lo, u - 1u);
+    }
+    __device__ __forceinline__ bool moderate() const { return lo >= (65u << 24) - 1u && hi < (190u << 24); }
+};
 __device__ __forceinline__ void scale_put(const BlockView& q, int64_t scale_row, int64_t block, uint32_t b) {
     const int64_t at = scale_row * q.srow + block * q.sblk;
     if (q.e8m0) static_cast<uint8_t*>(q.scales)[at] = (uint8_t)b;

@@ -1,0 +1,82 @@
+"""Products of 8-bit matrices whose scales are far apart: what is finite stays finite and keeps its bits."""
+import numpy as np
+import pytest
+import torch
+
+from tests import layer_plain as plain
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def codes_of(rows, K, seed, device):
+    r = np.random.default_rng(seed)
+    v = np.clip(r.standard_t(4.0, (rows, K)).astype(np.float32) * 20.0, -448, 448)
+    return torch.from_numpy(v).to(device).to(torch.float8_e4m3fn)
+
+
+def values(q):
+    """A block matrix in 64 bits, on its device."""
+    return torch.from_numpy(plain.values(q.codes.view(torch.uint8).cpu().numpy(), None if q.scales is None else q.scales.cpu().numpy(),
+                                         q.scale_rows)).to(q.device)
+
+
+def check_product(x, w, dtype, bias=None):
+    from paper_2508_13437_amd import dmmv
+
+    X, W, K = values(x), values(w), x.cols
+    want, size = X @ W.t(), X.abs() @ W.abs().t()
+    if bias is not None:
+        want, size = want + bias.double(), size + bias.double().abs()
+    got = dmmv.dmmv_block_product(x, w, bias, dtype).double()
+    # a sum of K exact products, three roundings for scales; bf16: what the 8-bit instructions drop, and the result's 8 bits
+    e, half = (K + 8) * 2 * U * size, U
+    if dtype == torch.bfloat16:
+        e, half = e + 2.0 ** -10 * size, 2.0 ** -8
+    assert bool(torch.isfinite(got).all())
+    assert bool(((got - want).abs() <= e + half * 1.01 * (want.abs() + e)).all())
+    assert float((got - want).norm()) <= (2e-6 + 1.01 * half) * float(want.norm()) + 1e-6 * float(size.norm()) / K ** 0.5
+
+
+def powers(rows, blocks, exponent, seed, device):
+    """Scales of 24 bits around 2^exponent (subnormal ones are exact multiples of 2^-149)."""
+    r = np.random.default_rng(seed)
+    s = np.ldexp(r.uniform(1.0, 1.9, (rows, blocks)), r.integers(exponent, exponent + 2, (rows, blocks)))
+    return torch.from_numpy(s.astype(np.float32)).to(device)
+
+
+APART = [(100, -100), (-100, 100), (125, -130), (-130, 125), (-145, 118), (118, -145), (60, -75), (-80, -20), (70, 20), (-147, 20), (20, -147)]
+
+
+@pytest.mark.parametrize("T", [3, 24, 40, 65, 150])
+@pytest.mark.parametrize("ex,ew", APART)
+def test_scales_of_blocks_far_apart(gpu_device, T, ex, ew):
+    """32-bit scales per block, as a product that is moderate of factors that are not."""
+    from paper_2508_13437_amd import dmmv
+
+    K, O = 300, 70
+    for rows in (1, 128):
+        x = dmmv.BlockMatrix(codes_of(T, K, T, gpu_device), powers(T, 3, ex, 1, gpu_device))
+        w = dmmv.BlockMatrix(codes_of(O, K, 7, gpu_device), powers(-(-O // rows), 3, ew, 2, gpu_device), rows)
+        for dtype in (torch.float32, torch.bfloat16):
+            check_product(x, w, dtype)
+
+
+@pytest.mark.parametrize("T", [3, 40, 150])
+def test_blocks_of_many_sizes_in_a_sum(gpu_device, T):
+    """A block that is large in x is small in w, another for every block; a scale of zero beside the largest."""
+    from paper_2508_13437_amd import dmmv
+
+    K, O = 1024, 70
+    up = torch.tensor([[2.0 ** e for e in (120, -120, 0, 64, -90, 3, -3, 1)]], device=gpu_device)
+    for x_scale, w_scale in ((up, 1.0 / up), (up, 1.5 / up)):
+        x = dmmv.BlockMatrix(codes_of(T, K, T, gpu_device), x_scale.expand(T, -1))
+        w = dmmv.BlockMatrix(codes_of(O, K, 7, gpu_device), w_scale.expand(O, -1))
+        for dtype in (torch.float32, torch.bfloat16):
+            check_product(x, w, dtype, torch.randn(O, generator=torch.Generator().manual_seed(T)).to(gpu_device))
+    zero = up.clone()
+    zero[0, 0] = 0.0
+    x = dmmv.BlockMatrix(codes_of(T, K, T, gpu_device), zero.expand(T, -1))
+    w = dmmv.BlockMatrix(codes_of(O, K, 7, gpu_device), torch.where(up > 2.0 ** 100, up, 1.0 / up).expand(O, -1))
+    for dtype in (torch.float32, torch.bfloat16):
+        check_product(x, w, dtype)
