@@ -65,8 +65,8 @@ __device__ __forceinline__ intx8 words8(piece16 a, piece16 b) {
 // rows of w are the A operand, so that a lane's four results are consecutive outputs of one token.
 //   LDS row: 128 codes, the 16-byte chunk c of row r at c ^ (r & 7): neither the 8 lanes that write a row
 //   nor the 8 rows that are read together meet in a bank.
-// SCALED: power-of-two scales go into the instruction (8 bits) or the conversion to bf16 (32-bit results); scales that are
-// the same along a row are left to the end.  Otherwise a block's sum is multiplied by the product of its two scales in 32 bits.  That is
+// SCALED: power-of-two scales go into the instruction (8 bits) or the conversion to bf16 (32-bit results), and so does the exponent of a scale
+// that is the same along a row; the rest of that is multiplied at the end.  Otherwise a block's sum is multiplied by the product of its two scales in 32 bits.  That is
 // right while all scales are moderate; where a tile has met others, its sums are made once more by add_scaled (a branch in the loop would cost
 // every product a fifth).
 // Bound by the vector unit (conversions to 16 bits, sums of blocks) and by the waits of four wavefronts in step: 4096 x 11008 x 4096 in
@@ -108,9 +108,14 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
     sq.codes = mine_x ? x.codes : w.codes;
     sq.scales = mine_x ? x.scales : w.scales;
     sq.e8m0 = mine_x ? x.e8m0 : w.e8m0;
-    if (SCALED && !(mine_x ? how.x_blocks : how.w_blocks)) sq.scales = nullptr, sq.e8m0 = 1;
     const int64_t sblk = mine_x ? x.sblk : w.sblk;
     const int64_t sat = mine_x ? (min(t0 + tid, T_ - 1) >> x.shift) * x.srow : (min(o0 + max(tid - BM, 0), O - 1) >> w.shift) * w.srow;
+    uint32_t along = 127u;                           // SCALED: the exponent of a scale that is the same along the row
+    if (SCALED && !(mine_x ? how.x_blocks : how.w_blocks)) {
+        if (sq.scales) along = row_scale(sq.e8m0 ? e8m0_value(static_cast<const uint8_t*>(sq.scales)[sat]) : static_cast<const float*>(sq.scales)[sat]).byte;
+        sq.scales = nullptr;
+        sq.e8m0 = 1;
+    }
 
     struct Step {
         piece16 c[MI + NI];
@@ -128,7 +133,7 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
 #pragma unroll
         for (int u = 0; u < MI + NI; ++u) *reinterpret_cast<piece16*>(&codes[stage][put + u * 4096]) = r.c[u];
         const uint32_t bits = word_bits(sq, sat + kb * sblk, r.s);
-        const uint32_t s = !SCALED && sq.e8m0 ? __float_as_uint(e8m0_value(bits)) : bits;
+        const uint32_t s = SCALED ? (sq.scales ? bits : along) : sq.e8m0 ? __float_as_uint(e8m0_value(bits)) : bits;
         if (mine) scl[stage][tid] = s;
         if (!SCALED) met.take(__uint_as_float(s));
     };
@@ -247,13 +252,13 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
         for (int e = 0; e < 4; ++e) {
             const int64_t o = min(o0 + wo + 16 * i + lg * 4 + e, O - 1);
             bo[e] = bias ? bias[o] : 0.0f;
-            so[e] = SCALED && !how.w_blocks ? scale_at(w, o, 0) : 1.0f;
+            so[e] = SCALED && !how.w_blocks ? row_scale(scale_at(w, o, 0)).rest : 1.0f;
         }
 #pragma unroll
         for (int j = 0; j < MI; ++j) {
             const int64_t t = t0 + wt + 16 * j + lr, o = o0 + wo + 16 * i + lg * 4;
             if (t >= T_) continue;
-            const float st = SCALED && !how.x_blocks ? scale_at(x, t, 0) : 1.0f;
+            const float st = SCALED && !how.x_blocks ? row_scale(scale_at(x, t, 0)).rest : 1.0f;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (o + e < O) put_y(y + t * ldy + o + e, dmmv_fma(acc[i][j][e] * so[e], st, bo[e]));
@@ -265,7 +270,8 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
 // The same tiles, LDS rows and operands for bf16 results with SCALED scales, where rows are aligned to 16 bytes: the
 // codes go straight from memory into the LDS (NST stages of one block of 128), and the loop is written so that the matrix
 // unit has a product at all times: what else there is to do is placed in the products' shadows by hand.
-// WTILE: the scales of w are the same for 128 rows, or for a whole row.
+// Where the scales of w come from, WS: 0 a table of exponents of every row (those that are the same along a row repeated), 1 of every 128 rows,
+// 2 registers, as they are the same along a row.
 // T float: workgroup row y of the grid takes its share of the contraction, and y [share][T_][O] is joined by k_block_product_join.
 // 256 x 256 tiles, 128 x 128 a wavefront: 64 products a step from 16 + 16 fragments, which the LDS can deliver beside the requests;
 // smaller tiles are bound by it.  4096 x 11008 x 4096: 157 to 166 us (2.2 to 2.35 PFLOP/s), the matrix unit busy for 53 % of the
@@ -289,12 +295,12 @@ __device__ __forceinline__ void stage_exponents(const BlockView& q, int64_t row0
     }
 }
 
-constexpr int product_lds(int MI, int NI, int width, bool wtile, int nst) {
-    const int stages = nst * 128 * 32 * (MI + NI) + 68 * (32 * MI + (wtile ? (32 * NI + 127) / 128 : 32 * NI)), out = 32 * MI * (32 * NI * width + 16);
+constexpr int product_lds(int MI, int NI, int width, int ws, int nst) {
+    const int stages = nst * 128 * 32 * (MI + NI) + 68 * (32 * MI + (ws == 2 ? 0 : ws == 1 ? (32 * NI + 127) / 128 : 32 * NI)), out = 32 * MI * (32 * NI * width + 16);
     return stages > out ? stages : out;
 }
 
-template <class T, int MI, int NI, bool SCALED, bool WTILE, int NST>
+template <class T, int MI, int NI, bool SCALED, int WS, int NST>
 __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
                                                              const float* __restrict__ bias, T* __restrict__ y, int64_t ldy,
                                                              int32_t tiles_t, int32_t tiles_o) {
@@ -335,28 +341,42 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
 #pragma unroll
         for (int j = 0; j < MI; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    // Exponents of SB blocks of every row of the tile, one byte each (WTILE: of every 128 rows of w), past the stages; a
+    // Exponents of SB blocks of every row of the tile, one byte each (WS 1: of every 128 rows of w), past the stages; a
     // lane has those of two steps in a register.
-    constexpr int SB = 64, SROW = SB + 4, WROWS = WTILE ? ((BN + 127) / 128) : BN, NS = WTILE ? 1 : NI;
+    constexpr int SB = 64, SROW = SB + 4, WROWS = WS == 2 ? 0 : WS == 1 ? (BN + 127) / 128 : BN, NS = WS == 1 ? 1 : NI;
     uint8_t* scl = lds + NST * STAGE;
     uint32_t sx[MI], sw[NS];
-    auto scales_one = [&]() __attribute__((always_inline)) {         // what is not read from the tables is 1
-        if (!SCALED || (how.x_blocks && how.w_blocks)) return;
-        for (int i = tid; i < (BM + WROWS) * (SROW / 4); i += 256) reinterpret_cast<uint32_t*>(scl)[i] = 0x7F7F7F7Fu;
-        __syncthreads();
+    // Exponents of scales that are the same along a row, for all blocks: a row of the table a thread; requested ahead of the codes
+    static_assert(WS == 0 ? BM + BN <= 256 : BM <= 256, "a thread has one row");
+    const bool mine_x = tid < BM, fills = SCALED && (mine_x ? !how.x_blocks : WS == 0 && !how.w_blocks);
+    float along = 1.0f, along_w[WS == 2 ? NS : 1];
+    if (fills) along = mine_x ? scale_at(x, min(t0 + tid, T_ - 1), 0) : scale_at(w, min(o0 + tid - BM, O - 1), 0);
+    if constexpr (WS == 2)
+#pragma unroll
+        for (int i = 0; i < NS; ++i) along_w[i] = scale_at(w, min(o0 + wo + 16 * i + lr, O - 1), 0);
+    auto scales_along = [&]() __attribute__((always_inline)) {
+        if (fills) {
+            const uint32_t b = row_scale(along).byte * 0x01010101u;
+#pragma unroll
+            for (int i = 0; i < SROW / 4; ++i) reinterpret_cast<uint32_t*>(scl + tid * SROW)[i] = b;
+        }
+        if constexpr (WS == 2)
+#pragma unroll
+            for (int i = 0; i < NS; ++i) sw[i] = row_scale(along_w[i]).byte * 0x0101u;
     };
 #define BP_SCALES_STAGE(kb)                                                                                     \
     {                                                                                                           \
         if (how.x_blocks) stage_exponents(x, t0, T_, 1, BM, kb, min(nb - (kb), SB), scl, SROW);                 \
-        if (how.w_blocks) stage_exponents(w, o0, O, WTILE ? 128 : 1, WROWS, kb, min(nb - (kb), SB), scl + BM * SROW, SROW); \
+        if (WS < 2 && how.w_blocks) stage_exponents(w, o0, O, WS == 1 ? 128 : 1, WROWS, kb, min(nb - (kb), SB), scl + BM * SROW, SROW); \
     }
 #define BP_SCALES_TAKE(kb)                                                                                      \
     {                                                                                                           \
         const uint8_t* p_ = scl + ((kb) & (SB - 1));                                                            \
         _Pragma("unroll") for (int j = 0; j < MI; ++j)                                                          \
             sx[j] = *reinterpret_cast<const uint16_t*>(p_ + (wt + 16 * j + lr) * SROW);                         \
-        _Pragma("unroll") for (int i = 0; i < NS; ++i)                                                          \
-            sw[i] = *reinterpret_cast<const uint16_t*>(p_ + (BM + (WTILE ? wo >> 7 : wo + 16 * i + lr)) * SROW); \
+        if (WS < 2)                                                                                             \
+            _Pragma("unroll") for (int i = 0; i < NS; ++i)                                                      \
+                sw[i] = *reinterpret_cast<const uint16_t*>(p_ + (BM + (WS == 1 ? wo >> 7 : wo + 16 * i + lr)) * SROW); \
     }
 
     // Request i (of MI / 2) of this wavefront for half `h` of the wavefronts' rows of x (W 0) or w (W 1): 8 rows
@@ -373,7 +393,7 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
     const uint8_t* pw[2] = {lds + BM * 128 + (wo + lr) * 128 + c0, lds + BM * 128 + (wo + lr) * 128 + (c0 ^ 64)};
     auto mul = [&](auto byte, int i, int j) __attribute__((always_inline)) {
         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(words8(fw[i][0], fw[i][1]), words8(fx[j][0], fx[j][1]), acc[i][j], 0, 0,
-                                                                     byte.value, (int)sw[WTILE ? 0 : i], byte.value, (int)sx[j]);
+                                                                     byte.value, (int)sw[WS == 1 ? 0 : i], byte.value, (int)sx[j]);
     };
     auto frag_x = [&](int stage, int j, int h) __attribute__((always_inline)) {
         fx[j][h] = *reinterpret_cast<const piece16*>(px[h] + stage + j * 2048);
@@ -443,7 +463,7 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
                 else half(C1, C1);
             }
         }
-        scales_one();
+        scales_along();
         if (SCALED) BP_SCALES_STAGE(0);
         lds_requests_left<LEFT>();
         __syncthreads();
@@ -475,7 +495,7 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
     for (int kb = paired; kb < nb; ++kb) {
         const int left = (int)(K - kb * 128ll) - cchunk * 16;
         __syncthreads();
-        if (paired == 0 && kb == 0) scales_one();
+        if (paired == 0 && kb == 0) scales_along();
         if (SCALED && (kb == paired && (kb & (SB - 1)) == 0)) BP_SCALES_STAGE(kb);
 #pragma unroll 1
         for (int q = 0; q < MI; ++q) {
@@ -490,7 +510,7 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
 #pragma unroll
             for (int j = 0; j < MI; ++j) sx[j] >>= 8;
 #pragma unroll
-            for (int i = 0; i < NS; ++i) sw[i] >>= 8;
+            for (int i = 0; WS < 2 && i < NS; ++i) sw[i] >>= 8;
         }
 #pragma unroll
         for (int i = 0; i < NI; ++i)
@@ -514,11 +534,11 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
         for (int e = 0; e < 4; ++e) {
             const int64_t o = min(o0 + wo + 16 * i + lg * 4 + e, O - 1);
             bo[e] = bias ? bias[o] : 0.0f;
-            so[e] = SCALED && !how.w_blocks ? scale_at(w, o, 0) : 1.0f;
+            so[e] = SCALED && !how.w_blocks ? row_scale(scale_at(w, o, 0)).rest : 1.0f;
         }
 #pragma unroll
         for (int j = 0; j < MI; ++j) {
-            const float st = SCALED && !how.x_blocks ? scale_at(x, min(t0 + wt + 16 * j + lr, T_ - 1), 0) : 1.0f;
+            const float st = SCALED && !how.x_blocks ? row_scale(scale_at(x, min(t0 + wt + 16 * j + lr, T_ - 1), 0)).rest : 1.0f;
             float v[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = dmmv_fma(acc[i][j][e] * so[e], st, bo[e]);
@@ -580,13 +600,25 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
     auto exponent = [&](const BlockView& q, int64_t row, int b) __attribute__((always_inline)) {
         return (uint32_t)static_cast<const uint8_t*>(q.scales)[(row >> q.shift) * q.srow + b * q.sblk];
     };
+    // SCALED: scales that are the same along a row, and their exponents, taken when the first codes have been requested
+    float row_w = 1.0f, row_x[MT];
+    uint32_t along_w = 127u, along_x[MT];
+    if (SCALED && !how.w_blocks) row_w = scale_at(w, orow, 0);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        row_x[m] = SCALED && !how.x_blocks ? scale_at(x, trow[m], 0) : 1.0f;
+        along_x[m] = 127u;
+    }
+    auto exponents_along = [&]() __attribute__((always_inline)) {
+        along_w = row_scale(row_w).byte;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) along_x[m] = row_scale(row_x[m]).byte;
+    };
     auto scales = [&](Block& k, int b) __attribute__((always_inline)) {
         if constexpr (SCALED) {
-            k.ew = 127u;
             if (how.w_blocks) k.ew = exponent(w, orow, b);
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                k.ex[m] = 127u;
                 if (how.x_blocks) k.ex[m] = exponent(x, trow[m], b);
             }
         } else {
@@ -597,7 +629,13 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
         }
     };
     ScaleRange met;                                  // as in the general kernel: this lane's scales
-    auto multiply = [&](auto CAREFUL, const Block& k) __attribute__((always_inline)) {
+    auto multiply = [&](auto CAREFUL, Block& k) __attribute__((always_inline)) {
+        if constexpr (SCALED) {
+            if (!how.w_blocks) k.ew = along_w;
+            if (!how.x_blocks)
+#pragma unroll
+                for (int m = 0; m < MT; ++m) k.ex[m] = along_x[m];
+        }
         if constexpr (!SCALED) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) met.take(scale_of(w, k.fw[e]));
@@ -613,10 +651,11 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
                 const floatx4 p = block_sum<WIDE>(a, b);
                 if constexpr (SCALED) {
                     // 32-bit results, exponents: a row of w belongs to lane lr, its results to lanes of another order
-                    const float fx = e8m0_value(k.ex[m]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        acc[m][e] = dmmv_fma(p[e] * e8m0_value((uint32_t)__shfl((int)k.ew, lg * 4 + e, 64)), fx, acc[m][e]);
+                    for (int e = 0; e < 4; ++e) {
+                        const int ew = __shfl((int)k.ew, lg * 4 + e, 64), ex = (int)k.ex[m];
+                        acc[m][e] += max(ew, ex) == 255 ? __uint_as_float(0x7FC00000u) : __builtin_amdgcn_ldexpf(p[e], ew + ex - 254);
+                    }
                 } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -637,6 +676,7 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
 #pragma unroll
             for (int h = 0; h < 2; ++h) k.x[m][h] = chunk_tail(xr[m] + (int64_t)b * 128 + 16 * h, left - 16 * h, b * 128ll + lg * 32 + 16 * h);
         scales(k, b);
+        if (SCALED && b == b0) exponents_along();
         multiply(CAREFUL, k);
     };
 #pragma unroll
@@ -654,6 +694,7 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
                 for (int h = 0; h < 2; ++h) k[u].x[m][h] = *reinterpret_cast<const piece16_any*>(xr[m] + (int64_t)(b + u) * 128 + 16 * h);
             scales(k[u], b + u);
         }
+        if (SCALED && b == b0) exponents_along();
 #pragma unroll
         for (int u = 0; u < U; ++u) multiply(std::false_type{}, k[u]);
     }
@@ -676,12 +717,12 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
         for (int i = 1; i < WAVES; ++i) v += part[i][m][lane];
         const int64_t t = t0 + 16 * m + lr;
         if (t >= T_) continue;
-        const float st = SCALED && !how.x_blocks ? scale_at(x, t, 0) : 1.0f;
+        const float st = SCALED && !how.x_blocks ? row_scale(scale_at(x, t, 0)).rest : 1.0f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int64_t o = o0 + lg * 4 + e;
             if (o >= O) continue;
-            const float so = SCALED && !how.w_blocks ? scale_at(w, o, 0) : 1.0f;
+            const float so = SCALED && !how.w_blocks ? row_scale(scale_at(w, o, 0)).rest : 1.0f;
             put_y(y + t * ldy + o, dmmv_fma(v[e] * so, st, bias ? bias[o] : 0.0f));
         }
     }
@@ -735,16 +776,16 @@ __global__ __launch_bounds__(256) void k_block_product_join(int64_t T_, int64_t 
     store8(y + t * ldy, o, O, v);
 }
 
-template <class T, int MI, int NI, bool SCALED, bool WTILE, int NST>
+template <class T, int MI, int NI, bool SCALED, int WS, int NST>
 static dmmv_status launch_tiled(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, T* y, int64_t ldy, hipStream_t s,
                                 int32_t shares = 1) {
     const int64_t tiles_t = ceil_div(x->rows, 32 * MI), tiles_o = ceil_div(w->rows, 32 * NI);
     if (tiles_t > INT32_MAX / 4 / tiles_o) return fail(DMMV_ERR_SHAPE, "y: more tiles than a launch takes");
-    const void* kern = (const void*)k_block_product_tiled<T, MI, NI, SCALED, WTILE, NST>;
-    constexpr int bytes = product_lds(MI, NI, sizeof(T), WTILE, NST);
+    const void* kern = (const void*)k_block_product_tiled<T, MI, NI, SCALED, WS, NST>;
+    constexpr int bytes = product_lds(MI, NI, sizeof(T), WS, NST);
     DMMV_TRY(ensure_dynamic_lds(kern, bytes));
     const ProductScales how = {!constant_rows(x), !constant_rows(w)};
-    hipLaunchKernelGGL((k_block_product_tiled<T, MI, NI, SCALED, WTILE, NST>), dim3((unsigned)(tiles_t * tiles_o), (unsigned)shares), dim3(256), bytes, s, x->rows, w->rows,
+    hipLaunchKernelGGL((k_block_product_tiled<T, MI, NI, SCALED, WS, NST>), dim3((unsigned)(tiles_t * tiles_o), (unsigned)shares), dim3(256), bytes, s, x->rows, w->rows,
                        x->cols, layer_view(x), layer_view(w), how, bias, y, ldy, (int32_t)tiles_t, (int32_t)tiles_o);
     DMMV_LAUNCH_CHECK();
     return DMMV_OK;
@@ -774,21 +815,22 @@ static dmmv_status product_tiled(const dmmv_block_matrix* x, const dmmv_block_ma
                                  hipStream_t s) {
     const int32_t shares = part ? product_shares(x->rows, w->rows, x->cols) : 1;
     if (shares > 1) {
-        DMMV_TRY((launch_tiled<float, 4, 4, true, false, 4>(x, w, nullptr, part, w->rows, s, shares)));
+        DMMV_TRY((launch_tiled<float, 4, 4, true, 0, 4>(x, w, nullptr, part, w->rows, s, shares)));
         hipLaunchKernelGGL(k_block_product_join, dim3((unsigned)ceil_div(x->rows, 4), (unsigned)ceil_div(w->rows, 512)), dim3(256), 0, s, x->rows,
                            w->rows, shares, part, bias, y, ldy);
         DMMV_LAUNCH_CHECK();
         return DMMV_OK;
     }
-    const bool wtile = constant_rows(w) || w->scale_rows == 128;
+    const bool along = constant_rows(w);
     int dev = 0, cus = 0;
     DMMV_HIP_CHECK(hipGetDevice(&dev));
     DMMV_HIP_CHECK(hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev));
     const int64_t small = ceil_div(x->rows, 128) * ceil_div(w->rows, 128), large = ceil_div(x->rows, 256) * ceil_div(w->rows, 256);
     // a round of large tiles takes 2.25 times one of small ones (K = 4096: 46 us and 20.5; 1024 x 4096 x 11008 54 and 62 us,
     // 2048 x 4096 x 4096 51 and 44)
-    if (wtile && 9 * ceil_div(large, cus) < 4 * ceil_div(small, cus)) return launch_tiled<bf16_t, 8, 8, true, true, 2>(x, w, bias, y, ldy, s);
-    return launch_tiled<bf16_t, 4, 4, true, false, 4>(x, w, bias, y, ldy, s);
+    if ((along || w->scale_rows == 128) && 9 * ceil_div(large, cus) < 4 * ceil_div(small, cus))
+        return along ? launch_tiled<bf16_t, 8, 8, true, 2, 2>(x, w, bias, y, ldy, s) : launch_tiled<bf16_t, 8, 8, true, 1, 2>(x, w, bias, y, ldy, s);
+    return launch_tiled<bf16_t, 4, 4, true, 0, 4>(x, w, bias, y, ldy, s);
 }
 
 // Rows that are no multiple of 16 codes are laid out for the large tiles where the general kernel would

@@ -162,6 +162,16 @@ struct ScaleRange {
     }
     __device__ __forceinline__ bool moderate() const { return lo >= (65u << 24) - 1u && hi < (190u << 24); }
 };
+// A scale that is the same along a row leaves the sum, but its exponent (as a scale's byte) goes in where those of blocks go, so that the sum
+// has the result's size; what is left of it, `rest`, is 1 to 2 (for exponents outside what scaled8 takes a little more or less; 0, infinite or NaN as the scale).
+struct RowScale {
+    uint32_t byte;
+    float rest;
+};
+__device__ __forceinline__ RowScale row_scale(float s) {
+    const uint32_t e = (__float_as_uint(s) >> 23) & 255u, byte = e == 255u ? 127u : min(max(e, 3u), 246u);
+    return RowScale{byte, s * __uint_as_float((254u - byte) << 23)};         // exact
+}
 __device__ __forceinline__ void scale_put(const BlockView& q, int64_t scale_row, int64_t block, uint32_t b) {
     const int64_t at = scale_row * q.srow + block * q.sblk;
     if (q.e8m0) static_cast<uint8_t*>(q.scales)[at] = (uint8_t)b;

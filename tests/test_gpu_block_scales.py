@@ -80,3 +80,34 @@ def test_blocks_of_many_sizes_in_a_sum(gpu_device, T):
     w = dmmv.BlockMatrix(codes_of(O, K, 7, gpu_device), torch.where(up > 2.0 ** 100, up, 1.0 / up).expand(O, -1))
     for dtype in (torch.float32, torch.bfloat16):
         check_product(x, w, dtype)
+
+
+def matrix(rows, K, kind, exponent, seed, device, g=1):
+    """kind: blocks (exponent bytes), row (32 bits, one per row, the second 0), byte row (an exponent per row)."""
+    from paper_2508_13437_amd import dmmv
+
+    nb = -(-K // 128)
+    if kind == "row":
+        s = powers(rows, 1, exponent, seed, device)
+        if rows > 1:
+            s[1] = 0.0
+        s = s.expand(-1, nb)
+    else:
+        b = np.random.default_rng(seed).integers(127 + exponent, 129 + exponent, (-(-rows // g), nb if kind == "blocks" else 1)).astype(np.uint8)
+        s = torch.from_numpy(b).to(device).expand(-1, nb)
+    return dmmv.BlockMatrix(codes_of(rows, K, seed, device), s, g if kind == "blocks" else 1)
+
+
+# few tokens, unaligned rows, the two sizes of the large tiles, a shared contraction, rows laid out first, a last block that is not whole
+ROW_SIZES = [(3, 70, 300), (24, 70, 384), (40, 70, 300), (150, 70, 300), (200, 300, 528), (70, 600, 4112), (2304, 4600, 400), (2304, 2900, 900)]
+
+
+@pytest.mark.parametrize("kx,kw,ex,ew", [("blocks", "row", 118, -118), ("blocks", "row", 118, -140), ("blocks", "row", -118, 118), ("row", "blocks", -118, 118),
+                                         ("row", "blocks", 118, -118), ("row", "row", 118, -118), ("row", "row", -140, 120), ("blocks", "byte row", 118, -118),
+                                         ("byte row", "blocks", -120, 118), ("byte row", "row", 118, -120)])
+@pytest.mark.parametrize("T,O,K", ROW_SIZES)
+def test_scales_of_rows_far_from_those_of_blocks(gpu_device, T, O, K, kx, kw, ex, ew):
+    for g in (1, 128) if kw == "blocks" else (1,):
+        x, w = matrix(T, K, kx, ex, T, gpu_device), matrix(O, K, kw, ew, O, gpu_device, g)
+        for dtype in (torch.bfloat16, torch.float32) if T < 2000 else (torch.bfloat16,):
+            check_product(x, w, dtype, torch.randn(O, generator=torch.Generator().manual_seed(T)).to(gpu_device))
