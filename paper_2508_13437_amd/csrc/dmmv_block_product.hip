@@ -67,14 +67,53 @@ __device__ __forceinline__ intx8 words8(piece16 a, piece16 b) {
 //   nor the 8 rows that are read together meet in a bank.
 // SCALED: power-of-two scales go into the instruction (8 bits) or the conversion to bf16 (32-bit results), and so does the exponent of a scale
 // that is the same along a row; the rest of that is multiplied at the end.  Otherwise a block's sum is multiplied by the product of its two scales in 32 bits.  That is
-// right while all scales are moderate; where a tile has met others, its sums are made once more by add_scaled (a branch in the loop would cost
-// every product a fifth).
+// right while all scales are moderate, and a conversion to bf16 is while exponents are (scaled8); where a tile has met others, its sums are made
+// once more by tile_any (a branch in the loop would cost every product a fifth).
 // Bound by the vector unit (conversions to 16 bits, sums of blocks) and by the waits of four wavefronts in step: 4096 x 11008 x 4096 in
 // 32 bits 490 to 514 us, 0.72 PFLOP/s, with 32-bit scales per block 570; 500 x 1777 x 2731 in 32 bits 20 us.  Tiles of 64 x 64 keep the chip
 // full at such sizes (224 tiles); larger ones would leave most of it idle.
 struct ProductScales {
     int32_t x_blocks, w_blocks;         // SCALED: exponents per block, else constant along the row
 };
+
+// 16 x 16 results with any scales, straight from memory: lane (lr, lg) has 32 codes of row lr of each operand and block, and the results
+// of outputs 4 lg .. of token lr.
+template <class T, bool SCALED>
+__device__ __forceinline__ void tile_any(int64_t t0, int64_t T_, int64_t o0, int64_t O, int64_t K, const BlockView& x, const BlockView& w, ProductScales how,
+                                         const float* __restrict__ bias, T* __restrict__ y, int64_t ldy) {
+    int lane = threadIdx.x & 63;
+    floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+    for (int64_t at = 0; at < K; at += 128) {
+        asm volatile("" : "+v"(lane));               // (addresses are made again for every block: few registers)
+        const int lr = lane & 15, lg = lane >> 4;
+        const int64_t t = min(t0 + lr, T_ - 1), o = min(o0 + lr, O - 1);
+        const int left = (int)min(K - at, (int64_t)128) - lg * 32;
+        const uint8_t* px = x.codes + t * x.ld + at + lg * 32;
+        const uint8_t* pw = w.codes + o * w.ld + at + lg * 32;
+        const intx8 fx = words8(chunk_tail(px, left, at + lg * 32), chunk_tail(px + 16, left - 16, at + lg * 32 + 16));
+        const intx8 fw = words8(chunk_tail(pw, left, at + lg * 32), chunk_tail(pw + 16, left - 16, at + lg * 32 + 16));
+        const floatx4 p = block_sum<sizeof(T) == 4>(fw, fx);
+        const int64_t b = at >> 7;
+        const uint32_t sx = SCALED && !how.x_blocks ? row_scale(scale_at(x, t, 0)).byte : scale_bits(x, t, b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t oe = min(o0 + lg * 4 + e, O - 1);
+            const uint32_t sw = SCALED && !how.w_blocks ? row_scale(scale_at(w, oe, 0)).byte : scale_bits(w, oe, b);
+            acc[e] = SCALED ? acc[e] + times_exponents(p[e], sw, sx) : add_scaled(p[e], scale_of(w, sw), scale_of(x, sx), acc[e]);
+        }
+    }
+    const int lr = lane & 15, lg = lane >> 4;
+    const int64_t t = t0 + lr;
+    if (t >= T_) return;
+    const float st = SCALED && !how.x_blocks ? row_scale(scale_at(x, t, 0)).rest : 1.0f;
+    for (int e = 0; e < 4; ++e) {
+        const int64_t oe = o0 + lg * 4 + e;
+        if (oe >= O) break;
+        const float so = SCALED && !how.w_blocks ? row_scale(scale_at(w, oe, 0)).rest : 1.0f;
+        put_y(y + t * ldy + oe, dmmv_fma(acc[e] * so, st, bias ? bias[oe] : 0.0f));
+    }
+}
 
 // WAVES: wavefronts a SIMD that the registers leave room for at least.  32-bit results with 32-bit scales have more than three allow: where a compute
 // unit gets one tile they stay (500 x 1777 x 2731 20.6 us, 21.5 with three), else not (4096 x 11008 x 4096 570 us, 650 without).
@@ -85,8 +124,9 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
     constexpr int MI = 2, NI = 2, BM = 32 * MI, BN = 32 * NI;
     __shared__ __align__(16) uint8_t codes[2][128 * (BM + BN)];
     __shared__ __align__(16) uint32_t scl[2][BM + BN];
-    __shared__ int again;                            // !SCALED: some scale is not moderate
-    if (!SCALED && threadIdx.x == 0) again = 0;      // (a barrier follows before it is set)
+    constexpr bool RANGED = !SCALED || WIDE;         // (the 8-bit instruction takes every exponent)
+    __shared__ int again;                            // RANGED: some scale is not moderate
+    if (RANGED && threadIdx.x == 0) again = 0;       // (a barrier follows before it is set)
     const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wt = (wv & 1) * (16 * MI), wo = (wv >> 1) * (16 * NI);
@@ -129,6 +169,7 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
         r.s = *scale_word(sq, sat + kb * sblk);
     };
     ScaleRange met;                                  // this thread's scales
+    bool exact = true;                               // and exponents: those that scaled8 takes
     auto deposit = [&](const Step& r, int kb, int stage) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < MI + NI; ++u) *reinterpret_cast<piece16*>(&codes[stage][put + u * 4096]) = r.c[u];
@@ -136,10 +177,11 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
         const uint32_t s = SCALED ? (sq.scales ? bits : along) : sq.e8m0 ? __float_as_uint(e8m0_value(bits)) : bits;
         if (mine) scl[stage][tid] = s;
         if (!SCALED) met.take(__uint_as_float(s));
+        else if (WIDE) exact &= s - 3u <= 243u || s == 255u;
     };
     floatx4 acc[NI][MI];
     const int c0 = (lg ^ (lr & 7)) << 4;
-    auto multiply = [&](auto CAREFUL, int stage) __attribute__((always_inline)) {
+    auto multiply = [&](int stage) __attribute__((always_inline)) {
         const uint8_t* px = &codes[stage][(wt + lr) * 128];
         const uint8_t* pw = &codes[stage][(BM + wo + lr) * 128];
         intx8 fx[MI], fw[NI];
@@ -186,8 +228,7 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
                 for (int j = 0; j < MI; ++j) {
                     const floatx4 p = block_sum<WIDE>(fw[i], fx[j]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        acc[i][j][e] = CAREFUL.value ? add_scaled(p[e], sw[e], sx[j], acc[i][j][e]) : dmmv_fma(p[e], sw[e] * sx[j], acc[i][j][e]);
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = dmmv_fma(p[e], sw[e] * sx[j], acc[i][j][e]);
                 }
             }
         }
@@ -195,26 +236,11 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
     // The whole blocks.  Requests are made without a condition, or a use would wait for all of them; those past the end ask for
     // the last block again.
     const int full = (int)(K >> 7), most = full - 1;
-    auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < NI; ++i)
+    for (int i = 0; i < NI; ++i)
 #pragma unroll
-            for (int j = 0; j < MI; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-    };
+        for (int j = 0; j < MI; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
     Step r0, r1;
-    auto one = [&](auto CAREFUL, int kb) __attribute__((always_inline)) {     // any block, zeros past the row's end
-        const int64_t at = kb * 128ll;
-        const int left = (int)(K - at) - cchunk * 16;
-#pragma unroll
-        for (int u = 0; u < MI; ++u) r0.c[u] = chunk_tail(xr[u] + at, left, at + cchunk * 16);
-#pragma unroll
-        for (int u = 0; u < NI; ++u) r0.c[MI + u] = chunk_tail(wr[u] + at, left, at + cchunk * 16);
-        r0.s = *scale_word(sq, sat + kb * sblk);
-        deposit(r0, kb, 0);
-        __syncthreads();
-        multiply(CAREFUL, 0);
-    };
-    clear();
     if (full > 0) {
         request(r0, 0);
         request(r1, min(1, most));
@@ -224,25 +250,33 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
         for (int kb = 0; kb < full; kb += 2) {
             deposit(r1, min(kb + 1, most), 1);
             request(r1, min(kb + 3, most));
-            multiply(std::false_type{}, 0);
+            multiply(0);
             __syncthreads();
             deposit(r0, min(kb + 2, most), 0);
             request(r0, min(kb + 4, most));
-            if (kb + 1 < full) multiply(std::false_type{}, 1);
+            if (kb + 1 < full) multiply(1);
             __syncthreads();
         }
     }
-    if (full < nb) one(std::false_type{}, full);
-    if constexpr (!SCALED) {
-        if (!met.moderate()) again = 1;
+    if (full < nb) {                                 // the last block, zeros past the row's end
+        const int64_t at = full * 128ll;
+        const int left = (int)(K - at) - cchunk * 16;
+#pragma unroll
+        for (int u = 0; u < MI; ++u) r0.c[u] = chunk_tail(xr[u] + at, left, at + cchunk * 16);
+#pragma unroll
+        for (int u = 0; u < NI; ++u) r0.c[MI + u] = chunk_tail(wr[u] + at, left, at + cchunk * 16);
+        r0.s = *scale_word(sq, sat + full * sblk);
+        deposit(r0, full, 0);
+        __syncthreads();
+        multiply(0);
+    }
+    if constexpr (RANGED) {
+        if (!(SCALED ? exact : met.moderate())) again = 1;
         __syncthreads();
         if (again) {
-            clear();
 #pragma unroll 1
-            for (int kb = 0; kb < nb; ++kb) {
-                one(std::true_type{}, kb);
-                __syncthreads();
-            }
+            for (int q = 0; q < NI * MI; ++q) tile_any<T, SCALED>(t0 + wt + 16 * (q % MI), T_, o0 + wo + 16 * (q / MI), O, K, x, w, how, bias, y, ldy);
+            return;
         }
     }
 #pragma unroll
@@ -652,10 +686,7 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
                 if constexpr (SCALED) {
                     // 32-bit results, exponents: a row of w belongs to lane lr, its results to lanes of another order
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int ew = __shfl((int)k.ew, lg * 4 + e, 64), ex = (int)k.ex[m];
-                        acc[m][e] += max(ew, ex) == 255 ? __uint_as_float(0x7FC00000u) : __builtin_amdgcn_ldexpf(p[e], ew + ex - 254);
-                    }
+                    for (int e = 0; e < 4; ++e) acc[m][e] += times_exponents(p[e], (uint32_t)__shfl((int)k.ew, lg * 4 + e, 64), k.ex[m]);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {

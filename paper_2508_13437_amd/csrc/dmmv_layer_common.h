@@ -152,6 +152,10 @@ __device__ __forceinline__ float add_scaled(float p, float a, float b, float acc
     if (__builtin_amdgcn_classf(c, 0x108) || a == 0.0f || b == 0.0f) return dmmv_fma(p, c, acc);
     return fabsf(a) > fabsf(b) ? dmmv_fma(p * a, b, acc) : dmmv_fma(p * b, a, acc);
 }
+// the same with scales that are exponent bytes
+__device__ __forceinline__ float times_exponents(float p, uint32_t a, uint32_t b) {
+    return max(a, b) == 255u ? __uint_as_float(0x7FC00000u) : __builtin_amdgcn_ldexpf(p, (int)(a + b) - 254);
+}
 // The scales met so far need no such care: all are 2^-62 to 2^63 or 0, so that products of two are normal numbers or 0
 struct ScaleRange {
     uint32_t lo = ~0u, hi = 0u;                      // magnitudes as bits, doubled; lo less 1, so that 0 does not count
@@ -367,7 +371,7 @@ __device__ __forceinline__ void tile_of_workgroup(int tiles_t, int tiles_o, int&
     tile_t = __builtin_amdgcn_readfirstlane(4 * band + in % high);
 }
 
-// eight codes as bf16, times 2^(b - 127): exact
+// eight codes as bf16, times 2^(b - 127): exact for b from 3 (the smallest code is 2^-133 then, as bf16 is) to 246; NaN for 255
 __device__ __forceinline__ bf16x8_t scaled8(int lo, int hi, uint32_t b) {
     const float s = __uint_as_float(b << 23);
     const auto p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true);

@@ -111,3 +111,48 @@ def test_scales_of_rows_far_from_those_of_blocks(gpu_device, T, O, K, kx, kw, ex
         x, w = matrix(T, K, kx, ex, T, gpu_device), matrix(O, K, kw, ew, O, gpu_device, g)
         for dtype in (torch.bfloat16, torch.float32) if T < 2000 else (torch.bfloat16,):
             check_product(x, w, dtype, torch.randn(O, generator=torch.Generator().manual_seed(T)).to(gpu_device))
+
+
+def small_and_large_codes(rows, K, seed, device):
+    """Codes of every size down to the smallest, 2^-9."""
+    c = np.random.default_rng(seed).integers(0, 254, (rows, K)).astype(np.uint8)
+    return torch.from_numpy(np.where(c & 127 == 127, 1, c).astype(np.uint8)).to(device)
+
+
+@pytest.mark.parametrize("K,bx", [(1, [250]), (300, [250, 250, 250]), (300, [0, 1, 2]), (300, [4, 254, 127]), (1024, [250, 4, 0, 254, 127, 1, 246, 3])])
+@pytest.mark.parametrize("T", [3, 24, 64, 65, 150])
+def test_exponents_beyond_the_range_of_bf16(gpu_device, T, K, bx):
+    """Bytes 0 to 254 whose products are moderate, for any number of tokens; the values of one operand alone may leave the range."""
+    from paper_2508_13437_amd import dmmv
+
+    O = 70
+    b = torch.tensor([bx], dtype=torch.uint8, device=gpu_device)
+    for g in (1, 128):
+        for d in (0, 7):
+            x = dmmv.BlockMatrix(small_and_large_codes(T, K, T, gpu_device), b.expand(T, -1))
+            w = dmmv.BlockMatrix(small_and_large_codes(O, K, 7, gpu_device), (254 - b.int()).add(d).clamp(0, 254).to(torch.uint8).expand(1 if g == 128 else O, -1), g)
+            for p, q in ((x, w), (dmmv.BlockMatrix(small_and_large_codes(T, K, T, gpu_device), w.scales[:1].expand(T, -1)),
+                                  dmmv.BlockMatrix(small_and_large_codes(O, K, 7, gpu_device), b.expand(O, -1)))):
+                for dtype in (torch.float32, torch.bfloat16):
+                    check_product(p, q, dtype)
+
+
+@pytest.mark.parametrize("T,O,K", ROW_SIZES)
+def test_exponent_bytes_0_and_255(gpu_device, T, O, K):
+    """255 is NaN, for its block's row alone, and 0 is 2^-127, in the 8-bit instructions as in 32 bits."""
+    from paper_2508_13437_amd import dmmv
+
+    nb = -(-K // 128)
+    bx, bw = torch.full((T, nb), 127, dtype=torch.uint8), torch.full((O, nb), 127, dtype=torch.uint8)
+    bx[0, nb - 1] = bw[3, 0] = 0
+    x, w = (dmmv.BlockMatrix(codes_of(n, K, n, gpu_device), s.to(gpu_device)) for n, s in ((T, bx), (O, bw)))
+    kinds = (torch.bfloat16, torch.float32) if T < 2000 else (torch.bfloat16,)
+    for dtype in kinds:
+        check_product(x, w, dtype)
+    want = {dtype: dmmv.dmmv_block_product(x, w, dtype=dtype) for dtype in kinds}
+    x.scales[T - 1, nb // 2], w.scales[O - 2, nb - 1] = 255, 255
+    for dtype in kinds:
+        got = dmmv.dmmv_block_product(x, w, dtype=dtype)
+        assert bool(torch.isnan(got[T - 1]).all()) and bool(torch.isnan(got[:, O - 2]).all())
+        rest = [o for o in range(O) if o != O - 2]
+        assert torch.equal(got[:T - 1, rest], want[dtype][:T - 1, rest])
