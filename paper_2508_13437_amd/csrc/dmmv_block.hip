@@ -62,7 +62,7 @@ BlockView layer_view(const dmmv_block_matrix* q) {
     if (!q) return v;
     v.codes = static_cast<uint8_t*>(q->codes);
     v.ld = q->ld;
-    v.scales = q->scales;
+    v.scales = q->rows == 0 || q->cols == 0 ? nullptr : q->scales;      // (an empty matrix need not have any)
     v.srow = q->scale_row_stride;
     v.sblk = q->scale_block_stride;
     v.e8m0 = q->scale_type == DMMV_E8M0;

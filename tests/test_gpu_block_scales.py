@@ -156,3 +156,22 @@ def test_exponent_bytes_0_and_255(gpu_device, T, O, K):
         assert bool(torch.isnan(got[T - 1]).all()) and bool(torch.isnan(got[:, O - 2]).all())
         rest = [o for o in range(O) if o != O - 2]
         assert torch.equal(got[:T - 1, rest], want[dtype][:T - 1, rest])
+
+
+@pytest.mark.parametrize("T", [4, 40, 150])
+@pytest.mark.parametrize("kind", ["f32", "e8m0"])
+def test_scales_of_a_matrix_without_columns_are_not_read(gpu_device, T, kind):
+    """K = 0 by the C entry with a table of scales that holds NaN: the product is the bias."""
+    from paper_2508_13437_amd import dmmv
+
+    O = 70
+    table = torch.full((256,), float("nan"), device=gpu_device) if kind == "f32" else torch.full((256,), 255, dtype=torch.uint8, device=gpu_device)
+    codes = torch.zeros(256, dtype=torch.uint8, device=gpu_device)
+    empty = lambda rows: dmmv._BlockMatrix(rows, 0, codes.data_ptr(), 0, table.data_ptr(), 1, 0, dmmv.DMMV_F32 if kind == "f32" else dmmv.DMMV_E8M0, 1)  # noqa: E731
+    x, w = empty(T), empty(O)
+    bias = torch.randn(O, generator=torch.Generator().manual_seed(T)).to(gpu_device)
+    for dtype, name in ((torch.float32, dmmv.DMMV_F32), (torch.bfloat16, dmmv.DMMV_BF16)):
+        y = torch.empty(T, O, dtype=dtype, device=gpu_device)
+        dmmv._check(dmmv.load().dmmv_block_product(dmmv.C.addressof(x), dmmv.C.addressof(w), bias.data_ptr(), name, y.data_ptr(), O, None, 0,
+                                                   torch.cuda.current_stream().cuda_stream))
+        assert torch.equal(y, bias.to(dtype).expand(T, O))
