@@ -516,9 +516,14 @@ class BlockMatrix:
     """A matrix in 8 bits: e4m3 codes [rows][cols] (uint8 or float8_e4m3fn) and a scale for every 128
     columns of a row (scale_rows = 1) or of 128 rows (scale_rows = 128).  scales [rows / scale_rows]
     [cols / 128], rounded up, holds exponent bytes (uint8 or float8_e8m0fnu: 2^(byte - 127)) or float32,
-    with any strides: a scale per row is s[:, None].expand(-1, blocks).  None: all 1."""
+    with any strides: a scale per row is s[:, None].expand(-1, blocks).  None: all 1.
 
-    __slots__ = ("codes", "scales", "scale_rows", "rows", "cols", "_c", "_p")
+    It stands for the tensors' memory: numbers written into that are seen (unless the codes' rows are not
+    contiguous: those are copied here).  The tensors themselves and the sizes are fixed; other ones are
+    another BlockMatrix."""
+
+    # (what the calls read is out of reach: codes and scales are given away as views)
+    __slots__ = ("_codes", "_scales", "_scale_rows", "_rows", "_cols", "_c", "_p")
 
     def __init__(self, codes: torch.Tensor, scales: Optional[torch.Tensor] = None, scale_rows: int = 1):
         if codes.dim() != 2:
@@ -529,7 +534,7 @@ class BlockMatrix:
             raise DmmvError(-6, "tensors must live on the GPU")
         if scale_rows not in (1, 128):
             raise DmmvError(-2, "scale_rows must be 1 or 128")
-        codes = _rows(codes)
+        codes = _rows(codes.detach())
         rows, cols = codes.shape
         if scales is None:
             self._fill(codes, None, scale_rows, rows, cols, codes.stride(0), None, 0, 0, DMMV_E8M0)
@@ -541,22 +546,36 @@ class BlockMatrix:
             raise DmmvError(-2, f"scales must be {-(-rows // scale_rows)} x {-(-cols // 128)}")
         if scales.device != codes.device:
             raise DmmvError(-6, "codes and scales are on different devices")
+        scales = scales.detach()
         self._fill(codes, scales, scale_rows, rows, cols, codes.stride(0), scales.data_ptr(), *scales.stride(), kind)
 
     def _fill(self, codes, scales, scale_rows, rows, cols, ld, scales_ptr, row_stride, block_stride, kind):
-        self.codes, self.scales, self.scale_rows = codes, scales, scale_rows
-        self.rows, self.cols = rows, cols
+        self._codes, self._scales, self._scale_rows = codes, scales, scale_rows
+        self._rows, self._cols = rows, cols
         self._c = c = _BlockMatrix(rows, cols, codes.data_ptr(), ld, scales_ptr, row_stride, block_stride, kind, scale_rows)
         self._p = C.addressof(c)
 
     @property
+    def codes(self) -> torch.Tensor:
+        return self._codes.detach()
+
+    @property
+    def scales(self) -> Optional[torch.Tensor]:
+        return None if self._scales is None else self._scales.detach()
+
+    scale_rows = property(lambda self: self._scale_rows)
+    rows = property(lambda self: self._rows)
+    cols = property(lambda self: self._cols)
+
+    @property
     def values8(self) -> torch.Tensor:
         """The codes as float8_e4m3fn."""
-        return self.codes.view(torch.float8_e4m3fn)
+        v = self._codes.view(torch.float8_e4m3fn)
+        return v.detach() if v is self._codes else v
 
     @property
     def device(self) -> torch.device:
-        return self.codes.device
+        return self._codes.device
 
 
 _SCALE_TYPES = {torch.float32: DMMV_F32, torch.uint8: DMMV_E8M0, torch.float8_e8m0fnu: DMMV_E8M0}
@@ -650,8 +669,8 @@ def dmmv_block_quantize(x: torch.Tensor, scale_rows: int = 1, scale_dtype: torch
 def dmmv_block_dequantize(q: BlockMatrix, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """The values that q stands for."""
     kind = _layer_dtype(dtype)
-    x = torch.empty(q.rows, q.cols, dtype=dtype, device=q.codes.device)
-    _enqueue(x.get_device(), load().dmmv_block_dequantize, q._p, kind, x.data_ptr(), q.cols)
+    x = torch.empty(q._rows, q._cols, dtype=dtype, device=q._codes.device)
+    _enqueue(x.get_device(), load().dmmv_block_dequantize, q._p, kind, x.data_ptr(), q._cols)
     return x
 
 
@@ -659,12 +678,12 @@ def dmmv_block_product(x: BlockMatrix, w: BlockMatrix, bias: Optional[torch.Tens
                        dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """y = x w^T + bias, [x.rows][w.rows]."""
     kind = _layer_dtype(dtype)
-    dev = x.codes.get_device()
-    _same(w.codes, dev)
-    T, O = x.rows, w.rows
+    dev = x._codes.get_device()
+    _same(w._codes, dev)
+    T, O = x._rows, w._rows
     b = _vector(bias, O, dev, "bias")
-    y = torch.empty(T, O, dtype=dtype, device=x.codes.device)
-    nbytes = _workspace("dmmv_block_product_workspace_bytes", T, O, x.cols)
+    y = torch.empty(T, O, dtype=dtype, device=x._codes.device)
+    nbytes = _workspace("dmmv_block_product_workspace_bytes", T, O, x._cols)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=y.device) if nbytes else None
     _enqueue(dev, load().dmmv_block_product, x._p, w._p, _addr(b), kind, y.data_ptr(), O, _addr(ws), nbytes)
     return y
@@ -680,12 +699,12 @@ def dmmv_block_backward(dy: torch.Tensor, x: Optional[BlockMatrix], w: Optional[
     dy = _matrix(dy, "dy")
     kind = _layer_dtype(dy.dtype)
     T, O = dy.shape
-    K = w.cols if w is not None else x.cols if x is not None else 0
+    K = w._cols if w is not None else x._cols if x is not None else 0
     dev, on = dy.get_device(), dy.device
     if dw:
-        _same(x.codes, dev)
+        _same(x._codes, dev)
     if dx:
-        _same(w.codes, dev)
+        _same(w._codes, dev)
     gx = torch.empty(T, K, dtype=dy.dtype, device=on) if dx else None
     gw = torch.empty(O, K, dtype=torch.float32, device=on) if dw else None
     gb = torch.empty(O, dtype=torch.float32, device=on) if dbias else None
@@ -734,9 +753,9 @@ def dmmv_layernorm_backward(dy: torch.Tensor, x, gamma: Optional[torch.Tensor], 
     T, F = dy.shape
     dev, on = dy.get_device(), dy.device
     if isinstance(x, BlockMatrix):
-        if x.rows != T or x.cols != F:
-            raise DmmvError(-2, f"x is {x.rows} x {x.cols}, expected {T} x {F}")
-        _same(x.codes, dev)
+        if x._rows != T or x._cols != F:
+            raise DmmvError(-2, f"x is {x._rows} x {x._cols}, expected {T} x {F}")
+        _same(x._codes, dev)
         px, ldx, pq = None, 0, x._p
     else:
         x = _matrix(x, "x")
