@@ -246,13 +246,17 @@ __global__ __launch_bounds__(THREADS) void k_layernorm_grad(int64_t rows, int64_
         for (int e = 0; e < 8; ++e) a[e] = nd.get(e);
         nx.get(in, row, col, cols, h);
         request(r0 + gridDim.x * (int64_t)TEAMS);    // (past the last: the last again)
-        // (past the row's end dy is zero, and so is what follows from it)
         float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] = (h[e] - mu) * rs;
+        // past the row's end dy is zero, and so is what follows from it, if h is not infinite
+        if (col + 8 > cols)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[e] = col + e < cols ? h[e] : 0.0f;
         if (there)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float d = a[e];
-                h[e] = (h[e] - mu) * rs;
                 dg[e] = dmmv_fma(d, h[e], dg[e]);
                 db[e] += d;
                 a[e] = d * g[e];
@@ -319,9 +323,9 @@ __global__ __launch_bounds__(256) void k_layernorm_grad_sums(int64_t cols, const
         if (gamma) load8(gamma, col, cols, g);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float a = d[e] * g[e];
+            const float a = d[e] * g[e], h = col + e < cols ? (v[e] - mu) * rs : 0.0f;
             s1 += a;
-            s2 = dmmv_fma(a, (v[e] - mu) * rs, s2);
+            s2 = dmmv_fma(a, h, s2);
         }
     }
     s1 = team_sum<256>(s1, sh);
