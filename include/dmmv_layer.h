@@ -80,8 +80,12 @@ dmmv_status dmmv_block_product(const dmmv_block_matrix* x, const dmmv_block_matr
  * Each of the three may be NULL.  They are the gradients with respect to the values that the 8-bit
  * matrices stand for.  T, O, K are the sizes.  Every product is exact or rounded to 24 bits; bf16 dx and scales that are the same
  * along a row of w: to 16.  The workspace (256-byte aligned) holds partial sums, and dy as up to three bf16 parts and
- * codes with aligned rows where a large gradient is made from those. */
+ * codes with aligned rows where a large gradient is made from those.  ..._for is what the call with these arguments needs (dx
+ * and dw are asked for if not NULL; nothing is read but the two descriptors), some 2 MB for a large one in bf16 with aligned rows and scales that are
+ * powers of two; 0 where the call would be refused.  ..._bytes serves every call of these sizes. */
 size_t dmmv_block_backward_workspace_bytes(int64_t T, int64_t O, int64_t K);
+size_t dmmv_block_backward_workspace_for(int32_t dtype, int64_t T, int64_t O, int64_t K, const void* dy, int64_t lddy,
+                                         const dmmv_block_matrix* x, const dmmv_block_matrix* w, const void* dx, const float* dw);
 dmmv_status dmmv_block_backward(int32_t dtype, int64_t T, int64_t O, int64_t K, const void* dy, int64_t lddy,
                                 const dmmv_block_matrix* x, const dmmv_block_matrix* w, void* dx, int64_t lddx, float* dw,
                                 int64_t lddw, float* dbias, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -653,14 +653,62 @@ static size_t lay_bytes(int64_t T, int64_t O, int64_t K) {
     const int64_t rows = T > O ? T : O;
     return (size_t)((dx3 || dw3 ? 3 : 1) * up(T, 128) * up(O, 128) * 2) + (size_t)(rows * up(K, 16));
 }
-// one after the other: dx, dw and dbias use the same bytes
+static size_t bias_bytes(int64_t T, int64_t O) { return T > 0 && O > 0 ? ((size_t)bias_strips(T, O) * O * 4 + 255) / 256 * 256 : 0; }
+// Any call of these sizes; dx, dw and dbias use the same bytes one after the other
 static size_t backward_workspace(int64_t T, int64_t O, int64_t K) {
     if (T <= 0 || O <= 0) return 0;
-    size_t n = ((size_t)bias_strips(T, O) * O * 4 + 255) / 256 * 256;
+    size_t n = bias_bytes(T, O);
     const size_t small = lay_small_bytes(T, O), gx = small + grad_part_bytes(T, K, O), gw = small + grad_part_bytes(O, K, T), lay = K > 0 ? (lay_bytes(T, O, K) + 255) / 256 * 256 : 0;
     if (gx > n) n = gx;
     if (gw > n) n = gw;
     return lay > n ? lay : n;
+}
+
+// How a gradient is made, and the bytes that takes: what the call does and what its workspace is measured by.
+struct GradPlan {
+    enum Path { NOTHING, DIRECT, LAID, LAID_SMALL, GENERAL } path;
+    bool exact, codes_aligned;           // scales that are powers of two; rows of whole aligned chunks
+    int parts;                           // bf16 parts of dy
+    size_t bytes;
+};
+// trans: dw [O][K] from x [T][K]; else dx [T][K] from w [O][K]
+static GradPlan grad_plan(bool trans, int32_t dtype, int64_t T, int64_t O, int64_t K, const void* dy, int64_t ld, const dmmv_block_matrix* b) {
+    GradPlan p = {GradPlan::NOTHING, false, false, 1, 0};
+    const int64_t M = trans ? O : T, Kc = trans ? T : O;
+    if (M == 0 || K == 0) return p;
+    const bool f32 = dtype == DMMV_F32, f32_result = f32 || trans;
+    p.exact = !b->scales || b->scale_type == DMMV_E8M0;
+    p.codes_aligned = K % 16 == 0 && b->ld % 16 == 0 && (uintptr_t)b->codes % 16 == 0 && b->ld < 1 << 23;
+    // (offsets of 24 x 24 bits, of 32 bits along a row)
+    const bool near = !b->scales || (b->scale_row_stride < 1 << 23 && b->scale_block_stride < 1 << 23 && ceil_div(K, 128) * b->scale_block_stride < 1 << 30);
+    const bool dy_aligned = O % 8 == 0 && ld % 8 == 0 && ld < 1 << 22 && (uintptr_t)dy % 16 == 0;
+    if (!f32 && p.exact && near && p.codes_aligned && dy_aligned && large_tiles(M, K, Kc, 1, 0.0)) {
+        p.path = GradPlan::DIRECT;
+        return p;
+    }
+    const bool rowwise = !p.exact && (b->scale_block_stride == 0 || K <= 128);
+    p.parts = f32 ? 3 : p.exact ? 1 : f32_result ? 3 : 2;
+    const int64_t Tp = up(T, 128), Op = up(O, 128);
+    const bool fits = K < 1 << 22 && Op < 1 << 22 && Tp <= 1 << 25 && Kc > 0;
+    if ((p.exact ? near : rowwise) && fits && large_tiles(M, K, Kc, p.parts, 2.0 * T * O) && large_tiles(M, K, Kc, p.parts == 1 ? 1 : 3, 2.0 * T * O)) {
+        p.path = GradPlan::LAID;
+        p.bytes = (size_t)p.parts * Tp * Op * 2 + (p.codes_aligned ? 0 : (size_t)Kc * up(K, 16));
+    } else if (f32 && (p.exact || rowwise) && fits && lay_small(T, O, K, p.exact)) {
+        p.path = GradPlan::LAID_SMALL;
+        p.bytes = lay_small_bytes(T, O) + grad_part_bytes(M, K, Kc);
+    } else {
+        p.path = GradPlan::GENERAL;
+        p.bytes = grad_part_bytes(M, K, Kc);
+    }
+    return p;
+}
+// a call with these arguments (checked)
+static size_t backward_needs(int32_t dtype, int64_t T, int64_t O, int64_t K, const void* dy, int64_t lddy, const dmmv_block_matrix* x,
+                             const dmmv_block_matrix* w, bool dx, bool dw) {
+    size_t n = bias_bytes(T, O);
+    const size_t a = dx ? grad_plan(false, dtype, T, O, K, dy, lddy, w).bytes : 0, b = dw ? grad_plan(true, dtype, T, O, K, dy, lddy, x).bytes : 0;
+    if (a > n) n = a;
+    return b > n ? b : n;
 }
 
 template <class TA, bool TRANS, int PA, int PB, class TC>
@@ -716,55 +764,50 @@ static dmmv_status lay_gradient(int64_t T, int64_t O, const TA* dy, int64_t ld, 
 template <class TA, bool TRANS, class TC>
 static dmmv_status grad(int64_t T, int64_t O, int64_t K, const TA* dy, int64_t ld, const dmmv_block_matrix* b, TC* c, int64_t ldc, char* ws,
                         bool* laid, hipStream_t s) {
-    const int64_t M = TRANS ? O : T, Kc = TRANS ? T : O;
-    if (M == 0 || K == 0) return DMMV_OK;
     constexpr int PA = sizeof(TA) == 4 ? 3 : 1;
-    const bool exact = !b->scales || b->scale_type == DMMV_E8M0;
-    const bool codes_aligned = K % 16 == 0 && b->ld % 16 == 0 && (uintptr_t)b->codes % 16 == 0 && b->ld < 1 << 23;
-    // (offsets of 24 x 24 bits, of 32 bits along a row)
-    const bool near = !b->scales || (b->scale_row_stride < 1 << 23 && b->scale_block_stride < 1 << 23 && ceil_div(K, 128) * b->scale_block_stride < 1 << 30);
-    const bool dy_aligned = O % 8 == 0 && ld % 8 == 0 && ld < 1 << 22 && (uintptr_t)dy % 16 == 0;
-    if constexpr (PA == 1)
-        if (exact && near && codes_aligned && dy_aligned && large_tiles(M, K, Kc, 1, 0.0))
-            return grad_tiled<TRANS, TC>(M, K, Kc, dy, ld, 1, 0, layer_view(b), Kc, c, ldc, s);
-    const bool rowwise = !exact && (b->scale_block_stride == 0 || K <= 128);
-    const int parts = PA == 3 ? 3 : exact ? 1 : sizeof(TC) == 2 ? 2 : 3;
-    const int64_t Tp = up(T, 128), Op = up(O, 128);
+    const GradPlan plan = grad_plan(TRANS, PA == 3 ? DMMV_F32 : DMMV_BF16, T, O, K, dy, ld, b);
+    const int64_t M = TRANS ? O : T, Kc = TRANS ? T : O, Tp = up(T, 128), Op = up(O, 128);
     uint16_t* lay = reinterpret_cast<uint16_t*>(ws);
     BlockView v = layer_view(b);
     // dy in parts, at the workspace's start; scales that are the same along a row go into it
     auto lay_out = [&]() {
         constexpr int BY = TRANS ? 2 : 1;
-        if (exact && *laid) return DMMV_OK;
-        *laid = exact;
-        if (exact) return lay_gradient<TA, PA, 0>(T, O, dy, ld, v, lay, s);
+        if (plan.exact && *laid) return DMMV_OK;
+        *laid = plan.exact;
+        if (plan.exact) return lay_gradient<TA, PA, 0>(T, O, dy, ld, v, lay, s);
         BlockView by = v;
         v.scales = nullptr;
-        if (parts == 2) return lay_gradient<TA, 2, BY>(T, O, dy, ld, by, lay, s);
+        if (plan.parts == 2) return lay_gradient<TA, 2, BY>(T, O, dy, ld, by, lay, s);
         return lay_gradient<TA, 3, BY>(T, O, dy, ld, by, lay, s);
     };
-    const bool fits = K < 1 << 22 && Op < 1 << 22 && Tp <= 1 << 25 && Kc > 0;
-    if ((exact ? near : rowwise) && fits && large_tiles(M, K, Kc, parts, 2.0 * T * O) && large_tiles(M, K, Kc, parts == 1 ? 1 : 3, 2.0 * T * O)) {
+    switch (plan.path) {
+    case GradPlan::NOTHING: return DMMV_OK;
+    case GradPlan::DIRECT:
+        if constexpr (PA == 1) return grad_tiled<TRANS, TC>(M, K, Kc, dy, ld, 1, 0, v, Kc, c, ldc, s);
+        break;
+    case GradPlan::LAID:
         DMMV_TRY(lay_out());
-        if (!codes_aligned) {
+        if (!plan.codes_aligned) {
             const int64_t Kp = up(K, 16);
-            uint8_t* to = reinterpret_cast<uint8_t*>(lay + (size_t)parts * Tp * Op);
+            uint8_t* to = reinterpret_cast<uint8_t*>(lay + (size_t)plan.parts * Tp * Op);
             DMMV_TRY(layer_lay_codes(b, to, Kp, s));
             v.codes = to;
             v.ld = Kp;
         }
-        return grad_tiled<TRANS, TC>(M, K, TRANS ? Tp : Op, reinterpret_cast<const bf16_t*>(lay), Op, parts, Tp * Op, v, Kc, c, ldc, s);
-    }
-    if constexpr (PA == 3)
-        if ((exact || rowwise) && fits && lay_small(T, O, K, exact)) {
+        return grad_tiled<TRANS, TC>(M, K, TRANS ? Tp : Op, reinterpret_cast<const bf16_t*>(lay), Op, plan.parts, Tp * Op, v, Kc, c, ldc, s);
+    case GradPlan::LAID_SMALL:
+        if constexpr (PA == 3) {
             DMMV_TRY(lay_out());
             return grad_any<bf16_t, TRANS, 3, 1, TC>(M, K, Kc, reinterpret_cast<const bf16_t*>(lay), Op, v, c, ldc,
                                                      reinterpret_cast<float*>(ws + lay_small_bytes(T, O)), s, Tp * Op);
         }
+        break;
+    case GradPlan::GENERAL: break;
+    }
     *laid = false;                                   // the slices go there
     float* part = reinterpret_cast<float*>(ws);
-    return exact ? grad_any<TA, TRANS, PA, 1, TC>(M, K, Kc, dy, ld, v, c, ldc, part, s)
-                 : grad_any<TA, TRANS, PA, 3, TC>(M, K, Kc, dy, ld, v, c, ldc, part, s);
+    return plan.exact ? grad_any<TA, TRANS, PA, 1, TC>(M, K, Kc, dy, ld, v, c, ldc, part, s)
+                      : grad_any<TA, TRANS, PA, 3, TC>(M, K, Kc, dy, ld, v, c, ldc, part, s);
 }
 
 template <class T>
@@ -798,9 +841,8 @@ extern "C" size_t dmmv_block_backward_workspace_bytes(int64_t T, int64_t O, int6
     return backward_workspace(T, O, K);
 }
 
-extern "C" dmmv_status dmmv_block_backward(int32_t dtype, int64_t T, int64_t O, int64_t K, const void* dy, int64_t lddy,
-                                           const dmmv_block_matrix* x, const dmmv_block_matrix* w, void* dx, int64_t lddx, float* dw,
-                                           int64_t lddw, float* dbias, void* workspace, size_t workspace_bytes, void* hip_stream) {
+static dmmv_status check_backward(int32_t dtype, int64_t T, int64_t O, int64_t K, const void* dy, int64_t lddy, const dmmv_block_matrix* x,
+                                  const dmmv_block_matrix* w, const void* dx, int64_t lddx, const float* dw, int64_t lddw) {
     DMMV_TRY(layer_check_dtype(dtype));
     DMMV_TRY(layer_check_sizes(T, O, "dy"));
     DMMV_TRY(layer_check_sizes(O, K, "w"));
@@ -816,8 +858,24 @@ extern "C" dmmv_status dmmv_block_backward(int32_t dtype, int64_t T, int64_t O, 
         if (x->rows != T || x->cols != K) return fail(DMMV_ERR_SHAPE, "x is not %lld x %lld", (long long)T, (long long)K);
         DMMV_TRY(layer_check_array(dw, O, K, lddw, 4, "dw"));
     }
+    return DMMV_OK;
+}
+
+extern "C" size_t dmmv_block_backward_workspace_for(int32_t dtype, int64_t T, int64_t O, int64_t K, const void* dy, int64_t lddy, const dmmv_block_matrix* x,
+                                                    const dmmv_block_matrix* w, const void* dx, const float* dw) {
+    alignas(16) static const float wanted[4] = {};   // (any place will do for results that are asked for)
+    dx = dx ? wanted : nullptr;
+    dw = dw ? wanted : nullptr;
+    if (check_backward(dtype, T, O, K, dy, lddy, x, w, dx, K, dw, K) != DMMV_OK) return 0;
+    return backward_needs(dtype, T, O, K, dy, lddy, x, w, dx, dw);
+}
+
+extern "C" dmmv_status dmmv_block_backward(int32_t dtype, int64_t T, int64_t O, int64_t K, const void* dy, int64_t lddy,
+                                           const dmmv_block_matrix* x, const dmmv_block_matrix* w, void* dx, int64_t lddx, float* dw,
+                                           int64_t lddw, float* dbias, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    DMMV_TRY(check_backward(dtype, T, O, K, dy, lddy, x, w, dx, lddx, dw, lddw));
     if ((uintptr_t)dbias % 4) return fail(DMMV_ERR_SHAPE, "dbias is not aligned to its elements");
-    DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, backward_workspace(T, O, K)));
+    DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, backward_needs(dtype, T, O, K, dy, lddy, x, w, dx, dw)));
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     if (dtype == DMMV_F32)
         return backward(T, O, K, static_cast<const float*>(dy), lddy, x, w, static_cast<float*>(dx), lddx, dw, lddw, dbias, workspace, s);

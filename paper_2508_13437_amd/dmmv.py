@@ -31,7 +31,7 @@ EXPORTS = ("dmmv_workspace_bytes", "dmmv_create", "dmmv_destroy", "dmmv_set_x",
            "dmmv_l2_changes",
            "dmmv_time_eval", "dmmv_time_l2", "dmmv_loop_in_use", "dmmv_scoring_in_use",
            "dmmv_block_quantize", "dmmv_block_dequantize", "dmmv_block_product_workspace_bytes",
-           "dmmv_block_product", "dmmv_block_backward_workspace_bytes", "dmmv_block_backward",
+           "dmmv_block_product", "dmmv_block_backward_workspace_bytes", "dmmv_block_backward_workspace_for", "dmmv_block_backward",
            "dmmv_layernorm", "dmmv_layernorm_workspace_bytes", "dmmv_layernorm_backward",
            "dmmv_last_error",
            "dmmv_version")
@@ -126,6 +126,8 @@ def load() -> C.CDLL:
         fn = getattr(lib, name)
         fn.restype = C.c_size_t
         fn.argtypes = [i64] * nargs
+    lib.dmmv_block_backward_workspace_for.restype = C.c_size_t
+    lib.dmmv_block_backward_workspace_for.argtypes = [i32, i64, i64, i64, p, i64, p, p, p, p]
     lib.dmmv_last_error.restype = C.c_char_p
     lib.dmmv_version.restype = C.c_char_p
     _lib = lib
@@ -708,10 +710,10 @@ def dmmv_block_backward(dy: torch.Tensor, x: Optional[BlockMatrix], w: Optional[
     gx = torch.empty(T, K, dtype=dy.dtype, device=on) if dx else None
     gw = torch.empty(O, K, dtype=torch.float32, device=on) if dw else None
     gb = torch.empty(O, dtype=torch.float32, device=on) if dbias else None
-    nbytes = _workspace("dmmv_block_backward_workspace_bytes", T, O, K)
+    lib, px, pw, ax, aw = load(), x._p if dw else None, w._p if dx else None, _addr(gx), _addr(gw)
+    nbytes = lib.dmmv_block_backward_workspace_for(kind, T, O, K, dy.data_ptr(), dy.stride(0), px, pw, ax, aw)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=on) if nbytes else None
-    _enqueue(dev, load().dmmv_block_backward, kind, T, O, K, dy.data_ptr(), dy.stride(0), x._p if dw else None,
-             w._p if dx else None, _addr(gx), K, _addr(gw), K, _addr(gb), _addr(ws), nbytes)
+    _enqueue(dev, lib.dmmv_block_backward, kind, T, O, K, dy.data_ptr(), dy.stride(0), px, pw, ax, K, aw, K, _addr(gb), _addr(ws), nbytes)
     return gx, gw, gb
 
 
