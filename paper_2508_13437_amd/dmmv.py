@@ -759,6 +759,8 @@ def dmmv_layernorm_backward(dy: torch.Tensor, x, gamma: Optional[torch.Tensor], 
             raise DmmvError(-2, f"x is {x._rows} x {x._cols}, expected {T} x {F}")
         _same(x._codes, dev)
         px, ldx, pq = None, 0, x._p
+    elif x is None:
+        raise DmmvError(-1, "x is None")
     else:
         x = _matrix(x, "x")
         if x.dtype != dy.dtype:
@@ -767,6 +769,8 @@ def dmmv_layernorm_backward(dy: torch.Tensor, x, gamma: Optional[torch.Tensor], 
             raise DmmvError(-2, f"x is {x.shape[0]} x {x.shape[1]}, expected {T} x {F}")
         _same(x, dev)
         px, ldx, pq = x.data_ptr(), x.stride(0), None
+    if mean is None or rstd is None:
+        raise DmmvError(-1, "mean and rstd are those of the forward pass, not None")
     g, mu, rs = _vector(gamma, F, dev, "gamma"), _vector(mean, T, dev, "mean"), _vector(rstd, T, dev, "rstd")
     gx = torch.empty(T, F, dtype=dy.dtype, device=on) if dx else None
     gg = torch.empty(F, dtype=torch.float32, device=on) if dgamma else None

@@ -32,3 +32,14 @@ def test_gradient_of_rows_without_variance_far_from_zero(gpu_device, rows, cols,
     half = 2.0 ** -8 if dtype == torch.bfloat16 else U
     assert (np.abs(dx - want[0]) <= e + half * 1.01 * (np.abs(want[0]) + e)).all()
     assert (dgamma == 0).all() and (np.abs(dbeta - want[2]) <= (rows + 20) * U * np.abs(f64(dy)).sum(0)).all()
+
+
+def test_missing_arguments_are_refused(gpu_device):
+    from paper_2508_13437_amd import dmmv
+
+    x = torch.randn(4, 200, device=gpu_device)
+    r = dmmv.dmmv_layernorm(x, xq=True)
+    for args in ((x, None, None, r.mean, r.rstd), (x, x, None, None, r.rstd), (x, r.xq, None, r.mean, None)):
+        with pytest.raises(dmmv.DmmvError) as e:
+            dmmv.dmmv_layernorm_backward(*args)
+        assert e.value.status == -1
