@@ -27,8 +27,9 @@
  * all work enqueued on the given hipStream_t (NULL = the default stream) without waiting, statuses
  * and dmmv_last_error().  Matrices are row-major with a row stride >= the columns, any alignment
  * their element type allows; 16-byte aligned rows are the fast ones.  Inputs and outputs do not
- * overlap.  Empty matrices are allowed.  Sums are held in 32 bits, in an order that sizes, types and
- * alignments fix: equal calls give equal bits.  NaN and infinities of the inputs stay visible in what depends on them.
+ * overlap.  Empty matrices are allowed.  Sums are held in 32 bits (what bf16 products of 8-bit matrices lose on the
+ * way there stands at dmmv_block_product), in an order that sizes, types and alignments fix: equal calls give equal
+ * bits.  NaN and infinities of the inputs stay visible in what depends on them.
  */
 #ifndef DMMV_LAYER_H
 #define DMMV_LAYER_H
@@ -57,18 +58,22 @@ typedef struct {
  * |x| of a block's finite values, its scale is the smallest power of two >= a / 448, at least 2^-126,
  * and 1 if a = 0; a code is x / scale (exact) rounded to the nearest e4m3 value, ties to even; NaN and
  * infinities become the NaN code.  Powers of two cost no significant bit of a floating-point code,
- * and code * scale is then exact in bf16. */
+ * and code * scale is then exact in bf16 where it is a multiple of 2^-133 (blocks whose largest |x| is over 2^-116 have
+ * no other).  Beyond 248 * 2^120 the nearest value is 2^128, infinite when restored. */
 dmmv_status dmmv_block_quantize(int32_t dtype, const void* x, int64_t ldx, const dmmv_block_matrix* q, void* hip_stream);
 
-/* x <- the values of q, rounded once to dtype (exact for scales that are powers of two, down to the
- * type's smallest number). */
+/* x <- the values of q, rounded once to dtype (exact for scales that are powers of two, between the
+ * type's smallest number and its largest). */
 dmmv_status dmmv_block_dequantize(const dmmv_block_matrix* q, int32_t dtype, void* x, int64_t ldx, void* hip_stream);
 
 /* y[t][o] = sum_k x(t, k) w(o, k) + bias[o], x [T][K], w [O][K], y [T][ldy] of dtype DMMV_F32 or
  * DMMV_BF16, bias float [O] or NULL.  A 32-bit result is summed in 32 bits; a bf16 result by the 8-bit
- * matrix instructions, whose sums carry an error of about 5e-5 of the result's norm before the rounding
- * to bf16 (1.7e-3).  The workspace (size from the HOST function, 0 is possible, 256-byte aligned) holds the operands of a
- * large product once more where their rows are no multiples of 16 codes, and partial sums where few tiles share a long contraction. */
+ * matrix instructions, which drop what lies some 13 bits below the largest product of a step: an error
+ * of about 5e-5 of the result's norm, up to 2^-11 of sum |x w| for a single one, before the rounding to
+ * bf16 (1.7e-3).  Who needs the sum takes it in 32 bits.  Scales may be far apart: what counts is that
+ * the products x w, their sum and the result are in the range.  The workspace (size from the HOST
+ * function, 0 is possible, 256-byte aligned) holds the operands of a large product once more where
+ * their rows are no multiples of 16 codes, and partial sums where few tiles share a long contraction. */
 size_t dmmv_block_product_workspace_bytes(int64_t T, int64_t O, int64_t K);
 dmmv_status dmmv_block_product(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, int32_t dtype,
                                void* y, int64_t ldy, void* workspace, size_t workspace_bytes, void* hip_stream);
@@ -78,11 +83,16 @@ dmmv_status dmmv_block_product(const dmmv_block_matrix* x, const dmmv_block_matr
  *   dw[o][k] = sum_t dy[t][o] x(t, k)       [O][lddw] float        (x may be NULL if dw is)
  *   dbias[o] = sum_t dy[t][o]               [O] float
  * Each of the three may be NULL.  They are the gradients with respect to the values that the 8-bit
- * matrices stand for.  T, O, K are the sizes.  Every product is exact or rounded to 24 bits; bf16 dx and scales that are the same
- * along a row of w: to 16.  The workspace (256-byte aligned) holds partial sums, and dy as up to three bf16 parts and
- * codes with aligned rows where a large gradient is made from those.  ..._for is what the call with these arguments needs (dx
- * and dw are asked for if not NULL; nothing is read but the two descriptors), some 2 MB for a large one in bf16 with aligned rows and scales that are
- * powers of two; 0 where the call would be refused.  ..._bytes serves every call of these sizes. */
+ * matrices stand for.  T, O, K are the sizes.  Every product is exact or rounded to 24 bits; with bf16
+ * dx and 32-bit scales that are the same along a row of w it may come from 16 (dx has 8).  They are
+ * made of bf16 numbers: values of exponents are exact for bytes 3 to 246 and multiples of 2^-133 below
+ * (infinite beyond the type's largest); of dy, of values with 32-bit scales and of dy times the scale
+ * of a row 24 bits count from 2^-110 up, multiples of 2^-133 below.  The workspace (256-byte aligned)
+ * holds partial sums, and dy as up to three bf16 parts and codes with aligned rows where a large
+ * gradient is made from those.  ..._for is what the call with these arguments needs (dx and dw are
+ * asked for if not NULL; nothing is read but the two descriptors), some 2 MB for a large one in bf16
+ * with aligned rows and scales that are powers of two; 0 where the call would be refused.  ..._bytes
+ * serves every call of these sizes. */
 size_t dmmv_block_backward_workspace_bytes(int64_t T, int64_t O, int64_t K);
 size_t dmmv_block_backward_workspace_for(int32_t dtype, int64_t T, int64_t O, int64_t K, const void* dy, int64_t lddy,
                                          const dmmv_block_matrix* x, const dmmv_block_matrix* w, const void* dx, const float* dw);

@@ -526,7 +526,8 @@ __global__ __launch_bounds__(256) void k_block_grad_tiled(int64_t M, int64_t N, 
     }
 }
 
-// dy as PARTS bf16 parts that sum to it (32 bits, or bf16 times scales of 32 bits; two keep 16 bits, for results in bf16), or as
+// dy as PARTS bf16 parts that sum to it (32 bits, or bf16 times scales of 32 bits; two keep 16 bits, for results in bf16: what they cut off
+// is under 2^-15 of sum |dy w|, where dy itself has been rounded to 2^-8 and dx will be, and a third part costs half as much again), or as
 // it is, [Tp][Op] each with zeros in the margin.  A scale that is the same along a row of the block matrix belongs to
 // a place of the contraction: BY 1, a column of dy (dx); BY 2, a row (dw).  Bound by memory at large sizes; 777 x 1365 6.6 us.
 template <class T, int PARTS, int BY>
