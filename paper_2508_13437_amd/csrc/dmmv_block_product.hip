@@ -334,7 +334,7 @@ constexpr int product_lds(int MI, int NI, int width, int ws, int nst) {
     return stages > out ? stages : out;
 }
 
-template <class T, int MI, int NI, bool SCALED, int WS, int NST>
+template <class T, int MI, int NI, int WS, int NST>
 __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
                                                              const float* __restrict__ bias, T* __restrict__ y, int64_t ldy,
                                                              int32_t tiles_t, int32_t tiles_o) {
@@ -382,7 +382,7 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
     uint32_t sx[MI], sw[NS];
     // Exponents of scales that are the same along a row, for all blocks: a row of the table a thread; requested ahead of the codes
     static_assert(WS == 0 ? BM + BN <= 256 : BM <= 256, "a thread has one row");
-    const bool mine_x = tid < BM, fills = SCALED && (mine_x ? !how.x_blocks : WS == 0 && !how.w_blocks);
+    const bool mine_x = tid < BM, fills = mine_x ? !how.x_blocks : WS == 0 && !how.w_blocks;
     float along = 1.0f, along_w[WS == 2 ? NS : 1];
     if (fills) along = mine_x ? scale_at(x, min(t0 + tid, T_ - 1), 0) : scale_at(w, min(o0 + tid - BM, O - 1), 0);
     if constexpr (WS == 2)
@@ -498,7 +498,7 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
             }
         }
         scales_along();
-        if (SCALED) BP_SCALES_STAGE(0);
+        BP_SCALES_STAGE(0);
         lds_requests_left<LEFT>();
         __syncthreads();
 #pragma unroll
@@ -511,7 +511,7 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
         for (int kb = 0;;) {
             const int end = min(kb + SB, paired);
             for (; kb < end; kb += 2) {
-                if (SCALED) BP_SCALES_TAKE(kb);
+                BP_SCALES_TAKE(kb);
                 const int at = NST == 2 ? 0 : (kb & (NST - 1)) * STAGE, after = NST == 2 ? 0 : ((kb + 2) & (NST - 1)) * STAGE;
                 const int before = NST == 2 ? STAGE : ((kb - 1) & (NST - 1)) * STAGE;
                 step(C0, C1, at, at + STAGE, before, kb + NST);
@@ -519,7 +519,7 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
             }
             if (kb >= paired) break;
             __syncthreads();
-            if (SCALED) BP_SCALES_STAGE(kb);
+            BP_SCALES_STAGE(kb);
             __syncthreads();
         }
         lds_requests_left<0>();
@@ -530,7 +530,7 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
         const int left = (int)(K - kb * 128ll) - cchunk * 16;
         __syncthreads();
         if (paired == 0 && kb == 0) scales_along();
-        if (SCALED && (kb == paired && (kb & (SB - 1)) == 0)) BP_SCALES_STAGE(kb);
+        if (kb == paired && (kb & (SB - 1)) == 0) BP_SCALES_STAGE(kb);
 #pragma unroll 1
         for (int q = 0; q < MI; ++q) {
             const uint32_t row = 8 * (wv * MI + q) + crow;
@@ -539,8 +539,8 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
             *reinterpret_cast<piece16*>(to + BM * 128) = chunk_tail(wb + kb * 128ll + min(row, lastw) * ldw + cchunk * 16, left, kb * 128ll + cchunk * 16);
         }
         __syncthreads();
-        if (SCALED) BP_SCALES_TAKE(kb & ~1);
-        if (SCALED && (kb & 1)) {
+        BP_SCALES_TAKE(kb & ~1);
+        if (kb & 1) {
 #pragma unroll
             for (int j = 0; j < MI; ++j) sx[j] >>= 8;
 #pragma unroll
@@ -568,11 +568,11 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
         for (int e = 0; e < 4; ++e) {
             const int64_t o = min(o0 + wo + 16 * i + lg * 4 + e, O - 1);
             bo[e] = bias ? bias[o] : 0.0f;
-            so[e] = SCALED && !how.w_blocks ? row_scale(scale_at(w, o, 0)).rest : 1.0f;
+            so[e] = !how.w_blocks ? row_scale(scale_at(w, o, 0)).rest : 1.0f;
         }
 #pragma unroll
         for (int j = 0; j < MI; ++j) {
-            const float st = SCALED && !how.x_blocks ? row_scale(scale_at(x, min(t0 + wt + 16 * j + lr, T_ - 1), 0)).rest : 1.0f;
+            const float st = !how.x_blocks ? row_scale(scale_at(x, min(t0 + wt + 16 * j + lr, T_ - 1), 0)).rest : 1.0f;
             float v[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = dmmv_fma(acc[i][j][e] * so[e], st, bo[e]);
@@ -807,16 +807,16 @@ __global__ __launch_bounds__(256) void k_block_product_join(int64_t T_, int64_t 
     store8(y + t * ldy, o, O, v);
 }
 
-template <class T, int MI, int NI, bool SCALED, int WS, int NST>
+template <class T, int MI, int NI, int WS, int NST>
 static dmmv_status launch_tiled(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, T* y, int64_t ldy, hipStream_t s,
                                 int32_t shares = 1) {
     const int64_t tiles_t = ceil_div(x->rows, 32 * MI), tiles_o = ceil_div(w->rows, 32 * NI);
     if (tiles_t > INT32_MAX / 4 / tiles_o) return fail(DMMV_ERR_SHAPE, "y: more tiles than a launch takes");
-    const void* kern = (const void*)k_block_product_tiled<T, MI, NI, SCALED, WS, NST>;
+    const void* kern = (const void*)k_block_product_tiled<T, MI, NI, WS, NST>;
     constexpr int bytes = product_lds(MI, NI, sizeof(T), WS, NST);
     DMMV_TRY(ensure_dynamic_lds(kern, bytes));
     const ProductScales how = {!constant_rows(x), !constant_rows(w)};
-    hipLaunchKernelGGL((k_block_product_tiled<T, MI, NI, SCALED, WS, NST>), dim3((unsigned)(tiles_t * tiles_o), (unsigned)shares), dim3(256), bytes, s, x->rows, w->rows,
+    hipLaunchKernelGGL((k_block_product_tiled<T, MI, NI, WS, NST>), dim3((unsigned)(tiles_t * tiles_o), (unsigned)shares), dim3(256), bytes, s, x->rows, w->rows,
                        x->cols, layer_view(x), layer_view(w), how, bias, y, ldy, (int32_t)tiles_t, (int32_t)tiles_o);
     DMMV_LAUNCH_CHECK();
     return DMMV_OK;
@@ -846,7 +846,7 @@ static dmmv_status product_tiled(const dmmv_block_matrix* x, const dmmv_block_ma
                                  hipStream_t s) {
     const int32_t shares = part ? product_shares(x->rows, w->rows, x->cols) : 1;
     if (shares > 1) {
-        DMMV_TRY((launch_tiled<float, 4, 4, true, 0, 4>(x, w, nullptr, part, w->rows, s, shares)));
+        DMMV_TRY((launch_tiled<float, 4, 4, 0, 4>(x, w, nullptr, part, w->rows, s, shares)));
         hipLaunchKernelGGL(k_block_product_join, dim3((unsigned)ceil_div(x->rows, 4), (unsigned)ceil_div(w->rows, 512)), dim3(256), 0, s, x->rows,
                            w->rows, shares, part, bias, y, ldy);
         DMMV_LAUNCH_CHECK();
@@ -860,8 +860,8 @@ static dmmv_status product_tiled(const dmmv_block_matrix* x, const dmmv_block_ma
     // a round of large tiles takes 2.25 times one of small ones (K = 4096: 46 us and 20.5; 1024 x 4096 x 11008 54 and 62 us,
     // 2048 x 4096 x 4096 51 and 44)
     if ((along || w->scale_rows == 128) && 9 * ceil_div(large, cus) < 4 * ceil_div(small, cus))
-        return along ? launch_tiled<bf16_t, 8, 8, true, 2, 2>(x, w, bias, y, ldy, s) : launch_tiled<bf16_t, 8, 8, true, 1, 2>(x, w, bias, y, ldy, s);
-    return launch_tiled<bf16_t, 4, 4, true, 0, 4>(x, w, bias, y, ldy, s);
+        return along ? launch_tiled<bf16_t, 8, 8, 2, 2>(x, w, bias, y, ldy, s) : launch_tiled<bf16_t, 8, 8, 1, 2>(x, w, bias, y, ldy, s);
+    return launch_tiled<bf16_t, 4, 4, 0, 4>(x, w, bias, y, ldy, s);
 }
 
 // Rows that are no multiple of 16 codes are laid out for the large tiles where the general kernel would

@@ -72,3 +72,10 @@ def test_refused_calls_need_nothing(mod):
     assert lib.dmmv_block_backward_workspace_for(mod.DMMV_F32, 8, 6, 300, P, 6, None, None, P, None) == 0 and lib.dmmv_last_error()
     # dx and dw only say what is asked for
     assert needs(mod, 8, 6, 300) > 0
+
+
+def test_a_norm_of_nothing_needs_nothing(mod):
+    lib = mod.load()
+    for sizes in ((0, 0), (0, 300), (8, 0), (-1, 300), (8, -1), (8, 1 << 31)):
+        assert lib.dmmv_layernorm_workspace_bytes(*sizes) == 0
+    assert lib.dmmv_layernorm_workspace_bytes(8, 300) > 0
