@@ -28,7 +28,7 @@ __device__ __forceinline__ piece8 read_transposed(const uint8_t* p) {
 //   [m][k] with chunk c of row m at c ^ (m & 7), read as it is.
 // The codes are the A operand of the instruction, so that a lane's results come in fours along a row of C.
 // Bound by the LDS and the waits of wavefronts in step, the more parts the more: 2048^3 bf16 50 us (345 TFLOP/s); dx of 777 x 1365 x 1003 in
-// 32 bits 23 us, 1.3 us a step and 7 for start, join and end.  Requesting all of a step's fragments ahead of the next
+// 32 bits 23 us, 1.3 us a step and 7 for start, join and end.  32-bit scales per block (three parts of the codes): dx and dw of 4096^3 bf16 1510 us.  Requesting all of a step's fragments ahead of the next
 // step's writes was no faster.
 template <class TA, bool TRANS, int PA, int PB, int KS, class TC>
 __global__ __launch_bounds__(256 * KS) void k_block_grad(int64_t M, int64_t N, int64_t Kc, const TA* __restrict__ a, int64_t lda, BlockView b,
@@ -266,8 +266,8 @@ __global__ __launch_bounds__(256) void k_block_grad_join(int64_t M, int64_t N, i
 // The codes are the A operand, so that a lane's results come in fours along a row of the output.
 // dy may come as several bf16 parts that sum to it (`planes`, `plane` numbers apart): the contraction then runs over all.
 // The loop is that of the large product: a quadrant of 16 products at a time, all else in their shadows.
-// 4096 x 11008 x 4096 bf16: dx 295 to 318 us (1.16 to 1.25 PFLOP/s, the matrix unit busy for 60 % of the cycles), dw 340 to 370 (its 180 MB of
-// results and the transposed reads of both operands; 49 %).
+// 4096 x 11008 x 4096 bf16, calls one after another: dx 282 to 289 us (1.28 to 1.31 PFLOP/s), dw 322 to 335 (its 180 MB of results and the
+// transposed reads of both operands).  Under the profiler 315 and 369, the matrix unit busy for 60 and 49 % of the cycles.
 constexpr int GT_STAGE = 65536, GT_LDS = 256 * (256 * 2 + 16) > 2 * GT_STAGE ? 256 * (256 * 2 + 16) : 2 * GT_STAGE;
 
 template <bool TRANS, class TC>

@@ -70,7 +70,7 @@ __device__ __forceinline__ intx8 words8(piece16 a, piece16 b) {
 // right while all scales are moderate, and a conversion to bf16 is while exponents are (scaled8); where a tile has met others, its sums are made
 // once more by tile_any (a branch in the loop would cost every product a fifth).
 // Bound by the vector unit (conversions to 16 bits, sums of blocks) and by the waits of four wavefronts in step: 4096 x 11008 x 4096 in
-// 32 bits 490 to 514 us, 0.72 PFLOP/s, with 32-bit scales per block 570; 500 x 1777 x 2731 in 32 bits 20 us.  Tiles of 64 x 64 keep the chip
+// 32 bits 490 to 514 us, 0.72 PFLOP/s, with 32-bit scales per block 560, in bf16 with those 450; 500 x 1777 x 2731 in 32 bits 20 us.  Tiles of 64 x 64 keep the chip
 // full at such sizes (224 tiles); larger ones would leave most of it idle.
 struct ProductScales {
     int32_t x_blocks, w_blocks;         // SCALED: exponents per block, else constant along the row
@@ -308,7 +308,7 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
 // 2 registers, as they are the same along a row.
 // T float: workgroup row y of the grid takes its share of the contraction, and y [share][T_][O] is joined by k_block_product_join.
 // 256 x 256 tiles, 128 x 128 a wavefront: 64 products a step from 16 + 16 fragments, which the LDS can deliver beside the requests;
-// smaller tiles are bound by it.  4096 x 11008 x 4096: 157 to 166 us (2.2 to 2.35 PFLOP/s), the matrix unit busy for 53 % of the
+// smaller tiles are bound by it.  4096 x 11008 x 4096: 158 to 167 us (2.2 to 2.35 PFLOP/s), the matrix unit busy for 53 % of the
 // cycles; 688 tiles are 2.7 rounds of the chip (256 tiles of K = 11008: 131 us, 2.8 PFLOP/s), the clock falls under this load.
 // exponents of `blocks` blocks from kb on for `rows` rows (or groups of `per` rows) of a tile, to bytes of the LDS
 __device__ __forceinline__ void stage_exponents(const BlockView& q, int64_t row0, int64_t last, int per, int rows, int kb, int blocks,
@@ -882,7 +882,8 @@ static dmmv_status product(const dmmv_block_matrix* x, const dmmv_block_matrix* 
     const ProductScales how = {!constant_rows(x), !constant_rows(w)};
     const bool scaled = (constant_rows(x) || x->scale_type == DMMV_E8M0) && (constant_rows(w) || w->scale_type == DMMV_E8M0);
     // Few tokens, us by registers and by tiles (T x O x K): 32 x 4096 x 4096 9.9 and 12.7, 24 x 8192 x 4096 15.3 and 16.1, 32 x 8192 x 4096
-    // 17.5 and 16.1, 24 x 11008 x 4096 21 and 16.5, 24 x 8192 x 8192 27.5 and 26; 64 x 4096 x 4096 16.4 and 13.8; where the large tiles
+    // 17.5 and 16.1, 24 x 11008 x 4096 21 and 16.5, 24 x 8192 x 8192 27.5 and 26; few outputs of a long contraction 24 x 4096 x 8192 15.2 and 26,
+// 24 x 4096 x 11008 18.7 and 34; 64 x 4096 x 4096 16.4 and 13.8; where the large tiles
     // do not apply, 64 (32 bits): 17.4 and 19.3, 128: 32.5 and 20.
     const bool tiles = sizeof(T) == 2 && scaled && aligned(x) && aligned(w);
     const bool wide = x->rows > 16 && w->rows >= 8192 && (double)x->rows * (double)w->rows * (double)x->cols >= 9e8;

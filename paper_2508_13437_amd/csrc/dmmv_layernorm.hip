@@ -57,7 +57,8 @@ __device__ __forceinline__ void norm8(const float (&x)[8], int64_t col, int64_t 
 
 // TPR threads a row, CH chunks of 8 TPR columns in registers: a row is read once, the two sums and the results come from the
 // registers.  A wavefront a row up to 1024 columns (sums by DPP alone, four rows a workgroup), then a workgroup a row.
-// Bound by memory: 4096 x 4096 bf16, y and xq 18 us, 4.7 TB/s with everything read and written once; 16384 x 1024 the same.
+// Bound by memory and by the wait for a row before its two sums, in which nothing is requested: 4096 x 4096 bf16, y alone 16.5 us (4.1 TB/s with
+// everything read and written once), the 8-bit result alone 18.0 (2.8), y and xq 18.6 (4.5), the 8-bit result and xq 21.7 (3.1).
 template <class T, int TPR, int CH>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm(int64_t rows, int64_t cols, const T* __restrict__ x, int64_t ldx,
                                                                      const float* __restrict__ gamma, const float* __restrict__ beta,
@@ -102,8 +103,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm(int64_t row
     }
 }
 
-// Rows of any length: one workgroup, three walks over the row (the second and third find it in the L2).  1024 x 40000 bf16,
-// y and xq: 46 us, 4.5 TB/s of what has to move.
+// Rows of any length: one workgroup, three walks over the row (the second and third find it in the L2).  1024 x 40000 bf16:
+// y 46 us (3.6 TB/s of what has to move), y and xq 53 (3.8).
 template <class T>
 __global__ __launch_bounds__(1024) void k_layernorm_wide(int64_t rows, int64_t cols, const T* __restrict__ x, int64_t ldx,
                                                          const float* __restrict__ gamma, const float* __restrict__ beta, float eps,
