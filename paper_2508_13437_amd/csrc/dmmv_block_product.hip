@@ -68,7 +68,7 @@ __device__ __forceinline__ intx8 words8(piece16 a, piece16 b) {
 // SCALED: power-of-two scales go into the instruction (8 bits) or the conversion to bf16 (32-bit results), and so does the exponent of a scale
 // that is the same along a row; the rest of that is multiplied at the end.  Otherwise a block's sum is multiplied by the product of its two scales in 32 bits.  That is
 // right while all scales are moderate, and a conversion to bf16 is while exponents are (scaled8); where a tile has met others, its sums are made
-// once more by tile_any (a branch in the loop would cost every product a fifth).
+// once more by tile_any, unless those scales are of zeros (a branch in the loop would cost every product a fifth).
 // Bound by the vector unit (conversions to 16 bits, sums of blocks) and by the waits of four wavefronts in step: 4096 x 11008 x 4096 in
 // 32 bits 490 to 514 us, 0.72 PFLOP/s, with 32-bit scales per block 560, in bf16 with those 450; 500 x 1777 x 2731 in 32 bits 20 us.  Tiles of 64 x 64 keep the chip
 // full at such sizes (224 tiles); larger ones would leave most of it idle.
@@ -76,47 +76,98 @@ struct ProductScales {
     int32_t x_blocks, w_blocks;         // SCALED: exponents per block, else constant along the row
 };
 
-// 16 x 16 results with any scales, straight from memory: lane (lr, lg) has 32 codes of row lr of each operand and block, and the results
-// of outputs 4 lg .. of token lr.
+// Whether exponents are beyond what the conversion to bf16 holds exactly (scaled8)
+__device__ __forceinline__ bool beyond_bf16(uint32_t b) { return b - 3u > 243u && b != 255u; }
+
+// Whether a row has a block whose scale the loop does not take.  Such scales are often those of blocks of zeros, where only
+// a large one does harm (a product of scales that is infinite): the codes are looked at, by a wavefront.
+template <bool SCALED>
+__device__ __forceinline__ bool row_beyond(const BlockView& q, int64_t row, int64_t K) {
+    bool bad = false;
+#pragma unroll 1
+    for (int64_t at = (threadIdx.x & 63) * 16; at < K; at += 1024) {
+        const uint32_t bits = scale_bits(q, row, at >> 7);
+        bool small;
+        if constexpr (SCALED) {
+            small = beyond_bf16(bits);
+        } else {
+            ScaleRange r;
+            r.take(scale_of(q, bits));
+            bad |= r.large();
+            small = r.small();
+        }
+        if (small) {
+            const piece16 v = chunk_tail(q.codes + row * q.ld + at, (int)min(K - at, (int64_t)16), at);
+            bad |= ((v[0] | v[1] | v[2] | v[3]) & 0x7F7F7F7Fu) != 0u;
+        }
+    }
+    return __any(bad);
+}
+
+// 32 x 32 results with any scales, straight from memory: lane (lr, lg) has 32 codes of two rows of each operand and block, and the results
+// of four outputs and two tokens twice.  500 x 1777 x 2731 in 32 bits with all scales of x
+// 2^-126: 133 us, the loop and then this; with those of zeros 39.
 template <class T, bool SCALED>
 __device__ __forceinline__ void tile_any(int64_t t0, int64_t T_, int64_t o0, int64_t O, int64_t K, const BlockView& x, const BlockView& w, ProductScales how,
                                          const float* __restrict__ bias, T* __restrict__ y, int64_t ldy) {
     int lane = threadIdx.x & 63;
-    floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    floatx4 acc[2][2];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) acc[q >> 1][q & 1] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 1
     for (int64_t at = 0; at < K; at += 128) {
         asm volatile("" : "+v"(lane));               // (addresses are made again for every block: few registers)
         const int lr = lane & 15, lg = lane >> 4;
-        const int64_t t = min(t0 + lr, T_ - 1), o = min(o0 + lr, O - 1);
-        const int left = (int)min(K - at, (int64_t)128) - lg * 32;
-        const uint8_t* px = x.codes + t * x.ld + at + lg * 32;
-        const uint8_t* pw = w.codes + o * w.ld + at + lg * 32;
-        const intx8 fx = words8(chunk_tail(px, left, at + lg * 32), chunk_tail(px + 16, left - 16, at + lg * 32 + 16));
-        const intx8 fw = words8(chunk_tail(pw, left, at + lg * 32), chunk_tail(pw + 16, left - 16, at + lg * 32 + 16));
-        const floatx4 p = block_sum<sizeof(T) == 4>(fw, fx);
         const int64_t b = at >> 7;
-        const uint32_t sx = SCALED && !how.x_blocks ? row_scale(scale_at(x, t, 0)).byte : scale_bits(x, t, b);
+        const int left = (int)min(K - at, (int64_t)128) - lg * 32;
+        intx8 fx[2], fw[2];
+        uint32_t sx[2], sw[2][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int64_t oe = min(o0 + lg * 4 + e, O - 1);
-            const uint32_t sw = SCALED && !how.w_blocks ? row_scale(scale_at(w, oe, 0)).byte : scale_bits(w, oe, b);
-            acc[e] = SCALED ? acc[e] + times_exponents(p[e], sw, sx) : add_scaled(p[e], scale_of(w, sw), scale_of(x, sx), acc[e]);
+        for (int j = 0; j < 2; ++j) {
+            const int64_t t = min(t0 + 16 * j + lr, T_ - 1), o = min(o0 + 16 * j + lr, O - 1);
+            const uint8_t* px = x.codes + t * x.ld + at + lg * 32;
+            const uint8_t* pw = w.codes + o * w.ld + at + lg * 32;
+            fx[j] = words8(chunk_tail(px, left, at + lg * 32), chunk_tail(px + 16, left - 16, at + lg * 32 + 16));
+            fw[j] = words8(chunk_tail(pw, left, at + lg * 32), chunk_tail(pw + 16, left - 16, at + lg * 32 + 16));
+            sx[j] = SCALED && !how.x_blocks ? row_scale(scale_at(x, t, 0)).byte : scale_bits(x, t, b);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t oe = min(o0 + 16 * j + lg * 4 + e, O - 1);
+                sw[j][e] = SCALED && !how.w_blocks ? row_scale(scale_at(w, oe, 0)).byte : scale_bits(w, oe, b);
+            }
         }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const floatx4 p = block_sum<sizeof(T) == 4>(fw[i], fx[j]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    acc[i][j][e] = SCALED ? acc[i][j][e] + times_exponents(p[e], sw[i][e], sx[j]) : add_scaled(p[e], scale_of(w, sw[i][e]), scale_of(x, sx[j]), acc[i][j][e]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
     }
     const int lr = lane & 15, lg = lane >> 4;
-    const int64_t t = t0 + lr;
-    if (t >= T_) return;
-    const float st = SCALED && !how.x_blocks ? row_scale(scale_at(x, t, 0)).rest : 1.0f;
-    for (int e = 0; e < 4; ++e) {
-        const int64_t oe = o0 + lg * 4 + e;
-        if (oe >= O) break;
-        const float so = SCALED && !how.w_blocks ? row_scale(scale_at(w, oe, 0)).rest : 1.0f;
-        put_y(y + t * ldy + oe, dmmv_fma(acc[e] * so, st, bias ? bias[oe] : 0.0f));
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int64_t t = t0 + 16 * j + lr;
+        if (t >= T_) break;
+        const float st = SCALED && !how.x_blocks ? row_scale(scale_at(x, t, 0)).rest : 1.0f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t oe = o0 + 16 * i + lg * 4 + e;
+                if (oe >= O) continue;
+                const float so = SCALED && !how.w_blocks ? row_scale(scale_at(w, oe, 0)).rest : 1.0f;
+                put_y(y + t * ldy + oe, dmmv_fma(acc[i][j][e] * so, st, bias ? bias[oe] : 0.0f));
+            }
     }
 }
 
-// WAVES: wavefronts a SIMD that the registers leave room for at least.  32-bit results with 32-bit scales have more than three allow: where a compute
-// unit gets one tile they stay (500 x 1777 x 2731 20.6 us, 21.5 with three), else not (4096 x 11008 x 4096 570 us, 650 without).
+// WAVES: wavefronts a SIMD that the registers leave room for at least.  32-bit results use more than three (32-bit scales) and four (exponents) allow:
+// where a compute unit gets one tile they stay (500 x 1777 x 2731 20.6 and 19.8 us, 21.5 and 20.4 with three and four), else not (4096 x 11008 x 4096
+// 570 and 500 us, 650 and 530 without).
 template <class T, bool SCALED, int WAVES>
 __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
                                                        const float* __restrict__ bias, T* __restrict__ y, int64_t ldy, int32_t tiles_t, int32_t tiles_o) {
@@ -125,7 +176,8 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
     __shared__ __align__(16) uint8_t codes[2][128 * (BM + BN)];
     __shared__ __align__(16) uint32_t scl[2][BM + BN];
     constexpr bool RANGED = !SCALED || WIDE;         // (the 8-bit instruction takes every exponent)
-    __shared__ int again;                            // RANGED: some scale is not moderate
+    __shared__ uint64_t far[2];                      // RANGED: rows whose scales are not all moderate
+    __shared__ int again;                            // and some of them count
     if (RANGED && threadIdx.x == 0) again = 0;       // (a barrier follows before it is set)
     const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -177,7 +229,7 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
         const uint32_t s = SCALED ? (sq.scales ? bits : along) : sq.e8m0 ? __float_as_uint(e8m0_value(bits)) : bits;
         if (mine) scl[stage][tid] = s;
         if (!SCALED) met.take(__uint_as_float(s));
-        else if (WIDE) exact &= s - 3u <= 243u || s == 255u;
+        else if (WIDE) exact &= !beyond_bf16(s);
     };
     floatx4 acc[NI][MI];
     const int c0 = (lg ^ (lr & 7)) << 4;
@@ -271,12 +323,24 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
         multiply(0);
     }
     if constexpr (RANGED) {
-        if (!(SCALED ? exact : met.moderate())) again = 1;
+        // rows of x (wavefront 0) and of w (wavefront 1) with scales that the loop does not take; do they count?
+        static_assert(BM == 64 && BN == 64, "a wavefront has an operand's scales");
+        const uint64_t rows = __ballot(!(SCALED ? exact : met.moderate()));
+        if (wv < 2 && lane == 0) far[wv] = rows;
         __syncthreads();
-        if (again) {
+        if (far[0] | far[1]) {
+            bool bad = false;
 #pragma unroll 1
-            for (int q = 0; q < NI * MI; ++q) tile_any<T, SCALED>(t0 + wt + 16 * (q % MI), T_, o0 + wo + 16 * (q / MI), O, K, x, w, how, bias, y, ldy);
-            return;
+            for (int r = wv; r < BM + BN; r += 4)
+                if ((far[r >> 6] >> (r & 63)) & 1)
+                    bad |= r < BM ? (!SCALED || how.x_blocks) && row_beyond<SCALED>(x, min(t0 + r, T_ - 1), K)
+                                  : (!SCALED || how.w_blocks) && row_beyond<SCALED>(w, min(o0 + r - BM, O - 1), K);
+            if (bad) again = 1;
+            __syncthreads();
+            if (again) {
+                tile_any<T, SCALED>(t0 + wt, T_, o0 + wo, O, K, x, w, how, bias, y, ldy);
+                return;
+            }
         }
     }
 #pragma unroll
@@ -662,7 +726,7 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
             for (int m = 0; m < MT; ++m) k.fx[m] = scale_bits(x, trow[m], b);
         }
     };
-    ScaleRange met;                                  // as in the general kernel: this lane's scales
+    ScaleRange met;                                  // as in the general kernel: this lane's scales (24 x 4096 x 4096: 11.5 us, 25 with a scale of 2^-126)
     auto multiply = [&](auto CAREFUL, Block& k) __attribute__((always_inline)) {
         if constexpr (SCALED) {
             if (!how.w_blocks) k.ew = along_w;
@@ -907,9 +971,10 @@ static dmmv_status product(const dmmv_block_matrix* x, const dmmv_block_matrix* 
         hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, x->rows, w->rows, x->cols, layer_view(x), layer_view(w), how, bias, y, ldy, (int32_t)tiles_t,
                            (int32_t)tiles_o);
     };
-    if (scaled) launch(k_block_product<T, true, 1>);
-    else if (sizeof(T) == 4 && tiles_t * tiles_o <= 256) launch(k_block_product<T, false, sizeof(T) == 4 ? 1 : 3>);
-    else launch(k_block_product<T, false, 3>);
+    const bool one_each = tiles_t * tiles_o <= 256;
+    if (sizeof(T) == 2) scaled ? launch(k_block_product<T, true, 1>) : launch(k_block_product<T, false, 3>);
+    else if (one_each) scaled ? launch(k_block_product<T, true, 1>) : launch(k_block_product<T, false, sizeof(T) == 4 ? 1 : 3>);
+    else scaled ? launch(k_block_product<T, true, sizeof(T) == 4 ? 4 : 1>) : launch(k_block_product<T, false, 3>);
     DMMV_LAUNCH_CHECK();
     return DMMV_OK;
 }

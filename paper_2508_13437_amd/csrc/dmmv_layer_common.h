@@ -156,15 +156,17 @@ __device__ __forceinline__ float add_scaled(float p, float a, float b, float acc
 __device__ __forceinline__ float times_exponents(float p, uint32_t a, uint32_t b) {
     return max(a, b) == 255u ? __uint_as_float(0x7FC00000u) : __builtin_amdgcn_ldexpf(p, (int)(a + b) - 254);
 }
-// The scales met so far need no such care: all are 2^-62 to 2^63 or 0, so that products of two are normal numbers or 0
+// The scales met so far need no such care: all are 2^-62 to 2^63, so that products of two are normal numbers, or 0, or not finite
 struct ScaleRange {
     uint32_t lo = ~0u, hi = 0u;                      // magnitudes as bits, doubled; lo less 1, so that 0 does not count
     __device__ __forceinline__ void take(float s) {
         const uint32_t u = __float_as_uint(s) << 1;
-        hi = max(hi, u);
+        hi = max(hi, u < 0xFF000000u ? u : 0u);
         lo = min(lo, u - 1u);
     }
-    __device__ __forceinline__ bool moderate() const { return lo >= (65u << 24) - 1u && hi < (190u << 24); }
+    __device__ __forceinline__ bool small() const { return lo < (65u << 24) - 1u; }
+    __device__ __forceinline__ bool large() const { return hi >= (190u << 24); }
+    __device__ __forceinline__ bool moderate() const { return !small() && !large(); }
 };
 // A scale that is the same along a row leaves the sum, but its exponent (as a scale's byte) goes in where those of blocks go, so that the sum
 // has the result's size; what is left of it, `rest`, is 1 to 2 (for exponents outside what scaled8 takes a little more or less; 0, infinite or NaN as the scale).

@@ -175,3 +175,27 @@ def test_scales_of_a_matrix_without_columns_are_not_read(gpu_device, T, kind):
         dmmv._check(dmmv.load().dmmv_block_product(dmmv.C.addressof(x), dmmv.C.addressof(w), bias.data_ptr(), name, y.data_ptr(), O, None, 0,
                                                    torch.cuda.current_stream().cuda_stream))
         assert torch.equal(y, bias.to(dtype).expand(T, O))
+
+
+@pytest.mark.parametrize("T", [3, 24, 65, 150])
+@pytest.mark.parametrize("kind", ["f32", "e8m0"])
+def test_blocks_of_zeros_have_any_scale(gpu_device, T, kind):
+    """Zeros of either sign with the smallest and the largest scales (what others put beside a block of zeros), in some blocks and whole rows."""
+    from paper_2508_13437_amd import dmmv
+
+    K, O = 700, 70
+    nb = -(-K // 128)
+    for small in (True, False):
+        pair = []
+        for rows, seed in ((T, 1), (O, 2)):
+            codes = codes_of(rows, K, seed, gpu_device).view(torch.uint8)
+            scales = torch.full((rows, nb), 127, dtype=torch.uint8, device=gpu_device) if kind == "e8m0" else powers(rows, nb, 0, seed, gpu_device)
+            zero = torch.zeros(rows, nb, dtype=torch.bool)
+            zero[:, 2], zero[rows // 2], zero[rows - 1, nb - 1] = True, True, True
+            zero = zero.to(gpu_device)
+            spread = zero.repeat_interleave(128, 1)[:, :K]
+            codes[spread] = torch.where(torch.arange(int(spread.sum()), device=gpu_device) % 2 == 0, 0x00, 0x80).to(torch.uint8)
+            scales[zero] = (0 if small else 254) if kind == "e8m0" else (2.0 ** -149 if small else 2.0 ** 127)
+            pair.append(dmmv.BlockMatrix(codes, scales))
+        for dtype in (torch.float32, torch.bfloat16):
+            check_product(*pair, dtype)
