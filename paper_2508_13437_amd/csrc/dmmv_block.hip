@@ -151,7 +151,7 @@ __global__ __launch_bounds__(256) void k_block_dequantize(int64_t rows, int64_t 
         decode8(c, 1.0f, v);
         ScaleRange r;
         r.take(s);
-        if (r.moderate()) {
+        if (r.moderate() && fabsf(s) < __builtin_huge_valf()) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = cut_product(v[e], s);
         } else {
