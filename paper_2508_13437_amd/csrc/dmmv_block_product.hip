@@ -66,12 +66,13 @@ __device__ __forceinline__ intx8 words8(piece16 a, piece16 b) {
 //   LDS row: 128 codes, the 16-byte chunk c of row r at c ^ (r & 7): neither the 8 lanes that write a row
 //   nor the 8 rows that are read together meet in a bank.
 // SCALED: power-of-two scales go into the instruction (8 bits) or the conversion to bf16 (32-bit results), and so does the exponent of a scale
-// that is the same along a row; the rest of that is multiplied at the end.  Otherwise a block's sum is multiplied by the product of its two scales in 32 bits.  That is
-// right while all scales are moderate, and a conversion to bf16 is while exponents are (scaled8); where a tile has met others, its sums are made
-// once more by tile_any, unless those scales are of zeros (a branch in the loop would cost every product a fifth).
+// that is the same along a row; the rest of that is multiplied at the end.  Otherwise a block's sum is multiplied by the product of its two
+// scales in 32 bits.  That is right while all scales are moderate, and a conversion to bf16 is while exponents are (scaled8); where a tile has
+// met others, its results are made once more by tile_any, unless those scales are of zeros (a branch in the loop would cost every product a
+// fifth).
 // Bound by the vector unit (conversions to 16 bits, sums of blocks) and by the waits of four wavefronts in step: 4096 x 11008 x 4096 in
-// 32 bits 490 to 514 us, 0.72 PFLOP/s, with 32-bit scales per block 560, in bf16 with those 450; 500 x 1777 x 2731 in 32 bits 20 us.  Tiles of 64 x 64 keep the chip
-// full at such sizes (224 tiles); larger ones would leave most of it idle.
+// 32 bits 490 to 514 us, 0.72 PFLOP/s, with 32-bit scales per block 560, in bf16 with those 450; 500 x 1777 x 2731 in 32 bits 20 us.  Tiles of
+// 64 x 64 keep the chip full at such sizes (224 tiles); larger ones would leave most of it idle.
 struct ProductScales {
     int32_t x_blocks, w_blocks;         // SCALED: exponents per block, else constant along the row
 };
@@ -105,8 +106,8 @@ __device__ __forceinline__ bool row_beyond(const BlockView& q, int64_t row, int6
 }
 
 // 32 x 32 results with any scales, straight from memory: lane (lr, lg) has 32 codes of two rows of each operand and block, and the results
-// of four outputs and two tokens twice.  500 x 1777 x 2731 in 32 bits with all scales of x
-// 2^-126: 133 us, the loop and then this; with those of zeros 39.
+// of four outputs and two tokens twice.  500 x 1777 x 2731 in 32 bits with all scales of x 2^-126: 133 us, the loop and then this; with those of
+// zeros 39.
 template <class T, bool SCALED>
 __device__ __forceinline__ void tile_any(int64_t t0, int64_t T_, int64_t o0, int64_t O, int64_t K, const BlockView& x, const BlockView& w, ProductScales how,
                                          const float* __restrict__ bias, T* __restrict__ y, int64_t ldy) {
@@ -947,7 +948,7 @@ static dmmv_status product(const dmmv_block_matrix* x, const dmmv_block_matrix* 
     const bool scaled = (constant_rows(x) || x->scale_type == DMMV_E8M0) && (constant_rows(w) || w->scale_type == DMMV_E8M0);
     // Few tokens, us by registers and by tiles (T x O x K): 32 x 4096 x 4096 9.9 and 12.7, 24 x 8192 x 4096 15.3 and 16.1, 32 x 8192 x 4096
     // 17.5 and 16.1, 24 x 11008 x 4096 21 and 16.5, 24 x 8192 x 8192 27.5 and 26; few outputs of a long contraction 24 x 4096 x 8192 15.2 and 26,
-// 24 x 4096 x 11008 18.7 and 34; 64 x 4096 x 4096 16.4 and 13.8; where the large tiles
+    // 24 x 4096 x 11008 18.7 and 34; 64 x 4096 x 4096 16.4 and 13.8; where the large tiles
     // do not apply, 64 (32 bits): 17.4 and 19.3, 128: 32.5 and 20.
     const bool tiles = sizeof(T) == 2 && scaled && aligned(x) && aligned(w);
     const bool wide = x->rows > 16 && w->rows >= 8192 && (double)x->rows * (double)w->rows * (double)x->cols >= 9e8;
