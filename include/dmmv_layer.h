@@ -72,8 +72,10 @@ dmmv_status dmmv_block_dequantize(const dmmv_block_matrix* q, int32_t dtype, voi
  * of about 5e-5 of the result's norm, up to 2^-11 of sum |x w| for a single one, before the rounding to
  * bf16 (1.7e-3).  Who needs the sum takes it in 32 bits.  Scales may be far apart: what counts is that
  * the products x w, their sum and the result are in the range.  The workspace (size from the HOST
- * function, 0 is possible, 256-byte aligned) holds the operands of a large product once more where
- * their rows are no multiples of 16 codes, and partial sums where few tiles share a long contraction. */
+ * function for every call of these sizes, 0 is possible, 256-byte aligned) holds, for bf16 results with
+ * exponents or scales along rows, the operands of a large product once more where their rows are no
+ * multiples of 16 codes, and partial sums where few tiles share a long contraction.  Other calls need
+ * none. */
 size_t dmmv_block_product_workspace_bytes(int64_t T, int64_t O, int64_t K);
 dmmv_status dmmv_block_product(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, int32_t dtype,
                                void* y, int64_t ldy, void* workspace, size_t workspace_bytes, void* hip_stream);

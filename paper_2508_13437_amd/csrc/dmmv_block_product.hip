@@ -942,21 +942,42 @@ static size_t product_workspace(int64_t T, int64_t O, int64_t K) {
     return lay + (product_shared(T, K, lay) ? product_part_bytes(T, O, K) : 0);
 }
 
-template <class T>
-static dmmv_status product(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, T* y, int64_t ldy, void* ws, hipStream_t s) {
-    const ProductScales how = {!constant_rows(x), !constant_rows(w)};
-    const bool scaled = (constant_rows(x) || x->scale_type == DMMV_E8M0) && (constant_rows(w) || w->scale_type == DMMV_E8M0);
+// How a product is made, and the bytes that takes: what the call does and what its workspace is measured by.
+struct ProductPlan {
+    enum Path { FEW, TILES, LAID, GENERAL } path;
+    bool scaled;
+    size_t lay, bytes;                   // codes laid out (whole 256 bytes), all
+};
+static ProductPlan product_plan(const dmmv_block_matrix* x, const dmmv_block_matrix* w, bool f32) {
+    const int64_t T = x->rows, O = w->rows, K = x->cols;
+    ProductPlan p = {ProductPlan::GENERAL, (constant_rows(x) || x->scale_type == DMMV_E8M0) && (constant_rows(w) || w->scale_type == DMMV_E8M0), 0, 0};
     // Few tokens, us by registers and by tiles (T x O x K): 32 x 4096 x 4096 9.9 and 12.7, 24 x 8192 x 4096 15.3 and 16.1, 32 x 8192 x 4096
     // 17.5 and 16.1, 24 x 11008 x 4096 21 and 16.5, 24 x 8192 x 8192 27.5 and 26; few outputs of a long contraction 24 x 4096 x 8192 15.2 and 26,
-    // 24 x 4096 x 11008 18.7 and 34; 64 x 4096 x 4096 16.4 and 13.8; where the large tiles
-    // do not apply, 64 (32 bits): 17.4 and 19.3, 128: 32.5 and 20.
-    const bool tiles = sizeof(T) == 2 && scaled && aligned(x) && aligned(w);
-    const bool wide = x->rows > 16 && w->rows >= 8192 && (double)x->rows * (double)w->rows * (double)x->cols >= 9e8;
-    if (x->rows <= (!tiles ? 64 : wide ? 16 : 32)) return launch_few(x, w, how, scaled, bias, y, ldy, s);
-    const size_t lay = product_lay_bytes(x->rows, w->rows, x->cols);
-    float* part = product_shared(x->rows, x->cols, lay) ? reinterpret_cast<float*>(static_cast<char*>(ws) + (lay + 255) / 256 * 256) : nullptr;
-    if (tiles) return product_tiled(x, w, bias, reinterpret_cast<bf16_t*>(y), ldy, part, s);
-    if (sizeof(T) == 2 && scaled && lay > 0) {
+    // 24 x 4096 x 11008 18.7 and 34; 64 x 4096 x 4096 16.4 and 13.8; where the large tiles do not apply, 64 (32 bits): 17.4 and 19.3, 128: 32.5 and 20.
+    const bool tiles = !f32 && p.scaled && aligned(x) && aligned(w);
+    const bool wide = T > 16 && O >= 8192 && (double)T * (double)O * (double)K >= 9e8;
+    if (T <= (!tiles ? 64 : wide ? 16 : 32)) {
+        p.path = ProductPlan::FEW;
+        return p;
+    }
+    const size_t lay = product_lay_bytes(T, O, K);
+    if (tiles) p.path = ProductPlan::TILES;
+    else if (!f32 && p.scaled && lay > 0) p.path = ProductPlan::LAID;
+    else return p;
+    if (p.path == ProductPlan::LAID) p.lay = (lay + 255) / 256 * 256;
+    p.bytes = p.lay + (product_shared(T, K, lay) ? product_part_bytes(T, O, K) : 0);
+    return p;
+}
+
+template <class T>
+static dmmv_status product(const ProductPlan& plan, const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, T* y, int64_t ldy, void* ws,
+                           hipStream_t s) {
+    const ProductScales how = {!constant_rows(x), !constant_rows(w)};
+    const bool scaled = plan.scaled;
+    if (plan.path == ProductPlan::FEW) return launch_few(x, w, how, scaled, bias, y, ldy, s);
+    float* part = plan.bytes > plan.lay ? reinterpret_cast<float*>(static_cast<char*>(ws) + plan.lay) : nullptr;
+    if (plan.path == ProductPlan::TILES) return product_tiled(x, w, bias, reinterpret_cast<bf16_t*>(y), ldy, part, s);
+    if (plan.path == ProductPlan::LAID) {
         dmmv_block_matrix lx = *x, lw = *w;
         lx.ld = lw.ld = ceil_div(x->cols, 128) * 128;
         lx.codes = ws;
@@ -997,9 +1018,10 @@ extern "C" dmmv_status dmmv_block_product(const dmmv_block_matrix* x, const dmmv
     if (x->cols != w->cols) return fail(DMMV_ERR_SHAPE, "x has %lld columns, w has %lld", (long long)x->cols, (long long)w->cols);
     DMMV_TRY(layer_check_array(y, x->rows, w->rows, ldy, layer_width(dtype), "y"));
     if ((uintptr_t)bias % 4) return fail(DMMV_ERR_SHAPE, "bias is not aligned to its elements");
-    DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, product_workspace(x->rows, w->rows, x->cols)));
     if (x->rows == 0 || w->rows == 0) return DMMV_OK;
+    const ProductPlan plan = product_plan(x, w, dtype == DMMV_F32);
+    DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, plan.bytes));
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    return dtype == DMMV_F32 ? product(x, w, bias, static_cast<float*>(y), ldy, workspace, s)
-                             : product(x, w, bias, static_cast<bf16_t*>(y), ldy, workspace, s);
+    return dtype == DMMV_F32 ? product(plan, x, w, bias, static_cast<float*>(y), ldy, workspace, s)
+                             : product(plan, x, w, bias, static_cast<bf16_t*>(y), ldy, workspace, s);
 }

@@ -685,7 +685,7 @@ def dmmv_block_product(x: BlockMatrix, w: BlockMatrix, bias: Optional[torch.Tens
     T, O = x._rows, w._rows
     b = _vector(bias, O, dev, "bias")
     y = torch.empty(T, O, dtype=dtype, device=x._codes.device)
-    nbytes = _workspace("dmmv_block_product_workspace_bytes", T, O, x._cols)
+    nbytes = _workspace("dmmv_block_product_workspace_bytes", T, O, x._cols) if kind == DMMV_BF16 else 0
     ws = torch.empty(nbytes, dtype=torch.uint8, device=y.device) if nbytes else None
     _enqueue(dev, load().dmmv_block_product, x._p, w._p, _addr(b), kind, y.data_ptr(), O, _addr(ws), nbytes)
     return y

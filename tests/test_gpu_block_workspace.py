@@ -42,3 +42,30 @@ def test_workspace_of_the_least_size(gpu_device, T, O, K, dtype, kx, kw):
         W, X, D = (dmmv.dmmv_block_dequantize(w, torch.float32).double(), dmmv.dmmv_block_dequantize(x, torch.float32).double(), dy.double())
         assert torch.equal(out[0], (D @ W).to(dtype))        # small integers: exact
         assert torch.equal(out[1].double(), D.t() @ X) and torch.equal(out[2].double(), D.sum(0))
+
+
+@pytest.mark.parametrize("dtype,kind,pad,needs", [(torch.float32, "e8m0", 1, "nothing"), (torch.float32, "f32", 0, "nothing"), (torch.bfloat16, "f32", 1, "nothing"),
+                                                  (torch.bfloat16, "e8m0", 1, "codes"), (torch.bfloat16, "row", 1, "codes")])
+def test_a_product_needs_a_workspace_where_it_uses_one(gpu_device, dtype, kind, pad, needs):
+    """A large product of unaligned rows: the codes are laid out for bf16 results with exponents, and nothing is for others."""
+    from paper_2508_13437_amd import dmmv
+
+    lib, name = dmmv.load(), dmmv.DMMV_F32 if dtype == torch.float32 else dmmv.DMMV_BF16
+    T, O, K = 200, 4000, 8191
+    x, w = matrix(T, K, kind, 1, gpu_device, pad), matrix(O, K, kind, 2, gpu_device, pad)
+    y = torch.empty(T, O, dtype=dtype, device=gpu_device)
+    most = lib.dmmv_block_product_workspace_bytes(T, O, K)
+    lay = (T + O) * 8192
+    assert most >= lay
+    stream = torch.cuda.current_stream().cuda_stream
+    call = lambda p, n: lib.dmmv_block_product(x._p, w._p, None, name, y.data_ptr(), O, p, n, stream)  # noqa: E731
+    if needs == "nothing":
+        dmmv._check(call(None, 0))
+    else:
+        assert call(None, 0) == -5
+        room = torch.full((most + 4096,), 0xA5, dtype=torch.uint8, device=gpu_device)
+        assert call(room.data_ptr(), lay - 1) == -5
+        dmmv._check(call(room.data_ptr(), most))
+        assert bool((room[most:] == 0xA5).all())
+    want = dmmv.dmmv_block_dequantize(x, torch.float32).double() @ dmmv.dmmv_block_dequantize(w, torch.float32).double().t()
+    assert torch.equal(y, want.to(dtype)) and torch.equal(dmmv.dmmv_block_product(x, w, dtype=dtype), y)
