@@ -10,6 +10,15 @@
  *   dmmv_block_product        y = x w^T + bias of two such matrices
  *   dmmv_block_backward       its gradients, from the checkpoint of x
  *
+ * and what stands around such layers in a residual block and its training step:
+ *
+ *   dmmv_block_linear         the product with an activation and a residual in its epilogue, in 8 bits too
+ *   dmmv_activation_backward  back through the activation, with the gradient of the bias
+ *   dmmv_residual_norm        the norm after a block, its gate, the residual scale and the next block's norm
+ *   dmmv_residual_norm_backward
+ *   dmmv_gradient_norm        the norm over all gradients of a step
+ *   dmmv_gradient_clip        and the gradients scaled to it
+ *
  * An 8-bit matrix ("block matrix") holds codes in the e4m3 format of the OCP 8-bit floating-point
  * specification (no infinities, largest value 448, 0x7F and 0xFF are NaN) and a scale for each
  * block of 128 columns:
@@ -123,6 +132,89 @@ dmmv_status dmmv_layernorm_backward(int32_t dtype, int64_t rows, int64_t cols, c
                                     int64_t ldx, const dmmv_block_matrix* xq, const float* gamma, const float* mean,
                                     const float* rstd, void* dx, int64_t lddx, float* dgamma, float* dbeta,
                                     void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- a residual block --------------------------------------------------------------------------- */
+
+/* Activations: max(u, 0); u Phi(u) with the normal distribution's function Phi; the same with its usual approximation
+ * 1 / (1 + exp(-2 z)), z = sqrt(2 / pi) (u + 0.044715 u^3); u / (1 + exp(-u)).  At infinities they have their limits.
+ * For bf16 results the last three are evaluated to a relative 2^-14, else to 32 bits. */
+enum { DMMV_ACT_NONE = 0, DMMV_ACT_RELU = 1, DMMV_ACT_GELU = 2, DMMV_ACT_GELU_TANH = 3, DMMV_ACT_SILU = 4 };
+
+/* u = x w^T + bias as dmmv_block_product has it, v = act(u) + residual, x [T][K], w [O][K], residual [T][ldr] of dtype or NULL.
+ * Outputs, each may be NULL: y [T][ldy] = v in dtype; q = v in 8 bits, quantised like dmmv_block_quantize from the 32-bit v
+ * (scale_rows 1); u [T][ldu] in dtype, for dmmv_activation_backward.  Sums are those of dmmv_block_product for dtype, but with q and
+ * up to 64 tokens those of 32 bits in any case.  The gradient of the residual is that of y; those of x, w and bias follow
+ * from u's by dmmv_block_backward.  The workspace (256-byte aligned) holds what that of dmmv_block_product holds, and the 32-bit v
+ * where q is made from it afterwards; ..._for is what the call with these arguments needs (nothing is read but the descriptors;
+ * has_q says whether there is a q; 0 where the call would be refused). */
+size_t dmmv_block_linear_workspace_for(const dmmv_block_matrix* x, const dmmv_block_matrix* w, int32_t dtype, int32_t has_q);
+dmmv_status dmmv_block_linear(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, int32_t act, const void* residual,
+                              int64_t ldr, int32_t dtype, void* y, int64_t ldy, const dmmv_block_matrix* q, void* u, int64_t ldu,
+                              void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* du = dy act'(u) [rows][lddu] and dbias = its sum over rows, float [cols]; dy [rows][lddy], u [rows][ldu], all of dtype, act not
+ * DMMV_ACT_NONE.  Either result may be NULL.  dbias sums the 32-bit products.  The derivative of max(u, 0) at 0 is 0; at infinities
+ * derivatives are their limits.  The workspace (256-byte aligned) is for dbias alone. */
+size_t dmmv_activation_workspace_bytes(int64_t rows, int64_t cols);
+dmmv_status dmmv_activation_backward(int32_t dtype, int64_t rows, int64_t cols, const void* dy, int64_t lddy, const void* u,
+                                     int64_t ldu, int32_t act, void* du, int64_t lddu, float* dbias, void* workspace,
+                                     size_t workspace_bytes, void* hip_stream);
+
+/* A norm of rows: (x - mean) rstd gamma + beta as dmmv_layernorm has it, or with rms = 1 without a mean,
+ * rstd = 1 / sqrt(sum x^2 / cols + eps).  gamma, beta float [cols], NULL = 1, 0. */
+typedef struct {
+    const float* gamma;
+    const float* beta;
+    float eps;                   /* >= 0 and finite */
+    int32_t rms;
+} dmmv_norm;
+
+/* What follows a block f of a residual stream h, both [rows][.] of dtype:
+ *   v = alpha h + gate post(f),   y = pre(v)
+ * with the norm after this block (post; NULL = f itself), the norm before the next one (pre; NULL = none, no y and q), a gate
+ * float [ceil(rows / gate_rows)][ldgate] for every gate_rows rows (NULL = 1; one for all with gate_rows >= rows), and a finite alpha.
+ * Outputs, each may be NULL: v [rows][ldv] and y [rows][ldy] of dtype, q = y in 8 bits (scale_rows 1), the norms' statistics float
+ * [rows] (means 0 with rms).  v is held in 32 bits until it has been normalised. */
+dmmv_status dmmv_residual_norm(int32_t dtype, int64_t rows, int64_t cols, const void* f, int64_t ldf, const void* h, int64_t ldh,
+                               float alpha, const float* gate, int64_t ldgate, int64_t gate_rows, const dmmv_norm* post,
+                               const dmmv_norm* pre, void* v, int64_t ldv, void* y, int64_t ldy, const dmmv_block_matrix* q,
+                               float* post_mean, float* post_rstd, float* mean, float* rstd, void* hip_stream);
+
+/* Its gradients, from those of y (dy; given if and only if pre is) and of v (dv, as the residual stream brings it; NULL = 0, only
+ * with dy), from f (needed with post or dgate) and v (with pre) and the forward pass's statistics (means not with rms):
+ *   e = dv + pre'(dy),  dh = alpha e,  df = post'(gate e),  dgate [groups][lddgate] = sum over a gate's rows of e post(f),
+ *   dpost_gamma, dpost_beta, dgamma, dbeta float [cols]
+ * Each may be NULL.  The workspace (256-byte aligned; gate_rows 0 without a gate) holds partial sums. */
+size_t dmmv_residual_norm_workspace_bytes(int64_t rows, int64_t cols, int64_t gate_rows);
+dmmv_status dmmv_residual_norm_backward(int32_t dtype, int64_t rows, int64_t cols, const void* dy, int64_t lddy, const void* dv,
+                                        int64_t lddv, const void* f, int64_t ldf, const void* v, int64_t ldv, float alpha,
+                                        const float* gate, int64_t ldgate, int64_t gate_rows, const dmmv_norm* post,
+                                        const dmmv_norm* pre, const float* post_mean, const float* post_rstd, const float* mean,
+                                        const float* rstd, void* df, int64_t lddf, void* dh, int64_t lddh, float* dgate,
+                                        int64_t lddgate, float* dpost_gamma, float* dpost_beta, float* dgamma, float* dbeta,
+                                        void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* One of many tensors: a matrix [rows][ld] of dtype DMMV_F32 or DMMV_BF16 (a contiguous tensor is one row). */
+typedef struct {
+    void* data;
+    int64_t rows, cols, ld;
+    int32_t dtype;
+} dmmv_gradient;
+
+/* norm (one float) <- the square root of the sum of squares over all numbers of all tensors, summed in 64 bits; the HOST array is read
+ * before the call returns.  The workspace (256-byte aligned) holds partial sums; its size serves any call with tensors of these
+ * sizes. */
+size_t dmmv_gradient_workspace_bytes(int64_t count, const dmmv_gradient* gradients);
+dmmv_status dmmv_gradient_norm(int64_t count, const dmmv_gradient* gradients, float* norm, void* workspace, size_t workspace_bytes,
+                               void* hip_stream);
+
+/* out <- c gradients with c = max_norm / (norm + eps), 1 where that is not below 1; out NULL = in place, where c = 1 writes nothing.
+ * out has the gradients' sizes, in either type.  given: a norm (one float) from elsewhere, over more gradients than these; NULL = the norm of
+ * these.  norm (or NULL) <- the norm that was used.  max_norm and eps are finite and not negative.  A norm that is infinite makes finite
+ * numbers 0 and others NaN, one that is NaN makes all NaN.  Tensors that are written must not share memory (refused).  The
+ * workspace, of dmmv_gradient_workspace_bytes, is not needed with given. */
+dmmv_status dmmv_gradient_clip(int64_t count, const dmmv_gradient* gradients, const dmmv_gradient* out, float max_norm, float eps,
+                               const float* given, float* norm, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -57,6 +57,19 @@ dmmv_status layer_check_workspace(const void* ws, size_t have, size_t need) {
     return DMMV_OK;
 }
 
+dmmv_status layer_check_vector(const float* p, bool needed, const char* what) {
+    if (needed && !p) return fail(DMMV_ERR_NULL, "%s is NULL", what);
+    if ((uintptr_t)p % 4) return fail(DMMV_ERR_SHAPE, "%s is not aligned to its elements", what);
+    return DMMV_OK;
+}
+
+dmmv_status layer_check_out_block(const dmmv_block_matrix* q, int64_t rows, int64_t cols, const char* what) {
+    DMMV_TRY(layer_check_block(q, true, what));
+    if (q->rows != rows || q->cols != cols) return fail(DMMV_ERR_SHAPE, "%s is not %lld x %lld", what, (long long)rows, (long long)cols);
+    if (q->scale_rows != 1) return fail(DMMV_ERR_UNSUPPORTED, "%s: a row's blocks have scales of their own (scale_rows 1)", what);
+    return DMMV_OK;
+}
+
 BlockView layer_view(const dmmv_block_matrix* q) {
     BlockView v = {};
     if (!q) return v;

@@ -7,7 +7,7 @@
 // 32-bit sum (8e-8) at half the rate: a code is exact in f16.
 #include <type_traits>
 
-#include "dmmv_layer_common.h"
+#include "dmmv_activation.h"
 
 namespace dmmv {
 
@@ -59,6 +59,80 @@ __device__ __forceinline__ intx8 words8(piece16 a, piece16 b) {
     return intx8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
 }
 
+// ---- what becomes of a product ---------------------------------------------------------------------
+// The result alone, or with EPI what follows it: v = act(u) + residual of the product u, as y, in 8 bits, or in 32 bits for a
+// pass that makes 8 bits of it; and u itself.
+template <class T, bool EPI>
+struct ProductOut {
+    T* y;
+    int64_t ldy;
+};
+template <class T>
+struct ProductOut<T, true> {
+    T* y;                                // each may be NULL
+    int64_t ldy;
+    const T* residual;
+    int64_t ldr;
+    T* u;
+    int64_t ldu;
+    float* v;                            // [T][O]
+    BlockView q;
+    int32_t act, has_q;
+};
+
+// eight columns of u from `col` on; r the residual's; with Q the 16 lanes of a block of 128 come together (`ok`: the row is there)
+template <bool Q, class T>
+__device__ __forceinline__ void finish8(const ProductOut<T, true>& o, int64_t row, int64_t col, int64_t cols, bool ok, float (&v)[8], const float (&r)[8]) {
+    if (ok && o.u) store8(o.u + row * o.ldu, col, cols, v);
+    act_values<sizeof(T) == 2>(o.act, v);
+    if (o.residual)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += r[e];
+    if (ok && o.y) store8(o.y + row * o.ldy, col, cols, v);
+    if constexpr (Q) {
+        if (!o.has_q) return;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = col + e < cols ? v[e] : 0.0f;
+        const uint32_t b = scale_byte(row16_max(max8_bits(v)));
+        if (ok && col < cols) {
+            store8_codes(o.q.codes + row * o.q.ld, col, cols, encode8(v, b));
+            if ((threadIdx.x & 15) == 0) scale_put(o.q, row, col >> 7, b);
+        }
+    } else {
+        if (ok && o.v) store8(o.v + row * cols, col, cols, v);
+    }
+}
+// one number of u
+template <class T>
+__device__ __forceinline__ void finish1(const ProductOut<T, true>& o, int64_t row, int64_t col, int64_t cols, float u) {
+    if (o.u) put_y(o.u + row * o.ldu + col, u);
+    float v[1] = {u};
+    act_values<false>(o.act, v);
+    if (o.residual) v[0] += value_of(o.residual[row * o.ldr + col]);
+    if (o.y) put_y(o.y + row * o.ldy + col, v[0]);
+    if (o.v) o.v[row * cols + col] = v[0];
+}
+// ROWS x COLS numbers of u in the LDS (rows of LD floats), the first at row0, col0; 256 threads
+template <int ROWS, int COLS, int LD, bool Q, class T, class F>
+__device__ __forceinline__ void finish_tile(const ProductOut<T, true>& o, const float* u, int64_t rows, int64_t cols, int64_t col0, F row_of) {
+    constexpr int PER_ROW = COLS / 8, TURNS = ROWS * PER_ROW / 256;
+#pragma unroll 1
+    for (int k = 0; k < TURNS; ++k) {
+        const int c = (int)threadIdx.x + 256 * k, r = c / PER_ROW, h = c % PER_ROW;
+        const int64_t row = row_of(r), col = col0 + h * 8;
+        const bool ok = row < rows && col < cols;
+        float v[8], b[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (ok && o.residual) load8(o.residual + row * o.ldr, col, cols, b);
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+            const floatx4 f = *reinterpret_cast<const floatx4*>(u + r * LD + h * 8 + e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[e + i] = f[i];
+        }
+        finish8<Q>(o, row, col, cols, ok, v, b);
+    }
+}
+
 // ---- any sizes, strides, scales ------------------------------------------------------------------
 // Tile of 64 tokens x 64 outputs, 4 wavefronts (2 x 2), one block of 128 a step.  A step's codes and scales go from
 // memory through registers, requested two steps ahead, into one of two LDS stages while the other is multiplied.  The
@@ -108,9 +182,9 @@ __device__ __forceinline__ bool row_beyond(const BlockView& q, int64_t row, int6
 // 32 x 32 results with any scales, straight from memory: lane (lr, lg) has 32 codes of two rows of each operand and block, and the results
 // of four outputs and two tokens twice.  500 x 1777 x 2731 in 32 bits with all scales of x 2^-126: 133 us, the loop and then this; with those of
 // zeros 39.
-template <class T, bool SCALED>
+template <class T, bool SCALED, class P>
 __device__ __forceinline__ void tile_any(int64_t t0, int64_t T_, int64_t o0, int64_t O, int64_t K, const BlockView& x, const BlockView& w, ProductScales how,
-                                         const float* __restrict__ bias, T* __restrict__ y, int64_t ldy) {
+                                         const float* __restrict__ bias, P put) {
     int lane = threadIdx.x & 63;
     floatx4 acc[2][2];
 #pragma unroll
@@ -161,7 +235,7 @@ __device__ __forceinline__ void tile_any(int64_t t0, int64_t T_, int64_t o0, int
                 const int64_t oe = o0 + 16 * i + lg * 4 + e;
                 if (oe >= O) continue;
                 const float so = SCALED && !how.w_blocks ? row_scale(scale_at(w, oe, 0)).rest : 1.0f;
-                put_y(y + t * ldy + oe, dmmv_fma(acc[i][j][e] * so, st, bias ? bias[oe] : 0.0f));
+                put(t, oe, dmmv_fma(acc[i][j][e] * so, st, bias ? bias[oe] : 0.0f));
             }
     }
 }
@@ -169,9 +243,9 @@ __device__ __forceinline__ void tile_any(int64_t t0, int64_t T_, int64_t o0, int
 // WAVES: wavefronts a SIMD that the registers leave room for at least.  32-bit results use more than three (32-bit scales) and four (exponents) allow:
 // where a compute unit gets one tile they stay (500 x 1777 x 2731 20.6 and 19.8 us, 21.5 and 20.4 with three and four), else not (4096 x 11008 x 4096
 // 570 and 500 us, 650 and 530 without).
-template <class T, bool SCALED, int WAVES>
+template <class T, bool SCALED, int WAVES, bool EPI>
 __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
-                                                       const float* __restrict__ bias, T* __restrict__ y, int64_t ldy, int32_t tiles_t, int32_t tiles_o) {
+                                                       const float* __restrict__ bias, ProductOut<T, EPI> out, int32_t tiles_t, int32_t tiles_o) {
     constexpr bool WIDE = sizeof(T) == 4;
     constexpr int MI = 2, NI = 2, BM = 32 * MI, BN = 32 * NI;
     __shared__ __align__(16) uint8_t codes[2][128 * (BM + BN)];
@@ -339,11 +413,18 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
             if (bad) again = 1;
             __syncthreads();
             if (again) {
-                tile_any<T, SCALED>(t0 + wt, T_, o0 + wo, O, K, x, w, how, bias, y, ldy);
+                tile_any<T, SCALED>(t0 + wt, T_, o0 + wo, O, K, x, w, how, bias, [&](int64_t t, int64_t o, float v) __attribute__((always_inline)) {
+                    if constexpr (EPI) finish1(out, t, o, O, v);
+                    else put_y(out.y + t * out.ldy + o, v);
+                });
                 return;
             }
         }
     }
+    constexpr int LDO = BN + 4;
+    static_assert(BM * LDO * 4 <= (int)sizeof(codes), "the results take the stages' place");
+    float* tile = reinterpret_cast<float*>(codes[0]);
+    if constexpr (EPI) __syncthreads();              // the last block has been read
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
         float bo[4], so[4];
@@ -358,10 +439,20 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
             const int64_t t = t0 + wt + 16 * j + lr, o = o0 + wo + 16 * i + lg * 4;
             if (t >= T_) continue;
             const float st = SCALED && !how.x_blocks ? row_scale(scale_at(x, t, 0)).rest : 1.0f;
+            if constexpr (EPI) {
+                *reinterpret_cast<floatx4*>(tile + (wt + 16 * j + lr) * LDO + wo + 16 * i + lg * 4) =
+                    floatx4{dmmv_fma(acc[i][j][0] * so[0], st, bo[0]), dmmv_fma(acc[i][j][1] * so[1], st, bo[1]), dmmv_fma(acc[i][j][2] * so[2], st, bo[2]),
+                            dmmv_fma(acc[i][j][3] * so[3], st, bo[3])};
+            } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (o + e < O) put_y(y + t * ldy + o + e, dmmv_fma(acc[i][j][e] * so[e], st, bo[e]));
+                for (int e = 0; e < 4; ++e)
+                    if (o + e < O) put_y(out.y + t * out.ldy + o + e, dmmv_fma(acc[i][j][e] * so[e], st, bo[e]));
+            }
         }
+    }
+    if constexpr (EPI) {
+        __syncthreads();
+        finish_tile<BM, BN, LDO, false>(out, tile, T_, O, o0, [&](int r) { return t0 + r; });
     }
 }
 
@@ -394,14 +485,15 @@ __device__ __forceinline__ void stage_exponents(const BlockView& q, int64_t row0
     }
 }
 
-constexpr int product_lds(int MI, int NI, int width, int ws, int nst) {
-    const int stages = nst * 128 * 32 * (MI + NI) + 68 * (32 * MI + (ws == 2 ? 0 : ws == 1 ? (32 * NI + 127) / 128 : 32 * NI)), out = 32 * MI * (32 * NI * width + 16);
+constexpr int product_lds(int MI, int NI, int width, int ws, int nst, bool epi) {
+    const int stages = nst * 128 * 32 * (MI + NI) + 68 * (32 * MI + (ws == 2 ? 0 : ws == 1 ? (32 * NI + 127) / 128 : 32 * NI));
+    const int out = epi ? 2 * 64 * (32 * NI * 4 + 16) : 32 * MI * (32 * NI * width + 16);
     return stages > out ? stages : out;
 }
 
-template <class T, int MI, int NI, int WS, int NST>
+template <class T, int MI, int NI, int WS, int NST, bool EPI>
 __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
-                                                             const float* __restrict__ bias, T* __restrict__ y, int64_t ldy,
+                                                             const float* __restrict__ bias, ProductOut<T, EPI> out,
                                                              int32_t tiles_t, int32_t tiles_o) {
     extern __shared__ __align__(16) uint8_t lds[];
     constexpr int BM = 32 * MI, BN = 32 * NI, STAGE = 128 * (BM + BN);
@@ -418,7 +510,7 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
         if (how.x_blocks) x.scales = static_cast<uint8_t*>(x.scales) + from * x.sblk;
         if (how.w_blocks) w.scales = static_cast<uint8_t*>(w.scales) + from * w.sblk;
         K = min(K - from * 128, share * 128);
-        y += (int64_t)blockIdx.y * T_ * O;
+        out.y += (int64_t)blockIdx.y * T_ * O;
     }
     const int nb = (int)((K + 127) >> 7);
 
@@ -624,6 +716,41 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
             for (int j = 0; j < MI; ++j) mul(C0, i, j);
     }
     __syncthreads();
+    if constexpr (EPI) {
+        // 64 rows at a time through the LDS in 32 bits, two places in turn: 32 of each half of the tile's rows
+        constexpr int LDF = BN + 4;
+        auto pass = [&](auto P) __attribute__((always_inline)) {
+            constexpr int p = P.value;
+            float* tile = reinterpret_cast<float*>(lds) + (p & 1) * 64 * LDF;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                float bo[4], so[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int64_t o = min(o0 + wo + 16 * i + lg * 4 + e, O - 1);
+                    bo[e] = bias ? bias[o] : 0.0f;
+                    so[e] = !how.w_blocks ? row_scale(scale_at(w, o, 0)).rest : 1.0f;
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float st = !how.x_blocks ? row_scale(scale_at(x, min(t0 + wt + 16 * (2 * p + j) + lr, T_ - 1), 0)).rest : 1.0f;
+                    float v[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = dmmv_fma(acc[i][2 * p + j][e] * so[e], st, bo[e]);
+                    put4(tile + ((wv & 1) * 32 + 16 * j + lr) * LDF + wo + 16 * i + lg * 4, v);
+                }
+            }
+            __syncthreads();
+            finish_tile<64, BN, LDF, true>(out, tile, T_, O, o0, [&](int r) { return t0 + (r >> 5) * (BM / 2) + 32 * p + (r & 31); });
+        };
+        pass(C0);
+        pass(C1);
+        if constexpr (MI == 8) {
+            pass(std::integral_constant<int, 2>{});
+            pass(std::integral_constant<int, 3>{});
+        }
+        return;
+    }
     // results through the LDS: rows of the tile, stored 16 bytes a lane
     constexpr int LDO = BN * (int)sizeof(T) + 16;
 #pragma unroll
@@ -651,7 +778,7 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
         const int64_t t = t0 + r, o = o0 + h * PER;
         if (t >= T_ || o >= O) continue;
         const piece16 v = *reinterpret_cast<const piece16*>(lds + r * LDO + h * 16);
-        T* dst = y + t * ldy + o;
+        T* dst = out.y + t * out.ldy + o;
         if (o + PER <= O) {
             *reinterpret_cast<piece16_any*>(dst) = v;
         } else {
@@ -668,10 +795,9 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
 // 16 MT tokens, its four wavefronts a share of the blocks each, joined in order through the LDS.  U blocks are
 // requested at a time.  One token of 4096 by 11008 outputs: 10.5 us, 4.3 TB/s; 24 tokens of 4096 by 4096: 9.9 us, two thirds of it start,
 // join and end (eight wavefronts a workgroup were no faster).
-template <class T, int MT, bool SCALED>
+template <class T, int MT, bool SCALED, bool WIDE, bool EPI>
 __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
-                                                                  const float* __restrict__ bias, T* __restrict__ y, int64_t ldy) {
-    constexpr bool WIDE = sizeof(T) == 4;
+                                                                  const float* __restrict__ bias, ProductOut<T, EPI> out) {
     constexpr int U = MT >= 4 ? 2 : 4, WAVES = 4;
     __shared__ floatx4 part[WAVES][MT][64];
     const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
@@ -819,31 +945,33 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
             const int64_t o = o0 + lg * 4 + e;
             if (o >= O) continue;
             const float so = SCALED && !how.w_blocks ? row_scale(scale_at(w, o, 0)).rest : 1.0f;
-            put_y(y + t * ldy + o, dmmv_fma(v[e] * so, st, bias ? bias[o] : 0.0f));
+            const float u = dmmv_fma(v[e] * so, st, bias ? bias[o] : 0.0f);
+            if constexpr (EPI) finish1(out, t, o, O, u);
+            else put_y(out.y + t * out.ldy + o, u);
         }
     }
 }
 
-template <class T, int MT>
+template <class T, int MT, bool WIDE, bool EPI>
 static dmmv_status launch_few_of(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const ProductScales& how, bool scaled, const float* bias,
-                                 T* y, int64_t ldy, hipStream_t s) {
+                                 const ProductOut<T, EPI>& out, hipStream_t s) {
     const dim3 grid((unsigned)ceil_div(w->rows, 16), (unsigned)ceil_div(x->rows, 16 * MT));
     if (scaled)
-        hipLaunchKernelGGL((k_block_product_few<T, MT, true>), grid, dim3(256), 0, s, (int32_t)x->rows, w->rows, x->cols, layer_view(x), layer_view(w),
-                           how, bias, y, ldy);
+        hipLaunchKernelGGL((k_block_product_few<T, MT, true, WIDE, EPI>), grid, dim3(256), 0, s, (int32_t)x->rows, w->rows, x->cols, layer_view(x),
+                           layer_view(w), how, bias, out);
     else
-        hipLaunchKernelGGL((k_block_product_few<T, MT, false>), grid, dim3(256), 0, s, (int32_t)x->rows, w->rows, x->cols, layer_view(x), layer_view(w),
-                           how, bias, y, ldy);
+        hipLaunchKernelGGL((k_block_product_few<T, MT, false, WIDE, EPI>), grid, dim3(256), 0, s, (int32_t)x->rows, w->rows, x->cols, layer_view(x),
+                           layer_view(w), how, bias, out);
     DMMV_LAUNCH_CHECK();
     return DMMV_OK;
 }
 
-template <class T>
+template <class T, bool WIDE, bool EPI>
 static dmmv_status launch_few(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const ProductScales& how, bool scaled, const float* bias,
-                              T* y, int64_t ldy, hipStream_t s) {
-    if (x->rows <= 16) return launch_few_of<T, 1>(x, w, how, scaled, bias, y, ldy, s);
-    if (x->rows <= 32) return launch_few_of<T, 2>(x, w, how, scaled, bias, y, ldy, s);
-    return launch_few_of<T, 4>(x, w, how, scaled, bias, y, ldy, s);
+                              const ProductOut<T, EPI>& out, hipStream_t s) {
+    if (x->rows <= 16) return launch_few_of<T, 1, WIDE, EPI>(x, w, how, scaled, bias, out, s);
+    if (x->rows <= 32) return launch_few_of<T, 2, WIDE, EPI>(x, w, how, scaled, bias, out, s);
+    return launch_few_of<T, 4, WIDE, EPI>(x, w, how, scaled, bias, out, s);
 }
 
 // scales that are the same along a row leave the sum
@@ -853,10 +981,11 @@ static bool constant_rows(const dmmv_block_matrix* q) { return !q->scales || q->
 static bool aligned(const dmmv_block_matrix* q) { return q->ld < 1 << 23 && q->ld % 16 == 0 && (uintptr_t)q->codes % 16 == 0; }
 
 // y = bias and the sum of the shares, by ascending share; 8 outputs a lane
+template <bool EPI>
 __global__ __launch_bounds__(256) void k_block_product_join(int64_t T_, int64_t O, int32_t shares, const float* __restrict__ part,
-                                                            const float* __restrict__ bias, bf16_t* __restrict__ y, int64_t ldy) {
+                                                            const float* __restrict__ bias, ProductOut<bf16_t, EPI> out) {
     const int64_t t = blockIdx.x * 4ll + (threadIdx.x >> 6), o = (blockIdx.y * 64ll + (threadIdx.x & 63)) * 8;
-    if (t >= T_ || o >= O) return;
+    if (t >= T_ || (!EPI && o >= O)) return;         // (whole wavefronts; the lanes of a block of 128 stay together)
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, p[8];
 #pragma unroll 4
     for (int i = 0; i < shares; ++i) {
@@ -869,20 +998,25 @@ __global__ __launch_bounds__(256) void k_block_product_join(int64_t T_, int64_t 
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += p[e];
     }
-    store8(y + t * ldy, o, O, v);
+    if constexpr (EPI) {
+        if (out.residual) load8(out.residual + t * out.ldr, o, O, p);
+        finish8<true>(out, t, o, O, o < O, v, p);
+    } else {
+        store8(out.y + t * out.ldy, o, O, v);
+    }
 }
 
-template <class T, int MI, int NI, int WS, int NST>
-static dmmv_status launch_tiled(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, T* y, int64_t ldy, hipStream_t s,
+template <class T, int MI, int NI, int WS, int NST, bool EPI>
+static dmmv_status launch_tiled(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, const ProductOut<T, EPI>& out, hipStream_t s,
                                 int32_t shares = 1) {
     const int64_t tiles_t = ceil_div(x->rows, 32 * MI), tiles_o = ceil_div(w->rows, 32 * NI);
     if (tiles_t > INT32_MAX / 4 / tiles_o) return fail(DMMV_ERR_SHAPE, "y: more tiles than a launch takes");
-    const void* kern = (const void*)k_block_product_tiled<T, MI, NI, WS, NST>;
-    constexpr int bytes = product_lds(MI, NI, sizeof(T), WS, NST);
+    const void* kern = (const void*)k_block_product_tiled<T, MI, NI, WS, NST, EPI>;
+    constexpr int bytes = product_lds(MI, NI, sizeof(T), WS, NST, EPI);
     DMMV_TRY(ensure_dynamic_lds(kern, bytes));
     const ProductScales how = {!constant_rows(x), !constant_rows(w)};
-    hipLaunchKernelGGL((k_block_product_tiled<T, MI, NI, WS, NST>), dim3((unsigned)(tiles_t * tiles_o), (unsigned)shares), dim3(256), bytes, s, x->rows, w->rows,
-                       x->cols, layer_view(x), layer_view(w), how, bias, y, ldy, (int32_t)tiles_t, (int32_t)tiles_o);
+    hipLaunchKernelGGL((k_block_product_tiled<T, MI, NI, WS, NST, EPI>), dim3((unsigned)(tiles_t * tiles_o), (unsigned)shares), dim3(256), bytes, s, x->rows,
+                       w->rows, x->cols, layer_view(x), layer_view(w), how, bias, out, (int32_t)tiles_t, (int32_t)tiles_o);
     DMMV_LAUNCH_CHECK();
     return DMMV_OK;
 }
@@ -907,13 +1041,14 @@ static size_t product_part_bytes(int64_t T, int64_t O, int64_t K) {
 }
 
 // bf16 results by the large tiles: 256 x 256, or 128 x 128 with more stages; part: room for the shares, or NULL
-static dmmv_status product_tiled(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, bf16_t* y, int64_t ldy, float* part,
+template <bool EPI>
+static dmmv_status product_tiled(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, const ProductOut<bf16_t, EPI>& out, float* part,
                                  hipStream_t s) {
     const int32_t shares = part ? product_shares(x->rows, w->rows, x->cols) : 1;
     if (shares > 1) {
-        DMMV_TRY((launch_tiled<float, 4, 4, 0, 4>(x, w, nullptr, part, w->rows, s, shares)));
-        hipLaunchKernelGGL(k_block_product_join, dim3((unsigned)ceil_div(x->rows, 4), (unsigned)ceil_div(w->rows, 512)), dim3(256), 0, s, x->rows,
-                           w->rows, shares, part, bias, y, ldy);
+        DMMV_TRY((launch_tiled<float, 4, 4, 0, 4, false>(x, w, nullptr, {part, w->rows}, s, shares)));
+        hipLaunchKernelGGL((k_block_product_join<EPI>), dim3((unsigned)ceil_div(x->rows, 4), (unsigned)ceil_div(w->rows, 512)), dim3(256), 0, s, x->rows,
+                           w->rows, shares, part, bias, out);
         DMMV_LAUNCH_CHECK();
         return DMMV_OK;
     }
@@ -925,8 +1060,8 @@ static dmmv_status product_tiled(const dmmv_block_matrix* x, const dmmv_block_ma
     // a round of large tiles takes 2.25 times one of small ones (K = 4096: 46 us and 20.5; 1024 x 4096 x 11008 54 and 62 us,
     // 2048 x 4096 x 4096 51 and 44)
     if ((along || w->scale_rows == 128) && 9 * ceil_div(large, cus) < 4 * ceil_div(small, cus))
-        return along ? launch_tiled<bf16_t, 8, 8, 2, 2>(x, w, bias, y, ldy, s) : launch_tiled<bf16_t, 8, 8, 1, 2>(x, w, bias, y, ldy, s);
-    return launch_tiled<bf16_t, 4, 4, 0, 4>(x, w, bias, y, ldy, s);
+        return along ? launch_tiled<bf16_t, 8, 8, 2, 2, EPI>(x, w, bias, out, s) : launch_tiled<bf16_t, 8, 8, 1, 2, EPI>(x, w, bias, out, s);
+    return launch_tiled<bf16_t, 4, 4, 0, 4, EPI>(x, w, bias, out, s);
 }
 
 // Rows that are no multiple of 16 codes are laid out for the large tiles where the general kernel would
@@ -969,36 +1104,69 @@ static ProductPlan product_plan(const dmmv_block_matrix* x, const dmmv_block_mat
     return p;
 }
 
-template <class T>
-static dmmv_status product(const ProductPlan& plan, const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, T* y, int64_t ldy, void* ws,
-                           hipStream_t s) {
+template <class T, bool WIDE, bool EPI>
+static dmmv_status product(const ProductPlan& plan, const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, const ProductOut<T, EPI>& out,
+                           void* ws, hipStream_t s) {
     const ProductScales how = {!constant_rows(x), !constant_rows(w)};
     const bool scaled = plan.scaled;
-    if (plan.path == ProductPlan::FEW) return launch_few(x, w, how, scaled, bias, y, ldy, s);
+    if (plan.path == ProductPlan::FEW) return launch_few<T, WIDE, EPI>(x, w, how, scaled, bias, out, s);
     float* part = plan.bytes > plan.lay ? reinterpret_cast<float*>(static_cast<char*>(ws) + plan.lay) : nullptr;
-    if (plan.path == ProductPlan::TILES) return product_tiled(x, w, bias, reinterpret_cast<bf16_t*>(y), ldy, part, s);
-    if (plan.path == ProductPlan::LAID) {
-        dmmv_block_matrix lx = *x, lw = *w;
-        lx.ld = lw.ld = ceil_div(x->cols, 128) * 128;
-        lx.codes = ws;
-        lw.codes = static_cast<uint8_t*>(ws) + x->rows * lx.ld;
-        DMMV_TRY(layer_lay_codes(x, static_cast<uint8_t*>(lx.codes), lx.ld, s));
-        DMMV_TRY(layer_lay_codes(w, static_cast<uint8_t*>(lw.codes), lw.ld, s));
-        return product_tiled(&lx, &lw, bias, reinterpret_cast<bf16_t*>(y), ldy, part, s);
+    if constexpr (sizeof(T) == 2) {
+        if (plan.path == ProductPlan::TILES) return product_tiled<EPI>(x, w, bias, out, part, s);
+        if (plan.path == ProductPlan::LAID) {
+            dmmv_block_matrix lx = *x, lw = *w;
+            lx.ld = lw.ld = ceil_div(x->cols, 128) * 128;
+            lx.codes = ws;
+            lw.codes = static_cast<uint8_t*>(ws) + x->rows * lx.ld;
+            DMMV_TRY(layer_lay_codes(x, static_cast<uint8_t*>(lx.codes), lx.ld, s));
+            DMMV_TRY(layer_lay_codes(w, static_cast<uint8_t*>(lw.codes), lw.ld, s));
+            return product_tiled<EPI>(&lx, &lw, bias, out, part, s);
+        }
     }
     const int64_t tiles_t = ceil_div(x->rows, 64), tiles_o = ceil_div(w->rows, 64);
     if (tiles_t > INT32_MAX / 4 / tiles_o) return fail(DMMV_ERR_SHAPE, "y: more tiles than a launch takes");
     const dim3 grid((unsigned)(tiles_t * tiles_o));
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, x->rows, w->rows, x->cols, layer_view(x), layer_view(w), how, bias, y, ldy, (int32_t)tiles_t,
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, x->rows, w->rows, x->cols, layer_view(x), layer_view(w), how, bias, out, (int32_t)tiles_t,
                            (int32_t)tiles_o);
     };
     const bool one_each = tiles_t * tiles_o <= 256;
-    if (sizeof(T) == 2) scaled ? launch(k_block_product<T, true, 1>) : launch(k_block_product<T, false, 3>);
-    else if (one_each) scaled ? launch(k_block_product<T, true, 1>) : launch(k_block_product<T, false, sizeof(T) == 4 ? 1 : 3>);
-    else scaled ? launch(k_block_product<T, true, sizeof(T) == 4 ? 4 : 1>) : launch(k_block_product<T, false, 3>);
+    if (sizeof(T) == 2) scaled ? launch(k_block_product<T, true, 1, EPI>) : launch(k_block_product<T, false, 3, EPI>);
+    else if (one_each) scaled ? launch(k_block_product<T, true, 1, EPI>) : launch(k_block_product<T, false, sizeof(T) == 4 ? 1 : 3, EPI>);
+    else scaled ? launch(k_block_product<T, true, sizeof(T) == 4 ? 4 : 1, EPI>) : launch(k_block_product<T, false, 3, EPI>);
     DMMV_LAUNCH_CHECK();
     return DMMV_OK;
+}
+
+// The same with what follows it.  8 bits come from the kernel that has whole blocks of 128 outputs of a row (tiles, shares); the others write
+// v in 32 bits, `v` bytes further on in the workspace.  Few tokens in 8 bits are bound by the weights' bytes, so the 16-bit instructions
+// sum them at no cost, in 32 bits: otherwise one number in some 500 goes to the other neighbour on the 8-bit grid.
+struct LinearPlan {
+    ProductPlan product;
+    size_t v, bytes;                     // where v begins (0 without one: bytes = product.bytes), all
+    bool pass;                           // 8 bits by a pass over v
+};
+static LinearPlan linear_plan(const dmmv_block_matrix* x, const dmmv_block_matrix* w, bool f32, bool has_q) {
+    LinearPlan p = {product_plan(x, w, f32), 0, 0, false};
+    if (has_q && x->rows <= 64) {
+        p.product.path = ProductPlan::FEW;
+        p.product.lay = p.product.bytes = 0;
+    }
+    p.pass = has_q && (p.product.path == ProductPlan::FEW || p.product.path == ProductPlan::GENERAL);
+    p.v = (p.product.bytes + 255) / 256 * 256;
+    p.bytes = p.pass ? p.v + (size_t)x->rows * w->rows * 4 : p.product.bytes;
+    return p;
+}
+
+template <class T>
+static dmmv_status linear(const LinearPlan& plan, const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, ProductOut<T, true> out,
+                          const dmmv_block_matrix* q, void* ws, hipStream_t s) {
+    if (plan.pass) out.v = reinterpret_cast<float*>(static_cast<char*>(ws) + plan.v);
+    else if (q) out.q = layer_view(q), out.has_q = 1;
+    if constexpr (sizeof(T) == 2)
+        if (!q) return product<T, false, true>(plan.product, x, w, bias, out, ws, s);
+    DMMV_TRY((product<T, true, true>(plan.product, x, w, bias, out, ws, s)));
+    return plan.pass ? dmmv_block_quantize(DMMV_F32, out.v, w->rows, q, s) : DMMV_OK;
 }
 
 }  // namespace dmmv
@@ -1022,6 +1190,38 @@ extern "C" dmmv_status dmmv_block_product(const dmmv_block_matrix* x, const dmmv
     const ProductPlan plan = product_plan(x, w, dtype == DMMV_F32);
     DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, plan.bytes));
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    return dtype == DMMV_F32 ? product(plan, x, w, bias, static_cast<float*>(y), ldy, workspace, s)
-                             : product(plan, x, w, bias, static_cast<bf16_t*>(y), ldy, workspace, s);
+    return dtype == DMMV_F32 ? product<float, true, false>(plan, x, w, bias, {static_cast<float*>(y), ldy}, workspace, s)
+                             : product<bf16_t, false, false>(plan, x, w, bias, {static_cast<bf16_t*>(y), ldy}, workspace, s);
+}
+
+extern "C" size_t dmmv_block_linear_workspace_for(const dmmv_block_matrix* x, const dmmv_block_matrix* w, int32_t dtype, int32_t has_q) {
+    if (layer_check_dtype(dtype) != DMMV_OK || layer_check_block(x, false, "x") != DMMV_OK || layer_check_block(w, false, "w") != DMMV_OK) return 0;
+    if (x->cols != w->cols || x->rows == 0 || w->rows == 0) return 0;
+    return linear_plan(x, w, dtype == DMMV_F32, has_q != 0).bytes;
+}
+
+extern "C" dmmv_status dmmv_block_linear(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const float* bias, int32_t act, const void* residual,
+                                         int64_t ldr, int32_t dtype, void* y, int64_t ldy, const dmmv_block_matrix* q, void* u, int64_t ldu,
+                                         void* workspace, size_t workspace_bytes, void* hip_stream) {
+    DMMV_TRY(layer_check_dtype(dtype));
+    DMMV_TRY(layer_check_act(act, true));
+    DMMV_TRY(layer_check_block(x, false, "x"));
+    DMMV_TRY(layer_check_block(w, false, "w"));
+    if (x->cols != w->cols) return fail(DMMV_ERR_SHAPE, "x has %lld columns, w has %lld", (long long)x->cols, (long long)w->cols);
+    const int width = layer_width(dtype);
+    DMMV_TRY(layer_check_vector(bias, false, "bias"));
+    if (residual) DMMV_TRY(layer_check_array(residual, x->rows, w->rows, ldr, width, "residual"));
+    if (y) DMMV_TRY(layer_check_array(y, x->rows, w->rows, ldy, width, "y"));
+    if (q) DMMV_TRY(layer_check_out_block(q, x->rows, w->rows, "q"));
+    if (u) DMMV_TRY(layer_check_array(u, x->rows, w->rows, ldu, width, "u"));
+    if (x->rows == 0 || w->rows == 0 || (!y && !q && !u)) return DMMV_OK;
+    const LinearPlan plan = linear_plan(x, w, dtype == DMMV_F32, q != nullptr);
+    DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, plan.bytes));
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    auto call = [&](auto* type) {
+        using T = std::remove_pointer_t<decltype(type)>;
+        const ProductOut<T, true> out = {static_cast<T*>(y), ldy, static_cast<const T*>(residual), ldr, static_cast<T*>(u), ldu, nullptr, BlockView{}, act, 0};
+        return linear<T>(plan, x, w, bias, out, q, workspace, s);
+    };
+    return dtype == DMMV_F32 ? call((float*)nullptr) : call((bf16_t*)nullptr);
 }

@@ -1,0 +1,288 @@
+// The norm over all gradients of a step, and the gradients scaled to it (include/dmmv_layer.h).
+//
+// Both passes are bound by memory.  The tensors' places come with the kernel's arguments, LIST of them a launch, so a call copies nothing to the
+// device and can be captured.  A tensor is cut into chunks of CHUNK numbers (rows with gaps into pieces of a row), and a workgroup has a run
+// of consecutive chunks.  Squares are summed in 64 bits: those of all 32-bit numbers are there, and no order of summing matters to 32 bits.
+#include <algorithm>
+#include <new>
+
+#include "dmmv_layer_common.h"
+
+namespace dmmv {
+
+constexpr int LIST = 64, CHUNK = 8192, GROUPS = 1024;        // tensors a launch, numbers a chunk, most partial sums a launch
+
+struct TensorPlace {
+    const void* in;
+    void* out;
+    int64_t cols, ld, ldo;               // one row, if the rows have no gaps
+    uint32_t first;                      // chunks of the tensors before
+    uint16_t in_bf16, out_bf16;
+};
+struct TensorList {
+    TensorPlace t[LIST];
+    int32_t count;
+    uint32_t chunks;
+};
+static_assert(sizeof(TensorList) <= 3584, "with the other arguments below 4 KB");
+
+// The workgroup's chunks in order: do(tensor, row, first column, columns of the chunk)
+template <class F>
+__device__ __forceinline__ void for_chunks(const TensorList& l, F f) {
+    const uint32_t a = (uint32_t)((uint64_t)l.chunks * blockIdx.x / gridDim.x), b = (uint32_t)((uint64_t)l.chunks * (blockIdx.x + 1) / gridDim.x);
+    if (a >= b) return;
+    int lo = 0, hi = l.count - 1;                            // the last tensor that begins at or before chunk a
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (l.t[mid].first <= a) lo = mid;
+        else hi = mid - 1;
+    }
+    for (uint32_t c = a; c < b; ++c) {
+        while (lo + 1 < l.count && l.t[lo + 1].first <= c) ++lo;
+        const TensorPlace& t = l.t[lo];
+        const uint32_t pieces = (uint32_t)((t.cols + CHUNK - 1) / CHUNK), i = c - t.first, row = i / pieces;
+        const int64_t col = (int64_t)(i - row * pieces) * CHUNK;
+        f(t, (int64_t)row, col, (int)min((int64_t)CHUNK, t.cols - col));
+    }
+}
+
+// sum over the 256 threads of the workgroup in a fixed order, in every thread
+__device__ __forceinline__ double group_sum(double v, double (&sh)[4]) {
+    v += dpp_mov<DPP_QUAD_XOR1>(v);
+    v += dpp_mov<DPP_QUAD_XOR2>(v);
+    v += dpp_mov<DPP_ROW_HALF_MIRROR>(v);
+    v += dpp_mov<DPP_ROW_MIRROR>(v);
+    v = (read_lane(v, 0) + read_lane(v, 16)) + (read_lane(v, 32) + read_lane(v, 48));
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (sh[0] + sh[1]) + (sh[2] + sh[3]);
+}
+
+template <class T>
+__device__ __forceinline__ void add_squares(const T* __restrict__ p, int n, double (&s)[2]) {
+#pragma unroll
+    for (int i = 0; i < CHUNK / 2048; ++i) {
+        float v[8];
+        load8(p, i * 2048 + threadIdx.x * 8, n, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e & 1] = __builtin_fma((double)v[e], (double)v[e], s[e & 1]);
+    }
+}
+
+// part[workgroup] = sum of the squares of its chunks
+__global__ __launch_bounds__(256) void k_gradient_squares(TensorList l, double* __restrict__ part) {
+    __shared__ double sh[4];
+    double s[2] = {0.0, 0.0};
+    for_chunks(l, [&](const TensorPlace& t, int64_t row, int64_t col, int n) {
+        if (t.in_bf16) add_squares(static_cast<const bf16_t*>(t.in) + row * t.ld + col, n, s);
+        else add_squares(static_cast<const float*>(t.in) + row * t.ld + col, n, s);
+    });
+    const double v = group_sum(s[0] + s[1], sh);
+    if (threadIdx.x == 0) part[blockIdx.x] = v;
+}
+
+// the norm of all parts, the same in every workgroup that asks
+__device__ __forceinline__ double norm_of(const double* __restrict__ part, int32_t parts, double (&sh)[4]) {
+    double s = 0.0;
+    for (int32_t i = threadIdx.x; i < parts; i += 256) s += part[i];
+    return __builtin_sqrt(group_sum(s, sh));
+}
+
+__global__ __launch_bounds__(256) void k_gradient_norm(const double* __restrict__ part, int32_t parts, float* __restrict__ norm) {
+    __shared__ double sh[4];
+    const double v = norm_of(part, parts, sh);
+    if (threadIdx.x == 0) *norm = (float)v;
+}
+
+template <class T, class U>
+__device__ __forceinline__ void scale_chunk(const T* in, U* out, int n, float c, float rest) {      // (out may be in)
+    float v[CHUNK / 2048][8];
+#pragma unroll
+    for (int i = 0; i < CHUNK / 2048; ++i) load8(in, i * 2048 + threadIdx.x * 8, n, v[i]);
+#pragma unroll
+    for (int i = 0; i < CHUNK / 2048; ++i) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] = v[i][e] * c * rest;
+        store8(out, i * 2048 + threadIdx.x * 8, n, v[i]);
+    }
+}
+
+// out = c in, with c = max_norm / (norm + eps) where that is below 1.  Tensors that stay where they are are not touched if c is 1.
+__global__ __launch_bounds__(256) void k_gradient_scale(TensorList l, const double* __restrict__ part, int32_t parts, const float* __restrict__ given,
+                                                        float max_norm, float eps, int32_t in_place, float* __restrict__ norm) {
+    __shared__ double sh[4];
+    const double v = given ? (double)*given : norm_of(part, parts, sh);
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
+    const double sum = v + (double)eps;
+    const double d = sum <= (double)max_norm ? 1.0 : (double)max_norm / sum;
+    if (d == 1.0 && in_place) return;
+    // a factor near the least normal number would lose bits that its product with a large number has
+    const float rest = d < 0x1p-64 ? 0x1p-64f : 1.0f, c = (float)(d < 0x1p-64 ? d * 0x1p64 : d);
+    for_chunks(l, [&](const TensorPlace& t, int64_t row, int64_t col, int n) {
+        const float* f = static_cast<const float*>(t.in) + row * t.ld + col;
+        const bf16_t* b = static_cast<const bf16_t*>(t.in) + row * t.ld + col;
+        float* fo = static_cast<float*>(t.out) + row * t.ldo + col;
+        bf16_t* bo = static_cast<bf16_t*>(t.out) + row * t.ldo + col;
+        if (t.in_bf16) t.out_bf16 ? scale_chunk(b, bo, n, c, rest) : scale_chunk(b, fo, n, c, rest);
+        else t.out_bf16 ? scale_chunk(f, bo, n, c, rest) : scale_chunk(f, fo, n, c, rest);
+    });
+}
+
+// ---- host ---------------------------------------------------------------------------------------
+static bool nothing(const dmmv_gradient& g) { return g.rows == 0 || g.cols == 0; }
+static bool no_gaps(const dmmv_gradient& g) { return g.rows == 1 || g.ld == g.cols; }
+
+static dmmv_status check_gradients(int64_t count, const dmmv_gradient* g, const char* what) {
+    if (count < 0 || count > 1 << 20) return fail(DMMV_ERR_SHAPE, "%s: count out of range", what);
+    if (count > 0 && !g) return fail(DMMV_ERR_NULL, "%s is NULL", what);
+    for (int64_t i = 0; i < count; ++i) {
+        DMMV_TRY(layer_check_dtype(g[i].dtype));
+        if (g[i].rows < 0 || g[i].cols < 0) return fail(DMMV_ERR_SHAPE, "%s: negative size", what);
+        if (g[i].rows > INT32_MAX || (g[i].rows > 0 && g[i].cols > ((int64_t)1 << 42) / g[i].rows)) return fail(DMMV_ERR_SHAPE, "%s: size out of range", what);
+        DMMV_TRY(layer_check_array(g[i].data, g[i].rows, g[i].cols, g[i].ld, layer_width(g[i].dtype), what));
+    }
+    return DMMV_OK;
+}
+
+struct Extent {
+    uintptr_t from, to;
+    int64_t i;
+};
+// whether two matrices whose extents meet share a number: columns of one matrix need not
+static bool share(const dmmv_gradient& a, const dmmv_gradient& b) {      // a begins first
+    const uintptr_t w = layer_width(a.dtype), ld = (uintptr_t)a.ld * w;
+    if (a.dtype != b.dtype || no_gaps(a) || a.ld != b.ld || b.rows == 1) return true;
+    const uintptr_t off = ((uintptr_t)b.data - (uintptr_t)a.data) % ld;
+    return off < (uintptr_t)a.cols * w || off + (uintptr_t)b.cols * w > ld;
+}
+static dmmv_status check_apart(int64_t count, const dmmv_gradient* g) {
+    Extent* e = new (std::nothrow) Extent[count > 0 ? count : 1];
+    if (!e) return fail(DMMV_ERR_WORKSPACE, "no host memory for %lld places", (long long)count);
+    int64_t n = 0;
+    for (int64_t i = 0; i < count; ++i)
+        if (!nothing(g[i])) {
+            const uintptr_t p = (uintptr_t)g[i].data;
+            e[n++] = {p, p + ((uintptr_t)((g[i].rows - 1) * (g[i].rows > 1 ? g[i].ld : 0)) + (uintptr_t)g[i].cols) * layer_width(g[i].dtype), i};
+        }
+    std::sort(e, e + n, [](const Extent& a, const Extent& b) { return a.from != b.from ? a.from < b.from : a.i < b.i; });
+    int64_t bad = -1, other = -1;
+    uintptr_t most = 0;
+    for (int64_t k = 0; k < n && bad < 0; ++k) {
+        if (e[k].from < most)
+            for (int64_t j = k - 1; j >= 0 && bad < 0; --j)
+                if (e[j].to > e[k].from && share(g[e[j].i], g[e[k].i])) bad = e[k].i, other = e[j].i;
+        most = std::max(most, e[k].to);
+    }
+    delete[] e;
+    return bad < 0 ? DMMV_OK : fail(DMMV_ERR_SHAPE, "gradients %lld and %lld share memory", (long long)std::min(bad, other), (long long)std::max(bad, other));
+}
+
+// lists of at most LIST tensors that hold something: do(list, its number)
+template <class F>
+static dmmv_status for_lists(int64_t count, const dmmv_gradient* g, const dmmv_gradient* out, F f) {
+    TensorList l;
+    l.count = 0;
+    l.chunks = 0;
+    int32_t k = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        if (nothing(g[i])) continue;
+        const bool whole = no_gaps(g[i]) && (!out || no_gaps(out[i]));
+        const int64_t rows = whole ? 1 : g[i].rows, cols = whole ? g[i].rows * g[i].cols : g[i].cols, chunks = rows * ceil_div(cols, CHUNK);
+        if (chunks > INT32_MAX) return fail(DMMV_ERR_SHAPE, "gradient %lld: more pieces than a launch takes", (long long)i);
+        if (l.count == LIST || l.chunks + (uint64_t)chunks > INT32_MAX) {
+            DMMV_TRY(f(l, k++));
+            l.count = 0;
+            l.chunks = 0;
+        }
+        TensorPlace& t = l.t[l.count++];
+        t.in = g[i].data;
+        t.out = out ? out[i].data : nullptr;
+        t.cols = cols;
+        t.ld = whole ? cols : g[i].ld;
+        t.ldo = whole ? cols : out ? out[i].ld : 0;
+        t.first = l.chunks;
+        t.in_bf16 = g[i].dtype == DMMV_BF16;
+        t.out_bf16 = out && out[i].dtype == DMMV_BF16;
+        l.chunks += (uint32_t)chunks;
+    }
+    return l.count ? f(l, k) : DMMV_OK;
+}
+
+// parts[n] of the lists, one after the other
+static dmmv_status squares(int64_t count, const dmmv_gradient* g, double* part, int32_t& parts, hipStream_t s) {
+    parts = 0;
+    return for_lists(count, g, nullptr, [&](const TensorList& l, int32_t) -> dmmv_status {
+        const int32_t n = (int32_t)std::min<uint32_t>(l.chunks, GROUPS);
+        hipLaunchKernelGGL(k_gradient_squares, dim3((unsigned)n), dim3(256), 0, s, l, part + parts);
+        DMMV_LAUNCH_CHECK();
+        parts += n;
+        return DMMV_OK;
+    });
+}
+
+// every list has LIST tensors but the last, or its chunks were too many
+static size_t gradient_workspace(int64_t count, const dmmv_gradient* g) {
+    size_t bytes = 0;
+    if (for_lists(count, g, nullptr, [&](const TensorList& l, int32_t) -> dmmv_status {
+            bytes += std::min<uint32_t>(l.chunks, GROUPS) * sizeof(double);
+            return DMMV_OK;
+        }) != DMMV_OK)
+        return 0;
+    return bytes;
+}
+
+}  // namespace dmmv
+
+using namespace dmmv;
+
+extern "C" size_t dmmv_gradient_workspace_bytes(int64_t count, const dmmv_gradient* gradients) {
+    if (check_gradients(count, gradients, "gradients") != DMMV_OK) return 0;
+    return gradient_workspace(count, gradients);
+}
+
+extern "C" dmmv_status dmmv_gradient_norm(int64_t count, const dmmv_gradient* gradients, float* norm, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    DMMV_TRY(check_gradients(count, gradients, "gradients"));
+    DMMV_TRY(layer_check_vector(norm, true, "norm"));
+    DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, gradient_workspace(count, gradients)));
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    int32_t parts = 0;
+    DMMV_TRY(squares(count, gradients, static_cast<double*>(workspace), parts, s));
+    hipLaunchKernelGGL(k_gradient_norm, dim3(1), dim3(256), 0, s, static_cast<const double*>(workspace), parts, norm);
+    DMMV_LAUNCH_CHECK();
+    return DMMV_OK;
+}
+
+extern "C" dmmv_status dmmv_gradient_clip(int64_t count, const dmmv_gradient* gradients, const dmmv_gradient* out, float max_norm, float eps,
+                                          const float* given, float* norm, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    DMMV_TRY(check_gradients(count, gradients, "gradients"));
+    if (out) {
+        DMMV_TRY(check_gradients(count, out, "out"));
+        for (int64_t i = 0; i < count; ++i)
+            if (out[i].rows != gradients[i].rows || out[i].cols != gradients[i].cols)
+                return fail(DMMV_ERR_SHAPE, "out: gradient %lld is %lld x %lld, expected %lld x %lld", (long long)i, (long long)out[i].rows, (long long)out[i].cols,
+                            (long long)gradients[i].rows, (long long)gradients[i].cols);
+    }
+    if (!(max_norm >= 0.0f && max_norm <= 3.4e38f)) return fail(DMMV_ERR_DOMAIN, "max_norm must be finite and not negative");
+    if (!(eps >= 0.0f && eps <= 3.4e38f)) return fail(DMMV_ERR_DOMAIN, "eps must be finite and not negative");
+    DMMV_TRY(layer_check_vector(given, false, "given"));
+    DMMV_TRY(layer_check_vector(norm, false, "norm"));
+    DMMV_TRY(check_apart(count, out ? out : gradients));
+    if (!given) DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, gradient_workspace(count, gradients)));
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    double* part = static_cast<double*>(workspace);
+    int32_t parts = 0, lists = 0;
+    if (!given) DMMV_TRY(squares(count, gradients, part, parts, s));
+    DMMV_TRY(for_lists(count, gradients, out ? out : gradients, [&](const TensorList& l, int32_t k) -> dmmv_status {
+        hipLaunchKernelGGL(k_gradient_scale, dim3((unsigned)std::min<uint32_t>(l.chunks, 2 * GROUPS)), dim3(256), 0, s, l, part, parts, given, max_norm, eps,
+                           (int32_t)!out, k == 0 ? norm : nullptr);
+        DMMV_LAUNCH_CHECK();
+        lists = k + 1;
+        return DMMV_OK;
+    }));
+    if (lists == 0 && norm) {                  // nothing to scale
+        if (given) return fail(DMMV_ERR_NULL, "norm and given without gradients");
+        hipLaunchKernelGGL(k_gradient_norm, dim3(1), dim3(256), 0, s, part, 0, norm);
+        DMMV_LAUNCH_CHECK();
+    }
+    return DMMV_OK;
+}

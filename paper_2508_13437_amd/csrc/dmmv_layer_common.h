@@ -23,6 +23,10 @@ dmmv_status layer_check_sizes(int64_t rows, int64_t cols, const char* what);
 // a row-major array of elements of `width` bytes (empty ones may be NULL)
 dmmv_status layer_check_array(const void* p, int64_t rows, int64_t cols, int64_t ld, int width, const char* what);
 dmmv_status layer_check_block(const dmmv_block_matrix* q, bool output, const char* what);
+// a float vector, contiguous
+dmmv_status layer_check_vector(const float* p, bool needed, const char* what);
+// an 8-bit result [rows][cols]
+dmmv_status layer_check_out_block(const dmmv_block_matrix* q, int64_t rows, int64_t cols, const char* what);
 dmmv_status layer_check_workspace(const void* ws, size_t have, size_t need);
 BlockView layer_view(const dmmv_block_matrix* q);      // all zero for NULL
 
@@ -252,6 +256,31 @@ __device__ __forceinline__ float wave_sum(float v) {
     return (read_lane(v, 0) + read_lane(v, 16)) + (read_lane(v, 32) + read_lane(v, 48));
 }
 
+// sum over the TPR threads of a team, in every thread; `sh` [TPR / 64]
+template <int TPR>
+__device__ __forceinline__ float team_sum(float v, float* sh) {
+    v = wave_sum(v);
+    if constexpr (TPR > 64) {
+        const int w = threadIdx.x >> 6;
+        __syncthreads();                     // the last round's values have been read
+        if ((threadIdx.x & 63) == 0) sh[w] = v;
+        __syncthreads();
+        v = sh[0];
+#pragma unroll
+        for (int i = 1; i < TPR / 64; ++i) v += sh[i];
+    }
+    return v;
+}
+
+template <class T>
+__device__ __forceinline__ void put_q(const BlockView& q, int64_t row, int64_t col, int64_t cols, const float (&v)[8]) {
+    const uint32_t b = scale_byte(row16_max(max8_bits(v)));
+    if (col < cols) {
+        store8_codes(q.codes + row * q.ld, col, cols, encode8(v, b));
+        if ((threadIdx.x & 15) == 0) scale_put(q, row, col >> 7, b);
+    }
+}
+
 // A 32-bit number as the sum of three bf16 (8 + 8 + 8 significant bits, by truncation).  An infinity or NaN
 // stays whole in the first.
 __device__ __forceinline__ void split3(float x, uint32_t (&p)[3]) {
@@ -383,6 +412,8 @@ __device__ __forceinline__ bf16x8_t scaled8(int lo, int hi, uint32_t b) {
 
 __device__ __forceinline__ void put_y(float* y, float v) { *y = v; }
 __device__ __forceinline__ void put_y(bf16_t* y, float v) { y->u = (uint16_t)bf16_bits(v); }
+__device__ __forceinline__ float value_of(float x) { return x; }
+__device__ __forceinline__ float value_of(bf16_t x) { return bf16_value(x.u); }
 
 // four results of a row to the LDS
 template <class T>

@@ -18,31 +18,6 @@ struct NormOut {
     int32_t has_q, has_xq;
 };
 
-// sum over the TPR threads of a team, in every thread; `sh` [TPR / 64]
-template <int TPR>
-__device__ __forceinline__ float team_sum(float v, float* sh) {
-    v = wave_sum(v);
-    if constexpr (TPR > 64) {
-        const int w = threadIdx.x >> 6;
-        __syncthreads();                     // the last round's values have been read
-        if ((threadIdx.x & 63) == 0) sh[w] = v;
-        __syncthreads();
-        v = sh[0];
-#pragma unroll
-        for (int i = 1; i < TPR / 64; ++i) v += sh[i];
-    }
-    return v;
-}
-
-template <class T>
-__device__ __forceinline__ void put_q(const BlockView& q, int64_t row, int64_t col, int64_t cols, const float (&v)[8]) {
-    const uint32_t b = scale_byte(row16_max(max8_bits(v)));
-    if (col < cols) {
-        store8_codes(q.codes + row * q.ld, col, cols, encode8(v, b));
-        if ((threadIdx.x & 15) == 0) scale_put(q, row, col >> 7, b);
-    }
-}
-
 // v = (x - mean) rstd gamma + beta of 8 columns, zero past the row's end
 __device__ __forceinline__ void norm8(const float (&x)[8], int64_t col, int64_t cols, float mu, float rs,
                                       const float* __restrict__ gamma, const float* __restrict__ beta, float (&v)[8]) {
@@ -461,19 +436,6 @@ static dmmv_status norm_backward_of(int64_t rows, int64_t cols, const void* dy, 
                                    dgamma, dbeta, static_cast<char*>(ws), s);
 }
 
-static dmmv_status check_vector(const float* p, bool needed, const char* what) {
-    if (needed && !p) return fail(DMMV_ERR_NULL, "%s is NULL", what);
-    if ((uintptr_t)p % 4) return fail(DMMV_ERR_SHAPE, "%s is not aligned to its elements", what);
-    return DMMV_OK;
-}
-
-static dmmv_status check_out_block(const dmmv_block_matrix* q, int64_t rows, int64_t cols, const char* what) {
-    DMMV_TRY(layer_check_block(q, true, what));
-    if (q->rows != rows || q->cols != cols) return fail(DMMV_ERR_SHAPE, "%s is not %lld x %lld", what, (long long)rows, (long long)cols);
-    if (q->scale_rows != 1) return fail(DMMV_ERR_UNSUPPORTED, "%s: a row's blocks have scales of their own (scale_rows 1)", what);
-    return DMMV_OK;
-}
-
 }  // namespace dmmv
 
 using namespace dmmv;
@@ -487,12 +449,12 @@ extern "C" dmmv_status dmmv_layernorm(int32_t dtype, int64_t rows, int64_t cols,
     const int w = layer_width(dtype);
     DMMV_TRY(layer_check_array(x, rows, cols, ldx, w, "x"));
     if (y) DMMV_TRY(layer_check_array(y, rows, cols, ldy, w, "y"));
-    if (q) DMMV_TRY(check_out_block(q, rows, cols, "q"));
-    if (xq) DMMV_TRY(check_out_block(xq, rows, cols, "xq"));
-    DMMV_TRY(check_vector(gamma, false, "gamma"));
-    DMMV_TRY(check_vector(beta, false, "beta"));
-    DMMV_TRY(check_vector(mean, false, "mean"));
-    DMMV_TRY(check_vector(rstd, false, "rstd"));
+    if (q) DMMV_TRY(layer_check_out_block(q, rows, cols, "q"));
+    if (xq) DMMV_TRY(layer_check_out_block(xq, rows, cols, "xq"));
+    DMMV_TRY(layer_check_vector(gamma, false, "gamma"));
+    DMMV_TRY(layer_check_vector(beta, false, "beta"));
+    DMMV_TRY(layer_check_vector(mean, false, "mean"));
+    DMMV_TRY(layer_check_vector(rstd, false, "rstd"));
     if (rows == 0) return DMMV_OK;             // (rows without columns: mean and rstd are 0 / 0)
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     if (dtype == DMMV_F32) {
@@ -526,11 +488,11 @@ extern "C" dmmv_status dmmv_layernorm_backward(int32_t dtype, int64_t rows, int6
             return fail(DMMV_ERR_SHAPE, "xq is not %lld x %lld", (long long)rows, (long long)cols);
     }
     if (dx) DMMV_TRY(layer_check_array(dx, rows, cols, lddx, w, "dx"));
-    DMMV_TRY(check_vector(gamma, false, "gamma"));
-    DMMV_TRY(check_vector(mean, !empty, "mean"));
-    DMMV_TRY(check_vector(rstd, !empty, "rstd"));
-    DMMV_TRY(check_vector(dgamma, false, "dgamma"));
-    DMMV_TRY(check_vector(dbeta, false, "dbeta"));
+    DMMV_TRY(layer_check_vector(gamma, false, "gamma"));
+    DMMV_TRY(layer_check_vector(mean, !empty, "mean"));
+    DMMV_TRY(layer_check_vector(rstd, !empty, "rstd"));
+    DMMV_TRY(layer_check_vector(dgamma, false, "dgamma"));
+    DMMV_TRY(layer_check_vector(dbeta, false, "dbeta"));
     DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, norm_workspace(rows, cols)));
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     if (cols == 0 || (!dx && !dgamma && !dbeta)) return DMMV_OK;

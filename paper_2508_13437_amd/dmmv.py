@@ -33,6 +33,9 @@ EXPORTS = ("dmmv_workspace_bytes", "dmmv_create", "dmmv_destroy", "dmmv_set_x",
            "dmmv_block_quantize", "dmmv_block_dequantize", "dmmv_block_product_workspace_bytes",
            "dmmv_block_product", "dmmv_block_backward_workspace_bytes", "dmmv_block_backward_workspace_for", "dmmv_block_backward",
            "dmmv_layernorm", "dmmv_layernorm_workspace_bytes", "dmmv_layernorm_backward",
+           "dmmv_block_linear_workspace_for", "dmmv_block_linear", "dmmv_activation_workspace_bytes", "dmmv_activation_backward",
+           "dmmv_residual_norm", "dmmv_residual_norm_workspace_bytes", "dmmv_residual_norm_backward",
+           "dmmv_gradient_workspace_bytes", "dmmv_gradient_norm", "dmmv_gradient_clip",
            "dmmv_last_error",
            "dmmv_version")
 
@@ -117,17 +120,28 @@ def load() -> C.CDLL:
             ("dmmv_block_product", [p, p, p, i32, p, i64, p, C.c_size_t, p]),
             ("dmmv_block_backward", [i32, i64, i64, i64, p, i64, p, p, p, i64, p, i64, p, p, C.c_size_t, p]),
             ("dmmv_layernorm", [i32, i64, i64, p, i64, p, p, f32, p, i64, p, p, p, p, p]),
-            ("dmmv_layernorm_backward", [i32, i64, i64, p, i64, p, i64, p, p, p, p, p, i64, p, p, p, C.c_size_t, p])):
+            ("dmmv_layernorm_backward", [i32, i64, i64, p, i64, p, i64, p, p, p, p, p, i64, p, p, p, C.c_size_t, p]),
+            ("dmmv_block_linear", [p, p, p, i32, p, i64, i32, p, i64, p, p, i64, p, C.c_size_t, p]),
+            ("dmmv_activation_backward", [i32, i64, i64, p, i64, p, i64, i32, p, i64, p, p, C.c_size_t, p]),
+            ("dmmv_residual_norm", [i32, i64, i64, p, i64, p, i64, f32, p, i64, i64, p, p, p, i64, p, i64, p, p, p, p, p, p]),
+            ("dmmv_residual_norm_backward", [i32, i64, i64, p, i64, p, i64, p, i64, p, i64, f32, p, i64, i64, p, p, p, p, p, p, p, i64, p, i64,
+                                             p, i64, p, p, p, p, p, C.c_size_t, p]),
+            ("dmmv_gradient_norm", [i64, p, p, p, C.c_size_t, p]),
+            ("dmmv_gradient_clip", [i64, p, p, f32, f32, p, p, p, C.c_size_t, p])):
         fn = getattr(lib, name)
         fn.restype = C.c_int
         fn.argtypes = args
     for name, nargs in (("dmmv_block_product_workspace_bytes", 3), ("dmmv_block_backward_workspace_bytes", 3),
-                        ("dmmv_layernorm_workspace_bytes", 2)):
+                        ("dmmv_layernorm_workspace_bytes", 2), ("dmmv_activation_workspace_bytes", 2), ("dmmv_residual_norm_workspace_bytes", 3)):
         fn = getattr(lib, name)
         fn.restype = C.c_size_t
         fn.argtypes = [i64] * nargs
     lib.dmmv_block_backward_workspace_for.restype = C.c_size_t
     lib.dmmv_block_backward_workspace_for.argtypes = [i32, i64, i64, i64, p, i64, p, p, p, p]
+    lib.dmmv_block_linear_workspace_for.restype = C.c_size_t
+    lib.dmmv_block_linear_workspace_for.argtypes = [p, p, i32, i32]
+    lib.dmmv_gradient_workspace_bytes.restype = C.c_size_t
+    lib.dmmv_gradient_workspace_bytes.argtypes = [i64, p]
     lib.dmmv_last_error.restype = C.c_char_p
     lib.dmmv_version.restype = C.c_char_p
     _lib = lib
@@ -780,3 +794,305 @@ def dmmv_layernorm_backward(dy: torch.Tensor, x, gamma: Optional[torch.Tensor], 
     _enqueue(dev, load().dmmv_layernorm_backward, kind, T, F, dy.data_ptr(), dy.stride(0), px, ldx, pq, _addr(g), mu.data_ptr(),
              rs.data_ptr(), _addr(gx), F, _addr(gg), _addr(gb), _addr(ws), nbytes)
     return gx, gg, gb
+
+
+# ---- a residual block around such layers -----------------------------------------------------------
+_ACTS = {None: 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+def _act_kind(act: Optional[str], none: bool) -> int:
+    kind = _ACTS.get(act)
+    if kind is None or (kind == 0 and not none):
+        raise DmmvError(-4, f"act is {act!r}, not one of {', '.join(repr(a) for a in _ACTS if a or none)}")
+    return kind
+
+
+def _like(t: torch.Tensor, shape, dtype: torch.dtype, dev: int, what: str) -> torch.Tensor:
+    """t, a matrix of that shape, type and device, with contiguous rows (a copy is the caller's to keep until its call is enqueued)."""
+    t = _matrix(t, what)
+    if t.dtype != dtype:
+        raise DmmvError(-3, f"{what} is {t.dtype}, not {dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise DmmvError(-2, f"{what} is {t.shape[0]} x {t.shape[1]}, expected {shape[0]} x {shape[1]}")
+    _same(t, dev)
+    return t
+
+
+@dataclass
+class BlockLinearResult:
+    y: Optional[torch.Tensor]     # [T][O] of the type asked for
+    q: Optional[BlockMatrix]      # the same in 8 bits
+    u: Optional[torch.Tensor]     # what the activation was given
+
+
+def dmmv_block_linear(x: BlockMatrix, w: BlockMatrix, bias: Optional[torch.Tensor] = None, act: Optional[str] = None,
+                      residual: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16, y: bool = True, q: bool = False,
+                      u: bool = False) -> BlockLinearResult:
+    """act(x w^T + bias) + residual.  act: None, "relu", "gelu", "gelu_tanh" or "silu"; residual [T][O] of dtype; y: the result in
+    dtype; q: the result in 8 bits, the next product's operand; u: x w^T + bias for dmmv_activation_backward."""
+    kind, code = _layer_dtype(dtype), _act_kind(act, True)
+    dev, on = x._codes.get_device(), x._codes.device
+    _same(w._codes, dev)
+    T, O = x._rows, w._rows
+    b = _vector(bias, O, dev, "bias")
+    r = None if residual is None else _like(residual, (T, O), dtype, dev, "residual")
+    oy = torch.empty(T, O, dtype=dtype, device=on) if y else None
+    oq = _new_block(T, O, 1, torch.uint8, on) if q else None
+    ou = torch.empty(T, O, dtype=dtype, device=on) if u else None
+    lib = load()
+    nbytes = lib.dmmv_block_linear_workspace_for(x._p, w._p, kind, 1 if q else 0)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=on) if nbytes else None
+    _enqueue(dev, lib.dmmv_block_linear, x._p, w._p, _addr(b), code, _addr(r), O if r is None else r.stride(0), kind, _addr(oy), O, oq._p if q else None,
+             _addr(ou), O, _addr(ws), nbytes)
+    return BlockLinearResult(oy, oq, ou)
+
+
+def dmmv_activation_backward(dy: torch.Tensor, u: torch.Tensor, act: str, du: bool = True, dbias: bool = True):
+    """Gradients (du of dy's type, dbias in float32; None for those not asked for) of u = x w^T + bias from those of act(u).  The
+    gradients of x and w follow from du by dmmv_block_backward, without its dbias."""
+    code = _act_kind(act, False)
+    dy = _matrix(dy, "dy")
+    kind = _layer_dtype(dy.dtype)
+    T, F = dy.shape
+    dev, on = dy.get_device(), dy.device
+    u = _like(u, dy.shape, dy.dtype, dev, "u")
+    gu = torch.empty(T, F, dtype=dy.dtype, device=on) if du else None
+    gb = torch.empty(F, dtype=torch.float32, device=on) if dbias else None
+    nbytes = _workspace("dmmv_activation_workspace_bytes", T, F) if dbias else 0
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=on) if nbytes else None
+    _enqueue(dev, load().dmmv_activation_backward, kind, T, F, dy.data_ptr(), dy.stride(0), u.data_ptr(), u.stride(0), code, _addr(gu), F, _addr(gb),
+             _addr(ws), nbytes)
+    return gu, gb
+
+
+class _Norm(C.Structure):
+    _fields_ = [("gamma", C.c_void_p), ("beta", C.c_void_p), ("eps", C.c_float), ("rms", C.c_int32)]
+
+
+@dataclass
+class Norm:
+    """A norm of rows: a layer norm, or with rms one without a mean; gamma and beta float32 vectors, None = 1 and 0."""
+    gamma: Optional[torch.Tensor] = None
+    beta: Optional[torch.Tensor] = None
+    eps: float = 1e-5
+    rms: bool = False
+
+    def _c(self, cols: int, dev: int, what: str):
+        g, b = _vector(self.gamma, cols, dev, what + ".gamma"), _vector(self.beta, cols, dev, what + ".beta")
+        return _Norm(_addr(g), _addr(b), self.eps, 1 if self.rms else 0), (g, b)
+
+
+@dataclass
+class ResidualNormResult:
+    h: Optional[torch.Tensor]             # [T][F] of the input's type: alpha h + gate post(f)
+    y: Optional[torch.Tensor]             # pre(h), of the same type
+    q: Optional[BlockMatrix]              # and in 8 bits
+    post_mean: Optional[torch.Tensor]     # [T] float32
+    post_rstd: Optional[torch.Tensor]
+    mean: Optional[torch.Tensor]
+    rstd: Optional[torch.Tensor]
+
+
+@dataclass
+class ResidualNormGradients:
+    df: Optional[torch.Tensor]            # [T][F] of the input's type
+    dh: Optional[torch.Tensor]
+    dgate: Optional[torch.Tensor]         # float32, of the gate's shape
+    dpost_gamma: Optional[torch.Tensor]   # [F] float32
+    dpost_beta: Optional[torch.Tensor]
+    dgamma: Optional[torch.Tensor]
+    dbeta: Optional[torch.Tensor]
+
+
+def _norms(post: Optional[Norm], pre: Optional[Norm], cols: int, dev: int):
+    a, keep_a = post._c(cols, dev, "post") if post is not None else (None, None)
+    b, keep_b = pre._c(cols, dev, "pre") if pre is not None else (None, None)
+    return a, b, (keep_a, keep_b)
+
+
+def _at(c) -> Optional[int]:
+    return None if c is None else C.addressof(c)
+
+
+def _gate(gate: Optional[torch.Tensor], gate_rows: Optional[int], T: int, F: int, dev: int):
+    """The gate as a matrix with a row for every gate_rows rows, and that number (0 without a gate)."""
+    if gate is None:
+        return None, 0
+    if gate_rows is None:
+        gate_rows = max(T, 1)
+    elif gate_rows < 1:
+        raise DmmvError(-2, "gate_rows must be positive")
+    m = gate[None, :] if gate.dim() == 1 else gate
+    groups = -(-T // gate_rows)
+    if T == 0 and m.dim() == 2:                           # (no rows: any number of gates)
+        groups = m.shape[0]
+    return _like(m, (groups, F), torch.float32, dev, "gate"), gate_rows
+
+
+def dmmv_residual_norm(f: torch.Tensor, h: torch.Tensor, post: Optional[Norm] = None, pre: Optional[Norm] = None,
+                       gate: Optional[torch.Tensor] = None, gate_rows: Optional[int] = None, alpha: float = 1.0, y: bool = True,
+                       q: bool = False, stream: bool = True) -> ResidualNormResult:
+    """What follows a block: the residual stream alpha h + gate post(f) and the next block's norm of it, pre, from one pass over f and h
+    (float32 or bfloat16).  gate: float32 [F], or [T / gate_rows][F] (rounded up), a row for every gate_rows tokens.  y: pre's result in
+    f's type; q: in 8 bits, the operand of dmmv_block_product (both only with pre); stream: the new residual stream, r.h."""
+    f = _matrix(f, "f")
+    kind = _layer_dtype(f.dtype)
+    T, F = f.shape
+    dev, on = f.get_device(), f.device
+    h = _like(h, f.shape, f.dtype, dev, "h")
+    y = y and pre is not None
+    if q and pre is None:
+        raise DmmvError(-1, "q needs pre")
+    a, b, keep = _norms(post, pre, F, dev)
+    g, rows = _gate(gate, gate_rows, T, F, dev)
+    new = functools.partial(torch.empty, dtype=torch.float32, device=on)
+    s = [new(T) if n is not None else None for n in (post, post, pre, pre)]
+    ov = torch.empty(T, F, dtype=f.dtype, device=on) if stream else None
+    oy = torch.empty(T, F, dtype=f.dtype, device=on) if y else None
+    oq = _new_block(T, F, 1, torch.uint8, on) if q else None
+    _enqueue(dev, load().dmmv_residual_norm, kind, T, F, f.data_ptr(), f.stride(0), h.data_ptr(), h.stride(0), alpha, _addr(g),
+             0 if g is None else g.stride(0), rows, _at(a), _at(b), _addr(ov), F, _addr(oy), F, oq._p if q else None, *map(_addr, s))
+    return ResidualNormResult(ov, oy, oq, *s)
+
+
+def dmmv_residual_norm_backward(dy: Optional[torch.Tensor], dv: Optional[torch.Tensor], f: Optional[torch.Tensor], r: ResidualNormResult,
+                                post: Optional[Norm] = None, pre: Optional[Norm] = None, gate: Optional[torch.Tensor] = None,
+                                gate_rows: Optional[int] = None, alpha: float = 1.0, df: bool = True, dh: bool = True,
+                                parameters: bool = True) -> ResidualNormGradients:
+    """Gradients of dmmv_residual_norm from those of y (dy, with pre) and of the new residual stream (dv; None = none arrives).  f is the
+    block's output (None where there is neither post nor a gate's gradient), r the forward pass's result: its h (with pre) and
+    statistics.  parameters: the gradients of the gate and of the gammas and betas that there are."""
+    if (dy is None) != (pre is None):
+        raise DmmvError(-1, "dy comes with pre, and pre with dy")
+    if dy is None and dv is None:
+        raise DmmvError(-1, "dy and dv are both None")
+    first = _matrix(dy if dy is not None else dv, "dy" if dy is not None else "dv")
+    kind = _layer_dtype(first.dtype)
+    T, F = first.shape
+    dev, on = first.get_device(), first.device
+    if dy is not None:
+        dy = first
+        dv = None if dv is None else _like(dv, dy.shape, dy.dtype, dev, "dv")
+    else:
+        dv = first
+    if f is not None:
+        f = _like(f, first.shape, first.dtype, dev, "f")
+    elif post is not None or (gate is not None and parameters):
+        raise DmmvError(-1, "f is None")
+    v = None
+    if pre is not None:
+        if r.h is None:
+            raise DmmvError(-1, "r.h is None")
+        v = _like(r.h, first.shape, first.dtype, dev, "r.h")
+    stats = [r.post_mean, r.post_rstd, r.mean, r.rstd]
+    for i, n in enumerate((post, post, pre, pre)):
+        if n is not None and stats[i] is None and not (n.rms and i % 2 == 0):
+            raise DmmvError(-1, "a statistic of the forward pass is None")
+        stats[i] = None if n is None else _vector(stats[i], T, dev, "a statistic")
+    a, b, keep = _norms(post, pre, F, dev)
+    g, rows = _gate(gate, gate_rows, T, F, dev)
+    like = functools.partial(torch.empty, T, F, dtype=first.dtype, device=on)
+    gf, gh = like() if df else None, like() if dh else None
+    gg = torch.empty(g.shape, dtype=torch.float32, device=on) if g is not None and parameters else None
+    of = [torch.empty(F, dtype=torch.float32, device=on) if parameters and t is not None else None
+          for n in (post, pre) for t in ((n.gamma, n.beta) if n is not None else (None, None))]
+    nbytes = _workspace("dmmv_residual_norm_workspace_bytes", T, F, rows)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=on) if nbytes else None
+    stride = lambda t: 0 if t is None else t.stride(0)  # noqa: E731
+    _enqueue(dev, load().dmmv_residual_norm_backward, kind, T, F, _addr(dy), stride(dy), _addr(dv), stride(dv), _addr(f), stride(f), _addr(v), stride(v),
+             alpha, _addr(g), stride(g), rows, _at(a), _at(b), *map(_addr, stats), _addr(gf), F, _addr(gh), F, _addr(gg), F, *map(_addr, of),
+             _addr(ws), nbytes)
+    if gg is not None:
+        if T == 0:
+            gg.zero_()
+        gg = gg.view(gate.shape)
+    return ResidualNormGradients(gf, gh, gg, *of)
+
+
+class _Gradient(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64), ("dtype", C.c_int32)]
+
+
+class Gradients:
+    """The gradients of a step, or the buffers that the clipped ones go to: float32 and bfloat16 tensors of one device, which stay where they
+    are.  Any shape without gaps in memory, in any order of its dimensions, and matrices or vectors with gaps."""
+
+    __slots__ = ("_tensors", "_order", "_c", "_p", "_dev", "_on", "_bytes")
+
+    def __init__(self, tensors: Sequence[torch.Tensor]):
+        self._tensors = [t.detach() for t in tensors]
+        if not self._tensors:
+            raise DmmvError(-2, "no gradients")
+        self._on = self._tensors[0].device
+        self._dev = self._tensors[0].get_device()
+        self._order = []
+        self._c = (_Gradient * len(self._tensors))()
+        for i, t in enumerate(self._tensors):
+            if not t.is_cuda:
+                raise DmmvError(-6, "tensors must live on the GPU")
+            kind = _layer_dtype(t.dtype)
+            _same(t, self._dev)
+            place, order = _place(t)
+            self._order.append(order)
+            self._c[i] = _Gradient(t.data_ptr(), *place, kind)
+        self._p = C.addressof(self._c)
+        self._bytes = load().dmmv_gradient_workspace_bytes(len(self._tensors), self._p)
+
+    tensors = property(lambda self: list(self._tensors))
+
+    def __len__(self) -> int:
+        return len(self._tensors)
+
+
+def _place(t: torch.Tensor):
+    """(rows, cols, row stride) of a tensor's memory, and its dimensions from the slowest to the fastest (those of one entry left out)."""
+    order = tuple(sorted((d for d in range(t.dim()) if t.shape[d] != 1), key=lambda d: -t.stride(d)))
+    n = t.numel()
+    if n == 0:
+        return (0, 0, 0), ()
+    dense, size = True, 1
+    for d in reversed(order):
+        dense &= t.stride(d) == size
+        size *= t.shape[d]
+    if len(order) == 2 and t.stride(order[1]) == 1 and t.stride(order[0]) >= t.shape[order[1]]:
+        return (t.shape[order[0]], t.shape[order[1]], t.stride(order[0])), order
+    if len(order) == 1 and t.stride(order[0]) > 0 and n < 1 << 31:
+        return (n, 1, t.stride(order[0])), order
+    if dense:
+        return (1, n, n), order
+    raise DmmvError(-8, f"a tensor of shape {tuple(t.shape)} and strides {t.stride()} has gaps that are not between rows")
+
+
+def _gradients(g) -> Gradients:
+    return g if isinstance(g, Gradients) else Gradients(g)
+
+
+def dmmv_gradient_norm(gradients) -> torch.Tensor:
+    """The norm over all numbers of all gradients (Gradients, or a list of tensors), a float32 scalar on the device."""
+    g = _gradients(gradients)
+    norm = torch.empty((), dtype=torch.float32, device=g._on)
+    ws = torch.empty(g._bytes, dtype=torch.uint8, device=g._on) if g._bytes else None
+    _enqueue(g._dev, load().dmmv_gradient_norm, len(g._tensors), g._p, norm.data_ptr(), _addr(ws), g._bytes)
+    return norm
+
+
+def dmmv_gradient_clip(gradients, max_norm: float, eps: float = 1e-6, out=None, norm: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Scales the gradients (Gradients, or a list of tensors), in place or into `out`, by max_norm / (norm + eps) where that is below 1, and
+    returns the norm.  norm: one from elsewhere (a float32 scalar on the device) over more gradients than these."""
+    g = _gradients(gradients)
+    o = None
+    if out is not None:
+        o = _gradients(out)
+        if o._dev != g._dev:
+            raise DmmvError(-6, "tensors are on different devices")
+        for i, (a, b) in enumerate(zip(g._tensors, o._tensors)):
+            if a.shape != b.shape or g._order[i] != o._order[i]:
+                raise DmmvError(-2, f"out[{i}] differs from its gradient in shape or in the order of its memory")
+        if len(g) != len(o):
+            raise DmmvError(-2, f"{len(o)} tensors in out for {len(g)} gradients")
+    given = None if norm is None else _vector(norm.reshape(1), 1, g._dev, "norm")
+    used = torch.empty((), dtype=torch.float32, device=g._on)
+    ws = torch.empty(g._bytes, dtype=torch.uint8, device=g._on) if g._bytes and given is None else None
+    _enqueue(g._dev, load().dmmv_gradient_clip, len(g._tensors), g._p, None if o is None else o._p, max_norm, eps, _addr(given), used.data_ptr(),
+             _addr(ws), 0 if ws is None else g._bytes)
+    return used
