@@ -102,34 +102,85 @@ __device__ __forceinline__ void finish8(const ProductOut<T, true>& o, int64_t ro
         if (ok && o.v) store8(o.v + row * cols, col, cols, v);
     }
 }
-// one number of u
-template <class T>
-__device__ __forceinline__ void finish1(const ProductOut<T, true>& o, int64_t row, int64_t col, int64_t cols, float u) {
+// one number of u; v
+template <bool SHORT, class T>
+__device__ __forceinline__ float finish1(const ProductOut<T, true>& o, int64_t row, int64_t col, int64_t cols, float u) {
     if (o.u) put_y(o.u + row * o.ldu + col, u);
     float v[1] = {u};
-    act_values<false>(o.act, v);
+    act_values<SHORT>(o.act, v);
     if (o.residual) v[0] += value_of(o.residual[row * o.ldr + col]);
     if (o.y) put_y(o.y + row * o.ldy + col, v[0]);
     if (o.v) o.v[row * cols + col] = v[0];
+    return v[0];
 }
-// ROWS x COLS numbers of u in the LDS (rows of LD floats), the first at row0, col0; 256 threads
-template <int ROWS, int COLS, int LD, bool Q, class T, class F>
-__device__ __forceinline__ void finish_tile(const ProductOut<T, true>& o, const float* u, int64_t rows, int64_t cols, int64_t col0, F row_of) {
+// What makes u of the sums in a tile, for its columns and rows: u = fma(sum * so, st, bias).  In the LDS.
+struct TileScales {
+    float *bias, *so, *st;
+};
+// ROWS x COLS numbers in the LDS (rows of LD floats): u, or with SUMS sums that become it.  256 threads, eight columns a turn.  Columns that
+// the matrix's end cuts go one by one, through the LDS: code that runs once is bound by its fetching, so there is little of it.
+template <int ROWS, int COLS, int LD, bool Q, bool SUMS, class T, class F>
+__device__ __forceinline__ void finish_tile(const ProductOut<T, true>& o, float* tile, const TileScales& k, int64_t row0, int64_t rows, int64_t cols, int64_t col0,
+                                            F row_of) {
     constexpr int PER_ROW = COLS / 8, TURNS = ROWS * PER_ROW / 256;
 #pragma unroll 1
-    for (int k = 0; k < TURNS; ++k) {
-        const int c = (int)threadIdx.x + 256 * k, r = c / PER_ROW, h = c % PER_ROW;
-        const int64_t row = row_of(r), col = col0 + h * 8;
-        const bool ok = row < rows && col < cols;
-        float v[8], b[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (ok && o.residual) load8(o.residual + row * o.ldr, col, cols, b);
+    for (int turn = 0; turn < TURNS; ++turn) {
+        const int c = (int)threadIdx.x + 256 * turn, r = c / PER_ROW, h = c % PER_ROW, place = row_of(r);
+        const int64_t row = row0 + place, col = col0 + h * 8;
+        const bool ok = row < rows && col < cols, whole = row < rows && col + 8 <= cols;
+        float* at = tile + r * LD + h * 8;
+        float v[8], b[8];
+        const bool add = whole && o.residual;
+        Raw8<T> res;
+        if (add) res.load(o.residual + row * o.ldr + col);
+        auto get8 = [&](const float* p, float (&w)[8]) __attribute__((always_inline)) {
+            const floatx4 f0 = *reinterpret_cast<const floatx4*>(p), f1 = *reinterpret_cast<const floatx4*>(p + 4);
 #pragma unroll
-        for (int e = 0; e < 8; e += 4) {
-            const floatx4 f = *reinterpret_cast<const floatx4*>(u + r * LD + h * 8 + e);
+            for (int i = 0; i < 4; ++i) { w[i] = f0[i]; w[4 + i] = f1[i]; }
+        };
+        get8(at, v);
+        if constexpr (SUMS) {
+            const float st = k.st[place];
+            if (k.so) {
+                get8(k.so + h * 8, b);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[e + i] = f[i];
+                for (int e = 0; e < 8; ++e) v[e] *= b[e];
+            }
+            get8(k.bias + h * 8, b);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = dmmv_fma(v[e], st, b[e]);
         }
-        finish8<Q>(o, row, col, cols, ok, v, b);
+        if (whole) {
+            if (o.u) store8(o.u + row * o.ldu, col, col + 8, v);
+            act_values<sizeof(T) == 2>(o.act, v);
+            if (add)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += res.get(e);
+            if (o.y) store8(o.y + row * o.ldy, col, col + 8, v);
+            if (!Q && o.v) store8(o.v + row * cols, col, col + 8, v);
+        } else if (ok) {
+            if constexpr (SUMS)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) at[e] = v[e];
+#pragma unroll 1
+            for (int e = 0; col + e < cols; ++e) at[e] = finish1<sizeof(T) == 2>(o, row, col + e, cols, at[e]);
+            get8(at, v);
+        }
+        if constexpr (Q) {
+            if (!o.has_q) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = ok && col + e < cols ? v[e] : 0.0f;
+            const uint32_t scale = scale_byte(row16_max(max8_bits(v)));
+            const piece8 code = encode8(v, scale);
+            uint8_t* to = o.q.codes + row * o.q.ld + col;
+            if (whole) {
+                *reinterpret_cast<piece8_any*>(to) = code;
+            } else if (ok) {
+#pragma unroll 1
+                for (int e = 0; col + e < cols; ++e) to[e] = (uint8_t)((e < 4 ? code[0] : code[1]) >> (8 * (e & 3)));
+            }
+            if (ok && (threadIdx.x & 15) == 0) scale_put(o.q, row, col >> 7, scale);
+        }
     }
 }
 
@@ -414,7 +465,7 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
             __syncthreads();
             if (again) {
                 tile_any<T, SCALED>(t0 + wt, T_, o0 + wo, O, K, x, w, how, bias, [&](int64_t t, int64_t o, float v) __attribute__((always_inline)) {
-                    if constexpr (EPI) finish1(out, t, o, O, v);
+                    if constexpr (EPI) finish1<false>(out, t, o, O, v);
                     else put_y(out.y + t * out.ldy + o, v);
                 });
                 return;
@@ -452,7 +503,7 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
     }
     if constexpr (EPI) {
         __syncthreads();
-        finish_tile<BM, BN, LDO, false>(out, tile, T_, O, o0, [&](int r) { return t0 + r; });
+        finish_tile<BM, BN, LDO, false, false>(out, tile, TileScales{}, t0, T_, O, o0, [](int r) { return r; });
     }
 }
 
@@ -487,7 +538,7 @@ __device__ __forceinline__ void stage_exponents(const BlockView& q, int64_t row0
 
 constexpr int product_lds(int MI, int NI, int width, int ws, int nst, bool epi) {
     const int stages = nst * 128 * 32 * (MI + NI) + 68 * (32 * MI + (ws == 2 ? 0 : ws == 1 ? (32 * NI + 127) / 128 : 32 * NI));
-    const int out = epi ? 2 * 64 * (32 * NI * 4 + 16) : 32 * MI * (32 * NI * width + 16);
+    const int out = epi ? 2 * 64 * (32 * NI * 4 + 16) + 4 * (64 * NI + 32 * MI) : 32 * MI * (32 * NI * width + 16);
     return stages > out ? stages : out;
 }
 
@@ -719,29 +770,24 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
     if constexpr (EPI) {
         // 64 rows at a time through the LDS in 32 bits, two places in turn: 32 of each half of the tile's rows
         constexpr int LDF = BN + 4;
+        float* const first = reinterpret_cast<float*>(lds);
+        const TileScales k = {first + 2 * 64 * LDF, WS == 1 ? nullptr : first + 2 * 64 * LDF + BN, first + 2 * 64 * LDF + 2 * BN};
+        if (tid < BN) {
+            const int64_t o = min(o0 + tid, O - 1);
+            k.bias[tid] = bias ? bias[o] : 0.0f;
+            if constexpr (WS != 1) k.so[tid] = !how.w_blocks ? row_scale(scale_at(w, o, 0)).rest : 1.0f;
+        }
+        if (tid < BM) k.st[tid] = !how.x_blocks ? row_scale(scale_at(x, min(t0 + tid, T_ - 1), 0)).rest : 1.0f;
         auto pass = [&](auto P) __attribute__((always_inline)) {
             constexpr int p = P.value;
-            float* tile = reinterpret_cast<float*>(lds) + (p & 1) * 64 * LDF;
+            float* tile = first + (p & 1) * 64 * LDF;
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                float bo[4], so[4];
+            for (int i = 0; i < NI; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int64_t o = min(o0 + wo + 16 * i + lg * 4 + e, O - 1);
-                    bo[e] = bias ? bias[o] : 0.0f;
-                    so[e] = !how.w_blocks ? row_scale(scale_at(w, o, 0)).rest : 1.0f;
-                }
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const float st = !how.x_blocks ? row_scale(scale_at(x, min(t0 + wt + 16 * (2 * p + j) + lr, T_ - 1), 0)).rest : 1.0f;
-                    float v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = dmmv_fma(acc[i][2 * p + j][e] * so[e], st, bo[e]);
-                    put4(tile + ((wv & 1) * 32 + 16 * j + lr) * LDF + wo + 16 * i + lg * 4, v);
-                }
-            }
+                for (int j = 0; j < 2; ++j)
+                    *reinterpret_cast<floatx4*>(tile + ((wv & 1) * 32 + 16 * j + lr) * LDF + wo + 16 * i + lg * 4) = acc[i][2 * p + j];
             __syncthreads();
-            finish_tile<64, BN, LDF, true>(out, tile, T_, O, o0, [&](int r) { return t0 + (r >> 5) * (BM / 2) + 32 * p + (r & 31); });
+            finish_tile<64, BN, LDF, true, true>(out, tile, k, t0, T_, O, o0, [](int r) { return (r >> 5) * (BM / 2) + 32 * p + (r & 31); });
         };
         pass(C0);
         pass(C1);
@@ -946,7 +992,7 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
             if (o >= O) continue;
             const float so = SCALED && !how.w_blocks ? row_scale(scale_at(w, o, 0)).rest : 1.0f;
             const float u = dmmv_fma(v[e] * so, st, bias ? bias[o] : 0.0f);
-            if constexpr (EPI) finish1(out, t, o, O, u);
+            if constexpr (EPI) finish1<false>(out, t, o, O, u);
             else put_y(out.y + t * out.ldy + o, u);
         }
     }
