@@ -20,7 +20,7 @@ __device__ __forceinline__ Logistic logistic(float x) {
 constexpr float GELU_2C = 1.5957691216057308f, GELU_A = 0.044715f;       // 2 sqrt(2 / pi)
 
 // 0 below every number that matters, so that -infinity gives act's limit there
-__device__ __forceinline__ float above(float u, float least) { return u < least ? least : u; }       // (NaN stays)
+__device__ __forceinline__ float above(float u, float least) { return __builtin_elementwise_maximum(u, least); }       // (NaN stays)
 
 template <int ACT>
 __device__ __forceinline__ float act_value(float u) {
@@ -46,7 +46,7 @@ __device__ __forceinline__ float act_value(float u) {
 template <int ACT>
 __device__ __forceinline__ float act_value_short(float u) {
     if constexpr (ACT == DMMV_ACT_GELU) {
-        const float t = fminf(fabsf(u), 13.3f);
+        const float t = __builtin_elementwise_minimum(fabsf(u), 13.3f);
         float p = 1.8800052625778108e-09f;
         p = dmmv_fma(p, t, -1.3789509978323622e-07f);
         p = dmmv_fma(p, t, 4.445783815754112e-06f);

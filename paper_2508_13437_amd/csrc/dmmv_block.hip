@@ -94,9 +94,10 @@ __global__ __launch_bounds__(256) void k_block_quantize_rows(int64_t rows, int64
     const int64_t col = blk * 128 + (threadIdx.x & 15) * 8;
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (row < rows) load8(x + row * ldx, col, cols, v);
-    const uint32_t b = scale_byte(row16_max(max8_bits(v)));
+    uint32_t b;
+    const piece8 code = quantize8(v, b);
     if (row >= rows) return;
-    store8_codes(q.codes + row * q.ld, col, cols, encode8(v, b));
+    store8_codes(q.codes + row * q.ld, col, cols, code);
     if ((threadIdx.x & 15) == 0) scale_put(q, row, blk, b);
 }
 

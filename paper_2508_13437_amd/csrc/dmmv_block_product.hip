@@ -93,9 +93,10 @@ __device__ __forceinline__ void finish8(const ProductOut<T, true>& o, int64_t ro
         if (!o.has_q) return;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = col + e < cols ? v[e] : 0.0f;
-        const uint32_t b = scale_byte(row16_max(max8_bits(v)));
+        uint32_t b;
+        const piece8 code = quantize8(v, b);
         if (ok && col < cols) {
-            store8_codes(o.q.codes + row * o.q.ld, col, cols, encode8(v, b));
+            store8_codes(o.q.codes + row * o.q.ld, col, cols, code);
             if ((threadIdx.x & 15) == 0) scale_put(o.q, row, col >> 7, b);
         }
     } else {
@@ -117,69 +118,93 @@ __device__ __forceinline__ float finish1(const ProductOut<T, true>& o, int64_t r
 struct TileScales {
     float *bias, *so, *st;
 };
-// ROWS x COLS numbers in the LDS (rows of LD floats): u, or with SUMS sums that become it.  256 threads, eight columns a turn.  Columns that
-// the matrix's end cuts go one by one, through the LDS: code that runs once is bound by its fetching, so there is little of it.
+// ROWS x COLS numbers in the LDS (rows of LD floats): u, or with SUMS sums that become it.  256 threads, eight columns of a row a turn, always the
+// same ones, and the rows (256 * 8 / COLS a turn) are those of the thread at turn 0 and rows_on(turn) further.  What a turn reads of the LDS
+// is requested in the turn before.  Columns that the matrix's end cuts go one by one, through the LDS: code that runs once is bound by its
+// fetching, so there is little of it.
 template <int ROWS, int COLS, int LD, bool Q, bool SUMS, class T, class F>
 __device__ __forceinline__ void finish_tile(const ProductOut<T, true>& o, float* tile, const TileScales& k, int64_t row0, int64_t rows, int64_t cols, int64_t col0,
-                                            F row_of) {
-    constexpr int PER_ROW = COLS / 8, TURNS = ROWS * PER_ROW / 256;
-#pragma unroll 1
+                                            F rows_on) {
+    constexpr int PER_ROW = COLS / 8, STEP = 256 / PER_ROW, TURNS = ROWS / STEP;
+    const int r0 = (int)threadIdx.x / PER_ROW, h = (int)threadIdx.x % PER_ROW;
+    const int64_t col = col0 + h * 8, at0 = row0 + r0;
+    const int left = (int)min(cols - col, (int64_t)8), below = (int)min(rows - at0, (int64_t)1 << 20);      // of the columns, of the rows
+    T* const y = o.y + at0 * o.ldy + col;
+    T* const u = o.u + at0 * o.ldu + col;
+    const T* const residual = o.residual + at0 * o.ldr + col;
+    uint8_t* const codes = Q ? o.q.codes + at0 * o.q.ld + col : nullptr;
+    const int64_t scale0 = Q ? at0 * o.q.srow + (col >> 7) * o.q.sblk : 0;
+    auto get8 = [&](const float* p, float (&w)[8]) __attribute__((always_inline)) {
+        const floatx4 f0 = *reinterpret_cast<const floatx4*>(p), f1 = *reinterpret_cast<const floatx4*>(p + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { w[i] = f0[i]; w[4 + i] = f1[i]; }
+    };
+    float* at = tile + r0 * LD + h * 8;
+    float so[8], bias[8], next[8], nst = 1.0f;
+    if constexpr (SUMS) {
+        if (k.so) get8(k.so + h * 8, so);
+        get8(k.bias + h * 8, bias);
+        nst = k.st[r0 + rows_on(0)];
+    }
+    get8(at, next);
+#pragma unroll 2
     for (int turn = 0; turn < TURNS; ++turn) {
-        const int c = (int)threadIdx.x + 256 * turn, r = c / PER_ROW, h = c % PER_ROW, place = row_of(r);
-        const int64_t row = row0 + place, col = col0 + h * 8;
-        const bool ok = row < rows && col < cols, whole = row < rows && col + 8 <= cols;
-        float* at = tile + r * LD + h * 8;
-        float v[8], b[8];
+        const int on = rows_on(turn);                // (the same for all)
+        const bool ok = on < below && left > 0, whole = on < below && left >= 8;
         const bool add = whole && o.residual;
-        Raw8<T> res;
-        if (add) res.load(o.residual + row * o.ldr + col);
-        auto get8 = [&](const float* p, float (&w)[8]) __attribute__((always_inline)) {
-            const floatx4 f0 = *reinterpret_cast<const floatx4*>(p), f1 = *reinterpret_cast<const floatx4*>(p + 4);
+        Raw8<T> res;                                 // (a turn ahead it would wait for the stores before it: 28 us more at 4096 x 11008 x 4096)
+        if (add) res.load(residual + on * o.ldr);
+        float v[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { w[i] = f0[i]; w[4 + i] = f1[i]; }
-        };
-        get8(at, v);
+        for (int e = 0; e < 8; ++e) v[e] = next[e];
+        const float st = nst;
+        float* const here = at;
+        if (turn + 1 < TURNS) {
+            at += STEP * LD;
+            get8(at, next);
+            if constexpr (SUMS) nst = k.st[r0 + rows_on(turn + 1)];
+        }
         if constexpr (SUMS) {
-            const float st = k.st[place];
-            if (k.so) {
-                get8(k.so + h * 8, b);
+            if (k.so)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= b[e];
-            }
-            get8(k.bias + h * 8, b);
+                for (int e = 0; e < 8; ++e) v[e] *= so[e];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = dmmv_fma(v[e], st, b[e]);
+            for (int e = 0; e < 8; ++e) v[e] = dmmv_fma(v[e], st, bias[e]);
         }
         if (whole) {
-            if (o.u) store8(o.u + row * o.ldu, col, col + 8, v);
+            if (o.u) store8(u + on * o.ldu, 0, 8, v);
             act_values<sizeof(T) == 2>(o.act, v);
             if (add)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += res.get(e);
-            if (o.y) store8(o.y + row * o.ldy, col, col + 8, v);
-            if (!Q && o.v) store8(o.v + row * cols, col, col + 8, v);
+            if (o.y) store8(y + on * o.ldy, 0, 8, v);
+            if (!Q && o.v) store8(o.v + (at0 + on) * cols + col, 0, 8, v);
         } else if (ok) {
             if constexpr (SUMS)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) at[e] = v[e];
+                for (int e = 0; e < 8; ++e) here[e] = v[e];
 #pragma unroll 1
-            for (int e = 0; col + e < cols; ++e) at[e] = finish1<sizeof(T) == 2>(o, row, col + e, cols, at[e]);
-            get8(at, v);
+            for (int e = 0; e < left; ++e) here[e] = finish1<sizeof(T) == 2>(o, at0 + on, col + e, cols, here[e]);
+            get8(here, v);
         }
         if constexpr (Q) {
             if (!o.has_q) continue;
+            if (!whole)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = ok && col + e < cols ? v[e] : 0.0f;
-            const uint32_t scale = scale_byte(row16_max(max8_bits(v)));
-            const piece8 code = encode8(v, scale);
-            uint8_t* to = o.q.codes + row * o.q.ld + col;
+                for (int e = 0; e < 8; ++e) v[e] = ok && e < left ? v[e] : 0.0f;
+            uint32_t scale;
+            const piece8 code = quantize8(v, scale);
+            uint8_t* to = codes + on * o.q.ld;
             if (whole) {
                 *reinterpret_cast<piece8_any*>(to) = code;
             } else if (ok) {
 #pragma unroll 1
-                for (int e = 0; col + e < cols; ++e) to[e] = (uint8_t)((e < 4 ? code[0] : code[1]) >> (8 * (e & 3)));
+                for (int e = 0; e < left; ++e) to[e] = (uint8_t)((e < 4 ? code[0] : code[1]) >> (8 * (e & 3)));
             }
-            if (ok && (threadIdx.x & 15) == 0) scale_put(o.q, row, col >> 7, scale);
+            if (ok && (threadIdx.x & 15) == 0) {
+                if (o.q.e8m0) static_cast<uint8_t*>(o.q.scales)[scale0 + on * o.q.srow] = (uint8_t)scale;
+                else static_cast<float*>(o.q.scales)[scale0 + on * o.q.srow] = e8m0_value(scale);
+            }
         }
     }
 }
@@ -503,7 +528,7 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
     }
     if constexpr (EPI) {
         __syncthreads();
-        finish_tile<BM, BN, LDO, false, false>(out, tile, TileScales{}, t0, T_, O, o0, [](int r) { return r; });
+        finish_tile<BM, BN, LDO, false, false>(out, tile, TileScales{}, t0, T_, O, o0, [](int turn) { return 32 * turn; });
     }
 }
 
@@ -787,7 +812,10 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
                 for (int j = 0; j < 2; ++j)
                     *reinterpret_cast<floatx4*>(tile + ((wv & 1) * 32 + 16 * j + lr) * LDF + wo + 16 * i + lg * 4) = acc[i][2 * p + j];
             __syncthreads();
-            finish_tile<64, BN, LDF, true, true>(out, tile, k, t0, T_, O, o0, [](int r) { return (r >> 5) * (BM / 2) + 32 * p + (r & 31); });
+            finish_tile<64, BN, LDF, true, true>(out, tile, k, t0, T_, O, o0, [](int turn) {
+                constexpr int STEP = 2048 / BN;              // rows a turn
+                return turn * STEP / 32 * (BM / 2 - 32) + turn * STEP + 32 * p;
+            });
         };
         pass(C0);
         pass(C1);

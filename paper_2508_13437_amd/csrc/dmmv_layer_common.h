@@ -206,20 +206,28 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t a) {
     const int e = (int)(a >> 23) - 8 + ((a & 0x7FFFFFu) > 0x600000u ? 1 : 0);
     return e < 1 ? 1u : (uint32_t)e;
 }
-// eight values to codes, scale 2^(b - 127) with 1 <= b <= 247; the conversion rounds to nearest even
-__device__ __forceinline__ piece8 encode8(const float (&v)[8], uint32_t b) {
+// eight finite values to codes, scale 2^(b - 127) with 1 <= b <= 247; the conversion rounds to nearest even
+__device__ __forceinline__ piece8 encode8_finite(const float (&v)[8], uint32_t b) {
     const float inv = __uint_as_float((254u - b) << 23);
     piece8 r;
-    uint32_t most = 0u;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h] * inv, v[4 * h + 1] * inv, 0, false);
         w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h + 2] * inv, v[4 * h + 3] * inv, w, true);
         r[h] = (uint32_t)w;
     }
+    return r;
+}
+// the largest |x| of eight as bits, infinities and NaN among them
+__device__ __forceinline__ uint32_t most8(const float (&v)[8]) {
+    uint32_t most = 0u;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    if (most >= 0x7F800000u) {               // infinities and NaN: one code for all
+    for (int i = 0; i < 8; i += 2) most = max(max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu), __float_as_uint(v[i + 1]) & 0x7FFFFFFFu);
+    return most;
+}
+__device__ __forceinline__ piece8 encode8(const float (&v)[8], uint32_t b) {
+    piece8 r = encode8_finite(v, b);
+    if (most8(v) >= 0x7F800000u) {           // infinities and NaN: one code for all
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if ((__float_as_uint(v[i]) & 0x7FFFFFFFu) >= 0x7F800000u)
@@ -253,6 +261,16 @@ __device__ __forceinline__ uint32_t max8_bits(const float (&v)[8]) {
     for (int i = 0; i < 8; ++i) a = max(a, finite_bits(v[i]));
     return a;
 }
+// Eight values of a lane in 8 bits, 16 lanes a block: the codes, and the scale's byte.  All 64 lanes active; what is not finite is looked for once.
+__device__ __forceinline__ piece8 quantize8(const float (&v)[8], uint32_t& scale) {
+    const uint32_t most = most8(v);
+    if (__any(most >= 0x7F800000u)) {
+        scale = scale_byte(row16_max(max8_bits(v)));
+        return encode8(v, scale);
+    }
+    scale = scale_byte(row16_max(most));
+    return encode8_finite(v, scale);
+}
 // sum over the wavefront in a fixed order, the same value in every lane; all 64 lanes active
 __device__ __forceinline__ float wave_sum(float v) {
     v += dpp_mov<DPP_QUAD_XOR1>(v);
@@ -280,9 +298,10 @@ __device__ __forceinline__ float team_sum(float v, float* sh) {
 
 template <class T>
 __device__ __forceinline__ void put_q(const BlockView& q, int64_t row, int64_t col, int64_t cols, const float (&v)[8]) {
-    const uint32_t b = scale_byte(row16_max(max8_bits(v)));
+    uint32_t b;
+    const piece8 code = quantize8(v, b);
     if (col < cols) {
-        store8_codes(q.codes + row * q.ld, col, cols, encode8(v, b));
+        store8_codes(q.codes + row * q.ld, col, cols, code);
         if ((threadIdx.x & 15) == 0) scale_put(q, row, col >> 7, b);
     }
 }
