@@ -9,13 +9,32 @@ dmmv_status layer_check_act(int32_t act, bool none);
 
 #ifdef __HIPCC__
 
-// 1 / (1 + e^-x) and 1 less that, neither from the other: e^-|x| <= 1
+// 1 / (1 + e^-x) and 1 less that, neither from the other: e^-|x| <= 1.  Off by some |x| + 6 units of 2^-24.
 struct Logistic {
     float s, rest;
 };
 __device__ __forceinline__ Logistic logistic(float x) {
-    const float e = expf(-fabsf(x)), r = 1.0f / (1.0f + e);
+    const float e = __builtin_amdgcn_exp2f(fabsf(x) * -1.4426950408889634f), r = __builtin_amdgcn_rcpf(1.0f + e);
     return x < 0.0f ? Logistic{e * r, r} : Logistic{r, e * r};
+}
+// e^(-t^2 / 2) and the normal distribution's function at -t, t >= 0.  Their quotient falls slowly, from 1/2 as 1 / t: k times a polynomial in
+// k = 1 / (1 + 0.3 t), of least largest relative error over 0 to 32 (2^-25; its sum in 32 bits 5.6 units of 2^-24, and 1/2 exactly at 0).
+struct NormalTail {
+    float e, q;
+};
+__device__ __forceinline__ NormalTail normal_tail(float t) {
+    const float e = __builtin_amdgcn_exp2f(t * t * -0.72134752044448170f), k = __builtin_amdgcn_rcpf(dmmv_fma(0.3f, t, 1.0f));
+    float p = -0.018033696338534355f;
+    p = dmmv_fma(p, k, 0.0994100347161293f);
+    p = dmmv_fma(p, k, -0.20012778043746948f);
+    p = dmmv_fma(p, k, 0.15783672034740448f);
+    p = dmmv_fma(p, k, -0.05417666584253311f);
+    p = dmmv_fma(p, k, 0.08422795683145523f);
+    p = dmmv_fma(p, k, 0.0819549635052681f);
+    p = dmmv_fma(p, k, 0.10958808660507202f);
+    p = dmmv_fma(p, k, 0.11963638663291931f);
+    p = dmmv_fma(p, k, 0.11968399584293365f);
+    return NormalTail{e, p * k * e};
 }
 constexpr float GELU_2C = 1.5957691216057308f, GELU_A = 0.044715f;       // 2 sqrt(2 / pi)
 
@@ -26,8 +45,8 @@ template <int ACT>
 __device__ __forceinline__ float act_value(float u) {
     if constexpr (ACT == DMMV_ACT_RELU) return above(u, 0.0f);
     if constexpr (ACT == DMMV_ACT_GELU) {
-        u = above(u, -30.0f);
-        return 0.5f * u * erfcf(-0.70710678118654752f * u);
+        const float t = __builtin_elementwise_minimum(fabsf(u), 30.0f);
+        return dmmv_fma(-t, normal_tail(t).q, above(u, 0.0f));           // u Phi(u) = max(u, 0) - |u| Phi(-|u|)
     }
     if constexpr (ACT == DMMV_ACT_GELU_TANH) {
         u = above(u, -30.0f);
@@ -73,8 +92,10 @@ __device__ __forceinline__ float act_slope(float u) {
     if constexpr (ACT == DMMV_ACT_RELU) return u != u ? u : u > 0.0f ? 1.0f : 0.0f;
     // beyond 30 the slopes of GELU are 0 and 1 (their rest is below e^-430), and the products below leave the range
     if constexpr (ACT == DMMV_ACT_GELU || ACT == DMMV_ACT_GELU_TANH) u = u > 30.0f ? 30.0f : u < -30.0f ? -30.0f : u;
-    if constexpr (ACT == DMMV_ACT_GELU)
-        return dmmv_fma(0.5f, erfcf(-0.70710678118654752f * u), u * 0.39894228040143268f * expf(-0.5f * u * u));
+    if constexpr (ACT == DMMV_ACT_GELU) {
+        const NormalTail n = normal_tail(fabsf(u));
+        return dmmv_fma(u * 0.39894228040143268f, n.e, u < 0.0f ? n.q : 1.0f - n.q);
+    }
     if constexpr (ACT == DMMV_ACT_GELU_TANH) {
         const Logistic l = logistic(GELU_2C * u * dmmv_fma(GELU_A * u, u, 1.0f));
         return dmmv_fma(u * GELU_2C * dmmv_fma(3.0f * GELU_A * u, u, 1.0f), l.s * l.rest, l.s);
