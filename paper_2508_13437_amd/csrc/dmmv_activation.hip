@@ -61,10 +61,10 @@ __global__ __launch_bounds__(256) void k_activation_backward(int64_t rows, int64
     if (col < cols) store8(part + blockIdx.x * cols, col, cols, s);
 }
 
-// Strips of rows: some 2048 workgroups, a strip at least eight rounds of the workgroup's rows.
+// Strips of rows: some 1536 workgroups (4096 x 11008 bf16 64 us, 68 with 2048, 72 with 1024), a strip at least eight rounds of the workgroup's rows.
 static int act_lanes(int64_t cols) { return cols <= 128 ? 16 : cols <= 512 ? 64 : 256; }
 static int64_t act_rows(int64_t rows, int64_t cols) {
-    const int64_t lanes = act_lanes(cols), teams = 256 / lanes, want = ceil_div(2048, ceil_div(cols, 8 * lanes));
+    const int64_t lanes = act_lanes(cols), teams = 256 / lanes, want = ceil_div(1536, ceil_div(cols, 8 * lanes));
     const int64_t per = ceil_div(rows, want), least = 8 * teams;
     return per > least ? per : least;
 }

@@ -225,7 +225,7 @@ struct ResidualGrad {
     int64_t lddf, lddh;
     float* dgate;                        // groups that a team has for itself are written where they belong
     int64_t lddgate;
-    float* part;                         // [workgroup][5][cols]: dgamma, dbeta, dpost_gamma, dpost_beta, dgate
+    float* part;                         // [workgroup][4][cols]: GradSums, or where groups are not split the gates' products with the last two
     int32_t sums;                        // which of them are wanted, by bits
 };
 
@@ -249,56 +249,80 @@ __device__ __forceinline__ TeamRows team_rows(const RowStrips& s, int64_t rows, 
     return {r0, min(r0 + s.per, rows), 1};
 }
 
-// Eight columns of one row: everything but the sums over the row.
-struct GradRow {
-    float dy[8], e[8], n[8], m[8];
+// What a column's sums over rows are made of:  sum dy n,  sum dy,  A = sum e m,  B = sum e.  Within a gate group, dgate = post_gamma A +
+// post_beta B, and a group's share of dpost_gamma and dpost_beta is gate A and gate B.
+struct GradSums {
+    float dy_n[8], dy[8], e_m[8], e[8];
 };
-struct GradVectors {
-    float g1[8], g0[8], b0[8];
-};
-__device__ __forceinline__ void grad_vectors(const NormView& pre, const NormView& post, int64_t col, int64_t cols, GradVectors& k) {
+__device__ __forceinline__ void load_or(const float* __restrict__ p, float value, int64_t col, int64_t cols, float (&v)[8]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) { k.g1[e] = k.g0[e] = 1.0f; k.b0[e] = 0.0f; }
-    if (pre.gamma) load8(pre.gamma, col, cols, k.g1);
-    if (post.gamma) load8(post.gamma, col, cols, k.g0);
-    if (post.beta) load8(post.beta, col, cols, k.b0);
+    for (int e = 0; e < 8; ++e) v[e] = value;
+    if (p) load8(p, col, cols, v);
 }
 __device__ __forceinline__ void load_gate(const GateView& gate, int64_t row, int64_t col, int64_t cols, float (&g)[8]) {
+    load_or(gate.g ? gate.g + ((uint32_t)row / gate.per) * gate.ld : nullptr, 1.0f, col, cols, g);
+}
+// a group of a team's own has ended: its gate's gradient, and what it adds to those of the norm after the block
+template <class T>
+__device__ __forceinline__ void end_group(const ResidualGrad<T>& a, int64_t row, int64_t col, int64_t cols, GradSums& s, float (&to_gamma)[8], float (&to_beta)[8]) {
+    float g[8], b[8];
+    if (a.dgate) {
+        load_or(a.post.gamma, 1.0f, col, cols, g);
+        load_or(a.post.beta, 0.0f, col, cols, b);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) g[e] = 1.0f;
-    if (gate.g) load8(gate.g + ((uint32_t)row / gate.per) * gate.ld, col, cols, g);
+        for (int e = 0; e < 8; ++e) g[e] = dmmv_fma(g[e], s.e_m[e], b[e] * s.e[e]);
+        store8(a.dgate + ((uint32_t)row / a.gate.per) * a.lddgate, col, cols, g);
+    }
+    load_gate(a.gate, row, col, cols, g);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        to_gamma[e] = dmmv_fma(g[e], s.e_m[e], to_gamma[e]);
+        to_beta[e] = dmmv_fma(g[e], s.e[e], to_beta[e]);
+        s.e_m[e] = s.e[e] = 0.0f;
+    }
+}
+// gate post_gamma of a row
+template <class T>
+__device__ __forceinline__ void load_factor(const ResidualGrad<T>& a, int64_t row, int64_t col, int64_t cols, float (&f)[8]) {
+    float g[8];
+    load_gate(a.gate, row, col, cols, f);
+    load_or(a.post.gamma, 1.0f, col, cols, g);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] *= g[e];
 }
 
 // Rows of up to 4096 columns: a team of TPR threads holds a row in registers between the two pairs of sums, and keeps its columns' share of the
 // sums over rows; the teams of a workgroup join theirs at the end, in order, in the LDS.  Everything is read once, and the next row is requested before
-// this one's sums are waited for.
-template <class T, int TPR, int THREADS>
-__global__ __launch_bounds__(THREADS) void k_residual_norm_grad(int64_t rows, int64_t cols, ResidualGrad<T> a, RowStrips strips) {
+// this one's sums are waited for.  SPLIT: a workgroup has rows of one gate group only.  BETAS: sum dy or sum e are wanted.
+template <class T, int TPR, int THREADS, bool SPLIT, bool BETAS>
+__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && SPLIT ? 4 : 2) void k_residual_norm_grad(int64_t rows, int32_t cols, ResidualGrad<T> a, RowStrips strips) {
     constexpr int TEAMS = THREADS / TPR, WAVES = TPR / 64;
     __shared__ float2 sh[2][2][TEAMS][WAVES];
     __shared__ float join[TEAMS > 1 ? TPR * 8 : 1];
-    const int team = threadIdx.x / TPR, t = threadIdx.x % TPR;
+    const int team = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR), t = threadIdx.x % TPR;
     const float inv_n = 1.0f / (float)cols;
-    const int64_t col = t * 8ll;
-    GradVectors k;
-    grad_vectors(a.pre, a.post, col, cols, k);
-    float sum[5][8], gate[8];
+    const int32_t col = t * 8;
+    const bool in = col < cols;
+    float g1[8], factor[8], to_gamma[SPLIT ? 1 : 8], to_beta[SPLIT ? 1 : 8];
+    load_or(a.pre.gamma, 1.0f, col, cols, g1);
+    GradSums sum;
 #pragma unroll
-    for (int i = 0; i < 5; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum[i][e] = 0.0f;
+    for (int e = 0; e < 8; ++e) {
+        sum.dy_n[e] = sum.dy[e] = sum.e_m[e] = sum.e[e] = 0.0f;
+        if constexpr (!SPLIT) to_gamma[e] = to_beta[e] = 0.0f;
+    }
     const TeamRows r = team_rows(strips, rows, a.gate.per, team, TEAMS);
     const int64_t last = rows - 1;
     int64_t row = r.at;
-    load_gate(a.gate, min(row, last), col, cols, gate);
-    const int64_t passes = (strips.per + r.step - 1) / r.step;           // the same for all teams
-    Raw8<T> rdy, rdv, rf, rv;
+    load_factor(a, min(row, last), col, cols, factor);
+    const int32_t passes = (int32_t)((strips.per + r.step - 1) / r.step);           // the same for all teams
+    Raw8<T> rdy = {}, rdv = {}, rf = {}, rv = {};
     float nmu1 = 0.0f, nrs1 = 0.0f, nmu0 = 0.0f, nrs0 = 1.0f;
     auto request = [&](int64_t at) __attribute__((always_inline)) {
         const int64_t q = min(at, last);
         if (a.pre.kind) { nmu1 = a.pre.kind == 1 ? a.mean[q] : 0.0f; nrs1 = a.rstd[q]; }
         if (a.post.kind) { nmu0 = a.post.kind == 1 ? a.post_mean[q] : 0.0f; nrs0 = a.post_rstd[q]; }
-        if (col >= cols) return;                     // (whole wavefronts but one)
+        if (!in) return;                             // (whole wavefronts but one)
         raw_request(rdy, a.dy + q * a.lddy, col, cols);
         raw_request(rdv, a.dv + q * a.lddv, col, cols);
         raw_request(rf, a.f + q * a.ldf, col, cols);
@@ -311,113 +335,115 @@ __global__ __launch_bounds__(THREADS) void k_residual_norm_grad(int64_t rows, in
         if constexpr (WAVES > 1) {
             if ((t & 63) == 0) sh[set][parity][team][t >> 6] = make_float2(s1, s2);
             __syncthreads();
-            s1 = s2 = 0.0f;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) { s1 += sh[set][parity][team][w].x; s2 += sh[set][parity][team][w].y; }
+            // (the wavefronts' sums in turn over the lanes, and a tree over them)
+            const float2 w = sh[set][parity][team][t & (WAVES - 1)];
+            s1 = w.x + dpp_mov<DPP_QUAD_XOR1>(w.x);
+            s2 = w.y + dpp_mov<DPP_QUAD_XOR1>(w.y);
+            if constexpr (WAVES > 2) { s1 += dpp_mov<DPP_QUAD_XOR2>(s1); s2 += dpp_mov<DPP_QUAD_XOR2>(s2); }
+            if constexpr (WAVES > 4) { s1 += dpp_mov<DPP_ROW_HALF_MIRROR>(s1); s2 += dpp_mov<DPP_ROW_HALF_MIRROR>(s2); }
+            static_assert(WAVES <= 8, "eight lanes");
         }
         s1 *= inv_n;
         s2 *= inv_n;
     };
     request(row);
     int parity = 0;
-    for (int64_t p = 0; p < passes; ++p, row += r.step, parity ^= 1) {
+    for (int32_t p = 0; p < passes; ++p, row += r.step, parity ^= 1) {
         const bool there = row < r.end;
         const float mu1 = nmu1, rs1 = nrs1, mu0 = nmu0, rs0 = nrs0;
-        GradRow w;
-        raw_settle(rdy, col, cols, col < cols && a.pre.kind);
-        raw_settle(rdv, col, cols, col < cols && a.has_dv);
-        raw_settle(rf, col, cols, col < cols && a.need_f);
-        raw_settle(rv, col, cols, col < cols && a.pre.kind);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            w.dy[e] = rdy.get(e);
-            w.e[e] = rdv.get(e);
-            w.n[e] = (rv.get(e) - mu1) * rs1;
-            w.m[e] = (rf.get(e) - mu0) * rs0;
-        }
+        // this row as it is stored: numbers are made of it wherever they are used, which takes fewer registers than holding them
+        raw_settle(rdy, col, cols, in && a.pre.kind);
+        raw_settle(rdv, col, cols, in && a.has_dv);
+        raw_settle(rf, col, cols, in && a.need_f);
+        raw_settle(rv, col, cols, in && a.pre.kind);
+        const Raw8<T> cdy = rdy, cdv = rdv, cf = rf, cv = rv;
         request(row + r.step);                       // (past the last: the last again)
         // past the row's end dy and dv are zero, and so is what follows from them, if the rest is finite
-        if (col + 8 > cols)
+        const int32_t left = cols - col;
+        auto n_of = [&](int e) __attribute__((always_inline)) { return e < left ? (cv.get(e) - mu1) * rs1 : 0.0f; };
+        auto m_of = [&](int e) __attribute__((always_inline)) { return e < left ? (cf.get(e) - mu0) * rs0 : 0.0f; };
+        float x[8];                                  // e
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (col + e >= cols) w.n[e] = w.m[e] = 0.0f;
+        for (int e = 0; e < 8; ++e) x[e] = cdv.get(e);
         if (a.pre.kind) {
             float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float b = w.dy[e] * k.g1[e];
+                const float b = cdy.get(e) * g1[e];
                 s1 += b;
-                s2 = dmmv_fma(b, w.n[e], s2);
+                s2 = dmmv_fma(b, n_of(e), s2);
             }
             both(0, parity, s1, s2);
             if (a.pre.kind == 2) s1 = 0.0f;
-            if (there)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    sum[0][e] = dmmv_fma(w.dy[e], w.n[e], sum[0][e]);
-                    sum[1][e] += w.dy[e];
-                    w.e[e] = dmmv_fma(rs1, (w.dy[e] * k.g1[e] - s1) - w.n[e] * s2, w.e[e]);
+            for (int e = 0; e < 8; ++e) {
+                const float dy = cdy.get(e), n = n_of(e);
+                if (there) {
+                    sum.dy_n[e] = dmmv_fma(dy, n, sum.dy_n[e]);
+                    if constexpr (BETAS) sum.dy[e] += dy;
                 }
-            if (col + 8 > cols)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (col + e >= cols) w.e[e] = 0.0f;
+                x[e] = e < left ? dmmv_fma(rs1, (dy * g1[e] - s1) - n * s2, x[e]) : 0.0f;
+            }
         }
-        float s3 = 0.0f, s4 = 0.0f, d[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] = gate[e] * w.e[e];
         if (there)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                sum[2][e] = dmmv_fma(d[e], w.m[e], sum[2][e]);
-                sum[3][e] += d[e];
-                sum[4][e] = dmmv_fma(w.e[e], dmmv_fma(w.m[e], k.g0[e], k.b0[e]), sum[4][e]);
+                sum.e_m[e] = dmmv_fma(x[e], m_of(e), sum.e_m[e]);
+                if constexpr (BETAS) sum.e[e] += x[e];
             }
+        float d[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[e] = x[e] * factor[e];
         if (a.post.kind) {
+            float s3 = 0.0f, s4 = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                d[e] *= k.g0[e];
                 s3 += d[e];
-                s4 = dmmv_fma(d[e], w.m[e], s4);
+                s4 = dmmv_fma(d[e], m_of(e), s4);
             }
             both(1, parity, s3, s4);
             if (a.post.kind == 2) s3 = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) d[e] = rs0 * ((d[e] - s3) - w.m[e] * s4);
+            for (int e = 0; e < 8; ++e) d[e] = rs0 * ((d[e] - s3) - m_of(e) * s4);
         }
-        if (there && col < cols) {
+        if (there && in) {
             if (a.df) store8(a.df + row * a.lddf, col, cols, d);
             if (a.dh) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) d[e] = a.alpha * w.e[e];
+                for (int e = 0; e < 8; ++e) d[e] = a.alpha * x[e];
                 store8(a.dh + row * a.lddh, col, cols, d);
             }
         }
-        // a team's own group ends
-        if (!strips.split && there && ((uint32_t)(row + 1) % a.gate.per == 0 || row == last)) {
-            if (a.dgate && col < cols) store8(a.dgate + ((uint32_t)row / a.gate.per) * a.lddgate, col, cols, sum[4]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum[4][e] = 0.0f;
-            if (row + 1 < r.end) load_gate(a.gate, row + 1, col, cols, gate);
-        }
+        if constexpr (!SPLIT)
+            if (there && ((uint32_t)(row + 1) % a.gate.per == 0 || row == last)) {
+                if (in) end_group(a, row, col, cols, sum, to_gamma, to_beta);
+                if (row + 1 < r.end) load_factor(a, row + 1, col, cols, factor);
+            }
     }
     if (!a.part) return;
-    float* to = a.part + blockIdx.x * 5ll * cols;
-#pragma unroll
-    for (int i = 0; i < 5; ++i) {
-        if (!(a.sums >> i & 1)) continue;
+    float* to = a.part + blockIdx.x * 4ll * cols;
+    auto put = [&](int i, float (&v)[8]) __attribute__((always_inline)) {
         if constexpr (TEAMS > 1)
             for (int w = 1; w < TEAMS; ++w) {
                 __syncthreads();
                 if (team == w)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) join[e * TPR + t] = sum[i][e];
+                    for (int e = 0; e < 8; ++e) join[e * TPR + t] = v[e];
                 __syncthreads();
                 if (team == 0)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) sum[i][e] += join[e * TPR + t];
+                    for (int e = 0; e < 8; ++e) v[e] += join[e * TPR + t];
             }
-        if (team == 0 && col < cols) store8(to + i * cols, col, cols, sum[i]);
+        if (team == 0 && in) store8(to + i * (int64_t)cols, col, cols, v);
+    };
+    if (a.sums & 1) put(0, sum.dy_n);
+    if (a.sums & 2) put(1, sum.dy);
+    if constexpr (SPLIT) {
+        if (a.sums & 4) put(2, sum.e_m);
+        if (a.sums & 8) put(3, sum.e);
+    } else {
+        if (a.sums & 4) put(2, to_gamma);
+        if (a.sums & 8) put(3, to_beta);
     }
 }
 
@@ -478,16 +504,18 @@ __global__ __launch_bounds__(256) void k_residual_norm_grad_sums(int64_t cols, R
 }
 
 // 2048 columns of a strip of rows, one team: the results and the share of the sums over rows
-template <class T>
+template <class T, bool SPLIT>
 __global__ __launch_bounds__(256) void k_residual_norm_grad_apply(int64_t rows, int64_t cols, ResidualGrad<T> a, RowStrips strips,
                                                                   const floatx4* __restrict__ sums) {
     const int64_t col = (blockIdx.y * 256ll + threadIdx.x) * 8;
     if (col >= cols) return;
-    GradVectors k;
-    grad_vectors(a.pre, a.post, col, cols, k);
-    float sum[5][8] = {}, gate[8];
+    float g1[8], factor[8], to_gamma[8], to_beta[8];
+    load_or(a.pre.gamma, 1.0f, col, cols, g1);
+    GradSums sum;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum.dy_n[e] = sum.dy[e] = sum.e_m[e] = sum.e[e] = to_gamma[e] = to_beta[e] = 0.0f;
     const TeamRows r = team_rows(strips, rows, a.gate.per, 0, 1);
-    load_gate(a.gate, min(r.at, rows - 1), col, cols, gate);
+    load_factor(a, min(r.at, rows - 1), col, cols, factor);
     for (int64_t row = r.at; row < r.end; ++row) {
         floatx4 s = {0.0f, 0.0f, 0.0f, 0.0f};
         if (sums) s = sums[row];
@@ -500,9 +528,9 @@ __global__ __launch_bounds__(256) void k_residual_norm_grad_apply(int64_t rows, 
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 n[e] = (n[e] - mu1) * rs1;
-                sum[0][e] = dmmv_fma(x[e], n[e], sum[0][e]);
-                sum[1][e] += x[e];
-                e8[e] = dmmv_fma(rs1, (x[e] * k.g1[e] - s[0]) - n[e] * s[1], e8[e]);
+                sum.dy_n[e] = dmmv_fma(x[e], n[e], sum.dy_n[e]);
+                sum.dy[e] += x[e];
+                e8[e] = dmmv_fma(rs1, (x[e] * g1[e] - s[0]) - n[e] * s[1], e8[e]);
             }
         }
         const float mu0 = a.post.kind == 1 ? a.post_mean[row] : 0.0f, rs0 = a.post.kind ? a.post_rstd[row] : 1.0f;
@@ -510,35 +538,37 @@ __global__ __launch_bounds__(256) void k_residual_norm_grad_apply(int64_t rows, 
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             m[e] = (m[e] - mu0) * rs0;
-            d[e] = gate[e] * e8[e];
-            sum[2][e] = dmmv_fma(d[e], m[e], sum[2][e]);
-            sum[3][e] += d[e];
-            sum[4][e] = dmmv_fma(e8[e], dmmv_fma(m[e], k.g0[e], k.b0[e]), sum[4][e]);
-            if (a.post.kind) d[e] = rs0 * ((d[e] * k.g0[e] - s[2]) - m[e] * s[3]);
+            sum.e_m[e] = dmmv_fma(e8[e], m[e], sum.e_m[e]);
+            sum.e[e] += e8[e];
+            d[e] = e8[e] * factor[e];
+            if (a.post.kind) d[e] = rs0 * ((d[e] - s[2]) - m[e] * s[3]);
             e8[e] *= a.alpha;
         }
         if (a.df) store8(a.df + row * a.lddf, col, cols, d);
         if (a.dh) store8(a.dh + row * a.lddh, col, cols, e8);
-        if (!strips.split && ((uint32_t)(row + 1) % a.gate.per == 0 || row == rows - 1)) {
-            if (a.dgate) store8(a.dgate + ((uint32_t)row / a.gate.per) * a.lddgate, col, cols, sum[4]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum[4][e] = 0.0f;
-            if (row + 1 < r.end) load_gate(a.gate, row + 1, col, cols, gate);
-        }
+        if constexpr (!SPLIT)
+            if ((uint32_t)(row + 1) % a.gate.per == 0 || row == rows - 1) {
+                end_group(a, row, col, cols, sum, to_gamma, to_beta);
+                if (row + 1 < r.end) load_factor(a, row + 1, col, cols, factor);
+            }
     }
     if (!a.part) return;
-    float* to = a.part + blockIdx.x * 5ll * cols;
-#pragma unroll
-    for (int i = 0; i < 5; ++i)
-        if (a.sums >> i & 1) store8(to + i * cols, col, cols, sum[i]);
+    float* to = a.part + blockIdx.x * 4ll * cols;
+    if (a.sums & 1) store8(to, col, cols, sum.dy_n);
+    if (a.sums & 2) store8(to + cols, col, cols, sum.dy);
+    if (a.sums & 4) store8(to + 2 * cols, col, cols, SPLIT ? sum.e_m : to_gamma);
+    if (a.sums & 8) store8(to + 3 * cols, col, cols, SPLIT ? sum.e : to_beta);
 }
 
-// Sums of the workgroups' shares: rows 0 to 3 of the grid the norms' parameters over all of them, row 4 + g the gate of group g over its `each`.
-// 64 columns a workgroup, every 16th share a wavefront, joined in order.
+// Sums of the workgroups' shares: rows 0 to 3 of the grid the norms' parameters over all of them (those of the norm after the block times
+// the gate of each share, where groups are split), row 4 + g the gate of group g over its `each`.  64 columns a workgroup, every 16th share a
+// wavefront, joined in order.
 struct ResidualSums {
-    float* out[4];
+    float* out[4];                       // dgamma, dbeta, dpost_gamma, dpost_beta
     float* dgate;
     int64_t lddgate;
+    const float *gate, *post_gamma, *post_beta;
+    int64_t ldgate;
 };
 __global__ __launch_bounds__(1024) void k_residual_norm_join(const float* __restrict__ part, int64_t n, int64_t each, int64_t cols, int32_t first, ResidualSums o) {
     __shared__ float sh[16][64];
@@ -547,24 +577,38 @@ __global__ __launch_bounds__(1024) void k_residual_norm_join(const float* __rest
     float* out = seg < 4 ? o.out[seg] : o.dgate + g * o.lddgate;
     if (!out) return;                                // (the whole workgroup)
     const int64_t p0 = seg < 4 ? 0 : g * each, p1 = seg < 4 ? n : p0 + each;
-    const float* from = part + min(seg, 4) * cols + j;
-    float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const float *A = part + (seg < 4 ? seg : 2) * cols + j, *B = part + 3 * cols + j;
+    // (a single group's gate once, at the end)
+    const bool gates = seg >= 2 && seg < 4 && o.gate && each > 0, gated = gates && n > each, both = seg >= 4 && o.post_beta;
+    float ga = 1.0f, gb = 0.0f;
+    if (gates && !gated && j < cols) ga = o.gate[j];
+    if (seg >= 4 && j < cols) {
+        if (o.post_gamma) ga = o.post_gamma[j];
+        if (both) gb = o.post_beta[j];
+    }
+    float c[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    auto add = [&](int u, int64_t p) __attribute__((always_inline)) {
+        float v = A[p * 4 * cols];
+        if (gated) v *= o.gate[((uint32_t)p / (uint32_t)each) * o.ldgate + j];
+        if (both) v = dmmv_fma(ga, v, gb * B[p * 4 * cols]);
+        c[u] += v;
+    };
     if (j < cols) {
         int64_t p = p0 + w;
-        for (; p + 48 < p1; p += 64)
+        for (; p + 112 < p1; p += 128)               // eight shares requested together, a chain of sums for each
 #pragma unroll
-            for (int u = 0; u < 4; ++u) c[u] += from[(p + 16 * u) * 5 * cols];
+            for (int u = 0; u < 8; ++u) add(u, p + 16 * u);
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (p + 16 * u < p1) c[u] += from[(p + 16 * u) * 5 * cols];
+        for (int u = 0; u < 8; ++u)
+            if (p + 16 * u < p1) add(u, p + 16 * u);
     }
-    float s = (c[0] + c[1]) + (c[2] + c[3]);
+    float s = ((c[0] + c[1]) + (c[2] + c[3])) + ((c[4] + c[5]) + (c[6] + c[7]));
     sh[w][lane] = s;
     __syncthreads();
     if (w != 0 || j >= cols) return;
 #pragma unroll
     for (int i = 1; i < 16; ++i) s += sh[i][lane];
-    out[j] = s;
+    out[j] = both ? s : s * ga;
 }
 
 // ---- host ---------------------------------------------------------------------------------------
@@ -595,7 +639,7 @@ static RowStrips residual_strips(int64_t rows, int64_t cols, int64_t gate_rows) 
 static size_t residual_sums_bytes(int64_t rows, int64_t cols) { return cols <= RESIDUAL_REGS ? 0 : ((size_t)rows * 16 + 255) / 256 * 256; }
 static size_t residual_workspace(int64_t rows, int64_t cols, int64_t gate_rows) {
     if (rows <= 0 || cols <= 0) return 0;
-    return residual_sums_bytes(rows, cols) + (size_t)residual_strips(rows, cols, gate_rows).n * 5 * cols * 4;
+    return residual_sums_bytes(rows, cols) + (size_t)residual_strips(rows, cols, gate_rows).n * 4 * cols * 4;
 }
 
 template <class T>
@@ -621,17 +665,23 @@ static dmmv_status residual_backward(int64_t rows, int64_t cols, ResidualGrad<T>
     const RowStrips s = residual_strips(rows, cols, a.gate.per);
     a.sums = 0;
     for (int i = 0; i < 4; ++i) a.sums |= (o.out[i] ? 1 : 0) << i;
-    if (s.split && o.dgate) a.sums |= 16;
+    const bool gates = s.split && o.dgate;           // gates' gradients by the join
+    if (gates) a.sums |= o.post_beta ? 12 : 4;
     a.dgate = s.split ? nullptr : o.dgate;
     a.lddgate = o.lddgate;
     a.part = a.sums ? reinterpret_cast<float*>(ws + residual_sums_bytes(rows, cols)) : nullptr;
     if (cols <= RESIDUAL_REGS) {
+        const bool betas = o.out[1] || o.out[3] || (o.dgate && o.post_beta);         // sums of dy or e are wanted
 #define RESIDUAL_GRAD(TPR)                                                                                                       \
-    hipLaunchKernelGGL((k_residual_norm_grad<T, TPR, 512>), dim3((unsigned)s.n), dim3(512), 0, stream, rows, cols, a, s)
-        if (cols <= 512) RESIDUAL_GRAD(64);
-        else if (cols <= 1024) RESIDUAL_GRAD(128);
-        else if (cols <= 2048) RESIDUAL_GRAD(256);
-        else RESIDUAL_GRAD(512);
+    {                                                                                                                            \
+        auto kernel = s.split ? (betas ? k_residual_norm_grad<T, TPR, 512, true, true> : k_residual_norm_grad<T, TPR, 512, true, false>)    \
+                              : (betas ? k_residual_norm_grad<T, TPR, 512, false, true> : k_residual_norm_grad<T, TPR, 512, false, false>); \
+        hipLaunchKernelGGL(kernel, dim3((unsigned)s.n), dim3(512), 0, stream, rows, (int32_t)cols, a, s);                        \
+    }
+        if (cols <= 512) RESIDUAL_GRAD(64)
+        else if (cols <= 1024) RESIDUAL_GRAD(128)
+        else if (cols <= 2048) RESIDUAL_GRAD(256)
+        else RESIDUAL_GRAD(512)
 #undef RESIDUAL_GRAD
         DMMV_LAUNCH_CHECK();
     } else {
@@ -640,11 +690,13 @@ static dmmv_status residual_backward(int64_t rows, int64_t cols, ResidualGrad<T>
             hipLaunchKernelGGL((k_residual_norm_grad_sums<T>), dim3((unsigned)rows), dim3(256), 0, stream, cols, a, sums);
             DMMV_LAUNCH_CHECK();
         }
-        hipLaunchKernelGGL((k_residual_norm_grad_apply<T>), dim3((unsigned)s.n, (unsigned)ceil_div(cols, 2048)), dim3(256), 0, stream, rows, cols, a, s, sums);
+        auto kernel = s.split ? k_residual_norm_grad_apply<T, true> : k_residual_norm_grad_apply<T, false>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)s.n, (unsigned)ceil_div(cols, 2048)), dim3(256), 0, stream, rows, cols, a, s, sums);
         DMMV_LAUNCH_CHECK();
     }
     if (!a.sums) return DMMV_OK;
-    const int first = a.sums & 15 ? 0 : 4, rows_y = (a.sums & 16 ? 4 + (int)groups : 4) - first;
+    const bool parameters = o.out[0] || o.out[1] || o.out[2] || o.out[3];
+    const int first = parameters ? 0 : 4, rows_y = (gates ? 4 + (int)groups : 4) - first;
     hipLaunchKernelGGL(k_residual_norm_join, dim3((unsigned)ceil_div(cols, 64), (unsigned)rows_y), dim3(1024), 0, stream, a.part, s.n, s.each, cols, first, o);
     DMMV_LAUNCH_CHECK();
     return DMMV_OK;
@@ -774,7 +826,7 @@ extern "C" dmmv_status dmmv_residual_norm_backward(int32_t dtype, int64_t rows, 
     const uint32_t per = group_rows(rows, gate != nullptr, gate_rows);
     DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, residual_workspace(rows, cols, per)));
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    const ResidualSums o = {{dgamma, dbeta, dpost_gamma, dpost_beta}, dgate, lddgate};
+    const ResidualSums o = {{dgamma, dbeta, dpost_gamma, dpost_beta}, dgate, lddgate, gate, post ? post->gamma : nullptr, post ? post->beta : nullptr, ldgate};
     if (cols == 0 || (!df && !dh && !dgate && !dpost_gamma && !dpost_beta && !dgamma && !dbeta)) return DMMV_OK;
     if (rows == 0) {                           // sums over no rows; no gates
         hipLaunchKernelGGL(k_residual_norm_join, dim3((unsigned)ceil_div(cols, 64), 4), dim3(1024), 0, s, nullptr, (int64_t)0, (int64_t)0, cols, 0, o);

@@ -869,17 +869,44 @@ class _Norm(C.Structure):
     _fields_ = [("gamma", C.c_void_p), ("beta", C.c_void_p), ("eps", C.c_float), ("rms", C.c_int32)]
 
 
-@dataclass
 class Norm:
-    """A norm of rows: a layer norm, or with rms one without a mean; gamma and beta float32 vectors, None = 1 and 0."""
-    gamma: Optional[torch.Tensor] = None
-    beta: Optional[torch.Tensor] = None
-    eps: float = 1e-5
-    rms: bool = False
+    """A norm of rows: a layer norm, or with rms one without a mean; gamma and beta float32 vectors, None = 1 and 0.  It stands for the
+    vectors' memory: numbers written into that are seen (unless a vector has gaps: it is copied here).  Other vectors are another Norm."""
 
-    def _c(self, cols: int, dev: int, what: str):
-        g, b = _vector(self.gamma, cols, dev, what + ".gamma"), _vector(self.beta, cols, dev, what + ".beta")
-        return _Norm(_addr(g), _addr(b), self.eps, 1 if self.rms else 0), (g, b)
+    __slots__ = ("_gamma", "_beta", "_eps", "_rms", "_cols", "_dev", "_c", "_p")
+
+    def __init__(self, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, eps: float = 1e-5, rms: bool = False):
+        self._cols = self._dev = None
+        kept = []
+        for t, what in ((gamma, "gamma"), (beta, "beta")):
+            if t is not None:
+                if not t.is_cuda:
+                    raise DmmvError(-6, "tensors must live on the GPU")
+                if self._cols is None:
+                    self._dev, self._cols = t.get_device(), t.shape[0] if t.dim() == 1 else -1
+                t = _vector(t.detach(), self._cols, self._dev, what)
+            kept.append(t)
+        self._gamma, self._beta = kept
+        self._eps, self._rms = eps, bool(rms)
+        self._c = _Norm(_addr(self._gamma), _addr(self._beta), eps, 1 if rms else 0)
+        self._p = C.addressof(self._c)
+
+    gamma = property(lambda self: None if self._gamma is None else self._gamma.detach())
+    beta = property(lambda self: None if self._beta is None else self._beta.detach())
+    eps = property(lambda self: self._eps)
+    rms = property(lambda self: self._rms)
+
+
+def _norm_at(n: Optional[Norm], cols: int, dev: int, what: str) -> Optional[int]:
+    """The norm as the library takes it."""
+    if n is None:
+        return None
+    if n._cols is not None:
+        if n._cols != cols:
+            raise DmmvError(-2, f"{what} has vectors of {n._cols} entries, expected {cols}")
+        if n._dev != dev:
+            raise DmmvError(-6, "tensors are on different devices")
+    return n._p
 
 
 @dataclass
@@ -902,16 +929,6 @@ class ResidualNormGradients:
     dpost_beta: Optional[torch.Tensor]
     dgamma: Optional[torch.Tensor]
     dbeta: Optional[torch.Tensor]
-
-
-def _norms(post: Optional[Norm], pre: Optional[Norm], cols: int, dev: int):
-    a, keep_a = post._c(cols, dev, "post") if post is not None else (None, None)
-    b, keep_b = pre._c(cols, dev, "pre") if pre is not None else (None, None)
-    return a, b, (keep_a, keep_b)
-
-
-def _at(c) -> Optional[int]:
-    return None if c is None else C.addressof(c)
 
 
 def _gate(gate: Optional[torch.Tensor], gate_rows: Optional[int], T: int, F: int, dev: int):
@@ -940,19 +957,22 @@ def dmmv_residual_norm(f: torch.Tensor, h: torch.Tensor, post: Optional[Norm] = 
     T, F = f.shape
     dev, on = f.get_device(), f.device
     h = _like(h, f.shape, f.dtype, dev, "h")
-    y = y and pre is not None
-    if q and pre is None:
-        raise DmmvError(-1, "q needs pre")
-    a, b, keep = _norms(post, pre, F, dev)
+    if pre is None:
+        y = False
+        if q:
+            raise DmmvError(-1, "q needs pre")
+    a, b = _norm_at(post, F, dev, "post"), _norm_at(pre, F, dev, "pre")
     g, rows = _gate(gate, gate_rows, T, F, dev)
-    new = functools.partial(torch.empty, dtype=torch.float32, device=on)
-    s = [new(T) if n is not None else None for n in (post, post, pre, pre)]
+    s = torch.empty(4, T, dtype=torch.float32, device=on).unbind(0)
+    post_mean, post_rstd = s[:2] if post is not None else (None, None)
+    mean, rstd = s[2:] if pre is not None else (None, None)
     ov = torch.empty(T, F, dtype=f.dtype, device=on) if stream else None
     oy = torch.empty(T, F, dtype=f.dtype, device=on) if y else None
     oq = _new_block(T, F, 1, torch.uint8, on) if q else None
     _enqueue(dev, load().dmmv_residual_norm, kind, T, F, f.data_ptr(), f.stride(0), h.data_ptr(), h.stride(0), alpha, _addr(g),
-             0 if g is None else g.stride(0), rows, _at(a), _at(b), _addr(ov), F, _addr(oy), F, oq._p if q else None, *map(_addr, s))
-    return ResidualNormResult(ov, oy, oq, *s)
+             0 if g is None else g.stride(0), rows, a, b, _addr(ov), F, _addr(oy), F, oq._p if q else None, _addr(post_mean), _addr(post_rstd),
+             _addr(mean), _addr(rstd))
+    return ResidualNormResult(ov, oy, oq, post_mean, post_rstd, mean, rstd)
 
 
 def dmmv_residual_norm_backward(dy: Optional[torch.Tensor], dv: Optional[torch.Tensor], f: Optional[torch.Tensor], r: ResidualNormResult,
@@ -989,24 +1009,32 @@ def dmmv_residual_norm_backward(dy: Optional[torch.Tensor], dv: Optional[torch.T
         if n is not None and stats[i] is None and not (n.rms and i % 2 == 0):
             raise DmmvError(-1, "a statistic of the forward pass is None")
         stats[i] = None if n is None else _vector(stats[i], T, dev, "a statistic")
-    a, b, keep = _norms(post, pre, F, dev)
+    a, b = _norm_at(post, F, dev, "post"), _norm_at(pre, F, dev, "pre")
     g, rows = _gate(gate, gate_rows, T, F, dev)
-    like = functools.partial(torch.empty, T, F, dtype=first.dtype, device=on)
-    gf, gh = like() if df else None, like() if dh else None
-    gg = torch.empty(g.shape, dtype=torch.float32, device=on) if g is not None and parameters else None
-    of = [torch.empty(F, dtype=torch.float32, device=on) if parameters and t is not None else None
-          for n in (post, pre) for t in ((n.gamma, n.beta) if n is not None else (None, None))]
+    new = torch.empty
+    gf = new(T, F, dtype=first.dtype, device=on) if df else None
+    gh = new(T, F, dtype=first.dtype, device=on) if dh else None
+    gg = dg0 = db0 = dg1 = db1 = None
+    if parameters:
+        vector = lambda t: None if t is None else new(F, dtype=torch.float32, device=on)  # noqa: E731
+        if g is not None:
+            gg = new(g.shape, dtype=torch.float32, device=on)
+        if post is not None:
+            dg0, db0 = vector(post._gamma), vector(post._beta)
+        if pre is not None:
+            dg1, db1 = vector(pre._gamma), vector(pre._beta)
     nbytes = _workspace("dmmv_residual_norm_workspace_bytes", T, F, rows)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=on) if nbytes else None
-    stride = lambda t: 0 if t is None else t.stride(0)  # noqa: E731
-    _enqueue(dev, load().dmmv_residual_norm_backward, kind, T, F, _addr(dy), stride(dy), _addr(dv), stride(dv), _addr(f), stride(f), _addr(v), stride(v),
-             alpha, _addr(g), stride(g), rows, _at(a), _at(b), *map(_addr, stats), _addr(gf), F, _addr(gh), F, _addr(gg), F, *map(_addr, of),
+    ws = new(nbytes, dtype=torch.uint8, device=on) if nbytes else None
+    pm, pr, m, r1 = stats
+    _enqueue(dev, load().dmmv_residual_norm_backward, kind, T, F, _addr(dy), 0 if dy is None else dy.stride(0), _addr(dv), 0 if dv is None else dv.stride(0),
+             _addr(f), 0 if f is None else f.stride(0), _addr(v), 0 if v is None else v.stride(0), alpha, _addr(g), 0 if g is None else g.stride(0), rows,
+             a, b, _addr(pm), _addr(pr), _addr(m), _addr(r1), _addr(gf), F, _addr(gh), F, _addr(gg), F, _addr(dg0), _addr(db0), _addr(dg1), _addr(db1),
              _addr(ws), nbytes)
     if gg is not None:
         if T == 0:
             gg.zero_()
         gg = gg.view(gate.shape)
-    return ResidualNormGradients(gf, gh, gg, *of)
+    return ResidualNormGradients(gf, gh, gg, dg0, db0, dg1, db1)
 
 
 class _Gradient(C.Structure):
