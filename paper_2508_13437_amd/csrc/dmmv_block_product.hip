@@ -866,13 +866,16 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
 // ---- few tokens ------------------------------------------------------------------------------------
 // Up to 64 tokens: the weights are read once, straight into registers in the order of the operands (a lane 32 codes of
 // a row and block, 128 bytes of a row side by side), and nothing else counts.  A workgroup has 16 outputs and
-// 16 MT tokens, its four wavefronts a share of the blocks each, joined in order through the LDS.  U blocks are
-// requested at a time.  One token of 4096 by 11008 outputs: 10.5 us, 4.3 TB/s; 24 tokens of 4096 by 4096: 9.9 us, two thirds of it start,
-// join and end (eight wavefronts a workgroup were no faster).
+// 16 MT tokens, its four wavefronts a share of the blocks each, joined in order through the LDS.  U blocks are on their way at any time
+// (one token of 11008 by 4096 outputs 10.2 us, 13.2 with U of them requested together and waited for together).  One token of 4096 by 11008
+// outputs: 10.6 us, 4.3 TB/s, 14.0 in 8 bits with a pass for those; 24 tokens of 4096 by 4096: 9.6 us, two thirds of it start,
+// join and end (eight wavefronts a workgroup were no faster); 24 of 11008 by 4096 17.6: the tokens, read for every 16 outputs, from the L2.
 template <class T, int MT, bool SCALED, bool WIDE, bool EPI>
 __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
                                                                   const float* __restrict__ bias, ProductOut<T, EPI> out) {
-    constexpr int U = MT >= 4 ? 2 : 4, WAVES = 4;
+    // (BRIEF: a bf16 result that is summed in 32 bits, exponents)
+    constexpr bool BRIEF = SCALED && WIDE && sizeof(T) == 2, RING = SCALED && (!WIDE || BRIEF);
+    constexpr int U = RING ? (MT == 1 ? 6 : MT == 2 ? 5 : 2) : MT >= 4 ? 2 : 4, WAVES = 4;
     __shared__ floatx4 part[WAVES][MT][64];
     const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -896,10 +899,8 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
         uint32_t ew, ex[MT];           // SCALED: exponents
         uint32_t fw[4], fx[MT];        // else: scales of this lane's four outputs, of its tokens, as they are stored
     };
-    auto exponent = [&](const BlockView& q, int64_t row, int b) __attribute__((always_inline)) {
-        return (uint32_t)static_cast<const uint8_t*>(q.scales)[(row >> q.shift) * q.srow + b * q.sblk];
-    };
-    // SCALED: scales that are the same along a row, and their exponents, taken when the first codes have been requested
+    // SCALED: scales that are the same along a row, and their exponents, taken when the first codes have been requested.  A byte is loaded for every
+    // block all the same (of the codes, the same one): a branch around a load makes the compiler wait for all of them.
     float row_w = 1.0f, row_x[MT];
     uint32_t along_w = 127u, along_x[MT];
     if (SCALED && !how.w_blocks) row_w = scale_at(w, orow, 0);
@@ -913,13 +914,16 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
 #pragma unroll
         for (int m = 0; m < MT; ++m) along_x[m] = row_scale(row_x[m]).byte;
     };
+    const uint8_t* pw = how.w_blocks ? static_cast<const uint8_t*>(w.scales) + (orow >> w.shift) * w.srow : w.codes;
+    const uint8_t* px[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) px[m] = how.x_blocks ? static_cast<const uint8_t*>(x.scales) + (trow[m] >> x.shift) * x.srow : x.codes;
+    const int64_t step_w = how.w_blocks ? w.sblk : 0, step_x = how.x_blocks ? x.sblk : 0;
     auto scales = [&](Block& k, int b) __attribute__((always_inline)) {
         if constexpr (SCALED) {
-            if (how.w_blocks) k.ew = exponent(w, orow, b);
+            k.ew = pw[b * step_w];
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                if (how.x_blocks) k.ex[m] = exponent(x, trow[m], b);
-            }
+            for (int m = 0; m < MT; ++m) k.ex[m] = px[m][b * step_x];
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e) k.fw[e] = scale_bits(w, min(o0 + lg * 4 + e, O - 1), b);
@@ -927,7 +931,19 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
             for (int m = 0; m < MT; ++m) k.fx[m] = scale_bits(x, trow[m], b);
         }
     };
+    auto request = [&](Block& k, int b) __attribute__((always_inline)) {      // a whole block
+#pragma unroll
+        for (int h = 0; h < 2; ++h) k.w[h] = *reinterpret_cast<const piece16_any*>(wr + (int64_t)b * 128 + 16 * h);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) k.x[m][h] = *reinterpret_cast<const piece16_any*>(xr[m] + (int64_t)b * 128 + 16 * h);
+        scales(k, b);
+    };
+    // BRIEF: both operands become bf16 with their scales in them, as in the general kernel, and a wavefront that has met exponents which that does
+    // not hold exactly makes its sums again
     ScaleRange met;                                  // as in the general kernel: this lane's scales (24 x 4096 x 4096: 11.5 us, 25 with a scale of 2^-126)
+    bool exact = true;
     auto multiply = [&](auto CAREFUL, Block& k) __attribute__((always_inline)) {
         if constexpr (SCALED) {
             if (!how.w_blocks) k.ew = along_w;
@@ -941,9 +957,25 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
 #pragma unroll
             for (int m = 0; m < MT; ++m) met.take(scale_of(x, k.fx[m]));
         }
+        const intx8 a = words8(k.w[0], k.w[1]);
+        if constexpr (BRIEF && !CAREFUL.value) {
+            exact &= !beyond_bf16(k.ew);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) exact &= !beyond_bf16(k.ex[m]);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const bf16x8_t aw = scaled8(a[2 * s], a[2 * s + 1], k.ew);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    const intx8 b = words8(k.x[m][0], k.x[m][1]);
+                    acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aw, scaled8(b[2 * s], b[2 * s + 1], k.ex[m]), acc[m], 0, 0, 0);
+                }
+            }
+            return;
+        }
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-            const intx8 a = words8(k.w[0], k.w[1]), b = words8(k.x[m][0], k.x[m][1]);
+            const intx8 b = words8(k.x[m][0], k.x[m][1]);
             if constexpr (SCALED && !WIDE) {
                 acc[m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[m], 0, 0, 0, (int)k.ew, 0, (int)k.ex[m]);
             } else {
@@ -972,32 +1004,55 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
 #pragma unroll
             for (int h = 0; h < 2; ++h) k.x[m][h] = chunk_tail(xr[m] + (int64_t)b * 128 + 16 * h, left - 16 * h, b * 128ll + lg * 32 + 16 * h);
         scales(k, b);
-        if (SCALED && b == b0) exponents_along();
         multiply(CAREFUL, k);
     };
 #pragma unroll
     for (int m = 0; m < MT; ++m) acc[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
     int b = b0;
-    for (; b + U <= b1 && b + U <= full; b += U) {
+    if constexpr (RING) {
+        // Whole blocks: U of them are requested before the first is multiplied, and each one's place is taken by the block U further on.
+        const int end = min(b1, full);
         Block k[U];
+        if (b < end) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) request(k[u], min(b + u, end - 1));
+        }
+        exponents_along();
+        for (; b + 2 * U <= end; b += U)
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                multiply(std::false_type{}, k[u]);
+                request(k[u], b + u + U);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        // the last U to 2 U - 1 (or fewer than U altogether)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+            if (b + u < end) multiply(std::false_type{}, k[u]);
+            if (b + u + U < end) request(k[u], b + u + U);
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
-            for (int h = 0; h < 2; ++h) k[u].w[h] = *reinterpret_cast<const piece16_any*>(wr + (int64_t)(b + u) * 128 + 16 * h);
+        for (int u = 0; u < U - 1; ++u) {
+            if (b + u + U < end) multiply(std::false_type{}, k[u]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        b = max(b0, end);
+    } else {
+        for (; b + U <= b1 && b + U <= full; b += U) {
+            Block k[U];
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int u = 0; u < U; ++u) request(k[u], b + u);
+            if (SCALED && b == b0) exponents_along();
 #pragma unroll
-                for (int h = 0; h < 2; ++h) k[u].x[m][h] = *reinterpret_cast<const piece16_any*>(xr[m] + (int64_t)(b + u) * 128 + 16 * h);
-            scales(k[u], b + u);
+            for (int u = 0; u < U; ++u) multiply(std::false_type{}, k[u]);
         }
         if (SCALED && b == b0) exponents_along();
-#pragma unroll
-        for (int u = 0; u < U; ++u) multiply(std::false_type{}, k[u]);
     }
 #pragma unroll 1
     for (; b < b1; ++b) one(std::false_type{}, b);
-    if constexpr (!SCALED)
-        if (!__all(met.moderate())) {
+    if constexpr (!SCALED || BRIEF)
+        if (!__all(BRIEF ? exact : met.moderate())) {
 #pragma unroll
             for (int m = 0; m < MT; ++m) acc[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 1
@@ -1214,7 +1269,7 @@ static dmmv_status product(const ProductPlan& plan, const dmmv_block_matrix* x, 
 
 // The same with what follows it.  8 bits come from the kernel that has whole blocks of 128 outputs of a row (tiles, shares); the others write
 // v in 32 bits, `v` bytes further on in the workspace.  Few tokens in 8 bits are bound by the weights' bytes, so the 16-bit instructions
-// sum them at no cost, in 32 bits: otherwise one number in some 500 goes to the other neighbour on the 8-bit grid.
+// sum them, in 32 bits, for 0.5 us more at one token (4096 by 11008): otherwise one number in some 500 goes to the other neighbour on the 8-bit grid.
 struct LinearPlan {
     ProductPlan product;
     size_t v, bytes;                     // where v begins (0 without one: bytes = product.bytes), all

@@ -617,8 +617,8 @@ def _matrix(t: torch.Tensor, what: str) -> torch.Tensor:
 def _vector(t: Optional[torch.Tensor], n: int, dev: int, what: str) -> Optional[torch.Tensor]:
     """t, a float32 vector of n entries on the device, or a contiguous copy that the caller keeps until its call is enqueued (or
     the call's own results would be allocated in its place)."""
-    if t is None:
-        return None
+    if t is None or (t.dtype is torch.float32 and t.shape == (n,) and t.get_device() == dev and t.is_contiguous()):
+        return t
     if t.dtype != torch.float32:
         raise DmmvError(-3, f"{what} is {t.dtype}, not torch.float32")
     if t.dim() != 1 or t.shape[0] != n:
@@ -809,6 +809,8 @@ def _act_kind(act: Optional[str], none: bool) -> int:
 
 def _like(t: torch.Tensor, shape, dtype: torch.dtype, dev: int, what: str) -> torch.Tensor:
     """t, a matrix of that shape, type and device, with contiguous rows (a copy is the caller's to keep until its call is enqueued)."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+        return t
     t = _matrix(t, what)
     if t.dtype != dtype:
         raise DmmvError(-3, f"{what} is {t.dtype}, not {dtype}")
@@ -897,6 +899,9 @@ class Norm:
     rms = property(lambda self: self._rms)
 
 
+_NO_NORM = Norm()
+
+
 def _norm_at(n: Optional[Norm], cols: int, dev: int, what: str) -> Optional[int]:
     """The norm as the library takes it."""
     if n is None:
@@ -975,6 +980,14 @@ def dmmv_residual_norm(f: torch.Tensor, h: torch.Tensor, post: Optional[Norm] = 
     return ResidualNormResult(ov, oy, oq, post_mean, post_rstd, mean, rstd)
 
 
+def _stats(n: Optional[Norm], mean: Optional[torch.Tensor], rstd: Optional[torch.Tensor], rows: int, dev: int):
+    if n is None:
+        return None, None
+    if rstd is None or (mean is None and not n._rms):
+        raise DmmvError(-1, "a statistic of the forward pass is None")
+    return _vector(mean, rows, dev, "mean"), _vector(rstd, rows, dev, "rstd")
+
+
 def dmmv_residual_norm_backward(dy: Optional[torch.Tensor], dv: Optional[torch.Tensor], f: Optional[torch.Tensor], r: ResidualNormResult,
                                 post: Optional[Norm] = None, pre: Optional[Norm] = None, gate: Optional[torch.Tensor] = None,
                                 gate_rows: Optional[int] = None, alpha: float = 1.0, df: bool = True, dh: bool = True,
@@ -1004,11 +1017,8 @@ def dmmv_residual_norm_backward(dy: Optional[torch.Tensor], dv: Optional[torch.T
         if r.h is None:
             raise DmmvError(-1, "r.h is None")
         v = _like(r.h, first.shape, first.dtype, dev, "r.h")
-    stats = [r.post_mean, r.post_rstd, r.mean, r.rstd]
-    for i, n in enumerate((post, post, pre, pre)):
-        if n is not None and stats[i] is None and not (n.rms and i % 2 == 0):
-            raise DmmvError(-1, "a statistic of the forward pass is None")
-        stats[i] = None if n is None else _vector(stats[i], T, dev, "a statistic")
+    pm, pr = _stats(post, r.post_mean, r.post_rstd, T, dev)
+    m, r1 = _stats(pre, r.mean, r.rstd, T, dev)
     a, b = _norm_at(post, F, dev, "post"), _norm_at(pre, F, dev, "pre")
     g, rows = _gate(gate, gate_rows, T, F, dev)
     new = torch.empty
@@ -1016,16 +1026,15 @@ def dmmv_residual_norm_backward(dy: Optional[torch.Tensor], dv: Optional[torch.T
     gh = new(T, F, dtype=first.dtype, device=on) if dh else None
     gg = dg0 = db0 = dg1 = db1 = None
     if parameters:
-        vector = lambda t: None if t is None else new(F, dtype=torch.float32, device=on)  # noqa: E731
         if g is not None:
             gg = new(g.shape, dtype=torch.float32, device=on)
-        if post is not None:
-            dg0, db0 = vector(post._gamma), vector(post._beta)
-        if pre is not None:
-            dg1, db1 = vector(pre._gamma), vector(pre._beta)
+        p0, p1 = post if post is not None else _NO_NORM, pre if pre is not None else _NO_NORM
+        asked = [p0._gamma is not None, p0._beta is not None, p1._gamma is not None, p1._beta is not None]
+        if any(asked):
+            left = iter(new(sum(asked), F, dtype=torch.float32, device=on).unbind(0))      # (one allocation)
+            dg0, db0, dg1, db1 = [next(left) if k else None for k in asked]
     nbytes = _workspace("dmmv_residual_norm_workspace_bytes", T, F, rows)
     ws = new(nbytes, dtype=torch.uint8, device=on) if nbytes else None
-    pm, pr, m, r1 = stats
     _enqueue(dev, load().dmmv_residual_norm_backward, kind, T, F, _addr(dy), 0 if dy is None else dy.stride(0), _addr(dv), 0 if dv is None else dv.stride(0),
              _addr(f), 0 if f is None else f.stride(0), _addr(v), 0 if v is None else v.stride(0), alpha, _addr(g), 0 if g is None else g.stride(0), rows,
              a, b, _addr(pm), _addr(pr), _addr(m), _addr(r1), _addr(gf), F, _addr(gh), F, _addr(gg), F, _addr(dg0), _addr(db0), _addr(dg1), _addr(db1),

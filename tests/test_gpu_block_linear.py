@@ -138,6 +138,30 @@ def test_eight_bits_of_few_tokens_come_from_sums_in_32_bits(gpu_device):
         assert (got != codes).mean() <= 1e-3 and (q.scales.cpu().numpy() != scales).mean() <= 0.02
 
 
+@pytest.mark.parametrize("T", [1, 20, 64])
+def test_eight_bits_of_few_tokens_with_exponents_at_both_ends(gpu_device, T):
+    """Exponents that bf16 does not hold exactly, in some blocks and rows: sums are exact still, and so are codes and scales."""
+    from paper_2508_13437_amd import dmmv
+
+    O, K = 200, 1100
+    x, w = block(T, K, "e8m0", T, gpu_device, integers=True), block(O, K, "e8m0", 9, gpu_device, integers=True, g=128)
+    gen = torch.Generator().manual_seed(T)
+    low = torch.rand(1, x.scales.shape[1], generator=gen).to(gpu_device) < 0.4          # 2^-126 and 2^-125 against 2^123 and 2^122
+    for far in (low, torch.ones_like(low)):
+        xs, ws = x.scales.int(), w.scales.int()
+        xs, ws = torch.where(far, xs - 125, xs), torch.where(far, ws + 125 - 3, ws - 3)
+        a, b = dmmv.BlockMatrix(x.codes, xs.to(torch.uint8)), dmmv.BlockMatrix(w.codes, ws.to(torch.uint8), 128)
+        want = vals(a) @ vals(b).T
+        q = dmmv.dmmv_block_linear(a, b, y=False, q=True).q
+        codes, scales = plain.quantize(want)
+        got = q.codes.cpu().numpy()
+        assert np.array_equal(np.where(got & 127, got, 0), np.where(codes & 127, codes, 0)) and np.array_equal(q.scales.cpu().numpy(), scales)
+    ws = w.scales.clone()
+    ws[0, 0] = 255                                                                          # NaN: the first 128 outputs
+    q = dmmv.dmmv_block_linear(x, dmmv.BlockMatrix(w.codes, ws, 128), y=False, q=True).q
+    assert bool((q.codes[:, :128] & 127 == 127).all()) and bool((q.codes[:, 128:] & 127 != 127).all())
+
+
 def test_what_is_not_finite_stays_in_its_row(gpu_device):
     from paper_2508_13437_amd import dmmv
 
