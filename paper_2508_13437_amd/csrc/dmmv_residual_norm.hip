@@ -61,31 +61,46 @@ __device__ __forceinline__ void norm8(const float (&x)[8], int64_t col, int64_t 
     for (int e = 0; e < 8; ++e) v[e] = col + e < cols ? dmmv_fma((x[e] - st.mu) * st.rs, g[e], b[e]) : 0.0f;
 }
 
-// v of 8 columns from those of f, its norm, and h
+// v = alpha h + gate p of 8 columns, in the place of h; zero past the row's end
 template <class T>
-__device__ __forceinline__ void residual8(const ResidualIn<T>& in, int64_t row, int64_t col, int64_t cols, Stats st, const float (&f)[8], const float (&h)[8],
-                                          float (&v)[8]) {
-    float p[8];
-    if (in.post.kind) {
-        norm8(f, col, cols, st, in.post, p);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = f[e];
-    }
+__device__ __forceinline__ void combine8(const ResidualIn<T>& in, int64_t col, int64_t cols, const float (&p)[8], const float (&gate)[8], float (&h)[8]) {
     if (in.gate.g) {
-        float g[8];
-        load8(in.gate.g + ((uint32_t)row / in.gate.per) * in.gate.ld, col, cols, g);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = col + e < cols ? dmmv_fma(g[e], p[e], in.alpha * h[e]) : 0.0f;
+        for (int e = 0; e < 8; ++e) h[e] = col + e < cols ? dmmv_fma(gate[e], p[e], in.alpha * h[e]) : 0.0f;
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = col + e < cols ? dmmv_fma(in.alpha, h[e], p[e]) : 0.0f;
+        for (int e = 0; e < 8; ++e) h[e] = col + e < cols ? dmmv_fma(in.alpha, h[e], p[e]) : 0.0f;
     }
+}
+
+__device__ __forceinline__ void put_stats(float* mean, float* rstd, int64_t row, Stats st) {
+    if (mean) mean[row] = st.mu;
+    if (rstd) rstd[row] = st.rs;
+}
+
+// Sum over the TPR threads of a team in every thread, by one barrier: the wavefronts' sums go to `sh` (a place that no wavefront still reads), in turn
+// to the lanes, and a tree over them.
+template <int TPR>
+__device__ __forceinline__ float team_total(float v, float (&sh)[TPR / 64]) {
+    v = wave_sum(v);
+    if constexpr (TPR > 64) {
+        constexpr int WAVES = TPR / 64;
+        static_assert(WAVES <= 16, "sixteen lanes");
+        const int t = threadIdx.x % TPR;
+        if ((t & 63) == 0) sh[t >> 6] = v;
+        __syncthreads();
+        v = sh[t & (WAVES - 1)];
+        v += dpp_mov<DPP_QUAD_XOR1>(v);
+        if constexpr (WAVES > 2) v += dpp_mov<DPP_QUAD_XOR2>(v);
+        if constexpr (WAVES > 4) v += dpp_mov<DPP_ROW_HALF_MIRROR>(v);
+        if constexpr (WAVES > 8) v += dpp_mov<DPP_ROW_MIRROR>(v);
+    }
+    return v;
 }
 
 // mean (of a layer norm) and 1 / sqrt(sum of squared deviations / n + eps) of a row in registers
 template <int TPR, int CH>
-__device__ __forceinline__ Stats stats_of(const float (&v)[CH][8], int t, int64_t cols, const NormView& n, float* sh) {
+__device__ __forceinline__ Stats stats_of(const float (&v)[CH][8], int t, int64_t cols, const NormView& n, float (&sh)[2][TPR / 64]) {
     Stats st = {0.0f, 0.0f};
     const float len = (float)cols;
     float s = 0.0f;
@@ -94,7 +109,7 @@ __device__ __forceinline__ Stats stats_of(const float (&v)[CH][8], int t, int64_
         for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int e = 0; e < 8; ++e) s += v[c][e];
-        st.mu = team_sum<TPR>(s, sh) / len;
+        st.mu = team_total<TPR>(s, sh[0]) / len;
         s = 0.0f;
     }
 #pragma unroll
@@ -104,49 +119,68 @@ __device__ __forceinline__ Stats stats_of(const float (&v)[CH][8], int t, int64_
             const float d = (c * TPR + t) * 8ll + e < cols ? v[c][e] - st.mu : 0.0f;
             s = dmmv_fma(d, d, s);
         }
-    st.rs = 1.0f / __builtin_sqrtf(team_sum<TPR>(s, sh) / len + n.eps);
+    st.rs = 1.0f / __builtin_sqrtf(team_total<TPR>(s, sh[1]) / len + n.eps);
     return st;
 }
 
-__device__ __forceinline__ void put_stats(float* mean, float* rstd, int64_t row, Stats st) {
-    if (mean) mean[row] = st.mu;
-    if (rstd) rstd[row] = st.rs;
+__device__ __forceinline__ void load_or(const float* __restrict__ p, float value, int64_t col, int64_t cols, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = value;
+    if (p) load8(p, col, cols, v);
+}
+__device__ __forceinline__ void load_gate(const GateView& gate, int64_t row, int64_t col, int64_t cols, float (&g)[8]) {
+    load_or(gate.g ? gate.g + ((uint32_t)row / gate.per) * gate.ld : nullptr, 1.0f, col, cols, g);
 }
 
-// TPR threads a row, CH chunks of 8 TPR columns in registers.
+// TPR threads a row, CH chunks of 8 TPR columns in registers.  The gammas and the gate are requested with the row, so that no load waits for the sums.
 template <class T, int TPR, int CH>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_residual_norm(int64_t rows, int64_t cols, ResidualIn<T> in, ResidualOut<T> o) {
-    __shared__ float sh[TPR / 64];
-    constexpr int TEAMS = TPR < 256 ? 256 / TPR : 1;
+__global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void k_residual_norm(int64_t rows, int64_t cols, ResidualIn<T> in, ResidualOut<T> o) {
+    __shared__ float sh[2][2][TPR / 64];
+    constexpr int TEAMS = TPR == 64 ? 4 : 1;
     const int team = threadIdx.x / TPR, t = threadIdx.x % TPR;
     const int64_t row = blockIdx.x * (int64_t)TEAMS + team;
     if (row >= rows) return;                 // whole wavefronts; with TPR > 64 there is one team and none leaves
-    float f[CH][8], v[CH][8];
+    float f[CH][8], v[CH][8], g0[CH][8], gate[CH][8], g1[CH][8];
 #pragma unroll
     for (int c = 0; c < CH; ++c) load8(in.f + row * in.ldf, (c * TPR + t) * 8ll, cols, f[c]);
 #pragma unroll
     for (int c = 0; c < CH; ++c) load8(in.h + row * in.ldh, (c * TPR + t) * 8ll, cols, v[c]);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int64_t col = (c * TPR + t) * 8ll;
+        load_or(in.post.gamma, 1.0f, col, cols, g0[c]);
+        load_gate(in.gate, row, col, cols, gate[c]);
+        load_or(in.pre.gamma, 1.0f, col, cols, g1[c]);
+    }
     Stats st = {0.0f, 0.0f};
     if (in.post.kind) {
-        st = stats_of<TPR, CH>(f, t, cols, in.post, sh);
+        st = stats_of<TPR, CH>(f, t, cols, in.post, sh[0]);
         if (t == 0) put_stats(o.post_mean, o.post_rstd, row, st);
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int64_t col = (c * TPR + t) * 8ll;
-        residual8(in, row, col, cols, st, f[c], v[c], v[c]);
+        if (in.post.kind) {
+            float b[8];
+            load_or(in.post.beta, 0.0f, col, cols, b);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[c][e] = dmmv_fma((f[c][e] - st.mu) * st.rs, g0[c][e], b[e]);
+        }
+        combine8(in, col, cols, f[c], gate[c], v[c]);
         if (o.h) store8(o.h + row * o.ldh, col, cols, v[c]);
     }
     if (!in.pre.kind) return;
-    st = stats_of<TPR, CH>(v, t, cols, in.pre, sh);
+    st = stats_of<TPR, CH>(v, t, cols, in.pre, sh[1]);
     if (t == 0) put_stats(o.mean, o.rstd, row, st);
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int64_t col = (c * TPR + t) * 8ll;
-        float w[8];
-        norm8(v[c], col, cols, st, in.pre, w);
-        if (o.y) store8(o.y + row * o.ldy, col, cols, w);
-        if (o.has_q) put_q<T>(o.q, row, col, cols, w);
+        float b[8];
+        load_or(in.pre.beta, 0.0f, col, cols, b);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[c][e] = col + e < cols ? dmmv_fma((v[c][e] - st.mu) * st.rs, g1[c][e], b[e]) : 0.0f;
+        if (o.y) store8(o.y + row * o.ldy, col, cols, v[c]);
+        if (o.has_q) put_q<T>(o.q, row, col, cols, v[c]);
     }
 }
 
@@ -158,10 +192,16 @@ __global__ __launch_bounds__(1024) void k_residual_norm_wide(int64_t cols, Resid
     const float len = (float)cols;
     Stats st = {0.0f, 0.0f}, sv = {0.0f, 0.0f};
     auto value = [&](int64_t col, float (&v)[8]) __attribute__((always_inline)) {
-        float f[8], h[8];
+        float f[8], p[8], gate[8];
         load8(in.f + row * in.ldf, col, cols, f);
-        load8(in.h + row * in.ldh, col, cols, h);
-        residual8(in, row, col, cols, st, f, h, v);
+        load8(in.h + row * in.ldh, col, cols, v);
+        load_gate(in.gate, row, col, cols, gate);
+        if (!in.post.kind) {
+            combine8(in, col, cols, f, gate, v);
+            return;
+        }
+        norm8(f, col, cols, st, in.post, p);
+        combine8(in, col, cols, p, gate, v);
     };
     auto walk = [&](const NormView& n, Stats& s, auto get) __attribute__((always_inline)) {
         float a = 0.0f;
@@ -254,14 +294,6 @@ __device__ __forceinline__ TeamRows team_rows(const RowStrips& s, int64_t rows, 
 struct GradSums {
     float dy_n[8], dy[8], e_m[8], e[8];
 };
-__device__ __forceinline__ void load_or(const float* __restrict__ p, float value, int64_t col, int64_t cols, float (&v)[8]) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = value;
-    if (p) load8(p, col, cols, v);
-}
-__device__ __forceinline__ void load_gate(const GateView& gate, int64_t row, int64_t col, int64_t cols, float (&g)[8]) {
-    load_or(gate.g ? gate.g + ((uint32_t)row / gate.per) * gate.ld : nullptr, 1.0f, col, cols, g);
-}
 // a group of a team's own has ended: its gate's gradient, and what it adds to those of the norm after the block
 template <class T>
 __device__ __forceinline__ void end_group(const ResidualGrad<T>& a, int64_t row, int64_t col, int64_t cols, GradSums& s, float (&to_gamma)[8], float (&to_beta)[8]) {
@@ -291,7 +323,7 @@ __device__ __forceinline__ void load_factor(const ResidualGrad<T>& a, int64_t ro
     for (int e = 0; e < 8; ++e) f[e] *= g[e];
 }
 
-// Rows of up to 4096 columns: a team of TPR threads holds a row in registers between the two pairs of sums, and keeps its columns' share of the
+// Rows of up to 4096 columns (8192 in bf16): a team of TPR threads holds a row in registers between the two pairs of sums, and keeps its columns' share of the
 // sums over rows; the teams of a workgroup join theirs at the end, in order, in the LDS.  Everything is read once, and the next row is requested before
 // this one's sums are waited for.  SPLIT: a workgroup has rows of one gate group only.  BETAS: sum dy or sum e are wanted.
 template <class T, int TPR, int THREADS, bool SPLIT, bool BETAS>
@@ -341,7 +373,8 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && SPLIT ? 4 : 2) void k_re
             s2 = w.y + dpp_mov<DPP_QUAD_XOR1>(w.y);
             if constexpr (WAVES > 2) { s1 += dpp_mov<DPP_QUAD_XOR2>(s1); s2 += dpp_mov<DPP_QUAD_XOR2>(s2); }
             if constexpr (WAVES > 4) { s1 += dpp_mov<DPP_ROW_HALF_MIRROR>(s1); s2 += dpp_mov<DPP_ROW_HALF_MIRROR>(s2); }
-            static_assert(WAVES <= 8, "eight lanes");
+            if constexpr (WAVES > 8) { s1 += dpp_mov<DPP_ROW_MIRROR>(s1); s2 += dpp_mov<DPP_ROW_MIRROR>(s2); }
+            static_assert(WAVES <= 16, "sixteen lanes");
         }
         s1 *= inv_n;
         s2 *= inv_n;
@@ -612,16 +645,22 @@ __global__ __launch_bounds__(1024) void k_residual_norm_join(const float* __rest
 }
 
 // ---- host ---------------------------------------------------------------------------------------
-constexpr int64_t RESIDUAL_REGS = 4096;
-static int residual_team(int64_t cols) { return cols <= 512 ? 64 : cols <= 1024 ? 128 : cols <= 2048 ? 256 : 512; }
+static bool residual_regs(int64_t cols, bool bf16) { return cols <= (bf16 ? 8192 : 4096); }
+static int residual_team(int64_t cols) { return cols <= 512 ? 64 : cols <= 1024 ? 128 : cols <= 2048 ? 256 : cols <= 4096 ? 512 : 1024; }
 
-// Rows per workgroup: some 512 workgroups; groups that are longer are split, more than 1024 groups go to teams whole.
-static RowStrips residual_strips(int64_t rows, int64_t cols, int64_t gate_rows) {
-    const bool regs = cols <= RESIDUAL_REGS;
-    const int64_t want = regs ? 512 : (1024 / ceil_div(cols, 2048) > 1 ? 1024 / ceil_div(cols, 2048) : 1), teams = regs ? 512 / residual_team(cols) : 1;
+// Gradients: the threads of a workgroup (4096 x 4096 bf16: 51 us with 512 workgroups of 512, 52.6 with 256 of 1024, which have fewer shares to join
+// but wait for one another).
+static int residual_threads(int64_t cols) { return residual_team(cols) == 1024 ? 1024 : 512; }
+
+// Rows per workgroup: some 256 of 1024 threads or 512 of fewer; groups that are longer are split, more than 1024 groups go to teams whole.
+static RowStrips residual_strips(int64_t rows, int64_t cols, int64_t gate_rows, bool bf16) {
     const int64_t groups = ceil_div(rows, gate_rows);
     RowStrips s;
     s.split = groups <= 1024;
+    const bool regs = residual_regs(cols, bf16);
+    const int threads = residual_threads(cols);
+    const int64_t want = regs ? (threads == 1024 ? 256 : 512) : (1024 / ceil_div(cols, 2048) > 1 ? 1024 / ceil_div(cols, 2048) : 1);
+    const int64_t teams = regs ? threads / residual_team(cols) : 1;
     if (s.split) {
         int64_t each = want / groups, most = ceil_div(gate_rows, teams);
         if (each < 1) each = 1;
@@ -636,21 +675,27 @@ static RowStrips residual_strips(int64_t rows, int64_t cols, int64_t gate_rows) 
     }
     return s;
 }
-static size_t residual_sums_bytes(int64_t rows, int64_t cols) { return cols <= RESIDUAL_REGS ? 0 : ((size_t)rows * 16 + 255) / 256 * 256; }
+static size_t residual_sums_bytes(int64_t rows, int64_t cols, bool bf16) { return residual_regs(cols, bf16) ? 0 : ((size_t)rows * 16 + 255) / 256 * 256; }
+static size_t residual_workspace_of(int64_t rows, int64_t cols, int64_t gate_rows, bool bf16) {
+    return residual_sums_bytes(rows, cols, bf16) + (size_t)residual_strips(rows, cols, gate_rows, bf16).n * 4 * cols * 4;
+}
 static size_t residual_workspace(int64_t rows, int64_t cols, int64_t gate_rows) {
     if (rows <= 0 || cols <= 0) return 0;
-    return residual_sums_bytes(rows, cols) + (size_t)residual_strips(rows, cols, gate_rows).n * 4 * cols * 4;
+    const size_t a = residual_workspace_of(rows, cols, gate_rows, false), b = residual_workspace_of(rows, cols, gate_rows, true);
+    return a > b ? a : b;
 }
 
 template <class T>
 static dmmv_status residual_forward(int64_t rows, int64_t cols, const ResidualIn<T>& in, const ResidualOut<T>& o, hipStream_t stream) {
 #define RESIDUAL_LAUNCH(TPR, CH)                                                                                       \
-    hipLaunchKernelGGL((k_residual_norm<T, TPR, CH>), dim3((unsigned)ceil_div(rows, TPR < 256 ? 256 / TPR : 1)),       \
-                       dim3(TPR < 256 ? 256 : TPR), 0, stream, rows, cols, in, o)
+    hipLaunchKernelGGL((k_residual_norm<T, TPR, CH>), dim3((unsigned)ceil_div(rows, TPR == 64 ? 4 : 1)),               \
+                       dim3(TPR == 64 ? 256 : TPR), 0, stream, rows, cols, in, o)
+    // 8 columns a thread as long as a workgroup has 512: 4096 x 4096 bf16 with both norms and a gate 27.7 us, 30.7 with 256 threads of 16, the 8-bit
+    // result alone 26.6 and 30.0; but 2048 x 8192 35 us with 1024 threads of 8, 29.6 with 512 of 16
     if (cols <= 512) RESIDUAL_LAUNCH(64, 1);
-    else if (cols <= 1024) RESIDUAL_LAUNCH(64, 2);
+    else if (cols <= 1024) RESIDUAL_LAUNCH(128, 1);
     else if (cols <= 2048) RESIDUAL_LAUNCH(256, 1);
-    else if (cols <= 4096) RESIDUAL_LAUNCH(256, 2);
+    else if (cols <= 4096) RESIDUAL_LAUNCH(512, 1);
     else if (cols <= 8192) RESIDUAL_LAUNCH(512, 2);
     else if (cols <= 16384) RESIDUAL_LAUNCH(1024, 2);
     else hipLaunchKernelGGL((k_residual_norm_wide<T>), dim3((unsigned)rows), dim3(1024), 0, stream, cols, in, o);
@@ -662,26 +707,31 @@ static dmmv_status residual_forward(int64_t rows, int64_t cols, const ResidualIn
 template <class T>
 static dmmv_status residual_backward(int64_t rows, int64_t cols, ResidualGrad<T> a, const ResidualSums& o, char* ws, hipStream_t stream) {
     const int64_t groups = ceil_div(rows, (int64_t)a.gate.per);
-    const RowStrips s = residual_strips(rows, cols, a.gate.per);
+    constexpr bool bf16 = sizeof(T) == 2;
+    const RowStrips s = residual_strips(rows, cols, a.gate.per, bf16);
     a.sums = 0;
     for (int i = 0; i < 4; ++i) a.sums |= (o.out[i] ? 1 : 0) << i;
     const bool gates = s.split && o.dgate;           // gates' gradients by the join
     if (gates) a.sums |= o.post_beta ? 12 : 4;
     a.dgate = s.split ? nullptr : o.dgate;
     a.lddgate = o.lddgate;
-    a.part = a.sums ? reinterpret_cast<float*>(ws + residual_sums_bytes(rows, cols)) : nullptr;
-    if (cols <= RESIDUAL_REGS) {
+    a.part = a.sums ? reinterpret_cast<float*>(ws + residual_sums_bytes(rows, cols, bf16)) : nullptr;
+    if (residual_regs(cols, bf16)) {
         const bool betas = o.out[1] || o.out[3] || (o.dgate && o.post_beta);         // sums of dy or e are wanted
-#define RESIDUAL_GRAD(TPR)                                                                                                       \
-    {                                                                                                                            \
-        auto kernel = s.split ? (betas ? k_residual_norm_grad<T, TPR, 512, true, true> : k_residual_norm_grad<T, TPR, 512, true, false>)    \
-                              : (betas ? k_residual_norm_grad<T, TPR, 512, false, true> : k_residual_norm_grad<T, TPR, 512, false, false>); \
-        hipLaunchKernelGGL(kernel, dim3((unsigned)s.n), dim3(512), 0, stream, rows, (int32_t)cols, a, s);                        \
-    }
-        if (cols <= 512) RESIDUAL_GRAD(64)
-        else if (cols <= 1024) RESIDUAL_GRAD(128)
-        else if (cols <= 2048) RESIDUAL_GRAD(256)
-        else RESIDUAL_GRAD(512)
+        auto launch = [&](auto kernel, int threads) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)s.n), dim3((unsigned)threads), 0, stream, rows, (int32_t)cols, a, s);
+        };
+#define RESIDUAL_SPLIT(TPR, THREADS) \
+    betas ? launch(k_residual_norm_grad<T, TPR, THREADS, true, true>, THREADS) : launch(k_residual_norm_grad<T, TPR, THREADS, true, false>, THREADS);
+#define RESIDUAL_GRAD(TPR, THREADS)                                                              \
+    if (s.split) RESIDUAL_SPLIT(TPR, THREADS)                                                    \
+    else launch(k_residual_norm_grad<T, TPR, THREADS, false, true>, THREADS);
+        if (cols <= 512) { RESIDUAL_GRAD(64, 512) }
+        else if (cols <= 1024) { RESIDUAL_GRAD(128, 512) }
+        else if (cols <= 2048) { RESIDUAL_GRAD(256, 512) }
+        else if (cols <= 4096) { RESIDUAL_GRAD(512, 512) }
+        else if constexpr (bf16) { RESIDUAL_GRAD(1024, 1024) }
+#undef RESIDUAL_SPLIT
 #undef RESIDUAL_GRAD
         DMMV_LAUNCH_CHECK();
     } else {
