@@ -2,7 +2,7 @@
 //
 // Both passes are bound by memory.  The tensors' places come with the kernel's arguments, LIST of them a launch, so a call copies nothing to the
 // device and can be captured.  A tensor is cut into chunks of 8192 numbers, 2048 where there are few (rows with gaps into pieces of a row), and
-// a workgroup has a run of consecutive chunks.  Squares are summed in 64 bits: those of all 32-bit numbers are there, and no order of summing matters to 32 bits.
+// a workgroup has a run of consecutive chunks.  Short rows with gaps come several to a chunk, number by number.  Squares are summed in 64 bits: those of all 32-bit numbers are there, and no order of summing matters to 32 bits.
 #include <algorithm>
 #include <new>
 
@@ -11,12 +11,14 @@
 namespace dmmv {
 
 constexpr int LIST = 64, GROUPS = 1024;              // tensors a launch, most partial sums a launch
+constexpr int SHORT = 512;                           // columns of rows that come several to a chunk
 constexpr int PIECE = 2048;                          // numbers that 256 threads take at a time; a chunk is one of them, or four
 
 struct TensorPlace {
     const void* in;
     void* out;
     int64_t cols, ld, ldo;               // one row, if the rows have no gaps
+    uint32_t rows, many;                 // rows a chunk, 0: a chunk is a piece of a row
     uint32_t first;                      // chunks of the tensors before
     uint16_t in_bf16, out_bf16;
 };
@@ -25,11 +27,12 @@ struct TensorList {
     int32_t count;
     uint32_t chunks;
 };
-static_assert(sizeof(TensorList) <= 3584, "with the other arguments below 4 KB");
+static_assert(sizeof(TensorList) <= 3600, "with the other arguments below 4 KB");
 
-// The workgroup's chunks of CHUNK numbers, in order or from the last: f(tensor, row, first column, columns of the chunk)
-template <int CHUNK, bool BACK, class F>
-__device__ __forceinline__ void for_chunks(const TensorList& l, F f) {
+// The workgroup's chunks of CHUNK numbers, in order or from the last: piece(tensor, row, first column, columns of the chunk), or for short rows
+// one(tensor, row, column) for each of this thread's numbers
+template <int CHUNK, bool BACK, class F, class G>
+__device__ __forceinline__ void for_chunks(const TensorList& l, F piece, G one) {
     const uint32_t a = (uint32_t)((uint64_t)l.chunks * blockIdx.x / gridDim.x), b = (uint32_t)((uint64_t)l.chunks * (blockIdx.x + 1) / gridDim.x);
     if (a >= b) return;
     int at = 0, hi = l.count - 1;                            // the last tensor that begins at or before the first chunk to take
@@ -46,9 +49,18 @@ __device__ __forceinline__ void for_chunks(const TensorList& l, F f) {
             while (at + 1 < l.count && l.t[at + 1].first <= c) ++at;
         }
         const TensorPlace& t = l.t[at];
-        const uint32_t pieces = (uint32_t)((t.cols + CHUNK - 1) / CHUNK), i = c - t.first, row = i / pieces;
-        const int64_t col = (int64_t)(i - row * pieces) * CHUNK;
-        f(t, (int64_t)row, col, (int)min((int64_t)CHUNK, t.cols - col));
+        const uint32_t i = c - t.first;
+        if (t.many) {
+            const uint32_t row0 = i * t.many, cols = (uint32_t)t.cols, numbers = min(t.many, t.rows - row0) * cols;
+            for (uint32_t k = threadIdx.x; k < numbers; k += 256) {
+                const uint32_t r = k / cols;
+                one(t, (int64_t)(row0 + r), k - r * cols);
+            }
+        } else {
+            const uint32_t pieces = (uint32_t)((t.cols + CHUNK - 1) / CHUNK), row = i / pieces;
+            const int64_t col = (int64_t)(i - row * pieces) * CHUNK;
+            piece(t, (int64_t)row, col, (int)min((int64_t)CHUNK, t.cols - col));
+        }
     }
 }
 
@@ -75,14 +87,21 @@ __device__ __forceinline__ void add_squares(const T* __restrict__ p, int n, doub
     }
 }
 
+__device__ __forceinline__ float value_at(const TensorPlace& t, int64_t at) {
+    return t.in_bf16 ? value_of(static_cast<const bf16_t*>(t.in)[at]) : static_cast<const float*>(t.in)[at];
+}
+
 // part[workgroup] = sum of the squares of its chunks.  360 M numbers in 32 bits: 243 us, 5.9 TB/s.
 template <int CHUNK>
-__global__ __launch_bounds__(256) void k_gradient_squares(TensorList l, double* __restrict__ part) {
+__global__ __launch_bounds__(256, 4) void k_gradient_squares(TensorList l, double* __restrict__ part) {
     __shared__ double sh[4];
     double s[2] = {0.0, 0.0};
     for_chunks<CHUNK, false>(l, [&](const TensorPlace& t, int64_t row, int64_t col, int n) {
         if (t.in_bf16) add_squares<CHUNK>(static_cast<const bf16_t*>(t.in) + row * t.ld + col, n, s);
         else add_squares<CHUNK>(static_cast<const float*>(t.in) + row * t.ld + col, n, s);
+    }, [&](const TensorPlace& t, int64_t row, uint32_t col) {
+        const double v = value_at(t, row * t.ld + col);
+        s[0] = __builtin_fma(v, v, s[0]);
     });
     const double v = group_sum(s[0] + s[1], sh);
     if (threadIdx.x == 0) part[blockIdx.x] = v;
@@ -203,6 +222,10 @@ __global__ __launch_bounds__(256) void k_gradient_scale(TensorList l, const doub
         bf16_t* bo = static_cast<bf16_t*>(t.out) + row * t.ldo + col;
         if (t.in_bf16) t.out_bf16 ? scale_chunk<CHUNK>(b, bo, n, c, rest) : scale_chunk<CHUNK>(b, fo, n, c, rest);
         else t.out_bf16 ? scale_chunk<CHUNK>(f, bo, n, c, rest) : scale_chunk<CHUNK>(f, fo, n, c, rest);
+    }, [&](const TensorPlace& t, int64_t row, uint32_t col) {
+        const float v = value_at(t, row * t.ld + col) * c * rest;
+        if (t.out_bf16) put_y(static_cast<bf16_t*>(t.out) + row * t.ldo + col, v);
+        else put_y(static_cast<float*>(t.out) + row * t.ldo + col, v);
     });
 }
 
@@ -272,7 +295,9 @@ static dmmv_status for_lists(int64_t count, const dmmv_gradient* g, const dmmv_g
     for (int64_t i = 0; i < count; ++i) {
         if (nothing(g[i])) continue;
         const bool whole = no_gaps(g[i]) && (!out || no_gaps(out[i]));
-        const int64_t rows = whole ? 1 : g[i].rows, cols = whole ? g[i].rows * g[i].cols : g[i].cols, chunks = rows * ceil_div(cols, chunk);
+        const int64_t rows = whole ? 1 : g[i].rows, cols = whole ? g[i].rows * g[i].cols : g[i].cols;
+        const int64_t many = !whole && cols <= SHORT ? PIECE / cols : 0;
+        const int64_t chunks = many ? ceil_div(rows, many) : rows * ceil_div(cols, chunk);
         if (chunks > INT32_MAX) return fail(DMMV_ERR_SHAPE, "gradient %lld: more pieces than a launch takes", (long long)i);
         if (l.count == LIST || l.chunks + (uint64_t)chunks > INT32_MAX) {
             DMMV_TRY(f(l, k++));
@@ -285,6 +310,8 @@ static dmmv_status for_lists(int64_t count, const dmmv_gradient* g, const dmmv_g
         t.cols = cols;
         t.ld = whole ? cols : g[i].ld;
         t.ldo = whole ? cols : out ? out[i].ld : 0;
+        t.rows = (uint32_t)rows;
+        t.many = (uint32_t)many;
         t.first = l.chunks;
         t.in_bf16 = g[i].dtype == DMMV_BF16;
         t.out_bf16 = out && out[i].dtype == DMMV_BF16;
@@ -306,15 +333,12 @@ static dmmv_status squares(int64_t count, const dmmv_gradient* g, double* part, 
     });
 }
 
-// every list has LIST tensors but the last, or its chunks were too many
-static size_t gradient_workspace(int64_t count, const dmmv_gradient* g) {
-    size_t bytes = 0;
-    if (for_lists(count, g, nullptr, chunk_of(count, g), [&](const TensorList& l, int32_t) -> dmmv_status {
-            bytes += std::min<uint32_t>(l.chunks, GROUPS) * sizeof(double);
-            return DMMV_OK;
-        }) != DMMV_OK)
-        return 0;
-    return bytes;
+static dmmv_status gradient_workspace(int64_t count, const dmmv_gradient* g, size_t& bytes) {
+    bytes = 0;
+    return for_lists(count, g, nullptr, chunk_of(count, g), [&](const TensorList& l, int32_t) -> dmmv_status {
+        bytes += std::min<uint32_t>(l.chunks, GROUPS) * sizeof(double);
+        return DMMV_OK;
+    });
 }
 
 }  // namespace dmmv
@@ -322,14 +346,16 @@ static size_t gradient_workspace(int64_t count, const dmmv_gradient* g) {
 using namespace dmmv;
 
 extern "C" size_t dmmv_gradient_workspace_bytes(int64_t count, const dmmv_gradient* gradients) {
-    if (check_gradients(count, gradients, "gradients") != DMMV_OK) return 0;
-    return gradient_workspace(count, gradients);
+    size_t bytes = 0;
+    return check_gradients(count, gradients, "gradients") == DMMV_OK && gradient_workspace(count, gradients, bytes) == DMMV_OK ? bytes : 0;
 }
 
 extern "C" dmmv_status dmmv_gradient_norm(int64_t count, const dmmv_gradient* gradients, float* norm, void* workspace, size_t workspace_bytes, void* hip_stream) {
     DMMV_TRY(check_gradients(count, gradients, "gradients"));
     DMMV_TRY(layer_check_vector(norm, true, "norm"));
-    DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, gradient_workspace(count, gradients)));
+    size_t need = 0;
+    DMMV_TRY(gradient_workspace(count, gradients, need));
+    DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, need));
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     int32_t parts = 0;
     DMMV_TRY(squares(count, gradients, static_cast<double*>(workspace), parts, s));
@@ -353,12 +379,15 @@ extern "C" dmmv_status dmmv_gradient_clip(int64_t count, const dmmv_gradient* gr
     DMMV_TRY(layer_check_vector(given, false, "given"));
     DMMV_TRY(layer_check_vector(norm, false, "norm"));
     DMMV_TRY(check_apart(count, out ? out : gradients));
-    if (!given) DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, gradient_workspace(count, gradients)));
+    size_t need = 0;
+    DMMV_TRY(gradient_workspace(count, gradients, need));                // (refuses what the launches would)
+    if (!given) DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, need));
+    const int chunk = chunk_of(count, gradients);
+    if (out) DMMV_TRY(for_lists(count, gradients, out, chunk, [](const TensorList&, int32_t) -> dmmv_status { return DMMV_OK; }));
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     double* part = static_cast<double*>(workspace);
     int32_t parts = 0, lists = 0;
     if (!given) DMMV_TRY(squares(count, gradients, part, parts, s));
-    const int chunk = chunk_of(count, gradients);
     DMMV_TRY(for_lists(count, gradients, out ? out : gradients, chunk, [&](const TensorList& l, int32_t k) -> dmmv_status {
         hipLaunchKernelGGL(chunk == PIECE ? k_gradient_scale<PIECE> : k_gradient_scale<4 * PIECE>, dim3((unsigned)std::min<uint32_t>(l.chunks, GROUPS)), dim3(256), 0, s, l, part, parts, given, max_norm, eps,
                            (int32_t)!out, k == 0 ? norm : nullptr);

@@ -244,6 +244,24 @@ def test_rows_with_gaps_and_empty_ones(gpu_device, T, O, K):
             assert bool((rest == v[T, -1]).all())
 
 
+@pytest.mark.parametrize("T,O,K", [(3, 300, 256), (66, 300, 200), (300, 400, 1024), (70, 300, 4096)])
+def test_scales_of_32_bits_and_blocks_first(gpu_device, T, O, K):
+    """Through the C entry: the scales of the 8-bit result as floats, stored block by block."""
+    from paper_2508_13437_amd import dmmv
+
+    lib, nb = dmmv.load(), -(-O // 128)
+    x, w, bias, _ = operands(T, O, K, "e8m0", "e8m0", gpu_device, 128)
+    want = dmmv.dmmv_block_linear(x, w, bias, "gelu", y=False, q=True).q
+    codes = torch.empty(T, O, dtype=torch.uint8, device=gpu_device)
+    scales = torch.empty(nb, T + 3, dtype=torch.float32, device=gpu_device)
+    q = dmmv._BlockMatrix(T, O, codes.data_ptr(), O, scales.data_ptr(), 1, T + 3, dmmv.DMMV_F32, 1)
+    n = lib.dmmv_block_linear_workspace_for(x._p, w._p, dmmv.DMMV_BF16, 1)
+    ws = torch.empty(n + 1, dtype=torch.uint8, device=gpu_device)
+    assert lib.dmmv_block_linear(x._p, w._p, bias.data_ptr(), 2, None, 0, dmmv.DMMV_BF16, None, 0, C.addressof(q), None, 0, ws.data_ptr(), n,
+                                 torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(codes, want.codes) and np.array_equal(scales[:, :T].t().cpu().numpy(), plain.scale_values(want.scales.cpu().numpy()))
+
+
 def test_refusals(gpu_device):
     from paper_2508_13437_amd import dmmv
 

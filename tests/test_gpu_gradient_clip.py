@@ -91,6 +91,24 @@ def test_places_with_gaps_and_other_orders(gpu_device):
         check(ts, out, n, 0.5, 1e-6)
 
 
+@pytest.mark.parametrize("rows,cols,gap", [(1, 5, 3), (1000, 1, 1), (70000, 1, 2), (3000, 7, 1), (300, 511, 2), (300, 512, 1), (300, 513, 1), (5, 9000, 11)])
+def test_short_and_long_rows_with_gaps(gpu_device, rows, cols, gap):
+    """Several rows to a chunk, a row to a chunk, several chunks to a row; what lies between stays."""
+    from paper_2508_13437_amd import dmmv
+
+    for types in ((F32, F32), (BF16, F32), (F32, BF16), (BF16, BF16)):
+        g = torch.Generator().manual_seed(rows)
+        whole = torch.randn(rows, cols + gap, generator=g).to(types[0]).to(gpu_device)
+        t, keep = whole[:, gap:], whole.clone()
+        out = torch.full((rows, cols + 2), 7.0, dtype=types[1], device=gpu_device)
+        n = dmmv.dmmv_gradient_clip([t], 0.3, out=[out[:, 1:cols + 1]])
+        check([t], [out[:, 1:cols + 1]], n, 0.3, 1e-6)
+        assert bool((out[:, 0] == 7.0).all()) and bool((out[:, -1] == 7.0).all()) and torch.equal(whole, keep)
+        dmmv.dmmv_gradient_clip([t], 0.3)
+        check([keep[:, gap:]], [t], n, 0.3, 1e-6)
+        assert torch.equal(whole[:, :gap], keep[:, :gap])
+
+
 def test_large_small_and_not_finite_numbers(gpu_device):
     from paper_2508_13437_amd import dmmv
 

@@ -155,7 +155,7 @@ def test_gradient_refusals(mod):
     lib, f, b = mod.load(), mod.DMMV_F32, mod.DMMV_BF16
     one = gradients(mod, (P, 4, 10, 12, f))
     need = lib.dmmv_gradient_workspace_bytes(1, C.addressof(one))
-    assert need == 4 * 8
+    assert need == 8                                                  # one sum of the four rows
 
     def norm_of(g, n=1, out=P, ws=P, size=1 << 20):
         return lib.dmmv_gradient_norm(n, None if g is None else C.addressof(g), out, ws, size, None)
@@ -197,6 +197,15 @@ def test_gradients_that_share_memory_are_refused(mod):
     assert not apart((P, 1, 10, 10, b), (P + 18, 1, 1, 1, b)) and apart((P, 1, 10, 10, b), (P + 20, 1, 1, 1, b))
     # empty ones have no place
     assert apart((P, 0, 10, 10, f), (P, 1, 10, 10, f), (None, 4, 0, 0, f))
+
+
+def test_a_tensor_that_is_too_large_is_refused_before_any_launch(mod):
+    """After more tensors than a launch takes: none of those is launched either (no workspace is given)."""
+    lib, f = mod.load(), mod.DMMV_F32
+    g = gradients(mod, *[(P + 64 * i, 1, 1, 1, f) for i in range(70)], (1 << 40, (1 << 31) - 1, 8193, 8200, f))
+    at = C.addressof(g)
+    assert lib.dmmv_gradient_workspace_bytes(71, at) == 0 and lib.dmmv_last_error()
+    assert lib.dmmv_gradient_norm(71, at, P, None, 0, None) == -2 and lib.dmmv_gradient_clip(71, at, None, 1.0, 0.0, P, None, None, 0, None) == -2
 
 
 def test_gradient_workspace_counts_every_launch(mod):
