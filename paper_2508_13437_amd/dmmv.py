@@ -643,9 +643,13 @@ def _addr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+# (the stream's address without a Stream object around it, a tenth of a short call, where PyTorch has that)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
 def _enqueue(dev: int, fn, *args):
     """One call on the current stream of device `dev`."""
-    stream = torch.cuda.current_stream(dev).cuda_stream
+    stream = _raw_stream(dev)
     if torch.cuda.current_device() == dev:
         status = fn(*args, stream)
     else:
