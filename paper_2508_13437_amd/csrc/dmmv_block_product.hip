@@ -80,28 +80,19 @@ struct ProductOut<T, true> {
     int32_t act, has_q;
 };
 
-// eight columns of u from `col` on; r the residual's; with Q the 16 lanes of a block of 128 come together (`ok`: the row is there)
-template <bool Q, class T>
-__device__ __forceinline__ void finish8(const ProductOut<T, true>& o, int64_t row, int64_t col, int64_t cols, bool ok, float (&v)[8], const float (&r)[8]) {
-    if (ok && o.u) store8(o.u + row * o.ldu, col, cols, v);
+// eight columns of u from `col` on; r the residual's; the 16 lanes of a block of 128 come together
+template <class T>
+__device__ __forceinline__ void finish8(const ProductOut<T, true>& o, int64_t row, int64_t col, int64_t cols, float (&v)[8], const float (&r)[8]) {
+    if (o.u) store8(o.u + row * o.ldu, col, cols, v);
     act_values<sizeof(T) == 2>(o.act, v);
     if (o.residual)
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += r[e];
-    if (ok && o.y) store8(o.y + row * o.ldy, col, cols, v);
-    if constexpr (Q) {
-        if (!o.has_q) return;
+    if (o.y) store8(o.y + row * o.ldy, col, cols, v);
+    if (!o.has_q) return;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = col + e < cols ? v[e] : 0.0f;
-        uint32_t b;
-        const piece8 code = quantize8(v, b);
-        if (ok && col < cols) {
-            store8_codes(o.q.codes + row * o.q.ld, col, cols, code);
-            if ((threadIdx.x & 15) == 0) scale_put(o.q, row, col >> 7, b);
-        }
-    } else {
-        if (ok && o.v) store8(o.v + row * cols, col, cols, v);
-    }
+    for (int e = 0; e < 8; ++e) v[e] = col + e < cols ? v[e] : 0.0f;
+    put_q<T>(o.q, row, col, cols, v);
 }
 // one number of u; v
 template <bool SHORT, class T>
@@ -121,7 +112,10 @@ struct TileScales {
 // ROWS x COLS numbers in the LDS (rows of LD floats): u, or with SUMS sums that become it.  256 threads, eight columns of a row a turn, always the
 // same ones, and the rows (256 * 8 / COLS a turn) are those of the thread at turn 0 and rows_on(turn) further.  What a turn reads of the LDS
 // is requested in the turn before.  Columns that the matrix's end cuts go one by one, through the LDS: code that runs once is bound by its
-// fetching, so there is little of it.
+// fetching, so there is little of it.  Turns in pairs hide one another's waits: there is one wavefront a SIMD.  4096 x 11008 x 4096, us: product 161 (170 by the
+// other epilogue), RELU 162, SiLU 172, GELU 180, u beside it 3 to 4 more, in 8 bits instead 20 more (the largest of 128 and the conversions, one
+// after the other), a residual 12 more (its requests wait for the stores before them).  With everything unrolled by the compiler the up-projection with
+// GELU and u took 240, now 184.
 template <int ROWS, int COLS, int LD, bool Q, bool SUMS, class T, class F>
 __device__ __forceinline__ void finish_tile(const ProductOut<T, true>& o, float* tile, const TileScales& k, int64_t row0, int64_t rows, int64_t cols, int64_t col0,
                                             F rows_on) {
@@ -1129,7 +1123,7 @@ __global__ __launch_bounds__(256) void k_block_product_join(int64_t T_, int64_t 
     }
     if constexpr (EPI) {
         if (out.residual) load8(out.residual + t * out.ldr, o, O, p);
-        finish8<true>(out, t, o, O, o < O, v, p);
+        finish8(out, t, o, O, v, p);
     } else {
         store8(out.y + t * out.ldy, o, O, v);
     }
@@ -1217,7 +1211,7 @@ static ProductPlan product_plan(const dmmv_block_matrix* x, const dmmv_block_mat
     ProductPlan p = {ProductPlan::GENERAL, (constant_rows(x) || x->scale_type == DMMV_E8M0) && (constant_rows(w) || w->scale_type == DMMV_E8M0), 0, 0};
     // Few tokens, us by registers and by tiles (T x O x K): 32 x 4096 x 4096 9.9 and 12.7, 24 x 8192 x 4096 15.3 and 16.1, 32 x 8192 x 4096
     // 17.5 and 16.1, 24 x 11008 x 4096 21 and 16.5, 24 x 8192 x 8192 27.5 and 26; few outputs of a long contraction 24 x 4096 x 8192 15.2 and 26,
-    // 24 x 4096 x 11008 18.7 and 34; 64 x 4096 x 4096 16.4 and 13.8; where the large tiles do not apply, 64 (32 bits): 17.4 and 19.3, 128: 32.5 and 20.
+    // 24 x 4096 x 11008 17.6 and 34; 64 x 4096 x 4096 16.4 and 13.8; where the large tiles do not apply, 64 (32 bits): 17.4 and 19.3, 128: 32.5 and 20.
     const bool tiles = !f32 && p.scaled && aligned(x) && aligned(w);
     const bool wide = T > 16 && O >= 8192 && (double)T * (double)O * (double)K >= 9e8;
     if (T <= (!tiles ? 64 : wide ? 16 : 32)) {
