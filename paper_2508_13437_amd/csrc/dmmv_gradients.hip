@@ -396,8 +396,10 @@ extern "C" dmmv_status dmmv_gradient_clip(int64_t count, const dmmv_gradient* gr
         return DMMV_OK;
     }));
     if (lists == 0 && norm) {                  // nothing to scale
-        if (given) return fail(DMMV_ERR_NULL, "norm and given without gradients");
-        hipLaunchKernelGGL(k_gradient_norm, dim3(1), dim3(256), 0, s, part, 0, norm);
+        TensorList none;
+        none.count = 0;
+        none.chunks = 0;
+        hipLaunchKernelGGL(k_gradient_scale<PIECE>, dim3(1), dim3(256), 0, s, none, part, 0, given, max_norm, eps, 1, norm);
         DMMV_LAUNCH_CHECK();
     }
     return DMMV_OK;

@@ -142,6 +142,9 @@ def test_a_norm_from_elsewhere(gpu_device):
     n = dmmv.dmmv_gradient_norm(ts)
     assert torch.equal(dmmv.dmmv_gradient_clip(other[:2], 0.01, norm=n), n) and torch.equal(dmmv.dmmv_gradient_clip(other[2:], 0.01, norm=n), n)
     check(ts, other, n, 0.01, 1e-6)
+    none = [torch.empty(0, 5, device=gpu_device), torch.empty(0, device=gpu_device)]
+    assert float(dmmv.dmmv_gradient_clip(none, 1.0)) == 0.0 and float(dmmv.dmmv_gradient_norm(none)) == 0.0
+    assert torch.equal(dmmv.dmmv_gradient_clip(none, 1.0, norm=n), n)
     huge = [torch.ones(9, device=gpu_device)]
     dmmv.dmmv_gradient_clip(huge, 1.0, norm=torch.tensor(math.nan, device=gpu_device))
     assert huge[0].isnan().all()
@@ -158,6 +161,22 @@ def test_more_numbers_than_32_bits_count(gpu_device):
     m = t[:n - 1].view(-1, 2)[:, :1]                                       # and rows with gaps, one number a row
     with pytest.raises(dmmv.DmmvError):                                    # more rows than 31 bits count: refused
         dmmv.dmmv_gradient_norm([m])
+
+
+def test_out_may_be_the_gradients_themselves_and_the_norm_its_own_place(gpu_device):
+    from paper_2508_13437_amd import dmmv
+
+    ts = tensors([(300, 400), (7,)], [F32, BF16], 2, gpu_device)
+    other = [t.clone() for t in ts]
+    n = dmmv.dmmv_gradient_clip(ts, 0.01)
+    g = dmmv.Gradients(other)
+    assert torch.equal(dmmv.dmmv_gradient_clip(g, 0.01, out=g), n) and all(torch.equal(a, b) for a, b in zip(ts, other))
+    # gradients that are only read may be the same numbers twice: both count
+    a = torch.ones(100, device=gpu_device)
+    assert float(dmmv.dmmv_gradient_norm([a, a, a, a[:100]])) == 20.0
+    out = [torch.empty(100, device=gpu_device) for _ in range(2)]
+    dmmv.dmmv_gradient_clip([a, a], 1.0, 0.0, out=out)
+    assert torch.equal(out[0], out[1]) and abs(float(out[0][0]) * 200 ** 0.5 - 1.0) < 1e-6
 
 
 def test_streams_and_graphs(gpu_device):
