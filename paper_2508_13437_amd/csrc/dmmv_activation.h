@@ -1,4 +1,4 @@
-// The activations of a layer (include/dmmv_layer.h), on eight numbers at a time: one uniform branch for all of them.
+// The activations of a layer (include/dmmv_layer.h), on several numbers at a time: one uniform branch for all of them.
 #pragma once
 
 #include "dmmv_layer_common.h"
@@ -106,11 +106,12 @@ __device__ __forceinline__ float act_slope(float u) {
     return dmmv_fma(u, l.s * l.rest, l.s);
 }
 
-template <bool SHORT, int N>
-__device__ __forceinline__ void act_values(int32_t act, float (&v)[N]) {
-#define ACT_CASE(A)                                                                                                 \
-    case A:                                                                                                         \
-        _Pragma("unroll") for (int e = 0; e < N; ++e) v[e] = SHORT ? act_value_short<A>(v[e]) : act_value<A>(v[e]); \
+template <bool SHORT, int M, int N>
+__device__ __forceinline__ void act_values(int32_t act, float (&v)[M][N]) {
+#define ACT_CASE(A)                                                                                                     \
+    case A:                                                                                                             \
+        _Pragma("unroll") for (int i = 0; i < M; ++i)                                                                   \
+            _Pragma("unroll") for (int e = 0; e < N; ++e) v[i][e] = SHORT ? act_value_short<A>(v[i][e]) : act_value<A>(v[i][e]); \
         break;
     switch (act) {
         ACT_CASE(DMMV_ACT_RELU)
@@ -120,6 +121,8 @@ __device__ __forceinline__ void act_values(int32_t act, float (&v)[N]) {
     }
 #undef ACT_CASE
 }
+template <bool SHORT, int N>
+__device__ __forceinline__ void act_values(int32_t act, float (&v)[N]) { act_values<SHORT, 1, N>(act, reinterpret_cast<float (&)[1][N]>(v)); }
 
 #endif  // __HIPCC__
 

@@ -113,13 +113,13 @@ struct TileScales {
 // same ones, and the rows (256 * 8 / COLS a turn) are those of the thread at turn 0 and rows_on(turn) further.  What a turn reads of the LDS
 // is requested in the turn before.  Columns that the matrix's end cuts go one by one, through the LDS: code that runs once is bound by its
 // fetching, so there is little of it.  Turns in pairs hide one another's waits: there is one wavefront a SIMD.  4096 x 11008 x 4096, us: product 161 (170 by the
-// other epilogue), RELU 162, SiLU 172, GELU 180, u beside it 3 to 4 more, in 8 bits instead 20 more (the largest of 128 and the conversions, one
-// after the other), a residual 12 more (its requests wait for the stores before them).  With everything unrolled by the compiler the up-projection with
-// GELU and u took 240, now 184.
+// other epilogue), RELU 162, SiLU 172, GELU 180, u beside it 3 to 4 more, in 8 bits instead 10 more (20 with one turn after the other), a residual 4 more
+// (12; its requests wait for the stores before them).  With everything unrolled by the compiler the up-projection with GELU and u took 240, now 184.
 template <int ROWS, int COLS, int LD, bool Q, bool SUMS, class T, class F>
 __device__ __forceinline__ void finish_tile(const ProductOut<T, true>& o, float* tile, const TileScales& k, int64_t row0, int64_t rows, int64_t cols, int64_t col0,
                                             F rows_on) {
     constexpr int PER_ROW = COLS / 8, STEP = 256 / PER_ROW, TURNS = ROWS / STEP;
+    static_assert(TURNS % 2 == 0, "turns in pairs");
     const int r0 = (int)threadIdx.x / PER_ROW, h = (int)threadIdx.x % PER_ROW;
     const int64_t col = col0 + h * 8, at0 = row0 + r0;
     const int left = (int)min(cols - col, (int64_t)8), below = (int)min(rows - at0, (int64_t)1 << 20);      // of the columns, of the rows
@@ -133,72 +133,123 @@ __device__ __forceinline__ void finish_tile(const ProductOut<T, true>& o, float*
 #pragma unroll
         for (int i = 0; i < 4; ++i) { w[i] = f0[i]; w[4 + i] = f1[i]; }
     };
-    float* at = tile + r0 * LD + h * 8;
-    float so[8], bias[8], next[8], nst = 1.0f;
+    float so[8], bias[8];
     if constexpr (SUMS) {
         if (k.so) get8(k.so + h * 8, so);
         get8(k.bias + h * 8, bias);
-        nst = k.st[r0 + rows_on(0)];
     }
-    get8(at, next);
-#pragma unroll 2
-    for (int turn = 0; turn < TURNS; ++turn) {
-        const int on = rows_on(turn);                // (the same for all)
-        const bool ok = on < below && left > 0, whole = on < below && left >= 8;
-        const bool add = whole && o.residual;
-        Raw8<T> res;                                 // (a turn ahead it would wait for the stores before it: 28 us more at 4096 x 11008 x 4096)
-        if (add) res.load(residual + on * o.ldr);
-        float v[8];
+    float* const mine = tile + r0 * LD + h * 8;
+    // u of a turn
+    struct Sums {
+        float v[8], st;
+    };
+    auto read = [&](int turn, Sums& x) __attribute__((always_inline)) {
+        get8(mine + turn * (STEP * LD), x.v);
+        if constexpr (SUMS) x.st = k.st[r0 + rows_on(turn)];
+    };
+    auto u_of = [&](const Sums& x, float* v) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = next[e];
-        const float st = nst;
-        float* const here = at;
-        if (turn + 1 < TURNS) {
-            at += STEP * LD;
-            get8(at, next);
-            if constexpr (SUMS) nst = k.st[r0 + rows_on(turn + 1)];
+        for (int e = 0; e < 8; ++e) {
+            v[e] = x.v[e];
+            if constexpr (SUMS) v[e] = dmmv_fma(k.so ? v[e] * so[e] : v[e], x.st, bias[e]);
         }
-        if constexpr (SUMS) {
-            if (k.so)
+    };
+    auto scale_to = [&](int on, uint32_t scale) __attribute__((always_inline)) {
+        if ((threadIdx.x & 15) != 0) return;
+        if (o.q.e8m0) static_cast<uint8_t*>(o.q.scales)[scale0 + on * o.q.srow] = (uint8_t)scale;
+        else static_cast<float*>(o.q.scales)[scale0 + on * o.q.srow] = e8m0_value(scale);
+    };
+    Sums next[2];
+    read(0, next[0]);
+    read(1, next[1]);
+#pragma unroll 1
+    for (int turn = 0; turn < TURNS; turn += 2) {
+        const int on[2] = {rows_on(turn), rows_on(turn + 1)};        // (the same for all)
+        // (rows come in order; a wavefront's lanes go together, for the largest of 128)
+        if (__all(on[1] < below && left >= 8)) {
+            float v[2][8];
+            Raw8<T> res[2];                          // (a turn ahead they would wait for the stores before them: 28 us more at 4096 x 11008 x 4096)
+            if (o.residual) {
+                res[0].load(residual + on[0] * o.ldr);
+                res[1].load(residual + on[1] * o.ldr);
+            }
+            u_of(next[0], v[0]);
+            u_of(next[1], v[1]);
+            if (turn + 2 < TURNS) {
+                read(turn + 2, next[0]);
+                read(turn + 3, next[1]);
+            }
+            if (o.u)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= so[e];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = dmmv_fma(v[e], st, bias[e]);
-        }
-        if (whole) {
-            if (o.u) store8(u + on * o.ldu, 0, 8, v);
+                for (int i = 0; i < 2; ++i) store8(u + on[i] * o.ldu, 0, 8, v[i]);
             act_values<sizeof(T) == 2>(o.act, v);
-            if (add)
+            if (o.residual)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += res.get(e);
-            if (o.y) store8(y + on * o.ldy, 0, 8, v);
-            if (!Q && o.v) store8(o.v + (at0 + on) * cols + col, 0, 8, v);
-        } else if (ok) {
-            if constexpr (SUMS)
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[i][e] += res[i].get(e);
+            if (o.y)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) store8(y + on[i] * o.ldy, 0, 8, v[i]);
+            if (!Q && o.v)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) store8(o.v + (at0 + on[i]) * cols + col, 0, 8, v[i]);
+            if constexpr (Q) {
+                if (!o.has_q) continue;
+                uint32_t most[2], scale[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) most[i] = row16_max(most8(v[i]));
+                piece8 code[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    scale[i] = scale_byte(most[i]);
+                    code[i] = encode8_finite(v[i], scale[i]);
+                }
+                if (__any(max(most[0], most[1]) >= 0x7F800000u))
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) code[i] = quantize8(v[i], scale[i]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    *reinterpret_cast<piece8_any*>(codes + on[i] * o.q.ld) = code[i];
+                    scale_to(on[i], scale[i]);
+                }
+            }
+            continue;
+        }
+        // the matrix ends in this wavefront's rows or columns
+#pragma unroll 1
+        for (int i = 0; i < 2; ++i) {
+            const int at = rows_on(turn + i);
+            const bool ok = at < below && left > 0;
+            float v[8];
+            Sums x;
+            read(turn + i, x);
+            u_of(x, v);
+            float* const here = mine + (turn + i) * (STEP * LD);
+            if (ok) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) here[e] = v[e];
 #pragma unroll 1
-            for (int e = 0; e < left; ++e) here[e] = finish1<sizeof(T) == 2>(o, at0 + on, col + e, cols, here[e]);
-            get8(here, v);
-        }
-        if constexpr (Q) {
-            if (!o.has_q) continue;
-            if (!whole)
+                for (int e = 0; e < min(left, 8); ++e) here[e] = finish1<sizeof(T) == 2>(o, at0 + at, col + e, cols, here[e]);
+                get8(here, v);
+            }
+            if constexpr (Q) {
+                if (!o.has_q) continue;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = ok && e < left ? v[e] : 0.0f;
-            uint32_t scale;
-            const piece8 code = quantize8(v, scale);
-            uint8_t* to = codes + on * o.q.ld;
-            if (whole) {
-                *reinterpret_cast<piece8_any*>(to) = code;
-            } else if (ok) {
+                uint32_t scale;
+                const piece8 code = quantize8(v, scale);
+                if (ok) {
+                    uint8_t* to = codes + at * o.q.ld;
 #pragma unroll 1
-                for (int e = 0; e < left; ++e) to[e] = (uint8_t)((e < 4 ? code[0] : code[1]) >> (8 * (e & 3)));
+                    for (int e = 0; e < min(left, 8); ++e) to[e] = (uint8_t)((e < 4 ? code[0] : code[1]) >> (8 * (e & 3)));
+                    scale_to(at, scale);
+                }
             }
-            if (ok && (threadIdx.x & 15) == 0) {
-                if (o.q.e8m0) static_cast<uint8_t*>(o.q.scales)[scale0 + on * o.q.srow] = (uint8_t)scale;
-                else static_cast<float*>(o.q.scales)[scale0 + on * o.q.srow] = e8m0_value(scale);
-            }
+        }
+        if (turn + 2 < TURNS) {
+            read(turn + 2, next[0]);
+            read(turn + 3, next[1]);
         }
     }
 }

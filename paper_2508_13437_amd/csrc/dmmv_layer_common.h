@@ -261,15 +261,17 @@ __device__ __forceinline__ uint32_t max8_bits(const float (&v)[8]) {
     for (int i = 0; i < 8; ++i) a = max(a, finite_bits(v[i]));
     return a;
 }
-// Eight values of a lane in 8 bits, 16 lanes a block: the codes, and the scale's byte.  All 64 lanes active; what is not finite is looked for once.
+// Eight values of a lane in 8 bits, 16 lanes a block: the codes, and the scale's byte.  All 64 lanes active; what is not finite is looked for once, and
+// last, so that no branch waits for the largest value.
 __device__ __forceinline__ piece8 quantize8(const float (&v)[8], uint32_t& scale) {
-    const uint32_t most = most8(v);
+    const uint32_t most = row16_max(most8(v));
+    scale = scale_byte(most);
+    piece8 code = encode8_finite(v, scale);
     if (__any(most >= 0x7F800000u)) {
         scale = scale_byte(row16_max(max8_bits(v)));
-        return encode8(v, scale);
+        code = encode8(v, scale);
     }
-    scale = scale_byte(row16_max(most));
-    return encode8_finite(v, scale);
+    return code;
 }
 // sum over the wavefront in a fixed order, the same value in every lane; all 64 lanes active
 __device__ __forceinline__ float wave_sum(float v) {
