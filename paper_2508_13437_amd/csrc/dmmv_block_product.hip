@@ -94,25 +94,24 @@ __device__ __forceinline__ void finish8(const ProductOut<T, true>& o, int64_t ro
     for (int e = 0; e < 8; ++e) v[e] = col + e < cols ? v[e] : 0.0f;
     put_q<T>(o.q, row, col, cols, v);
 }
-// one number of u; v
-template <bool SHORT, class T>
-__device__ __forceinline__ float finish1(const ProductOut<T, true>& o, int64_t row, int64_t col, int64_t cols, float u) {
+// one number of u
+template <class T>
+__device__ __forceinline__ void finish1(const ProductOut<T, true>& o, int64_t row, int64_t col, int64_t cols, float u) {
     if (o.u) put_y(o.u + row * o.ldu + col, u);
     float v[1] = {u};
-    act_values<SHORT>(o.act, v);
+    act_values<false>(o.act, v);
     if (o.residual) v[0] += value_of(o.residual[row * o.ldr + col]);
     if (o.y) put_y(o.y + row * o.ldy + col, v[0]);
     if (o.v) o.v[row * cols + col] = v[0];
-    return v[0];
 }
 // What makes u of the sums in a tile, for its columns and rows: u = fma(sum * so, st, bias).  In the LDS.
 struct TileScales {
     float *bias, *so, *st;
 };
 // ROWS x COLS numbers in the LDS (rows of LD floats): u, or with SUMS sums that become it.  256 threads, eight columns of a row a turn, always the
-// same ones, and the rows (256 * 8 / COLS a turn) are those of the thread at turn 0 and rows_on(turn) further.  What a turn reads of the LDS
-// is requested in the turn before.  Columns that the matrix's end cuts go one by one, through the LDS: code that runs once is bound by its
-// fetching, so there is little of it.  Turns in pairs hide one another's waits: there is one wavefront a SIMD.  4096 x 11008 x 4096, us: product 161 (170 by the
+// same ones, and the rows (256 * 8 / COLS a turn) are those of the thread at turn 0 and rows_on(turn) further.  What two turns read of the LDS
+// is requested in the two before.  Code that runs once is bound by its fetching, so there is little of it: one piece for whole wavefronts, one for the
+// matrix's ends.  Turns in pairs hide one another's waits: there is one wavefront a SIMD.  4096 x 11008 x 4096, us: product 161 (170 by the
 // other epilogue), RELU 162, SiLU 172, GELU 180, u beside it 3 to 4 more, in 8 bits instead 10 more (20 with one turn after the other), a residual 4 more
 // (12; its requests wait for the stores before them).  With everything unrolled by the compiler the up-projection with GELU and u took 240, now 184.
 template <int ROWS, int COLS, int LD, bool Q, bool SUMS, class T, class F>
@@ -225,26 +224,25 @@ __device__ __forceinline__ void finish_tile(const ProductOut<T, true>& o, float*
             Sums x;
             read(turn + i, x);
             u_of(x, v);
-            float* const here = mine + (turn + i) * (STEP * LD);
-            if (ok) {
+            const int there = ok ? left : 0;         // of the columns
+            if (o.u) store8(u + at * o.ldu, 0, there, v);
+            act_values<sizeof(T) == 2>(o.act, v);
+            if (o.residual) {
+                float r[8];
+                load8(residual + at * o.ldr, 0, there, r);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) here[e] = v[e];
-#pragma unroll 1
-                for (int e = 0; e < min(left, 8); ++e) here[e] = finish1<sizeof(T) == 2>(o, at0 + at, col + e, cols, here[e]);
-                get8(here, v);
+                for (int e = 0; e < 8; ++e) v[e] += r[e];
             }
+            if (o.y) store8(y + at * o.ldy, 0, there, v);
+            if (!Q && o.v) store8(o.v + (at0 + at) * cols + col, 0, there, v);
             if constexpr (Q) {
                 if (!o.has_q) continue;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = ok && e < left ? v[e] : 0.0f;
+                for (int e = 0; e < 8; ++e) v[e] = e < there ? v[e] : 0.0f;
                 uint32_t scale;
                 const piece8 code = quantize8(v, scale);
-                if (ok) {
-                    uint8_t* to = codes + at * o.q.ld;
-#pragma unroll 1
-                    for (int e = 0; e < min(left, 8); ++e) to[e] = (uint8_t)((e < 4 ? code[0] : code[1]) >> (8 * (e & 3)));
-                    scale_to(at, scale);
-                }
+                store8_codes(codes + at * o.q.ld, 0, there, code);
+                if (ok) scale_to(at, scale);
             }
         }
         if (turn + 2 < TURNS) {
@@ -535,7 +533,7 @@ __global__ __launch_bounds__(256, WAVES) void k_block_product(int64_t T_, int64_
             __syncthreads();
             if (again) {
                 tile_any<T, SCALED>(t0 + wt, T_, o0 + wo, O, K, x, w, how, bias, [&](int64_t t, int64_t o, float v) __attribute__((always_inline)) {
-                    if constexpr (EPI) finish1<false>(out, t, o, O, v);
+                    if constexpr (EPI) finish1(out, t, o, O, v);
                     else put_y(out.y + t * out.ldy + o, v);
                 });
                 return;
@@ -1120,7 +1118,7 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
             if (o >= O) continue;
             const float so = SCALED && !how.w_blocks ? row_scale(scale_at(w, o, 0)).rest : 1.0f;
             const float u = dmmv_fma(v[e] * so, st, bias ? bias[o] : 0.0f);
-            if constexpr (EPI) finish1<false>(out, t, o, O, u);
+            if constexpr (EPI) finish1(out, t, o, O, u);
             else put_y(out.y + t * out.ldy + o, u);
         }
     }
