@@ -203,7 +203,7 @@ typedef struct {
 
 /* norm (one float) <- the square root of the sum of squares over all numbers of all tensors, summed in 64 bits; the HOST array is read
  * before the call returns.  The workspace (256-byte aligned) holds partial sums; its size serves any call with tensors of these
- * sizes. */
+ * sizes and row strides. */
 size_t dmmv_gradient_workspace_bytes(int64_t count, const dmmv_gradient* gradients);
 dmmv_status dmmv_gradient_norm(int64_t count, const dmmv_gradient* gradients, float* norm, void* workspace, size_t workspace_bytes,
                                void* hip_stream);
