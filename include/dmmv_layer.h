@@ -153,7 +153,7 @@ dmmv_status dmmv_block_linear(const dmmv_block_matrix* x, const dmmv_block_matri
                               void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* du = dy act'(u) [rows][lddu] and dbias = its sum over rows, float [cols]; dy [rows][lddy], u [rows][ldu], all of dtype, act not
- * DMMV_ACT_NONE.  Either result may be NULL.  dbias sums the 32-bit products.  The derivative of max(u, 0) at 0 is 0; at infinities
+ * DMMV_ACT_NONE.  Either result may be NULL (dbias: at most 2^27 columns).  dbias sums the 32-bit products.  The derivative of max(u, 0) at 0 is 0; at infinities
  * derivatives are their limits.  The workspace (256-byte aligned) is for dbias alone. */
 size_t dmmv_activation_workspace_bytes(int64_t rows, int64_t cols);
 dmmv_status dmmv_activation_backward(int32_t dtype, int64_t rows, int64_t cols, const void* dy, int64_t lddy, const void* u,

@@ -12,14 +12,15 @@ dmmv_status layer_check_act(int32_t act, bool none) {
 // and are joined over the workgroup's rows in the LDS, in order.  Bound by memory: 4096 x 11008 bf16
 // GELU 56 us (4.8 TB/s; 103 with the library's erfc and exp), and 5 for the sum of the parts.
 template <class T, int ACT, int TPR>
-__global__ __launch_bounds__(256) void k_activation_backward(int64_t rows, int64_t cols, int64_t per, const T* __restrict__ dy, int64_t lddy,
+__global__ __launch_bounds__(256) void k_activation_backward(int64_t rows, int64_t cols, int64_t per, uint32_t strips, const T* __restrict__ dy, int64_t lddy,
                                                              const T* __restrict__ u, int64_t ldu, T* __restrict__ du, int64_t lddu,
                                                              float* __restrict__ part) {
     constexpr int TEAMS = 256 / TPR;
     __shared__ float join[TEAMS > 1 ? 256 * 8 : 1];
     const int team = threadIdx.x / TPR, t = threadIdx.x % TPR;
-    const int64_t col = (blockIdx.y * (int64_t)TPR + t) * 8;
-    const int64_t r0 = blockIdx.x * per, r1 = min(r0 + per, rows);
+    const uint32_t piece = blockIdx.x / strips, strip = blockIdx.x - piece * strips;
+    const int64_t col = (piece * (int64_t)TPR + t) * 8;
+    const int64_t r0 = strip * per, r1 = min(r0 + per, rows);
     float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (col < cols) {
         // two rows requested at a time
@@ -59,7 +60,7 @@ __global__ __launch_bounds__(256) void k_activation_backward(int64_t rows, int64
         for (int e = 0; e < 8; ++e)
             for (int w = 1; w < TEAMS; ++w) s[e] += join[(e * TEAMS + w) * TPR + t];
     }
-    if (col < cols) store8(part + blockIdx.x * cols, col, cols, s);
+    if (col < cols) store8(part + strip * cols, col, cols, s);
 }
 
 // Strips of rows: some 1536 workgroups (4096 x 11008 bf16 64 us, 68 with 2048, 72 with 1024), a strip at least eight rounds of the workgroup's rows.
@@ -78,9 +79,9 @@ static dmmv_status act_backward(int64_t rows, int64_t cols, const T* dy, int64_t
                                 float* dbias, float* part, hipStream_t s) {
     const int64_t per = act_rows(rows, cols), n = ceil_div(rows, per);
     const int lanes = act_lanes(cols);
-    const dim3 grid((unsigned)n, (unsigned)ceil_div(cols, 8 * lanes));
+    const dim3 grid((unsigned)(n * ceil_div(cols, 8 * lanes)));             // (at most some 1536 and 2^20)
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, rows, cols, per, dy, lddy, u, ldu, du, lddu, dbias ? part : nullptr);
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, rows, cols, per, (uint32_t)n, dy, lddy, u, ldu, du, lddu, dbias ? part : nullptr);
     };
 #define ACT_LAUNCH(A)                                                        \
     case A:                                                                  \
@@ -118,6 +119,7 @@ extern "C" dmmv_status dmmv_activation_backward(int32_t dtype, int64_t rows, int
     DMMV_TRY(layer_check_array(u, rows, cols, ldu, w, "u"));
     if (du) DMMV_TRY(layer_check_array(du, rows, cols, lddu, w, "du"));
     DMMV_TRY(layer_check_vector(dbias, false, "dbias"));
+    if (dbias && cols > 1 << 27) return fail(DMMV_ERR_SHAPE, "dbias: more than 2^27 columns");
     if (dbias) DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, act_workspace(rows, cols)));
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     if (cols == 0 || (!du && !dbias)) return DMMV_OK;

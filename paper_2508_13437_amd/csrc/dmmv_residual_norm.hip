@@ -189,7 +189,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void k_residual_norm(int64_t
 // Rows of any length: one workgroup, a walk over the row for every sum and one for the results.  1024 x 40000 bf16, both norms RMS: 119 us (2.8 TB/s
 // of what has to move; f and h come from the L2 or the chip's last cache for the later walks).
 template <class T>
-__global__ __launch_bounds__(1024) void k_residual_norm_wide(int64_t cols, ResidualIn<T> in, ResidualOut<T> o) {
+__global__ __launch_bounds__(1024) void k_residual_norm_wide(int64_t, int64_t cols, ResidualIn<T> in, ResidualOut<T> o) {
     __shared__ float sh[16];
     const int64_t row = blockIdx.x;
     const float len = (float)cols;
@@ -691,23 +691,27 @@ static size_t residual_workspace(int64_t rows, int64_t cols, int64_t gate_rows) 
     return a > b ? a : b;
 }
 
+static dmmv_status check_launch(int64_t groups, int threads) {
+    return groups * threads <= UINT32_MAX ? DMMV_OK : fail(DMMV_ERR_SHAPE, "f: more rows than a launch takes");
+}
+
 template <class T>
 static dmmv_status residual_forward(int64_t rows, int64_t cols, const ResidualIn<T>& in, const ResidualOut<T>& o, hipStream_t stream) {
-#define RESIDUAL_LAUNCH(TPR, CH)                                                                                       \
-    hipLaunchKernelGGL((k_residual_norm<T, TPR, CH>), dim3((unsigned)ceil_div(rows, TPR == 64 ? 4 : 1)),               \
-                       dim3(TPR == 64 ? 256 : TPR), 0, stream, rows, cols, in, o)
+    auto launch = [&](auto kernel, int threads, int64_t groups) -> dmmv_status {
+        DMMV_TRY(check_launch(groups, threads));
+        hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3((unsigned)threads), 0, stream, rows, cols, in, o);
+        DMMV_LAUNCH_CHECK();
+        return DMMV_OK;
+    };
     // 8 columns a thread as long as a workgroup has 512: 4096 x 4096 bf16 with both norms and a gate 27.7 us, 30.7 with 256 threads of 16, the 8-bit
     // result alone 26.6 and 30.0; but 2048 x 8192 35 us with 1024 threads of 8, 29.6 with 512 of 16
-    if (cols <= 512) RESIDUAL_LAUNCH(64, 1);
-    else if (cols <= 1024) RESIDUAL_LAUNCH(128, 1);
-    else if (cols <= 2048) RESIDUAL_LAUNCH(256, 1);
-    else if (cols <= 4096) RESIDUAL_LAUNCH(512, 1);
-    else if (cols <= 8192) RESIDUAL_LAUNCH(512, 2);
-    else if (cols <= 16384) RESIDUAL_LAUNCH(1024, 2);
-    else hipLaunchKernelGGL((k_residual_norm_wide<T>), dim3((unsigned)rows), dim3(1024), 0, stream, cols, in, o);
-#undef RESIDUAL_LAUNCH
-    DMMV_LAUNCH_CHECK();
-    return DMMV_OK;
+    if (cols <= 512) return launch(k_residual_norm<T, 64, 1>, 256, ceil_div(rows, 4));
+    if (cols <= 1024) return launch(k_residual_norm<T, 128, 1>, 128, rows);
+    if (cols <= 2048) return launch(k_residual_norm<T, 256, 1>, 256, rows);
+    if (cols <= 4096) return launch(k_residual_norm<T, 512, 1>, 512, rows);
+    if (cols <= 8192) return launch(k_residual_norm<T, 512, 2>, 512, rows);
+    if (cols <= 16384) return launch(k_residual_norm<T, 1024, 2>, 1024, rows);
+    return launch(k_residual_norm_wide<T>, 1024, rows);
 }
 
 template <class T>
@@ -741,6 +745,8 @@ static dmmv_status residual_backward(int64_t rows, int64_t cols, ResidualGrad<T>
 #undef RESIDUAL_GRAD
         DMMV_LAUNCH_CHECK();
     } else {
+        DMMV_TRY(check_launch(rows, 256));
+        if (cols > 65535 * 2048) return fail(DMMV_ERR_SHAPE, "f: longer rows than a launch takes");
         floatx4* sums = a.pre.kind || a.post.kind ? reinterpret_cast<floatx4*>(ws) : nullptr;
         if (sums) {
             hipLaunchKernelGGL((k_residual_norm_grad_sums<T>), dim3((unsigned)rows), dim3(256), 0, stream, cols, a, sums);

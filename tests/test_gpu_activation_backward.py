@@ -93,3 +93,14 @@ def test_no_rows_no_columns_and_refusals(gpu_device):
     want = dmmv.dmmv_activation_backward(a.t().contiguous(), b.t().contiguous(), "gelu")
     got = dmmv.dmmv_activation_backward(a.t(), b.t(), "gelu")
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_a_row_of_more_pieces_than_a_grid_is_high(gpu_device):
+    """65537 pieces of 2048 columns.  max(u, 0): the gradient is dy itself or 0."""
+    from paper_2508_13437_amd import dmmv
+
+    cols = 65536 * 2048 + 5
+    dy = torch.arange(cols, device=gpu_device, dtype=torch.int32).remainder_(251).to(torch.bfloat16)[None] + 1
+    u = torch.where(torch.arange(cols, device=gpu_device, dtype=torch.int32).remainder_(3) == 0, -1.0, 1.0).to(torch.bfloat16)[None]
+    du, db = dmmv.dmmv_activation_backward(dy, u, "relu", dbias=False)
+    assert db is None and torch.equal(du, torch.where(u > 0, dy, torch.zeros_like(dy)))

@@ -144,6 +144,25 @@ def test_residual_norm_workspace_is_partial_sums(mod):
                 assert 0 < n <= (1600 * 5 * cols) * 4 + 16 * rows + 256, (rows, cols, gate)
 
 
+def test_more_than_a_launch_takes_is_refused(mod):
+    """Rows times threads from 2^32 on, gradients of rows of more than 65535 x 2048 columns, bias gradients of more than 2^27: before any launch."""
+    lib, dtype, rms = mod.load(), mod.DMMV_BF16, norm(mod, rms=1)
+    ok = C.addressof(rms)
+
+    def forward(rows, cols):
+        return lib.dmmv_residual_norm(dtype, rows, cols, P, cols, P, cols, 1.0, None, 0, 0, ok, ok, P, cols, P, cols, None, None, P, None, P, None)
+
+    def backward(rows, cols):
+        return lib.dmmv_residual_norm_backward(dtype, rows, cols, P, cols, P, cols, P, cols, P, cols, 1.0, None, 0, 0, ok, ok, None, P, None, P, P, cols, P, cols,
+                                               None, 0, None, None, None, None, P, 1 << 60, None)
+
+    for rows, cols in ((1 << 25, 1000), (1 << 24, 2000), (1 << 23, 4096), (1 << 23, 8192), (1 << 22, 16384), (1 << 22, 40000), ((1 << 26) + 1, 512)):
+        assert forward(rows, cols) == -2 and b"launch" in lib.dmmv_last_error()
+    assert backward(1 << 24, 9000) == -2 and b"launch" in lib.dmmv_last_error()
+    assert backward(1, 65535 * 2048 + 1) == -2 and b"launch" in lib.dmmv_last_error()
+    assert lib.dmmv_activation_backward(dtype, 1, (1 << 27) + 1, P, 1 << 28, P, 1 << 28, 1, P, 1 << 28, P, P, 1 << 60, None) == -2
+
+
 def gradients(mod, *g):
     a = (mod._Gradient * max(len(g), 1))()
     for i, v in enumerate(g):
