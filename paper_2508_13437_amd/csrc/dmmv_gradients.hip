@@ -256,6 +256,7 @@ static bool share(const dmmv_gradient& a, const dmmv_gradient& b) {      // a be
     const uintptr_t off = ((uintptr_t)b.data - (uintptr_t)a.data) % ld;
     return off < (uintptr_t)a.cols * w || off + (uintptr_t)b.cols * w > ld;
 }
+constexpr int64_t PAIRS = 1 << 27;                   // most that are compared: half a second
 static dmmv_status check_apart(int64_t count, const dmmv_gradient* g) {
     Extent* e = new (std::nothrow) Extent[count > 0 ? count : 1];
     if (!e) return fail(DMMV_ERR_WORKSPACE, "no host memory for %lld places", (long long)count);
@@ -266,15 +267,17 @@ static dmmv_status check_apart(int64_t count, const dmmv_gradient* g) {
             e[n++] = {p, p + ((uintptr_t)((g[i].rows - 1) * (g[i].rows > 1 ? g[i].ld : 0)) + (uintptr_t)g[i].cols) * layer_width(g[i].dtype), i};
         }
     std::sort(e, e + n, [](const Extent& a, const Extent& b) { return a.from != b.from ? a.from < b.from : a.i < b.i; });
-    int64_t bad = -1, other = -1;
+    int64_t bad = -1, other = -1, pairs = 0, first = 0;      // (what comes before `first` ends before what comes next)
     uintptr_t most = 0;
-    for (int64_t k = 0; k < n && bad < 0; ++k) {
-        if (e[k].from < most)
-            for (int64_t j = k - 1; j >= 0 && bad < 0; --j)
+    for (int64_t k = 0; k < n && bad < 0 && pairs <= PAIRS; ++k) {
+        if (e[k].from >= most) first = k;
+        else if ((pairs += k - first) <= PAIRS)
+            for (int64_t j = k - 1; j >= first && bad < 0; --j)
                 if (e[j].to > e[k].from && share(g[e[j].i], g[e[k].i])) bad = e[k].i, other = e[j].i;
         most = std::max(most, e[k].to);
     }
     delete[] e;
+    if (pairs > PAIRS) return fail(DMMV_ERR_SHAPE, "gradients: too many parts of one matrix");
     return bad < 0 ? DMMV_OK : fail(DMMV_ERR_SHAPE, "gradients %lld and %lld share memory", (long long)std::min(bad, other), (long long)std::max(bad, other));
 }
 

@@ -214,6 +214,9 @@ def test_gradients_that_share_memory_are_refused(mod):
     # one that lies inside another, with a third between them in the order of addresses
     assert not apart((P, 50, 4, 10, f), (P + 16, 50, 2, 10, f), (P + 1600, 3, 4, 10, f))
     assert not apart((P, 1, 10, 10, b), (P + 18, 1, 1, 1, b)) and apart((P, 1, 10, 10, b), (P + 20, 1, 1, 1, b))
+    # many pairs of halves, and more columns of one matrix than are compared
+    assert apart(*[(P + 400 * i + 20 * k, 10, 5, 10, f) for i in range(20000) for k in (0, 1)])
+    assert not apart(*[(P + 4 * i, 2, 1, 20000, f) for i in range(20000)]) and b"too many" in lib.dmmv_last_error()
     # empty ones have no place
     assert apart((P, 0, 10, 10, f), (P, 1, 10, 10, f), (None, 4, 0, 0, f))
 
