@@ -249,6 +249,13 @@ struct Extent {
     uintptr_t from, to;
     int64_t i;
 };
+static Extent extent_of(const dmmv_gradient& g, int64_t i) {
+    const uintptr_t p = (uintptr_t)g.data;
+    return {p, p + ((uintptr_t)((g.rows - 1) * (g.rows > 1 ? g.ld : 0)) + (uintptr_t)g.cols) * layer_width(g.dtype), i};
+}
+static bool same_place(const dmmv_gradient& a, const dmmv_gradient& b) {
+    return a.data == b.data && a.dtype == b.dtype && a.rows == b.rows && a.cols == b.cols && (a.ld == b.ld || a.rows == 1);
+}
 // whether two matrices whose extents meet share a number: columns of one matrix need not
 static bool share(const dmmv_gradient& a, const dmmv_gradient& b) {      // a begins first
     const uintptr_t w = layer_width(a.dtype), ld = (uintptr_t)a.ld * w;
@@ -257,28 +264,67 @@ static bool share(const dmmv_gradient& a, const dmmv_gradient& b) {      // a be
     return off < (uintptr_t)a.cols * w || off + (uintptr_t)b.cols * w > ld;
 }
 constexpr int64_t PAIRS = 1 << 27;                   // most that are compared: half a second
-static dmmv_status check_apart(int64_t count, const dmmv_gradient* g) {
-    Extent* e = new (std::nothrow) Extent[count > 0 ? count : 1];
-    if (!e) return fail(DMMV_ERR_WORKSPACE, "no host memory for %lld places", (long long)count);
-    int64_t n = 0;
+// What is written, the `to` of each gradient, shares memory neither with what else is written nor with another gradient that is read (from NULL:
+// the gradients are their own place).  A gradient that is scaled where it is counts once.
+static dmmv_status check_apart(int64_t count, const dmmv_gradient* to, const dmmv_gradient* from) {
+    Extent* e = new (std::nothrow) Extent[count > 0 ? 2 * count : 1];
+    if (!e) return fail(DMMV_ERR_WORKSPACE, "no host memory for %lld places", (long long)(2 * count));
+    Extent* const r = e + count;
+    int64_t n = 0, m = 0;
     for (int64_t i = 0; i < count; ++i)
-        if (!nothing(g[i])) {
-            const uintptr_t p = (uintptr_t)g[i].data;
-            e[n++] = {p, p + ((uintptr_t)((g[i].rows - 1) * (g[i].rows > 1 ? g[i].ld : 0)) + (uintptr_t)g[i].cols) * layer_width(g[i].dtype), i};
+        if (!nothing(to[i])) {
+            e[n++] = extent_of(to[i], i);
+            if (from && !same_place(from[i], to[i])) r[m++] = extent_of(from[i], i);
         }
-    std::sort(e, e + n, [](const Extent& a, const Extent& b) { return a.from != b.from ? a.from < b.from : a.i < b.i; });
-    int64_t bad = -1, other = -1, pairs = 0, first = 0;      // (what comes before `first` ends before what comes next)
-    uintptr_t most = 0;
-    for (int64_t k = 0; k < n && bad < 0 && pairs <= PAIRS; ++k) {
-        if (e[k].from >= most) first = k;
-        else if ((pairs += k - first) <= PAIRS)
-            for (int64_t j = k - 1; j >= first && bad < 0; --j)
-                if (e[j].to > e[k].from && share(g[e[j].i], g[e[k].i])) bad = e[k].i, other = e[j].i;
-        most = std::max(most, e[k].to);
+    const auto before = [](const Extent& a, const Extent& b) { return a.from != b.from ? a.from < b.from : a.i < b.i; };
+    std::sort(e, e + n, before);
+    std::sort(r, r + m, before);
+    // in the order of their first numbers; those before `first` end before what comes next
+    struct Side {
+        const Extent* e;
+        const dmmv_gradient* g;
+        int64_t n, first, at;
+        uintptr_t most;
+    };
+    Side out = {e, to, n, 0, 0, 0}, in = {r, from, m, 0, 0, 0};
+    int64_t pairs = 0;
+    const Extent *bad = nullptr, *other = nullptr;
+    bool read = false;                               // one of the two is read
+    auto against = [&](Side& s, const dmmv_gradient& g, const Extent& x, bool reads) {
+        if (x.from >= s.most) s.first = s.at;
+        else if ((pairs += s.at - s.first) <= PAIRS)
+            for (int64_t j = s.at - 1; j >= s.first && !bad; --j)
+                if (s.e[j].to > x.from && share(s.g[s.e[j].i], g)) bad = &x, other = s.e + j, read = reads;
+    };
+    while (out.at + in.at < n + m && !bad && pairs <= PAIRS) {
+        const bool write = in.at == m || (out.at < n && e[out.at].from <= r[in.at].from);
+        Side& s = write ? out : in;
+        const Extent& x = s.e[s.at];
+        against(out, s.g[x.i], x, !write);
+        if (write) against(in, s.g[x.i], x, true);
+        else if (x.from >= in.most) in.first = in.at;
+        s.most = std::max(s.most, x.to);
+        ++s.at;
     }
+    const int64_t a = bad ? std::min(bad->i, other->i) : 0, b = bad ? std::max(bad->i, other->i) : 0;
     delete[] e;
     if (pairs > PAIRS) return fail(DMMV_ERR_SHAPE, "gradients: too many parts of one matrix");
-    return bad < 0 ? DMMV_OK : fail(DMMV_ERR_SHAPE, "gradients %lld and %lld share memory", (long long)std::min(bad, other), (long long)std::max(bad, other));
+    if (!bad) return DMMV_OK;
+    return read ? fail(DMMV_ERR_SHAPE, "gradients %lld and %lld: what one is written to shares memory with what the other is read from", (long long)a, (long long)b)
+                : fail(DMMV_ERR_SHAPE, "gradients %lld and %lld share memory", (long long)a, (long long)b);
+}
+// a norm is no number of tensors that are written, or that are read while it is
+static dmmv_status check_norm_apart(const float* p, int64_t count, const dmmv_gradient* g, const char* what) {
+    const uintptr_t at = (uintptr_t)p;
+    for (int64_t i = 0; p && i < count; ++i)
+        if (!nothing(g[i])) {
+            const Extent e = extent_of(g[i], i);
+            if (at + 4 > e.from && at < e.to) {
+                const uintptr_t w = layer_width(g[i].dtype), ld = (uintptr_t)(g[i].rows > 1 ? g[i].ld : g[i].cols) * w, off = at > e.from ? (at - e.from) % ld : 0;
+                if (off < (uintptr_t)g[i].cols * w || off + 4 > ld) return fail(DMMV_ERR_SHAPE, "%s is a number of gradient %lld", what, (long long)i);
+            }
+        }
+    return DMMV_OK;
 }
 
 // Numbers a chunk: PIECE while chunks of four would be fewer than the workgroups of a launch (norm and scaling of 1.3 M numbers: 8.4 us, 12 with four).
@@ -381,10 +427,13 @@ extern "C" dmmv_status dmmv_gradient_clip(int64_t count, const dmmv_gradient* gr
     if (!(eps >= 0.0f && eps <= 3.4e38f)) return fail(DMMV_ERR_DOMAIN, "eps must be finite and not negative");
     DMMV_TRY(layer_check_vector(given, false, "given"));
     DMMV_TRY(layer_check_vector(norm, false, "norm"));
-    DMMV_TRY(check_apart(count, out ? out : gradients));
+    DMMV_TRY(check_apart(count, out ? out : gradients, out ? gradients : nullptr));
     size_t need = 0;
     DMMV_TRY(gradient_workspace(count, gradients, need));                // (refuses what the launches would)
     if (!given) DMMV_TRY(layer_check_workspace(workspace, workspace_bytes, need));
+    DMMV_TRY(check_norm_apart(given, count, out ? out : gradients, "given"));
+    DMMV_TRY(check_norm_apart(norm, count, gradients, "norm"));
+    if (out) DMMV_TRY(check_norm_apart(norm, count, out, "norm"));
     const int chunk = chunk_of(count, gradients);
     if (out) DMMV_TRY(for_lists(count, gradients, out, chunk, [](const TensorList&, int32_t) -> dmmv_status { return DMMV_OK; }));
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
