@@ -120,6 +120,17 @@ __global__ __launch_bounds__(256) void k_gradient_norm(const double* __restrict_
     if (threadIdx.x == 0) *norm = (float)v;
 }
 
+// part[0] = the sum of all parts, in the order of norm_of: once for all launches of the scaling where there are more than two launches' parts, or their
+// reading would grow with the square of the launches.  Clipping of 1024 tensors of 262144 numbers (16384 parts) 770 us, 996 with every workgroup adding
+// up all of them, 4096 such 3060 and 7070; up to 2048 parts the launch costs as much as it saves (128 such 84 and 84, 256 of 8192 93 and 88).
+__global__ __launch_bounds__(256) void k_gradient_total(double* part, int32_t parts) {
+    __shared__ double sh[4];
+    double s = 0.0;
+    for (int32_t i = threadIdx.x; i < parts; i += 256) s += part[i];
+    s = group_sum(s, sh);                            // (its barrier comes after all parts have been read)
+    if (threadIdx.x == 0) part[0] = s;
+}
+
 // W consecutive numbers of which `left` are there, and back: past the caches, where what the sum of squares has read stays.  A wavefront's store
 // fills whole lines, 16 bytes a lane.  Norm and scaling of 34 M numbers in 32 bits 70 us, 84 by ordinary stores; of 360 M 817 and 839, and 899 past the
 // caches with 32 bytes a lane.
@@ -202,7 +213,7 @@ __device__ __forceinline__ void scale_chunk(const T* in, U* out, int n, float c,
 }
 
 // out = c in, with c = max_norm / (norm + eps) where that is below 1.  Tensors that stay where they are are not touched if c is 1.  Every workgroup
-// adds up the parts for itself, which costs less than a launch between.  360 M numbers in 32 bits: 570 us, 5.0 TB/s of reading and writing.
+// adds up the parts for itself, which costs less than a launch between where there are few (k_gradient_total).  360 M numbers in 32 bits: 570 us, 5.0 TB/s of reading and writing.
 template <int CHUNK>
 __global__ __launch_bounds__(256) void k_gradient_scale(TensorList l, const double* __restrict__ part, int32_t parts, const float* __restrict__ given,
                                                         float max_norm, float eps, int32_t in_place, float* __restrict__ norm) {
@@ -440,6 +451,11 @@ extern "C" dmmv_status dmmv_gradient_clip(int64_t count, const dmmv_gradient* gr
     double* part = static_cast<double*>(workspace);
     int32_t parts = 0, lists = 0;
     if (!given) DMMV_TRY(squares(count, gradients, part, parts, s));
+    if (parts > 2 * GROUPS) {
+        hipLaunchKernelGGL(k_gradient_total, dim3(1), dim3(256), 0, s, part, parts);
+        DMMV_LAUNCH_CHECK();
+        parts = 1;
+    }
     DMMV_TRY(for_lists(count, gradients, out ? out : gradients, chunk, [&](const TensorList& l, int32_t k) -> dmmv_status {
         hipLaunchKernelGGL(chunk == PIECE ? k_gradient_scale<PIECE> : k_gradient_scale<4 * PIECE>, dim3((unsigned)std::min<uint32_t>(l.chunks, GROUPS)), dim3(256), 0, s, l, part, parts, given, max_norm, eps,
                            (int32_t)!out, k == 0 ? norm : nullptr);
