@@ -1095,7 +1095,7 @@ def _place(t: torch.Tensor):
     for d in reversed(order):
         dense &= t.stride(d) == size
         size *= t.shape[d]
-    if len(order) == 2 and t.stride(order[1]) == 1 and t.stride(order[0]) >= t.shape[order[1]]:
+    if len(order) == 2 and t.stride(order[1]) == 1 and t.stride(order[0]) >= t.shape[order[1]] and not (dense and t.shape[order[0]] >= 1 << 31):
         return (t.shape[order[0]], t.shape[order[1]], t.stride(order[0])), order
     if len(order) == 1 and t.stride(order[0]) > 0 and n < 1 << 31:
         return (n, 1, t.stride(order[0])), order

@@ -73,3 +73,13 @@ def test_time_grows_with_the_tensors_not_with_their_square(gpu_device):
     norm = fastest(lambda i: dmmv.dmmv_gradient_norm(g))
     clip = fastest(lambda i: dmmv.dmmv_gradient_clip(g, 0.5 ** i))
     assert clip <= 6 * norm, (clip, norm)
+
+
+def test_more_rows_than_31_bits_count(gpu_device):
+    """Without gaps the rows need not be counted."""
+    from paper_2508_13437_amd import dmmv
+
+    t = torch.zeros((1 << 31) + 3, 2, dtype=BF16, device=gpu_device)
+    t[0, 1], t[1 << 31, 0], t[-1, 1] = 3.0, -4.0, 12.0
+    assert float(dmmv.dmmv_gradient_norm([t])) == 13.0 and float(dmmv.dmmv_gradient_clip([t], 6.5, 0.0, out=[t])) == 13.0
+    assert (float(t[0, 1]), float(t[1 << 31, 0]), float(t[-1, 1])) == (1.5, -2.0, 6.0)

@@ -53,3 +53,14 @@ def test_a_norm_is_no_number_of_the_gradients(mod):  # noqa: F811
     for at in (P, P + 36, P + 96, P + 4 * 96 + 36):
         assert refused(a, norm=at) and refused(a, given=at) and refused(a, to, norm=at) and refused(to, a, norm=at) and refused(to, a, given=at), at
     assert refused((P + 2, 1, 9, 9, h), norm=P) and refused((P + 2, 1, 9, 9, h), norm=P + 16)
+
+
+def test_a_tensor_without_gaps_may_have_any_number_of_rows(mod):  # noqa: F811
+    """Rows are counted in 31 bits; where there are no gaps they need not be counted."""
+    import torch
+
+    n = (1 << 31) + 3
+    for t, place in ((torch.empty(n, 2, device="meta"), (1, 2 * n, 2 * n)), (torch.empty(2, n, device="meta").t(), (2, n, n)),
+                     (torch.empty(n, device="meta"), (1, n, n)), (torch.empty(n - 4, 2, device="meta"), (n - 4, 2, 2)),
+                     (torch.empty(n, 3, device="meta")[:, :2], (n, 2, 3))):
+        assert mod._place(t)[0] == place, t.shape
