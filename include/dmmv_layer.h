@@ -137,7 +137,9 @@ dmmv_status dmmv_layernorm_backward(int32_t dtype, int64_t rows, int64_t cols, c
 
 /* Activations: max(u, 0); u Phi(u) with the normal distribution's function Phi; the same with its usual approximation
  * 1 / (1 + exp(-2 z)), z = sqrt(2 / pi) (u + 0.044715 u^3); u / (1 + exp(-u)).  At infinities they have their limits.
- * For bf16 results the last three are evaluated to a relative 2^-14, else to 32 bits. */
+ * For bf16 results the last three are evaluated to a relative 2^-14.  In 32 bits an exponential brings in what rounds in its argument: of
+ * themselves u Phi(u) is off by at most 1.2 u^2 + 20 units of 2^-24, its approximation by 15 |z| + 8, u / (1 + exp(-u)) by 1.3 |u| + 8 (far out on the negative
+ * side, where they vanish; beside 1 a few).  What is below 2^-118 may be 0 in either case. */
 enum { DMMV_ACT_NONE = 0, DMMV_ACT_RELU = 1, DMMV_ACT_GELU = 2, DMMV_ACT_GELU_TANH = 3, DMMV_ACT_SILU = 4 };
 
 /* u = x w^T + bias as dmmv_block_product has it, v = act(u) + residual, x [T][K], w [O][K], residual [T][ldr] of dtype or NULL.
@@ -154,7 +156,7 @@ dmmv_status dmmv_block_linear(const dmmv_block_matrix* x, const dmmv_block_matri
 
 /* du = dy act'(u) [rows][lddu] and dbias = its sum over rows, float [cols]; dy [rows][lddy], u [rows][ldu], all of dtype, act not
  * DMMV_ACT_NONE.  Either result may be NULL (dbias: at most 2^27 columns).  dbias sums the 32-bit products.  The derivative of max(u, 0) at 0 is 0; at infinities
- * derivatives are their limits.  The workspace (256-byte aligned) is for dbias alone. */
+ * derivatives are their limits.  For both types the two terms of a derivative are off by twice as many units as the activation at most, and 20 more.  The workspace (256-byte aligned) is for dbias alone. */
 size_t dmmv_activation_workspace_bytes(int64_t rows, int64_t cols);
 dmmv_status dmmv_activation_backward(int32_t dtype, int64_t rows, int64_t cols, const void* dy, int64_t lddy, const void* u,
                                      int64_t ldu, int32_t act, void* du, int64_t lddu, float* dbias, void* workspace,
