@@ -213,10 +213,12 @@ dmmv_status dmmv_gradient_norm(int64_t count, const dmmv_gradient* gradients, fl
 /* out <- c gradients with c = max_norm / (norm + eps), 1 where that is not below 1; out NULL = in place, where c = 1 writes nothing.
  * out has the gradients' sizes, in either type.  given: a norm (one float) from elsewhere, over more gradients than these; NULL = the norm of
  * these.  norm (or NULL) <- the norm that was used.  max_norm and eps are finite and not negative.  A norm that is infinite makes finite
- * numbers 0 and others NaN, one that is NaN makes all NaN.  Tensors that are written must not share memory (refused, and so are more than some
- * 16000 columns of one matrix as tensors of their own).  out[i] may be gradient i itself, the same place in the same type; otherwise
- * it shares memory with no gradient, and no tensor that is written holds the number at given, none at all that at norm (refused).  The workspace, of
- * dmmv_gradient_workspace_bytes, is not needed with given. */
+ * numbers 0 and others NaN, one that is NaN makes all NaN.  Tensors that are written must not share memory with one another or with another
+ * gradient: out[i] may be gradient i itself, the same place in the same type.  Refused are two tensors whose extents, from the first
+ * number to the last, meet, unless they are parts of one matrix (one type, one row stride, more than one row) with no number in common; so a
+ * single row, or a matrix of another type or stride, in the gaps of a matrix is refused too, and so are more than some 16000
+ * columns of one matrix as tensors of their own.  No tensor that is written holds the number at given, none at all that at norm
+ * (refused).  The workspace, of dmmv_gradient_workspace_bytes, is not needed with given. */
 dmmv_status dmmv_gradient_clip(int64_t count, const dmmv_gradient* gradients, const dmmv_gradient* out, float max_norm, float eps,
                                const float* given, float* norm, void* workspace, size_t workspace_bytes, void* hip_stream);
 

@@ -267,7 +267,8 @@ static Extent extent_of(const dmmv_gradient& g, int64_t i) {
 static bool same_place(const dmmv_gradient& a, const dmmv_gradient& b) {
     return a.data == b.data && a.dtype == b.dtype && a.rows == b.rows && a.cols == b.cols && (a.ld == b.ld || a.rows == 1);
 }
-// whether two matrices whose extents meet share a number: columns of one matrix need not
+// Whether two matrices whose extents (from the first number to the last) meet may share a number: parts of one matrix, of one type, row stride and more rows
+// than one, need not.  Others in the gaps of a matrix are not looked for: gradients are whole tensors or parts of one.
 static bool share(const dmmv_gradient& a, const dmmv_gradient& b) {      // a begins first
     const uintptr_t w = layer_width(a.dtype), ld = (uintptr_t)a.ld * w;
     if (a.dtype != b.dtype || no_gaps(a) || a.ld != b.ld || b.rows == 1) return true;
@@ -321,8 +322,8 @@ static dmmv_status check_apart(int64_t count, const dmmv_gradient* to, const dmm
     delete[] e;
     if (pairs > PAIRS) return fail(DMMV_ERR_SHAPE, "gradients: too many parts of one matrix");
     if (!bad) return DMMV_OK;
-    return read ? fail(DMMV_ERR_SHAPE, "gradients %lld and %lld: what one is written to shares memory with what the other is read from", (long long)a, (long long)b)
-                : fail(DMMV_ERR_SHAPE, "gradients %lld and %lld share memory", (long long)a, (long long)b);
+    return read ? fail(DMMV_ERR_SHAPE, "gradients %lld and %lld: what one is written to may share memory with what the other is read from: their extents meet", (long long)a, (long long)b)
+                : fail(DMMV_ERR_SHAPE, "gradients %lld and %lld may share memory: their extents meet", (long long)a, (long long)b);
 }
 // a norm is no number of tensors that are written, or that are read while it is
 static dmmv_status check_norm_apart(const float* p, int64_t count, const dmmv_gradient* g, const char* what) {

@@ -1055,8 +1055,9 @@ class _Gradient(C.Structure):
 
 
 class Gradients:
-    """The gradients of a step, or the buffers that the clipped ones go to: float32 and bfloat16 tensors of one device, which stay where they
-    are.  Any shape without gaps in memory, in any order of its dimensions, and matrices or vectors with gaps."""
+    """The gradients of a step, or the buffers that the clipped ones go to: one or more float32 and bfloat16 tensors of one device, which stay
+    where they are.  Any shape without gaps in memory, in any order of its dimensions, and matrices or vectors with gaps.  Those that are
+    written are apart from one another and from other gradients; in the gaps of a matrix only other columns of it may lie."""
 
     __slots__ = ("_tensors", "_order", "_c", "_p", "_dev", "_on", "_bytes")
 

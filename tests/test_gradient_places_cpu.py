@@ -64,3 +64,17 @@ def test_a_tensor_without_gaps_may_have_any_number_of_rows(mod):  # noqa: F811
                      (torch.empty(n, device="meta"), (1, n, n)), (torch.empty(n - 4, 2, device="meta"), (n - 4, 2, 2)),
                      (torch.empty(n, 3, device="meta")[:, :2], (n, 2, 3))):
         assert mod._place(t)[0] == place, t.shape
+
+
+def test_what_lies_in_the_gaps_of_a_matrix(mod):  # noqa: F811
+    """Columns of the same matrix are told apart number by number; anything else whose extent meets the matrix's is refused, as the header says, and the
+    message does not claim more than that."""
+    f, h = mod.DMMV_F32, mod.DMMV_BF16
+    m = (P, 10, 20, 64, f)
+    assert clip(mod, [m, (P + 80, 10, 44, 64, f)]) == -5 and clip(mod, [m, (P + 80 + 256, 3, 44, 64, f)]) == -5
+    assert clip(mod, [m, (P + 80, 10, 45, 64, f)]) == -2
+    for other in ((P + 80 + 256, 1, 44, 64, f), (P + 80, 3, 44, 128, f), (P + 80, 10, 88, 128, h)):
+        assert clip(mod, [m, other]) == -2 and b"gradients 0 and 1 may share memory: their extents meet" in mod.load().dmmv_last_error(), other
+        assert clip(mod, [m, other], [(1 << 20, 10, 20, 64, f), (1 << 21, *other[1:])]) == -5             # where they are only read
+    # beside the matrix, after its last number
+    assert clip(mod, [m, (P + 4 * (9 * 64 + 20), 1, 44, 64, f)]) == -5
