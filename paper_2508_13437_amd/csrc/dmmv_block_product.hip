@@ -1311,8 +1311,10 @@ static dmmv_status product(const ProductPlan& plan, const dmmv_block_matrix* x, 
 }
 
 // The same with what follows it.  8 bits come from the kernel that has whole blocks of 128 outputs of a row (tiles, shares); the others write
-// v in 32 bits, `v` bytes further on in the workspace.  Few tokens in 8 bits are bound by the weights' bytes, so the 16-bit instructions
-// sum them, in 32 bits, for 0.5 us more at one token (4096 by 11008): otherwise one number in some 500 goes to the other neighbour on the 8-bit grid.
+// v in 32 bits, `v` bytes further on in the workspace.  8 bits of up to 64 tokens come from the 16-bit instructions, which sum in 32 bits: by the
+// 8-bit ones a number in some 500 goes to the other neighbour on the 8-bit grid.  What that costs, in 8 bits with SiLU and weights from memory, us here and by the
+// rule of product_plan: one token of 4096 by 11008 0.5 (the instructions alone); 24 tokens of 4096 to 11008 outputs 25.2 and 24.0, 32 28.4 and 23.9, 64 44.6 and 24.6;
+// 64 of 11008 to 4096 33.6 and 23.6, of 4096 to 4096 18.8 and 14.8; 8192 to 8192 24 31.2 and 37.6 (the rule's own weak place), 64 56.8 and 23.4.
 struct LinearPlan {
     ProductPlan product;
     size_t v, bytes;                     // where v begins (0 without one: bytes = product.bytes), all
