@@ -909,16 +909,18 @@ __global__ __launch_bounds__(256) void k_block_product_tiled(int64_t T_, int64_t
 // ---- few tokens ------------------------------------------------------------------------------------
 // Up to 64 tokens: the weights are read once, straight into registers in the order of the operands (a lane 32 codes of
 // a row and block, 128 bytes of a row side by side), and nothing else counts.  A workgroup has 16 outputs and
-// 16 MT tokens, its four wavefronts a share of the blocks each, joined in order through the LDS.  U blocks are on their way at any time
-// (one token of 11008 by 4096 outputs 10.2 us, 13.2 with U of them requested together and waited for together).  One token of 4096 by 11008
+// 16 MT tokens, its four wavefronts a share of the blocks each, joined in order through the LDS.  RING: U blocks are on their way at any time; else
+// U of them are requested together and waited for together (few_in_ring).  One token of 4096 by 11008
 // outputs: 10.6 us, 4.3 TB/s, 14.0 in 8 bits with a pass for those; 24 tokens of 4096 by 4096: 9.6 us, two thirds of it start,
 // join and end (eight wavefronts a workgroup were no faster); 24 of 11008 by 4096 17.6: the tokens, read for every 16 outputs, from the L2.
-template <class T, int MT, bool SCALED, bool WIDE, bool EPI>
+constexpr int few_ring(int MT) { return MT == 1 ? 6 : MT == 2 ? 5 : 2; }
+template <class T, int MT, bool SCALED, bool WIDE, bool RING, bool EPI>
 __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O, int64_t K, BlockView x, BlockView w, ProductScales how,
                                                                   const float* __restrict__ bias, ProductOut<T, EPI> out) {
     // (BRIEF: a bf16 result that is summed in 32 bits, exponents)
-    constexpr bool BRIEF = SCALED && WIDE && sizeof(T) == 2, RING = SCALED && (!WIDE || BRIEF);
-    constexpr int U = RING ? (MT == 1 ? 6 : MT == 2 ? 5 : 2) : MT >= 4 ? 2 : 4, WAVES = 4;
+    constexpr bool BRIEF = SCALED && WIDE && sizeof(T) == 2;
+    static_assert(!RING || SCALED, "exponents");
+    constexpr int U = RING ? few_ring(MT) : MT >= 4 ? 2 : 4, WAVES = 4;
     __shared__ floatx4 part[WAVES][MT][64];
     const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -942,7 +944,10 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
         uint32_t ew, ex[MT];           // SCALED: exponents
         uint32_t fw[4], fx[MT];        // else: scales of this lane's four outputs, of its tokens, as they are stored
     };
-    // SCALED: scales that are the same along a row, and their exponents, taken when the first codes have been requested.  A byte is loaded for every
+    auto exponent = [&](const BlockView& q, int64_t row, int b) __attribute__((always_inline)) {
+        return (uint32_t)static_cast<const uint8_t*>(q.scales)[(row >> q.shift) * q.srow + b * q.sblk];
+    };
+    // SCALED: scales that are the same along a row, and their exponents, taken when the first codes have been requested.  RING: a byte is loaded for every
     // block all the same (of the codes, the same one): a branch around a load makes the compiler wait for all of them.
     float row_w = 1.0f, row_x[MT];
     uint32_t along_w = 127u, along_x[MT];
@@ -963,10 +968,16 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
     for (int m = 0; m < MT; ++m) px[m] = how.x_blocks ? static_cast<const uint8_t*>(x.scales) + (trow[m] >> x.shift) * x.srow : x.codes;
     const int64_t step_w = how.w_blocks ? w.sblk : 0, step_x = how.x_blocks ? x.sblk : 0;
     auto scales = [&](Block& k, int b) __attribute__((always_inline)) {
-        if constexpr (SCALED) {
+        if constexpr (RING) {
             k.ew = pw[b * step_w];
 #pragma unroll
             for (int m = 0; m < MT; ++m) k.ex[m] = px[m][b * step_x];
+        } else if constexpr (SCALED) {
+            if (how.w_blocks) k.ew = exponent(w, orow, b);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                if (how.x_blocks) k.ex[m] = exponent(x, trow[m], b);
+            }
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e) k.fw[e] = scale_bits(w, min(o0 + lg * 4 + e, O - 1), b);
@@ -1047,19 +1058,19 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
 #pragma unroll
             for (int h = 0; h < 2; ++h) k.x[m][h] = chunk_tail(xr[m] + (int64_t)b * 128 + 16 * h, left - 16 * h, b * 128ll + lg * 32 + 16 * h);
         scales(k, b);
+        if (SCALED && !RING && b == b0) exponents_along();
         multiply(CAREFUL, k);
     };
 #pragma unroll
     for (int m = 0; m < MT; ++m) acc[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
     int b = b0;
     if constexpr (RING) {
-        // Whole blocks: U of them are requested before the first is multiplied, and each one's place is taken by the block U further on.
+        // Whole blocks, U at least (few_in_ring): U of them are requested before the first is multiplied, and each one's place is taken by the block
+        // U further on.
         const int end = min(b1, full);
         Block k[U];
-        if (b < end) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) request(k[u], min(b + u, end - 1));
-        }
+        for (int u = 0; u < U; ++u) request(k[u], b + u);
         exponents_along();
         for (; b + 2 * U <= end; b += U)
 #pragma unroll
@@ -1068,10 +1079,10 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
                 request(k[u], b + u + U);
                 __builtin_amdgcn_sched_barrier(0);
             }
-        // the last U to 2 U - 1 (or fewer than U altogether)
+        // the last U to 2 U - 1
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (b + u < end) multiply(std::false_type{}, k[u]);
+            multiply(std::false_type{}, k[u]);
             if (b + u + U < end) request(k[u], b + u + U);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -1080,7 +1091,7 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
             if (b + u + U < end) multiply(std::false_type{}, k[u]);
             __builtin_amdgcn_sched_barrier(0);
         }
-        b = max(b0, end);
+        b = end;
     } else {
         for (; b + U <= b1 && b + U <= full; b += U) {
             Block k[U];
@@ -1090,7 +1101,6 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
 #pragma unroll
             for (int u = 0; u < U; ++u) multiply(std::false_type{}, k[u]);
         }
-        if (SCALED && b == b0) exponents_along();
     }
 #pragma unroll 1
     for (; b < b1; ++b) one(std::false_type{}, b);
@@ -1124,16 +1134,28 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
     }
 }
 
+// Whether blocks go in a ring: every wavefront has U whole ones at least, and where there are two tiles of tokens the registers of a ring (two workgroups a
+// compute unit, three without) leave no workgroup waiting.  In bf16, us with and without it: one token of 11008 to 4096 outputs 10.0 and 12.6, of 4096 to 4096 5.7
+// and 6.1, 24 of 11008 to 4096 17 and 18.5; with fewer blocks its first requests are for nothing, 32 of 512 to 4096 6.6 and 4.0, one of 1000 to 1000 4.6
+// and 3.7; 17 of 5632 to 11008 a seventh slower with it.  33 to 64 tokens have U blocks together and U in a ring of 2 alike: the result summed by 8-bit
+// instructions is faster without (33 of 3500 to 11008 21.3 and 20.1), 8 bits by the 16-bit ones with (33 of 2560 to 4096 11.5 and 12.2).
+// 32-bit results have no ring: their sums' registers leave none for it.
+static bool few_in_ring(const dmmv_block_matrix* w, int MT) {
+    const int64_t nb = ceil_div(w->cols, 128), full = w->cols / 128, U = few_ring(MT);
+    return nb / 4 >= U && full - 3 * nb / 4 >= U && (MT != 2 || w->rows <= 8192);
+}
+
 template <class T, int MT, bool WIDE, bool EPI>
 static dmmv_status launch_few_of(const dmmv_block_matrix* x, const dmmv_block_matrix* w, const ProductScales& how, bool scaled, const float* bias,
                                  const ProductOut<T, EPI>& out, hipStream_t s) {
     const dim3 grid((unsigned)ceil_div(w->rows, 16), (unsigned)ceil_div(x->rows, 16 * MT));
-    if (scaled)
-        hipLaunchKernelGGL((k_block_product_few<T, MT, true, WIDE, EPI>), grid, dim3(256), 0, s, (int32_t)x->rows, w->rows, x->cols, layer_view(x),
-                           layer_view(w), how, bias, out);
-    else
-        hipLaunchKernelGGL((k_block_product_few<T, MT, false, WIDE, EPI>), grid, dim3(256), 0, s, (int32_t)x->rows, w->rows, x->cols, layer_view(x),
-                           layer_view(w), how, bias, out);
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, (int32_t)x->rows, w->rows, x->cols, layer_view(x), layer_view(w), how, bias, out);
+    };
+    constexpr bool rings = sizeof(T) == 2 && (MT <= 2 || WIDE);
+    if (!scaled) launch(k_block_product_few<T, MT, false, WIDE, false, EPI>);
+    else if (rings && few_in_ring(w, MT)) launch(k_block_product_few<T, MT, true, WIDE, rings, EPI>);
+    else launch(k_block_product_few<T, MT, true, WIDE, false, EPI>);
     DMMV_LAUNCH_CHECK();
     return DMMV_OK;
 }
