@@ -1136,8 +1136,8 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
 
 // Whether blocks go in a ring: every wavefront has U whole ones at least, and where there are two tiles of tokens the registers of a ring (two workgroups a
 // compute unit, three without) leave no workgroup waiting.  In bf16, us with and without it: one token of 11008 to 4096 outputs 10.0 and 12.6, of 4096 to 4096 5.7
-// and 6.1, 24 of 11008 to 4096 17 and 18.5; with fewer blocks its first requests are for nothing, 32 of 512 to 4096 6.6 and 4.0, one of 1000 to 1000 4.6
-// and 3.7; 17 of 5632 to 11008 a seventh slower with it.  33 to 64 tokens have U blocks together and U in a ring of 2 alike: the result summed by 8-bit
+// and 6.1, 17 of 11008 to 4096 15.0 and 17.1; with fewer blocks its first requests are for nothing, 32 of 512 to 4096 6.6 and 4.0, one of 1000 to 1000 4.6
+// and 3.7; 17 of 3500 to 11008, a scale per row, 16.7 and 15.5.  33 to 64 tokens have U blocks together and U in a ring of 2 alike: the result summed by 8-bit
 // instructions is faster without (33 of 3500 to 11008 21.3 and 20.1), 8 bits by the 16-bit ones with (33 of 2560 to 4096 11.5 and 12.2).
 // 32-bit results have no ring: their sums' registers leave none for it.
 static bool few_in_ring(const dmmv_block_matrix* w, int MT) {
