@@ -1137,9 +1137,9 @@ __global__ __launch_bounds__(256) void k_block_product_few(int32_t T_, int64_t O
 // Whether blocks go in a ring: every wavefront has U whole ones at least, and where there are two tiles of tokens the registers of a ring (two workgroups a
 // compute unit, three without) leave no workgroup waiting.  In bf16, us with and without it: one token of 11008 to 4096 outputs 10.0 and 12.6, of 4096 to 4096 5.7
 // and 6.1, 17 of 11008 to 4096 15.0 and 17.1; with fewer blocks its first requests are for nothing, 32 of 512 to 4096 6.6 and 4.0, one of 1000 to 1000 4.6
-// and 3.7; 17 of 3500 to 11008, a scale per row, 16.7 and 15.5.  33 to 64 tokens have U blocks together and U in a ring of 2 alike: the result summed by 8-bit
-// instructions is faster without (33 of 3500 to 11008 21.3 and 20.1), 8 bits by the 16-bit ones with (33 of 2560 to 4096 11.5 and 12.2).
-// 32-bit results have no ring: their sums' registers leave none for it.
+// and 3.7; 17 of 3500 to 11008, a scale per row, 16.7 and 15.5.  33 to 64 tokens, U = 2 either way: sums by 8-bit
+// instructions are faster without it (33 of 3500 to 11008 21.3 and 20.1), 8 bits of sums by 16-bit ones with it (33 of 2560 to 4096 11.5 and 12.2).
+// 32-bit results have none built.
 static bool few_in_ring(const dmmv_block_matrix* w, int MT) {
     const int64_t nb = ceil_div(w->cols, 128), full = w->cols / 128, U = few_ring(MT);
     return nb / 4 >= U && full - 3 * nb / 4 >= U && (MT != 2 || w->rows <= 8192);
